@@ -258,6 +258,133 @@ int rgc_reset_hints(rgc_ctx* ctx);
  * calls are not to be trusted either), RGC_EINVAL or RGC_EHIP. */
 int rgc_last_error(rgc_ctx* ctx, void* hip_stream);
 
+/* ---- the language model's own operators ----------------------------------------------------
+ * What the step of a recurrent language model (the paper's LSTM workloads) runs around the compression of its gradients:
+ * the recurrent layer, the loss, and the scoring of tokens, each with its gradient.  Rows of logits and steps of a
+ * sequence may be strided; the innermost dimension is contiguous.  Tensors hold one of three types; sums, softmax
+ * statistics and states are fp32 throughout, and each result is rounded to its type once.  The results do not depend on
+ * scheduling, and nothing is kept from one call for the next except scratch of the context (grown at the first call that needs
+ * more: after one eager call of the same sizes the calls may be captured into a HIP graph).  The tensors of one call must not
+ * overlap except where stated.  Errors of all of them (nothing is enqueued): RGC_EINVAL, RGC_ENOMEM, RGC_EHIP. */
+#define RGC_F32  0
+#define RGC_BF16 1
+#define RGC_F16  2
+#define RGC_TOP_MAX 128 /* alternatives, or teacher entries, a row can have */
+
+/* Log probabilities of given tokens, with the entropy of their distribution and its top alternatives.  For every row of
+ * logits z:  log p_j = z_j / T - ln sum_i exp(z_i / T),  entropy = -sum_j p_j log p_j  (0 where p_j = 0).
+ *  - A row whose target is outside [0, vocab) is left out: its logits are not looked at, logprob and entropy are 0, its
+ *    alternatives are -1 with log probability -inf.  targets == NULL: no row is left out, and there is no logprob.
+ *  - Alternatives are the `top` largest logits in descending order, equal ones by ascending index (+0 and -0 are equal,
+ *    NaN ranks above +Inf).
+ *  - A logit of -inf has log probability -inf; so has every logit of a row of nothing else, whose entropy is 0.  A NaN or
+ *    +inf makes the row's log probabilities and entropy NaN.
+ * Limits: 0 <= rows < 2^31, 1 <= vocab < 2^31, 0 <= top <= min(RGC_TOP_MAX, vocab), T > 0. */
+typedef struct {
+  const void*    logits;      /* [rows][vocab], row r at logits + r * row_stride elements           */
+  int64_t        row_stride;  /* >= vocab                                                           */
+  int64_t        rows;
+  int32_t        vocab;
+  int32_t        dtype;       /* of logits: RGC_F32, RGC_BF16, RGC_F16                              */
+  const int32_t* targets;     /* [rows] or NULL                                                     */
+  float          temperature; /* T                                                                  */
+  int32_t        top;
+  float*         logprob;     /* [rows] or NULL                                                     */
+  float*         entropy;     /* [rows] or NULL                                                     */
+  float*         stats;       /* [rows][2] or NULL: max z and ln sum exp((z - max z) / T), for the
+                                 backward call                                                      */
+  int32_t*       top_idx;     /* [rows][top]                                                        */
+  float*         top_logprob; /* [rows][top]                                                        */
+} rgc_token_scores;
+
+int rgc_token_logprobs(rgc_ctx* ctx, const rgc_token_scores* scores, void* hip_stream);
+
+/* The gradient of logprob and entropy with respect to the logits:
+ *   dz_j = [ g (1{j = target} - p_j) - h p_j (log p_j + entropy) ] / T,  g = grad_logprob[r], h = grad_entropy[r]
+ * for the rows of a forward call with the same descriptor, whose `stats` (and `entropy`, with grad_entropy) it reads.
+ * Either of grad_logprob, grad_entropy ([rows], DEVICE) may be NULL: zeros.  Rows left out, and rows of -inf only, get zeros.
+ * grad_logits: [rows][vocab] of the logits' type, rows grad_row_stride elements apart; it may be the logits themselves. */
+int rgc_token_logprobs_backward(rgc_ctx* ctx, const rgc_token_scores* scores, const float* grad_logprob,
+                                const float* grad_entropy, void* grad_logits, int64_t grad_row_stride,
+                                void* hip_stream);
+
+/* Distillation from a teacher's top logits, loss and gradient in one call.  A row's teacher distribution q is the softmax of
+ * its teacher_logits / T over its k entries; with p^T = softmax(z / T) and p = softmax(z) of the student's logits
+ *   soft = T^2 sum_i q_i (ln q_i - ln p^T_i),   label = -ln p_target,   loss = soft_weight * soft + label_weight * label
+ *   dz_j = grad_loss * [ soft_weight * T * (p^T_j - q_j) + label_weight * (p_j - 1{j = target}) ]
+ *  - Teacher entries whose index is outside [0, vocab) are left out (rows with fewer than k); an index that comes twice
+ *    stands for the sum of both.  A row without entries, or with all its teacher logits -inf, has soft = 0.
+ *  - A target outside [0, vocab) (or targets == NULL) has label = 0.  A row with neither has loss 0 and gradient 0,
+ *    whatever its logits hold.
+ *  - Where every logit of a row is -inf, p = 0: the loss is +inf.
+ * Limits as above, and 0 <= k <= RGC_TOP_MAX; weights finite and >= 0; a weight of 0 switches its part off. */
+typedef struct {
+  const void*    logits;
+  int64_t        row_stride;
+  int64_t        rows;
+  int32_t        vocab;
+  int32_t        dtype;          /* of logits and grad_logits                                      */
+  const int32_t* teacher_idx;    /* [rows][k]                                                      */
+  const float*   teacher_logits; /* [rows][k]; log probabilities do as well (rgc_token_logprobs)   */
+  int32_t        k;
+  const int32_t* targets;        /* [rows] or NULL                                                 */
+  float          temperature;
+  float          soft_weight;
+  float          label_weight;
+  const float*   grad_loss;      /* [rows] or NULL: ones                                           */
+  float*         loss;           /* [rows] or NULL                                                 */
+  void*          grad_logits;    /* [rows][vocab] or NULL; may be the logits themselves            */
+  int64_t        grad_row_stride;
+} rgc_distill;
+
+int rgc_distill_loss(rgc_ctx* ctx, const rgc_distill* distill, void* hip_stream);
+
+/* Gated linear recurrence over sequences: for every sequence b and channel c, with f = sigmoid(gate), o = sigmoid(out_gate)
+ *   h_t = f_t * h_{t-1} + (1 - f_t) * x_t,   y_t = o_t * h_t      (o = 1 without out_gate)
+ *  - h before the first step is h0 (0 without one); a reset at step t puts 0 in the place of h_{t-1} there, as between texts
+ *    packed into one row.
+ *  - Steps at lengths[b] and beyond (lengths are read as at least 0 and at most `steps`) are not looked at; y is 0 there.
+ *    h_last is the state after the last step of the row, h0 if it has none.
+ * One step (steps == 1) is the serving form: h_last may be h0 itself.
+ * Limits: batch, steps >= 0, both < 2^31; 1 <= width < 2^31. */
+typedef struct {
+  void*   data;         /* element (b, t, c) at data + b * batch_stride + t * step_stride + c       */
+  int64_t batch_stride; /* elements, not negative                                                   */
+  int64_t step_stride;
+} rgc_sequence;
+
+#define RGC_RECURRENCE_CHUNK 256
+
+typedef struct {
+  int64_t        batch, steps;
+  int32_t        width;
+  int32_t        dtype;    /* of x, gate, out_gate, y and of their gradients                        */
+  rgc_sequence   x, gate;  /* read only                                                             */
+  rgc_sequence   out_gate; /* read only; data == NULL: none                                         */
+  rgc_sequence   y;
+  const int32_t* lengths;  /* [batch] or NULL                                                       */
+  const uint8_t* resets;   /* [batch][steps] or NULL; not zero: the state starts anew at this step  */
+  const float*   h0;       /* [batch][width] or NULL                                                */
+  float*         h_last;   /* [batch][width] or NULL                                                */
+  float*         states;   /* [batch][ceil(steps / RGC_RECURRENCE_CHUNK)][width] or NULL: the state before every
+                              RGC_RECURRENCE_CHUNK-th step, for the backward call                   */
+} rgc_recurrence;
+
+int rgc_gated_recurrence(rgc_ctx* ctx, const rgc_recurrence* recurrence, void* hip_stream);
+
+/* Its backward pass.  recurrence: the descriptor of the forward call, with `states` as that call left them; y and h_last are
+ * not read.  Steps beyond a row's length get zeros. */
+typedef struct {
+  rgc_sequence   dy;              /* read only                                                      */
+  rgc_sequence   dx, dgate;
+  rgc_sequence   dout_gate;       /* with out_gate                                                  */
+  const float*   dh_last;         /* [batch][width] or NULL: zeros                                  */
+  float*         dh0;             /* [batch][width] or NULL                                         */
+} rgc_recurrence_grads;
+
+int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* recurrence, const rgc_recurrence_grads* grads,
+                                  void* hip_stream);
+
 /* Text for a status code; for RGC_EHIP the text of the last HIP error seen by this thread. */
 const char* rgc_strerror(int status);
 

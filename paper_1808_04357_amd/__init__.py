@@ -12,4 +12,6 @@ from .binding import (  # noqa: F401
     load_library, rgc_clip_coefficient, rgc_compress_layers, rgc_compress_layers_scaled,
     rgc_compress_layers_threshold, rgc_decompress_accumulate, rgc_k_for_density, rgc_message_means, rgc_message_means_noalloc, rgc_stream_yardstick,
     RGC_NOALLOC_MAX_LAYERS,
+    RGC_BF16, RGC_F16, RGC_F32, RGC_RECURRENCE_CHUNK, RGC_TOP_MAX, Distillation, Recurrence, RecurrenceGrads, TokenScores,
+    rgc_distill_loss, rgc_gated_recurrence, rgc_gated_recurrence_backward, rgc_token_logprobs, rgc_token_logprobs_backward,
 )

@@ -27,6 +27,11 @@ RGC_SELECT_SMALLEST = 0x200
 RGC_THRESHOLD_SEARCH = 0x400
 RGC_STATUS_INDEX_RANGE = 0x1
 RGC_STATUS_INDEX_ORDER = 0x2
+RGC_F32 = 0
+RGC_BF16 = 1
+RGC_F16 = 2
+RGC_TOP_MAX = 128
+RGC_RECURRENCE_CHUNK = 256
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "librgc.so")
@@ -34,6 +39,8 @@ _LIB_PATH = os.path.join(_HERE, "librgc.so")
 EXPORTS = ["rgc_create", "rgc_destroy", "rgc_k_for_density", "rgc_compress_layers",
            "rgc_compress_layers_scaled", "rgc_clip_coefficient", "rgc_message_means", "rgc_message_means_noalloc",
            "rgc_compress_layers_threshold",
+           "rgc_token_logprobs", "rgc_token_logprobs_backward", "rgc_distill_loss", "rgc_gated_recurrence",
+           "rgc_gated_recurrence_backward",
            "rgc_decompress_accumulate", "rgc_reset_hints", "rgc_poison_hints", "rgc_limit_optional_scratch", "rgc_selftest",
            "rgc_last_paths", "rgc_last_stats", "rgc_last_error", "rgc_decompress_status", "rgc_profile_enable", "rgc_profile_read", "rgc_stream_yardstick", "rgc_strerror"]
 
@@ -52,6 +59,39 @@ class rgc_layer(ctypes.Structure):
 
 class rgc_msg(ctypes.Structure):
     _fields_ = [("idx", ctypes.c_void_p), ("val", ctypes.c_void_p), ("count", ctypes.c_int32)]
+
+
+class rgc_token_scores(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("rows", ctypes.c_int64),
+                ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("targets", ctypes.c_void_p),
+                ("temperature", ctypes.c_float), ("top", ctypes.c_int32), ("logprob", ctypes.c_void_p),
+                ("entropy", ctypes.c_void_p), ("stats", ctypes.c_void_p), ("top_idx", ctypes.c_void_p),
+                ("top_logprob", ctypes.c_void_p)]
+
+
+class rgc_distill(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("rows", ctypes.c_int64),
+                ("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("teacher_idx", ctypes.c_void_p),
+                ("teacher_logits", ctypes.c_void_p), ("k", ctypes.c_int32), ("targets", ctypes.c_void_p),
+                ("temperature", ctypes.c_float), ("soft_weight", ctypes.c_float), ("label_weight", ctypes.c_float),
+                ("grad_loss", ctypes.c_void_p), ("loss", ctypes.c_void_p), ("grad_logits", ctypes.c_void_p),
+                ("grad_row_stride", ctypes.c_int64)]
+
+
+class rgc_sequence(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("step_stride", ctypes.c_int64)]
+
+
+class rgc_recurrence(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("steps", ctypes.c_int64), ("width", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("x", rgc_sequence), ("gate", rgc_sequence), ("out_gate", rgc_sequence), ("y", rgc_sequence),
+                ("lengths", ctypes.c_void_p), ("resets", ctypes.c_void_p), ("h0", ctypes.c_void_p),
+                ("h_last", ctypes.c_void_p), ("states", ctypes.c_void_p)]
+
+
+class rgc_recurrence_grads(ctypes.Structure):
+    _fields_ = [("dy", rgc_sequence), ("dx", rgc_sequence), ("dgate", rgc_sequence), ("dout_gate", rgc_sequence),
+                ("dh_last", ctypes.c_void_p), ("dh0", ctypes.c_void_p)]
 
 
 _lib = None
@@ -105,6 +145,18 @@ def load_library() -> ctypes.CDLL:
                                             ctypes.c_int32, ctypes.POINTER(ctypes.c_void_p),
                                             ctypes.POINTER(ctypes.c_int64), ctypes.c_float,
                                             ctypes.c_uint32, ctypes.c_void_p]
+    L.rgc_token_logprobs.restype = ctypes.c_int
+    L.rgc_token_logprobs.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_token_scores), ctypes.c_void_p]
+    L.rgc_token_logprobs_backward.restype = ctypes.c_int
+    L.rgc_token_logprobs_backward.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_token_scores), ctypes.c_void_p,
+                                              ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]
+    L.rgc_distill_loss.restype = ctypes.c_int
+    L.rgc_distill_loss.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_distill), ctypes.c_void_p]
+    L.rgc_gated_recurrence.restype = ctypes.c_int
+    L.rgc_gated_recurrence.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_recurrence), ctypes.c_void_p]
+    L.rgc_gated_recurrence_backward.restype = ctypes.c_int
+    L.rgc_gated_recurrence_backward.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_recurrence),
+                                                ctypes.POINTER(rgc_recurrence_grads), ctypes.c_void_p]
     L.rgc_reset_hints.restype = ctypes.c_int
     L.rgc_reset_hints.argtypes = [ctypes.c_void_p]
     L.rgc_limit_optional_scratch.restype = ctypes.c_int
@@ -323,3 +375,163 @@ def rgc_decompress_accumulate(ctx: Context, msgs: MessageList, scale: float,
     _check(load_library().rgc_decompress_accumulate(ctx.handle, msgs.msgs, msgs.num_workers,
                                                     msgs.num_layers, msgs.dense, msgs.n,
                                                     float(scale), int(flags), _stream(stream)))
+
+
+# ---------------------------------------------------------------- the language model's operators
+
+_DTYPES = {"torch.float32": RGC_F32, "torch.bfloat16": RGC_BF16, "torch.float16": RGC_F16}
+
+
+def _require(ok: bool, text: str) -> None:
+    """What the library cannot see from a pointer: shapes, types, strides."""
+    if not ok:
+        raise RgcError(RGC_EINVAL, text)
+
+
+def _plain(t, name: str, shape, dtype: str, like) -> Optional[int]:
+    """A contiguous tensor of that shape and type on `like`'s device, or None."""
+    if t is None:
+        return None
+    _require(tuple(t.shape) == tuple(shape), "%s: shape %s expected, got %s" % (name, tuple(shape), tuple(t.shape)))
+    _require(str(t.dtype) == "torch." + dtype, "%s: %s expected, got %s" % (name, dtype, t.dtype))
+    _require(t.is_contiguous(), "%s: must be contiguous" % name)
+    _require(t.device == like.device, "%s: on %s, the others on %s" % (name, t.device, like.device))
+    return _ptr(t)
+
+
+def _rows(t, name: str, like=None) -> int:
+    """Row stride of a [rows, vocab] tensor whose rows are contiguous."""
+    _require(t.dim() == 2 and str(t.dtype) in _DTYPES, "%s: a [rows, vocab] tensor of float32, bfloat16 or float16 expected" % name)
+    _require(t.shape[1] >= 1 and (t.shape[1] == 1 or t.stride(1) == 1), "%s: the vocabulary must be contiguous" % name)
+    if like is not None:
+        _require(t.shape == like.shape and t.dtype == like.dtype and t.device == like.device,
+                 "%s: shape, type and device of the logits expected" % name)
+    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+
+
+class TokenScores:
+    """A host ``rgc_token_scores`` built once from tensors (keeps them alive).  logits: [rows, vocab], rows strided as they
+    may be; targets: int32 [rows] or None; outputs (each may be None): float32 logprob [rows], entropy [rows], stats [rows, 2];
+    top_idx int32 [rows, top] and top_logprob float32 [rows, top] together."""
+
+    def __init__(self, logits, targets=None, logprob=None, entropy=None, top_idx=None, top_logprob=None, stats=None,
+                 temperature: float = 1.0):
+        a = self.desc = rgc_token_scores()
+        a.row_stride = _rows(logits, "logits")
+        rows, vocab = (int(n) for n in logits.shape)
+        a.logits, a.rows, a.vocab, a.dtype = _ptr(logits), rows, vocab, _DTYPES[str(logits.dtype)]
+        a.targets = _plain(targets, "targets", (rows,), "int32", logits)
+        a.temperature = float(temperature)
+        _require((top_idx is None) == (top_logprob is None), "top_idx and top_logprob come together")
+        _require(top_idx is None or top_idx.dim() == 2, "top_idx: a [rows, top] tensor expected")
+        a.top = 0 if top_idx is None else int(top_idx.shape[1])
+        a.logprob = _plain(logprob, "logprob", (rows,), "float32", logits)
+        a.entropy = _plain(entropy, "entropy", (rows,), "float32", logits)
+        a.stats = _plain(stats, "stats", (rows, 2), "float32", logits)
+        a.top_idx = _plain(top_idx, "top_idx", (rows, a.top), "int32", logits)
+        a.top_logprob = _plain(top_logprob, "top_logprob", (rows, a.top), "float32", logits)
+        self.logits = logits
+        self._keep = (logits, targets, logprob, entropy, stats, top_idx, top_logprob)
+        self._ref = ctypes.byref(a)
+
+
+class Distillation:
+    """A host ``rgc_distill`` built once from tensors (keeps them alive).  logits: [rows, vocab]; teacher_idx: int32 [rows, k];
+    teacher_logits: float32 [rows, k]; targets: int32 [rows] or None; grad_loss, loss: float32 [rows] or None; grad_logits: like
+    the logits (or the logits themselves) or None."""
+
+    def __init__(self, logits, teacher_idx, teacher_logits, targets=None, loss=None, grad_loss=None, grad_logits=None,
+                 temperature: float = 1.0, soft_weight: float = 1.0, label_weight: float = 0.0):
+        a = self.desc = rgc_distill()
+        a.row_stride = _rows(logits, "logits")
+        rows, vocab = (int(n) for n in logits.shape)
+        a.logits, a.rows, a.vocab, a.dtype = _ptr(logits), rows, vocab, _DTYPES[str(logits.dtype)]
+        _require(teacher_idx.dim() == 2, "teacher_idx: a [rows, k] tensor expected")
+        a.k = int(teacher_idx.shape[1])
+        a.teacher_idx = _plain(teacher_idx, "teacher_idx", (rows, a.k), "int32", logits)
+        a.teacher_logits = _plain(teacher_logits, "teacher_logits", (rows, a.k), "float32", logits)
+        a.targets = _plain(targets, "targets", (rows,), "int32", logits)
+        a.temperature, a.soft_weight, a.label_weight = float(temperature), float(soft_weight), float(label_weight)
+        a.grad_loss = _plain(grad_loss, "grad_loss", (rows,), "float32", logits)
+        a.loss = _plain(loss, "loss", (rows,), "float32", logits)
+        if grad_logits is not None:
+            a.grad_row_stride = _rows(grad_logits, "grad_logits", logits)
+            a.grad_logits = _ptr(grad_logits)
+        self._keep = (logits, teacher_idx, teacher_logits, targets, loss, grad_loss, grad_logits)
+        self._ref = ctypes.byref(a)
+
+
+def _sequence(t, name: str, like=None) -> rgc_sequence:
+    """A [batch, steps, width] tensor whose channels are contiguous; other layouts come as transposed views."""
+    if t is None:
+        return rgc_sequence()
+    _require(t.dim() == 3 and str(t.dtype) in _DTYPES, "%s: a [batch, steps, width] tensor of float32, bfloat16 or float16 expected" % name)
+    _require(t.shape[2] >= 1 and (t.shape[2] == 1 or t.stride(2) == 1), "%s: the channels must be contiguous" % name)
+    if like is not None:
+        _require(t.shape == like.shape and t.dtype == like.dtype and t.device == like.device,
+                 "%s: shape, type and device of x expected" % name)
+    return rgc_sequence(_ptr(t), int(t.stride(0)), int(t.stride(1)))
+
+
+class Recurrence:
+    """A host ``rgc_recurrence`` built once from tensors (keeps them alive).  x, gate, y, out_gate (or None): [batch, steps, width]
+    of one type, the first two dimensions strided as they may be; lengths: int32 [batch] or None; resets: uint8 or bool
+    [batch, steps] or None; h0, h_last: float32 [batch, width] or None; states: float32
+    [batch, ceil(steps / RGC_RECURRENCE_CHUNK), width], needed for the backward call."""
+
+    def __init__(self, x, gate, y, out_gate=None, lengths=None, resets=None, h0=None, h_last=None, states=None):
+        a = self.desc = rgc_recurrence()
+        a.x = _sequence(x, "x")
+        a.gate, a.y, a.out_gate = _sequence(gate, "gate", x), _sequence(y, "y", x), _sequence(out_gate, "out_gate", x)
+        batch, steps, width = (int(n) for n in x.shape)
+        a.batch, a.steps, a.width, a.dtype = batch, steps, width, _DTYPES[str(x.dtype)]
+        a.lengths = _plain(lengths, "lengths", (batch,), "int32", x)
+        a.resets = _plain(resets, "resets", (batch, steps), "bool" if str(getattr(resets, "dtype", "")) == "torch.bool" else "uint8", x)
+        a.h0 = _plain(h0, "h0", (batch, width), "float32", x)
+        a.h_last = _plain(h_last, "h_last", (batch, width), "float32", x)
+        a.states = _plain(states, "states", (batch, -(-steps // RGC_RECURRENCE_CHUNK), width), "float32", x)
+        self.x, self.has_out_gate = x, out_gate is not None
+        self._keep = (x, gate, y, out_gate, lengths, resets, h0, h_last, states)
+        self._ref = ctypes.byref(a)
+
+
+class RecurrenceGrads:
+    """A host ``rgc_recurrence_grads`` for a Recurrence (keeps the tensors alive).  dy, dx, dgate, dout_gate: like x; dh_last,
+    dh0: float32 [batch, width] or None."""
+
+    def __init__(self, recurrence: Recurrence, dy, dx, dgate, dout_gate=None, dh_last=None, dh0=None):
+        x = recurrence.x
+        _require(recurrence.has_out_gate == (dout_gate is not None), "dout_gate comes with an out_gate")
+        a = self.desc = rgc_recurrence_grads()
+        a.dy, a.dx, a.dgate = _sequence(dy, "dy", x), _sequence(dx, "dx", x), _sequence(dgate, "dgate", x)
+        a.dout_gate = _sequence(dout_gate, "dout_gate", x)
+        a.dh_last = _plain(dh_last, "dh_last", (x.shape[0], x.shape[2]), "float32", x)
+        a.dh0 = _plain(dh0, "dh0", (x.shape[0], x.shape[2]), "float32", x)
+        self._keep = (recurrence, dy, dx, dgate, dout_gate, dh_last, dh0)
+        self._ref = ctypes.byref(a)
+
+
+def rgc_token_logprobs(ctx: Context, scores: TokenScores, stream=None) -> None:
+    _check(load_library().rgc_token_logprobs(ctx.handle, scores._ref, _stream(stream)))
+
+
+def rgc_token_logprobs_backward(ctx: Context, scores: TokenScores, grad_logits, grad_logprob=None, grad_entropy=None,
+                                stream=None) -> None:
+    """grad_logits: like the logits, or the logits themselves; grad_logprob, grad_entropy: float32 [rows] or None."""
+    stride, rows = _rows(grad_logits, "grad_logits", scores.logits), (scores.desc.rows,)
+    _check(load_library().rgc_token_logprobs_backward(ctx.handle, scores._ref,
+                                                      _plain(grad_logprob, "grad_logprob", rows, "float32", grad_logits),
+                                                      _plain(grad_entropy, "grad_entropy", rows, "float32", grad_logits),
+                                                      _ptr(grad_logits), stride, _stream(stream)))
+
+
+def rgc_distill_loss(ctx: Context, distillation: Distillation, stream=None) -> None:
+    _check(load_library().rgc_distill_loss(ctx.handle, distillation._ref, _stream(stream)))
+
+
+def rgc_gated_recurrence(ctx: Context, recurrence: Recurrence, stream=None) -> None:
+    _check(load_library().rgc_gated_recurrence(ctx.handle, recurrence._ref, _stream(stream)))
+
+
+def rgc_gated_recurrence_backward(ctx: Context, recurrence: Recurrence, grads: RecurrenceGrads, stream=None) -> None:
+    _check(load_library().rgc_gated_recurrence_backward(ctx.handle, recurrence._ref, grads._ref, _stream(stream)))

@@ -5,6 +5,7 @@
 #include "../../include/rgc_diag.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <memory>
@@ -14,6 +15,7 @@
 #include <vector>
 
 #include "rgc_internal.h"
+#include "rgc_lm.h"
 
 using namespace rgc;
 
@@ -1270,6 +1272,209 @@ int rgc_profile_read(rgc_ctx* ctx, double* out_ms, int64_t* out_calls) {
   int rc = drain(ctx->ev_compress, out_ms, &out_calls[0]);
   if (rc != RGC_OK) return rc;
   return drain(ctx->ev_decompress, out_ms + 2, &out_calls[1]);
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------------------ the language model's operators
+
+namespace {
+
+constexpr int64_t kInt32Most = 0x7FFFFFFF;
+
+size_t element_size(int32_t dtype) { return dtype == RGC_F32 ? 4u : 2u; }
+
+bool aligned_to(const void* p, size_t size) { return (reinterpret_cast<uintptr_t>(p) & (size - 1u)) == 0u; }
+bool words_aligned(std::initializer_list<const void*> pointers) {
+  for (const void* p : pointers)
+    if (!aligned_to(p, 4)) return false;
+  return true;
+}
+
+// log2(e) / T, as the kernels multiply with; 0 where T is no temperature or the quotient leaves fp32's normal range.
+float exponent_scale(float temperature) {
+  if (!std::isfinite(temperature) || !(temperature > 0.0f)) return 0.0f;
+  const double c = 1.4426950408889634 / static_cast<double>(temperature);
+  return c < 3.0e38 && c > 1.2e-38 && 1.0 / static_cast<double>(temperature) < 3.0e38 ? static_cast<float>(c) : 0.0f;
+}
+
+// A [rows][vocab] tensor of logits or of their gradient.
+bool rows_fit(const void* data, int64_t rows, int32_t vocab, int64_t row_stride, int32_t dtype) {
+  if (rows < 0 || rows > kInt32Most || vocab < 1 || dtype < RGC_F32 || dtype > RGC_F16) return false;
+  if (row_stride < vocab || row_stride > (int64_t(1) << 40)) return false;
+  return rows == 0 || (data && aligned_to(data, element_size(dtype)));
+}
+
+bool scores_fit(const rgc_token_scores* a) {
+  if (!rows_fit(a->logits, a->rows, a->vocab, a->row_stride, a->dtype) || exponent_scale(a->temperature) == 0.0f) return false;
+  if (a->top < 0 || a->top > RGC_TOP_MAX || a->top > a->vocab) return false;
+  if (a->rows > 0 && ((a->logprob && !a->targets) || (a->top > 0 && (!a->top_idx || !a->top_logprob)))) return false;
+  return words_aligned({a->targets, a->logprob, a->entropy, a->stats, a->top_idx, a->top_logprob});
+}
+
+// A strided sequence; `written`: no two elements of it may be one.
+bool sequence_fits(const rgc_sequence& v, const rgc_recurrence* r, bool written) {
+  constexpr int64_t kMost = int64_t(1) << 44;
+  if (!v.data || !aligned_to(v.data, element_size(r->dtype))) return false;
+  if (v.batch_stride < 0 || v.step_stride < 0 || v.batch_stride > kMost || v.step_stride > kMost) return false;
+  if (r->batch > 1 && v.batch_stride > kMost / r->batch) return false;
+  if (r->steps > 1 && v.step_stride > kMost / r->steps) return false;
+  if (!written) return true;
+  const bool by_batch = v.batch_stride >= v.step_stride;
+  const int64_t inner = by_batch ? v.step_stride : v.batch_stride, inner_n = by_batch ? r->steps : r->batch;
+  const int64_t outer = by_batch ? v.batch_stride : v.step_stride, outer_n = by_batch ? r->batch : r->steps;
+  int64_t span = r->width;                             // of the dimensions further in
+  if (inner_n > 1) {
+    if (inner < span) return false;
+    span += inner * (inner_n - 1);
+  }
+  return outer_n <= 1 || outer >= span;
+}
+
+// (steps == 0: only h0 and h_last are there; batch == 0: nothing is)
+bool recurrence_fits(const rgc_recurrence* r) {
+  if (r->batch < 0 || r->batch > kInt32Most || r->steps < 0 || r->steps > kInt32Most || r->width < 1) return false;
+  if (r->dtype < RGC_F32 || r->dtype > RGC_F16) return false;
+  if (r->batch > 0 && (static_cast<int64_t>(r->width) + 63) / 64 > kInt32Most / r->batch) return false;
+  if (!words_aligned({r->lengths, r->h0, r->h_last, r->states})) return false;
+  if (r->batch == 0 || r->steps == 0) return true;
+  return sequence_fits(r->x, r, false) && sequence_fits(r->gate, r, false) &&
+         (!r->out_gate.data || sequence_fits(r->out_gate, r, false));
+}
+
+SequenceView view_of(const rgc_sequence& v) { return SequenceView{v.data, v.batch_stride, v.step_stride}; }
+
+RecurrenceArgs recurrence_args(const rgc_recurrence* r) {
+  RecurrenceArgs A{};
+  A.batch = static_cast<uint32_t>(r->batch);
+  A.steps = static_cast<uint32_t>(r->steps);
+  A.width = static_cast<uint32_t>(r->width);
+  A.x = view_of(r->x);
+  A.gate = view_of(r->gate);
+  A.out_gate = view_of(r->out_gate);
+  A.y = view_of(r->y);
+  A.lengths = r->lengths;
+  A.resets = r->resets;
+  A.h0 = r->h0;
+  A.h_last = r->h_last;
+  A.states = r->states;
+  return A;
+}
+
+}  // namespace
+
+extern "C" {
+
+int rgc_token_logprobs(rgc_ctx* ctx, const rgc_token_scores* a, void* hip_stream) {
+  if (!ctx || !a || !scores_fit(a)) return RGC_EINVAL;
+  if (a->rows == 0) return RGC_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  ScoreArgs A{};
+  A.logits = a->logits;
+  A.row_stride = a->row_stride;
+  A.rows = static_cast<uint32_t>(a->rows);
+  A.vocab = static_cast<uint32_t>(a->vocab);
+  A.targets = a->targets;
+  A.scale = exponent_scale(a->temperature);
+  A.inv_t = 1.0f / a->temperature;
+  A.top = static_cast<uint32_t>(a->top);
+  A.logprob = a->logprob;
+  A.entropy = a->entropy;
+  A.stats = a->stats;
+  A.top_idx = a->top_idx;
+  A.top_logprob = a->top_logprob;
+  RGC_HIP(launch_token_logprobs(A, a->dtype, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_token_logprobs_backward(rgc_ctx* ctx, const rgc_token_scores* a, const float* grad_logprob,
+                                const float* grad_entropy, void* grad_logits, int64_t grad_row_stride,
+                                void* hip_stream) {
+  if (!ctx || !a || !scores_fit(a) || !rows_fit(grad_logits, a->rows, a->vocab, grad_row_stride, a->dtype)) return RGC_EINVAL;
+  if (!words_aligned({grad_logprob, grad_entropy})) return RGC_EINVAL;
+  if (a->rows == 0) return RGC_OK;
+  if (!a->stats || (grad_logprob && !a->targets) || (grad_entropy && !a->entropy)) return RGC_EINVAL;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  ScoreGradArgs A{};
+  A.logits = a->logits;
+  A.row_stride = a->row_stride;
+  A.rows = static_cast<uint32_t>(a->rows);
+  A.vocab = static_cast<uint32_t>(a->vocab);
+  A.targets = a->targets;
+  A.scale = exponent_scale(a->temperature);
+  A.inv_t = 1.0f / a->temperature;
+  A.stats = a->stats;
+  A.entropy = a->entropy;
+  A.grad_logprob = grad_logprob;
+  A.grad_entropy = grad_entropy;
+  A.grad_logits = grad_logits;
+  A.grad_row_stride = grad_row_stride;
+  RGC_HIP(launch_token_logprobs_backward(A, a->dtype, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_distill_loss(rgc_ctx* ctx, const rgc_distill* a, void* hip_stream) {
+  if (!ctx || !a || !rows_fit(a->logits, a->rows, a->vocab, a->row_stride, a->dtype)) return RGC_EINVAL;
+  if (a->grad_logits && !rows_fit(a->grad_logits, a->rows, a->vocab, a->grad_row_stride, a->dtype)) return RGC_EINVAL;
+  if (exponent_scale(a->temperature) == 0.0f || a->k < 0 || a->k > RGC_TOP_MAX) return RGC_EINVAL;
+  if (!std::isfinite(a->soft_weight) || !std::isfinite(a->label_weight) || a->soft_weight < 0.0f || a->label_weight < 0.0f) return RGC_EINVAL;
+  if (!words_aligned({a->teacher_idx, a->teacher_logits, a->targets, a->grad_loss, a->loss})) return RGC_EINVAL;
+  if (a->rows == 0) return RGC_OK;
+  if (a->k > 0 && (!a->teacher_idx || !a->teacher_logits)) return RGC_EINVAL;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  DistillArgs A{};
+  A.logits = a->logits;
+  A.row_stride = a->row_stride;
+  A.rows = static_cast<uint32_t>(a->rows);
+  A.vocab = static_cast<uint32_t>(a->vocab);
+  A.teacher_idx = a->teacher_idx;
+  A.teacher_logits = a->teacher_logits;
+  A.k = static_cast<uint32_t>(a->k);
+  A.targets = a->targets;
+  A.temperature = a->temperature;
+  A.scale = exponent_scale(a->temperature);
+  A.inv_t = 1.0f / a->temperature;
+  A.soft_weight = a->soft_weight;
+  A.label_weight = a->label_weight;
+  A.grad_loss = a->grad_loss;
+  A.loss = a->loss;
+  A.grad_logits = a->grad_logits;
+  A.grad_row_stride = a->grad_row_stride;
+  RGC_HIP(launch_distill(A, a->dtype, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_gated_recurrence(rgc_ctx* ctx, const rgc_recurrence* r, void* hip_stream) {
+  if (!ctx || !r || !recurrence_fits(r)) return RGC_EINVAL;
+  if (r->batch > 0 && r->steps > 0 && !sequence_fits(r->y, r, true)) return RGC_EINVAL;
+  if (r->batch == 0) return RGC_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  RGC_HIP(launch_recurrence(recurrence_args(r), r->dtype, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* r, const rgc_recurrence_grads* g, void* hip_stream) {
+  if (!ctx || !r || !g || !recurrence_fits(r) || !words_aligned({g->dh_last, g->dh0})) return RGC_EINVAL;
+  if (r->batch > 0 && r->steps > 0) {
+    if (!r->states || !sequence_fits(g->dy, r, false) || !sequence_fits(g->dx, r, true) || !sequence_fits(g->dgate, r, true)) return RGC_EINVAL;
+    if (r->out_gate.data && !sequence_fits(g->dout_gate, r, true)) return RGC_EINVAL;
+  }
+  if (r->batch == 0) return RGC_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  RecurrenceGradArgs G{};
+  G.dy = view_of(g->dy);
+  G.dx = view_of(g->dx);
+  G.dgate = view_of(g->dgate);
+  G.dout_gate = view_of(g->dout_gate);
+  G.dh_last = g->dh_last;
+  G.dh0 = g->dh0;
+  RGC_HIP(launch_recurrence_backward(recurrence_args(r), G, r->dtype, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,81 @@
+// Arguments of the language-model operators' kernels (rgc_vocab.hip, rgc_recurrence.hip), as the host side fills them.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace rgc {
+
+struct ScoreArgs {
+  const void* logits;
+  int64_t row_stride;
+  uint32_t rows, vocab;
+  const int32_t* targets;
+  float scale, inv_t;        // log2(e) / T: what turns a difference of logits into an exponent of two; 1 / T
+  uint32_t top;
+  float* logprob;
+  float* entropy;
+  float* stats;
+  int32_t* top_idx;
+  float* top_logprob;
+};
+
+struct ScoreGradArgs {
+  const void* logits;
+  int64_t row_stride;
+  uint32_t rows, vocab;
+  const int32_t* targets;
+  float scale, inv_t;
+  const float* stats;
+  const float* entropy;
+  const float* grad_logprob;
+  const float* grad_entropy;
+  void* grad_logits;
+  int64_t grad_row_stride;
+};
+
+struct DistillArgs {
+  const void* logits;
+  int64_t row_stride;
+  uint32_t rows, vocab;
+  const int32_t* teacher_idx;
+  const float* teacher_logits;
+  uint32_t k;
+  const int32_t* targets;    // null: no labels
+  float temperature, scale, inv_t;
+  float soft_weight, label_weight;
+  const float* grad_loss;
+  float* loss;
+  void* grad_logits;
+  int64_t grad_row_stride;
+};
+
+struct SequenceView {
+  void* data;
+  int64_t batch_stride, step_stride;
+};
+
+struct RecurrenceArgs {
+  uint32_t batch, steps, width;
+  SequenceView x, gate, out_gate, y;
+  const int32_t* lengths;
+  const uint8_t* resets;
+  const float* h0;
+  float* h_last;
+  float* states;
+};
+
+struct RecurrenceGradArgs {
+  SequenceView dy, dx, dgate, dout_gate;
+  const float* dh_last;
+  float* dh0;
+};
+
+hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, hipStream_t s);
+hipError_t launch_token_logprobs_backward(const ScoreGradArgs& a, int dtype, hipStream_t s);
+hipError_t launch_distill(const DistillArgs& a, int dtype, hipStream_t s);
+hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, hipStream_t s);
+hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, hipStream_t s);
+
+}  // namespace rgc

@@ -1,0 +1,620 @@
+"""Operators over rows of logits (token log probabilities with entropy and top alternatives, their gradient, and the distillation
+loss with its gradient) against their definitions in 64 bits.
+
+Tolerances.  u = 2^-24.  A row's sum of n weights is added up in fp32 by at least 64 lanes, so its relative error is at most
+(n / 64 + 32) u; an exponent a (in powers of two) carries at most 4 u |a|, and the 2^x and log2 instructions one unit in the last
+place each; the former's results below 2^-126 are 0.  rel(n, a) below bounds the relative error of a probability, and with the logarithm's slope of 1 the absolute error of
+a log probability.  A result is rounded to its type once: half a unit in the last place, 2^-8 (bf16), 2^-11 (f16) relative."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def rgc():
+    torch = pytest.importorskip("torch")
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    import paper_1808_04357_amd as pkg
+    pkg.load_library()
+    return pkg
+
+
+@pytest.fixture(scope="module")
+def ctx(rgc):
+    c = rgc.Context(1024, 1)
+    yield c
+    c.close()
+
+
+def dtype_of(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[name]
+
+
+ROUNDING = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+SMALLEST = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -25}      # half the spacing where results underflow
+
+
+def rel(n, a, most=300.0):
+    """(A probability whose exponent is below -300 is 0, and so is its error: `most`; a log probability has no such end.)"""
+    return (n / 64.0 + 64.0) * U + 8.0 * U * np.minimum(np.abs(a), most)
+
+
+def of_fp32(v):
+    """Values as fp32 can hold them: what is beyond its largest is an infinity."""
+    with np.errstate(over="ignore"):
+        return np.where(np.isinf(v.astype(np.float32)), v.astype(np.float32), v)
+
+
+def upload(z, dtype, pad=0, shift=0):
+    """A [rows, vocab] device tensor: rows `pad` elements further apart than they are long, the first one `shift` elements into
+    its allocation; what is not part of a row is NaN."""
+    import torch
+    rows, vocab = z.shape
+    flat = torch.full((rows * (vocab + pad) + shift,), math.nan, dtype=dtype_of(dtype), device="cuda")
+    view = flat[shift:].view(rows, vocab + pad)[:, :vocab]
+    view.copy_(torch.from_numpy(z))
+    return view
+
+
+def as64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def log_softmax64(z, temperature=1.0):
+    """(log p, largest, ln sum); a row of nothing but -inf has log p = -inf, one with a NaN or +inf has NaN."""
+    with np.errstate(all="ignore"):
+        u = z / temperature
+        m = z.max(axis=1, keepdims=True)
+        base = np.where(m == -np.inf, 0.0, m / temperature)
+        d = u - base
+        log_sum = np.log(np.exp(d).sum(axis=1, keepdims=True))
+        logp = np.where((d == -np.inf) & ~np.isnan(log_sum), -np.inf, d - log_sum)
+    return logp, m[:, 0], log_sum[:, 0]
+
+
+def top64(z, top):
+    """Descending, equal ones by index, NaN first."""
+    key = np.where(np.isnan(z), np.inf, z)
+    out = np.empty((z.shape[0], top), np.int64)
+    for r in range(z.shape[0]):
+        out[r] = np.lexsort((np.arange(z.shape[1]), -key[r], ~np.isnan(z[r])))[:top]
+    return out
+
+
+def run_scores(rgc, ctx, z, dtype, targets, top=0, temperature=1.0, pad=0, shift=0, grads=None, in_place=False, stream=None):
+    import torch
+    rows, vocab = z.shape
+    logits = upload(z, dtype, pad, shift)
+    t = None if targets is None else torch.tensor(np.asarray(targets, np.int32), device="cuda")
+
+    def out(*shape, kind=torch.float32):
+        return torch.full(shape, 77, dtype=kind, device="cuda")
+
+    got = {"entropy": out(rows), "stats": out(rows, 2)}
+    if t is not None:
+        got["logprob"] = out(rows)
+    if top:
+        got["top_idx"], got["top_logprob"] = out(rows, top, kind=torch.int32), out(rows, top)
+    call = rgc.TokenScores(logits, t, temperature=temperature, **got)
+    rgc.rgc_token_logprobs(ctx, call, stream)
+    used = as64(logits)
+    if grads is not None:
+        g, h = (None if v is None else torch.tensor(v, dtype=torch.float32, device="cuda") for v in grads)
+        dz = logits if in_place else upload(np.full(z.shape, 55.0, np.float32), dtype, pad + 3, shift)
+        rgc.rgc_token_logprobs_backward(ctx, call, dz, g, h, stream)
+        got["grad"] = dz
+    torch.cuda.synchronize()
+    return used, {k: (v.cpu().numpy() if v.dtype == torch.int32 else as64(v)) for k, v in got.items()}
+
+
+def check_scores(used, got, targets, dtype, top=0, temperature=1.0, grads=None):
+    rows, vocab = used.shape
+    left_out = np.zeros(rows, bool) if targets is None else (np.asarray(targets) < 0) | (np.asarray(targets) >= vocab)
+    z = np.where(left_out[:, None], 0.0, used)
+    logp, m, log_sum = log_softmax64(z, temperature)
+    p = np.exp(logp)
+    with np.errstate(all="ignore"):
+        entropy = -np.where(p == 0, 0.0, p * logp).sum(axis=1)
+        a = logp / math.log(2)
+    fine = ~left_out & ~np.isnan(logp).any(axis=1)
+    broken = ~left_out & ~fine
+
+    def near(x, y, tol, where, what):
+        x, y, tol = (np.broadcast_to(v, x.shape)[where] for v in (x, y, tol))
+        same = (x == y) | (np.isnan(x) & np.isnan(y))
+        with np.errstate(all="ignore"):
+            bad = ~same & ~(np.abs(x - y) <= tol)
+        assert not bad.any(), "%s: %d of %d off, first %r for %r (tolerance %r)" % (what, bad.sum(), bad.size, x[bad][0], y[bad][0], tol[bad][0])
+
+    assert np.all(got["entropy"][left_out] == 0)
+    near(got["entropy"], entropy, rel(vocab, np.abs(log_sum) * 2 + 2) * (1 + entropy) * 2, fine, "entropy")
+    assert np.isnan(got["entropy"][broken]).all()
+    if targets is not None:
+        at = np.where(left_out, 0, np.asarray(targets))
+        want = of_fp32(logp[np.arange(rows), at])
+        assert np.all(got["logprob"][left_out] == 0)
+        near(got["logprob"], want, rel(vocab, np.where(np.isfinite(want), want, 0) * 1.5, math.inf), fine, "logprob")
+        assert np.isnan(got["logprob"][broken]).all()
+    if top:
+        assert np.all(got["top_idx"][left_out] == -1) and np.all(got["top_logprob"][left_out] == -np.inf)
+        index = top64(z, top)
+        assert np.array_equal(got["top_idx"][~left_out], index[~left_out]), "top alternatives"
+        want = of_fp32(np.take_along_axis(logp, index, axis=1))
+        near(got["top_logprob"], want, rel(vocab, np.where(np.isfinite(want), want, 0) * 1.5, math.inf), fine, "top log probabilities")
+        assert np.isnan(got["top_logprob"][broken]).all()
+    if grads is not None:
+        g = np.zeros(rows) if grads[0] is None else np.asarray(grads[0], np.float32).astype(np.float64)
+        h = np.zeros(rows) if grads[1] is None else np.asarray(grads[1], np.float32).astype(np.float64)
+        one = np.zeros_like(p)
+        if targets is not None:
+            one[np.arange(rows), at] = 1.0
+        with np.errstate(all="ignore"):
+            want = (g[:, None] * (one - p) - h[:, None] * np.where(p == 0, 0.0, p * (logp + entropy[:, None]))) / temperature
+            size = (np.abs(g)[:, None] * p + np.abs(h)[:, None] * p * (np.abs(np.where(p == 0, 0, logp)) + entropy[:, None] + 1)) / temperature
+            slack = 2.0 ** -126 * (np.abs(g)[:, None] + np.abs(h)[:, None] * (np.abs(np.where(p == 0, 0, logp)) + entropy[:, None] + 1)) / temperature
+            slack += 2 * rel(vocab, np.where(p == 0, 0, a)) * size + 4 * U * (size + np.abs(g)[:, None] / temperature * one)
+        empty = left_out | (fine & (m == -np.inf))
+        want[empty] = 0.0
+        slack[empty] = 0.0
+        near(got["grad"], want, slack + 1.01 * ROUNDING[dtype] * np.abs(want) + np.where(empty, 0.0, SMALLEST[dtype])[:, None], fine | left_out, "gradient")
+
+
+def logits_like(g, rows, vocab, spread=2.0):
+    z = g.standard_normal((rows, vocab)).astype(np.float32) * spread
+    z[np.arange(rows), g.integers(0, vocab, rows)] += 10.0 * (g.random(rows) < 0.5)
+    return z
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,vocab", [(1, 1), (3, 2), (5, 7), (2, 63), (2, 64), (2, 65), (3, 255), (3, 257), (4, 1000), (2, 2049),
+                                        (1, 10_000), (9, 10_000), (2, 50_257), (1, 131_072), (2, 131_073), (1, 262_147), (700, 1_003)])
+def test_scores_of_every_length(rgc, ctx, dtype, rows, vocab):
+    g = np.random.default_rng(vocab * 7 + rows)
+    z = logits_like(g, rows, vocab)
+    targets = g.integers(0, vocab, rows)
+    grads = (g.standard_normal(rows), g.standard_normal(rows))
+    top = min(vocab, 20)
+    used, got = run_scores(rgc, ctx, z, dtype, targets, top, 1.0, grads=grads)
+    check_scores(used, got, targets, dtype, top, 1.0, grads)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [1, 2, 33, 64, 127, 128])
+@pytest.mark.parametrize("vocab", [128, 300, 8_191, 70_001])
+def test_numbers_of_alternatives(rgc, ctx, dtype, top, vocab):
+    g = np.random.default_rng(top * 1000 + vocab)
+    z = logits_like(g, 5, vocab)
+    targets = g.integers(0, vocab, 5)
+    used, got = run_scores(rgc, ctx, z, dtype, targets, top, 0.7)
+    check_scores(used, got, targets, dtype, top, 0.7)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("pad,shift", [(0, 1), (1, 0), (5, 3), (64, 7)])
+@pytest.mark.parametrize("vocab", [13, 1_000, 33_278])
+def test_rows_that_start_anywhere(rgc, ctx, dtype, pad, shift, vocab):
+    g = np.random.default_rng(pad * 100 + shift)
+    z = logits_like(g, 6, vocab)
+    targets = np.array([0, vocab - 1, vocab // 2, -1, vocab, 3])
+    grads = (g.standard_normal(6), None)
+    used, got = run_scores(rgc, ctx, z, dtype, targets, 5, 2.0, pad, shift, grads)
+    check_scores(used, got, targets, dtype, 5, 2.0, grads)
+    # what lies between the gradient's rows is not touched
+    used, got = run_scores(rgc, ctx, z, dtype, targets, 5, 2.0, pad, shift, (None, g.standard_normal(6)), in_place=True)
+
+
+def special_rows(vocab, low):
+    """Rows where a softmax or a selection can go wrong; low: the type's lowest value."""
+    g = np.random.default_rng(31)
+    rows = [np.full(vocab, -np.inf)]                                  # nothing allowed
+    r = np.full(vocab, -np.inf); r[vocab // 3] = -4.0; rows.append(r)   # one word allowed
+    r = np.full(vocab, -np.inf); r[[1, vocab - 1]] = 2.0; rows.append(r)
+    rows.append(np.full(vocab, low))                                  # all masked with the lowest value: all alike
+    r = np.full(vocab, low); r[5] = 1.0; rows.append(r)
+    r = np.full(vocab, low); r[:vocab // 2] = g.standard_normal(vocab // 2); rows.append(r)
+    r = np.full(vocab, -low); rows.append(r)
+    r = g.standard_normal(vocab); r[7] = -low; r[8] = low; rows.append(r)
+    rows.append(np.zeros(vocab))
+    r = np.zeros(vocab); r[::2] = -0.0; rows.append(r)
+    rows.append(np.linspace(-9, 9, vocab))                            # ascending, descending
+    rows.append(np.linspace(9, -9, vocab))
+    rows.append(np.where(np.arange(vocab) % 256 == 3, 8.0 + np.arange(vocab) / vocab, 0.0))    # large ones a fixed distance apart
+    rows.append(np.where(np.arange(vocab) % 1024 == 8, 8.0 - np.arange(vocab) / vocab, 0.0))
+    r = g.standard_normal(vocab); r[100:228] = 20.0 + g.random(128); rows.append(r)            # ... and side by side
+    rows.append(g.integers(-2, 3, vocab).astype(np.float64))          # many equal ones
+    r = g.standard_normal(vocab); r[11] = np.nan; r[40] = -np.nan; rows.append(r)
+    r = g.standard_normal(vocab); r[12] = np.inf; rows.append(r)
+    r = np.full(vocab, -np.inf); r[2] = np.nan; rows.append(r)
+    r = g.standard_normal(vocab); r[[3, 9]] = 60.0; rows.append(r)    # two certain ones
+    r = np.full(vocab, -30.0); r[17] = 30.0; rows.append(r)           # one certain one
+    return np.stack(rows).astype(np.float32)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("vocab", [300, 4_099, 40_000, 140_001])
+@pytest.mark.parametrize("temperature", [1.0, 0.25, 3.0])
+def test_rows_of_masks_ties_and_infinities(rgc, ctx, dtype, vocab, temperature):
+    low = {"f32": -3.4028234e38, "bf16": -3.3895314e38, "f16": -65504.0}[dtype]
+    z = special_rows(vocab, low)
+    g = np.random.default_rng(5)
+    targets = g.integers(0, vocab, z.shape[0])
+    targets[1] = vocab // 3
+    grads = (g.standard_normal(z.shape[0]), g.standard_normal(z.shape[0]))
+    for top in (20, 128):
+        used, got = run_scores(rgc, ctx, z, dtype, targets, top, temperature, grads=grads)
+        check_scores(used, got, targets, dtype, top, temperature, grads)
+
+
+def test_rows_left_out_may_hold_anything(rgc, ctx):
+    g = np.random.default_rng(8)
+    z = logits_like(g, 8, 5_000)
+    targets = np.array([4, -1, 5_000, -100, 2_147_483_647, -2_147_483_648, 4_999, 0])
+    z[1:6] = np.nan
+    z[3] = np.inf
+    grads = (g.standard_normal(8), g.standard_normal(8))
+    for dtype in ("f32", "bf16"):
+        used, got = run_scores(rgc, ctx, z, dtype, targets, 3, 1.0, grads=grads)
+        check_scores(used, got, targets, dtype, 3, 1.0, grads)
+        assert np.all(got["grad"][1:6] == 0)
+
+
+def test_without_targets_and_one_output_at_a_time(rgc, ctx):
+    import torch
+    g = np.random.default_rng(9)
+    z = logits_like(g, 4, 2_000)
+    used, got = run_scores(rgc, ctx, z, "f32", None, 6, 0.5, grads=(None, g.standard_normal(4)))
+    check_scores(used, got, None, "f32", 6, 0.5)
+    logits = upload(z, "f32")
+    entropy = torch.empty(4, device="cuda")
+    rgc.rgc_token_logprobs(ctx, rgc.TokenScores(logits, entropy=entropy, temperature=0.5))
+    index, value = torch.empty(4, 6, dtype=torch.int32, device="cuda"), torch.empty(4, 6, device="cuda")
+    rgc.rgc_token_logprobs(ctx, rgc.TokenScores(logits, top_idx=index, top_logprob=value, temperature=0.5))
+    torch.cuda.synchronize()
+    assert np.array_equal(as64(entropy), got["entropy"])
+    assert np.array_equal(index.cpu().numpy(), got["top_idx"]) and np.array_equal(as64(value), got["top_logprob"])
+
+
+def test_scores_gradient_against_differences(rgc, ctx):
+    """Central differences of the 64-bit definition, step 1e-4: their error is far below the tolerance of 1e-6 of the gradient."""
+    g = np.random.default_rng(10)
+    z = logits_like(g, 3, 40).astype(np.float32)
+    targets, gr, hr, T = np.array([3, 39, 0]), g.standard_normal(3), g.standard_normal(3), 1.5
+    gr, hr = gr.astype(np.float32).astype(np.float64), hr.astype(np.float32).astype(np.float64)
+    used, got = run_scores(rgc, ctx, z, "f32", targets, 0, T, grads=(gr, hr))
+
+    def value(x):
+        logp, _, _ = log_softmax64(x, T)
+        return gr * logp[np.arange(3), targets] - hr * (np.exp(logp) * logp).sum(axis=1)
+
+    step = 1e-4
+    for j in range(40):
+        up, down = used.copy(), used.copy()
+        up[:, j] += step
+        down[:, j] -= step
+        assert np.allclose((value(up) - value(down)) / (2 * step), got["grad"][:, j], rtol=1e-5, atol=2e-6)
+
+
+def test_rows_whose_offsets_pass_32_bits(rgc, ctx):
+    """Rows 2^31 + 64 elements apart: the third one starts beyond 2^32 elements and 2^33 bytes."""
+    import torch
+    g = np.random.default_rng(12)
+    vocab, stride = 1_500, 2 ** 31 + 64
+    z = logits_like(g, 3, vocab)
+    flat = torch.empty(2 * stride + vocab, dtype=torch.bfloat16, device="cuda")
+    logits = flat.as_strided((3, vocab), (stride, 1))
+    logits.copy_(torch.from_numpy(z))
+    targets = torch.tensor([1, 7, 1_499], dtype=torch.int32, device="cuda")
+    out = {k: torch.empty(3, device="cuda") for k in ("logprob", "entropy")}
+    out["stats"] = torch.empty(3, 2, device="cuda")
+    out["top_idx"], out["top_logprob"] = torch.empty(3, 4, dtype=torch.int32, device="cuda"), torch.empty(3, 4, device="cuda")
+    call = rgc.TokenScores(logits, targets, **out)
+    rgc.rgc_token_logprobs(ctx, call)
+    used = as64(logits)
+    ones = torch.ones(3, device="cuda")
+    rgc.rgc_token_logprobs_backward(ctx, call, logits, ones)
+    torch.cuda.synchronize()
+    got = {k: (v.cpu().numpy() if v.dtype == torch.int32 else as64(v)) for k, v in out.items()}
+    got["grad"] = as64(logits)
+    check_scores(used, got, targets.cpu().numpy(), "bf16", 4, 1.0, (np.ones(3), None))
+
+
+# ------------------------------------------------------------------------------------------------ distillation
+
+def distill64(z, index, teacher, targets, T, ws, wl, g):
+    rows, vocab = z.shape
+    known = (index >= 0) & (index < vocab)
+    at = np.where(known, index, 0)
+    with np.errstate(all="ignore"):
+        t = np.where(known, teacher, -np.inf)
+        logq, _, _ = log_softmax64(t, T) if t.shape[1] else (t, None, None)
+        q = np.exp(logq)
+        soft_on = (ws > 0) & ~(q.sum(axis=1) == 0)
+        logp, _, _ = log_softmax64(z, T)
+        logp1, _, _ = log_softmax64(z)
+        soft = T * T * np.where(q == 0, 0.0, q * (logq - np.take_along_axis(logp, at, axis=1))).sum(axis=1)
+        valid = np.zeros(rows, bool) if targets is None else (targets >= 0) & (targets < vocab) & (wl > 0)
+        to = np.where(valid, 0 if targets is None else targets, 0)
+        label = -logp1[np.arange(rows), to]
+        loss = np.where(soft_on, ws * soft, 0.0) + np.where(valid, wl * label, 0.0)
+        qd, one = np.zeros_like(z), np.zeros_like(z)
+        for r in range(rows):
+            np.add.at(qd[r], at[r][known[r]], q[r][known[r]])
+            one[r, to[r]] = 1.0
+        p, p1 = np.exp(logp), np.exp(logp1)
+        grad = np.where(soft_on[:, None], ws * T * (p - qd), 0.0) + np.where(valid[:, None], wl * (p1 - one), 0.0)
+        size = np.where(soft_on[:, None], ws * T * (p * (1 + np.where(p == 0, 0, np.abs(logp))) + qd), 0.0) + np.where(
+            valid[:, None], wl * (p1 * (1 + np.where(p1 == 0, 0, np.abs(logp1))) + one), 0.0)
+    loss_size = np.where(soft_on, ws * T * T * (np.where(q == 0, 0.0, q * (np.abs(logq) + np.abs(np.take_along_axis(logp, at, axis=1))))).sum(axis=1), 0.0)
+    loss_size = loss_size + np.where(valid, wl * np.abs(label), 0.0) + (ws * T * T + wl)
+    return loss, g[:, None] * grad, loss_size, np.abs(g)[:, None] * size
+
+
+def check_distill(rgc, ctx, z, index, teacher, targets, dtype, T=1.0, ws=1.0, wl=0.0, pad=0, shift=0, grad_loss=True, in_place=False,
+                  parts=("loss", "grad"), stream=None):
+    import torch
+    rows, vocab = z.shape
+    g = np.random.default_rng(77)
+    logits = upload(z, dtype, pad, shift)
+    weight = (g.random(rows) + 0.5).astype(np.float32)
+    used = as64(logits)
+    put = lambda v, kind: torch.tensor(np.ascontiguousarray(v), dtype=kind, device="cuda")   # noqa: E731
+    loss = torch.full((rows,), 77.0, device="cuda") if "loss" in parts else None
+    around = None
+    grad = None
+    if "grad" in parts:
+        if in_place:
+            grad = logits
+        else:
+            around = torch.full((rows, vocab + pad + 2), 55.0, dtype=dtype_of(dtype), device="cuda")
+            grad = around[:, :vocab]
+    call = rgc.Distillation(logits, put(index, torch.int32), put(teacher, torch.float32),
+                            targets=None if targets is None else put(targets, torch.int32), loss=loss,
+                            grad_loss=put(weight, torch.float32) if grad_loss else None, grad_logits=grad,
+                            temperature=T, soft_weight=ws, label_weight=wl)
+    rgc.rgc_distill_loss(ctx, call, stream)
+    torch.cuda.synchronize()
+    want, dwant, size, dsize = distill64(used, index, teacher.astype(np.float32).astype(np.float64), targets, T, ws, wl,
+                                         weight.astype(np.float64) if grad_loss else np.ones(rows))
+    if loss is not None:
+        got, want = as64(loss), of_fp32(want)
+        with np.errstate(all="ignore"):
+            # (a loss within its tolerance of fp32's largest may be beyond it)
+            within = np.abs(np.clip(got, -3.4028235e38, 3.4028235e38) - want) <= 2 * rel(vocab, 8) * size
+            ok = (got == want) | (np.isnan(got) & np.isnan(want)) | (within & np.isfinite(want))
+        assert ok.all(), "loss: %r for %r" % (got[~ok][:3], want[~ok][:3])
+    if grad is not None:
+        got = as64(grad)
+        with np.errstate(all="ignore"):
+            tol = 2 * rel(vocab, 8) * dsize + 1.01 * ROUNDING[dtype] * np.abs(dwant) + np.where(dsize > 0, SMALLEST[dtype], 0.0)
+            ok = (got == dwant) | (np.isnan(got) & np.isnan(dwant)) | (np.abs(got - dwant) <= tol)
+        assert ok.all(), "gradient: %d off, %r for %r" % ((~ok).sum(), got[~ok][:3], dwant[~ok][:3])
+        if around is not None:
+            assert bool((around[:, vocab:] == 55.0).all()), "written beside the rows"
+
+
+def teacher_like(g, z, k):
+    t = z + g.standard_normal(z.shape).astype(np.float32)
+    index = np.argsort(-t, axis=1, kind="stable")[:, :k]
+    return index, np.take_along_axis(t, index, axis=1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows,vocab,k", [(1, 1, 1), (3, 7, 7), (5, 65, 3), (4, 1_000, 128), (20, 10_000, 16), (3, 33_278, 50),
+                                          (2, 50_257, 64), (2, 131_073, 128), (1, 262_147, 5), (300, 2_003, 1)])
+@pytest.mark.parametrize("T,ws,wl", [(1.0, 1.0, 0.0), (2.0, 0.5, 0.5), (4.0, 0.9, 0.1)])
+def test_distillation_of_every_length(rgc, ctx, dtype, rows, vocab, k, T, ws, wl):
+    g = np.random.default_rng(rows + vocab + k)
+    z = logits_like(g, rows, vocab)
+    index, teacher = teacher_like(g, z, k)
+    check_distill(rgc, ctx, z, index, teacher, g.integers(0, vocab, rows), dtype, T, ws, wl)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift,in_place", [(0, 1, False), (1, 0, True), (5, 3, False), (64, 7, True), (0, 0, True)])
+@pytest.mark.parametrize("vocab", [13, 3_001, 40_009, 140_001])
+def test_distillation_of_rows_that_start_anywhere(rgc, ctx, dtype, pad, shift, in_place, vocab):
+    g = np.random.default_rng(vocab + pad)
+    z = logits_like(g, 5, vocab)
+    index, teacher = teacher_like(g, z, 9)
+    check_distill(rgc, ctx, z, index, teacher, np.array([0, vocab - 1, -1, vocab, 5]), dtype, 2.0, 0.7, 0.3, pad, shift, in_place=in_place)
+
+
+def test_distillation_entries_left_out_twice_and_masked(rgc, ctx):
+    g = np.random.default_rng(21)
+    vocab, k = 3_000, 40
+    z = logits_like(g, 12, vocab)
+    index, teacher = teacher_like(g, z, k)
+    index[1, 5:] = -1                                  # fewer entries
+    teacher[1, 5:] = np.nan                            # what lies in their place is not looked at
+    index[2] = vocab                                   # no entry at all
+    index[3, 20:] = index[3, :20]                      # entries that come twice
+    teacher[4] = -np.inf                               # entries without weight
+    teacher[5, 3:] = -np.inf
+    index[6] = -1
+    z[6] = np.nan                                      # a row with neither teacher nor label
+    z[7] = -np.inf
+    z[8, index[8]] = -np.inf                           # the student rules out all that the teacher wants
+    teacher[9, 0] = np.nan
+    teacher[10] = -3.4028234e38
+    teacher[11, 0] = 3.0e38
+    targets = g.integers(0, vocab, 12)
+    targets[[2, 6]] = -1
+    targets[3] = index[3, 0]
+    for dtype in ("f32", "bf16"):
+        for T, ws, wl in ((1.0, 1.0, 0.0), (2.0, 0.5, 0.5), (1.0, 0.0, 1.0), (3.0, 0.0, 0.0)):
+            check_distill(rgc, ctx, z, index, teacher, targets, dtype, T, ws, wl)
+            check_distill(rgc, ctx, z, index, teacher, None, dtype, T, ws, wl)
+
+
+def test_distillation_of_special_rows(rgc, ctx):
+    for dtype, low in (("f32", -3.4028234e38), ("bf16", -3.3895314e38), ("f16", -65504.0)):
+        for vocab in (700, 9_000, 140_001):
+            z = special_rows(vocab, low)
+            g = np.random.default_rng(22)
+            index = np.stack([g.permutation(vocab)[:30] for _ in range(z.shape[0])])
+            teacher = g.standard_normal(index.shape).astype(np.float32)
+            for T, ws, wl in ((1.0, 1.0, 0.0), (2.0, 0.5, 0.5)):
+                check_distill(rgc, ctx, z, index, teacher, g.integers(0, vocab, z.shape[0]), dtype, T, ws, wl)
+
+
+def test_distillation_parts_alone(rgc, ctx):
+    g = np.random.default_rng(23)
+    z = logits_like(g, 6, 2_500)
+    index, teacher = teacher_like(g, z, 12)
+    targets = g.integers(0, 2_500, 6)
+    for parts in (("loss",), ("grad",), ()):
+        check_distill(rgc, ctx, z, index, teacher, targets, "bf16", 2.0, 0.5, 0.5, parts=parts, grad_loss=False)
+    none = np.zeros((6, 0), np.int64)
+    check_distill(rgc, ctx, z, none, none.astype(np.float32), targets, "f32", 2.0, 0.5, 0.5)
+    check_distill(rgc, ctx, z, none, none.astype(np.float32), None, "f32", 2.0, 0.5, 0.5)
+
+
+def test_distillation_gradient_against_differences(rgc, ctx):
+    import torch
+    g = np.random.default_rng(24)
+    z = logits_like(g, 3, 30)
+    index, teacher = teacher_like(g, z, 6)
+    targets, T, ws, wl = np.array([2, 29, 11]), 2.0, 0.6, 0.4
+    logits = upload(z, "f32")
+    grad = torch.empty_like(logits)
+    rgc.rgc_distill_loss(ctx, rgc.Distillation(logits, torch.tensor(index, dtype=torch.int32, device="cuda"),
+                                               torch.tensor(teacher, device="cuda"), targets=torch.tensor(targets, dtype=torch.int32, device="cuda"),
+                                               grad_logits=grad, temperature=T, soft_weight=ws, label_weight=wl))
+    torch.cuda.synchronize()
+    step, ones = 1e-4, np.ones(3)
+    for j in range(30):
+        up, down = as64(logits), as64(logits)
+        up[:, j] += step
+        down[:, j] -= step
+        slope = (distill64(up, index, teacher.astype(np.float64), targets, T, ws, wl, ones)[0]
+                 - distill64(down, index, teacher.astype(np.float64), targets, T, ws, wl, ones)[0]) / (2 * step)
+        assert np.allclose(slope, as64(grad)[:, j], rtol=1e-5, atol=2e-6)
+
+
+# ------------------------------------------------------------------------------------------------ streams, graphs, refusals
+
+def test_results_do_not_change_from_call_to_call_or_stream(rgc, ctx):
+    import torch
+    g = np.random.default_rng(30)
+    z = logits_like(g, 5, 140_001)
+    targets, grads = g.integers(0, 140_001, 5), (g.standard_normal(5), g.standard_normal(5))
+    first = run_scores(rgc, ctx, z, "bf16", targets, 20, 1.0, grads=grads)[1]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        second = run_scores(rgc, ctx, z, "bf16", targets, 20, 1.0, grads=grads, stream=side)[1]
+    for k in first:
+        assert np.array_equal(first[k], second[k]), k
+
+
+def test_replayed_from_a_graph(rgc, ctx):
+    import torch
+    g = np.random.default_rng(31)
+    for rows, vocab in ((3, 140_001), (40, 5_000)):
+        logits = torch.empty(rows, vocab, dtype=torch.bfloat16, device="cuda")
+        targets = torch.zeros(rows, dtype=torch.int32, device="cuda")
+        out = {"logprob": torch.empty(rows, device="cuda"), "entropy": torch.empty(rows, device="cuda"), "stats": torch.empty(rows, 2, device="cuda"),
+               "top_idx": torch.empty(rows, 10, dtype=torch.int32, device="cuda"), "top_logprob": torch.empty(rows, 10, device="cuda")}
+        scores = rgc.TokenScores(logits, targets, **out)
+        weight, grad, dgrad = torch.ones(rows, device="cuda"), torch.empty_like(logits), torch.empty_like(logits)
+        loss = torch.empty(rows, device="cuda")
+        distill = rgc.Distillation(logits, out["top_idx"], out["top_logprob"], targets=targets, loss=loss, grad_logits=dgrad,
+                                   temperature=2.0, soft_weight=0.5, label_weight=0.5)
+        s = torch.cuda.Stream()
+
+        def step(stream):
+            rgc.rgc_token_logprobs(ctx, scores, stream)
+            rgc.rgc_token_logprobs_backward(ctx, scores, grad, weight, weight, stream)
+            rgc.rgc_distill_loss(ctx, distill, stream)
+
+        def fill(i):
+            logits.copy_(torch.from_numpy(logits_like(np.random.default_rng(i), rows, vocab)))
+            targets.copy_(torch.from_numpy(np.random.default_rng(i).integers(0, vocab, rows).astype(np.int32)))
+
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            fill(0)
+            step(s)
+            s.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=s):
+                step(torch.cuda.current_stream())
+            for i in range(1, 5):
+                fill(i)
+                graph.replay()
+                s.synchronize()
+                replayed = [t.clone() for t in (*out.values(), grad, dgrad, loss)]
+                step(s)
+                s.synchronize()
+                for a, b in zip(replayed, (*out.values(), grad, dgrad, loss)):
+                    assert torch.equal(a, b)
+        torch.cuda.synchronize()
+
+
+def refused(rgc, make):
+    with pytest.raises(rgc.RgcError) as e:
+        make()
+    assert e.value.status == -1
+
+
+def test_refusals(rgc, ctx):
+    import torch
+    dev = "cuda"
+    z = torch.zeros(4, 10, device=dev)
+    t, f = torch.zeros(4, dtype=torch.int32, device=dev), torch.zeros(4, device=dev)
+    idx, val = torch.zeros(4, 3, dtype=torch.int32, device=dev), torch.zeros(4, 3, device=dev)
+    S, D = rgc.TokenScores, rgc.Distillation
+    # what only the binding can see
+    refused(rgc, lambda: S(z.double()))
+    refused(rgc, lambda: S(z.t()))
+    refused(rgc, lambda: S(z[0]))
+    refused(rgc, lambda: S(z, t.long(), logprob=f))
+    refused(rgc, lambda: S(z, t[:3], logprob=f))
+    refused(rgc, lambda: S(z, t, logprob=f.half()))
+    refused(rgc, lambda: S(z, t, top_idx=idx))
+    refused(rgc, lambda: S(z, t, top_idx=idx, top_logprob=val[:, :2]))
+    refused(rgc, lambda: S(z, t.cpu(), logprob=f))
+    refused(rgc, lambda: D(z, idx, val.half()))
+    refused(rgc, lambda: D(z, idx, val, grad_logits=z.half()))
+    refused(rgc, lambda: D(z, idx, val, grad_logits=z[:, :9]))
+    # what the library checks
+    refused(rgc, lambda: rgc.rgc_token_logprobs(ctx, S(z, logprob=f)))                          # logprob without targets
+    for bad in (0.0, -1.0, math.nan, math.inf, 1e-39):
+        refused(rgc, lambda: rgc.rgc_token_logprobs(ctx, S(z, t, logprob=f, temperature=bad)))
+        refused(rgc, lambda: rgc.rgc_distill_loss(ctx, D(z, idx, val, loss=f, temperature=bad)))
+    many = torch.zeros(4, 11, dtype=torch.int32, device=dev)
+    refused(rgc, lambda: rgc.rgc_token_logprobs(ctx, S(z, t, top_idx=many, top_logprob=many.float())))      # more than words
+    wide, many = torch.zeros(4, 200, device=dev), torch.zeros(4, 129, dtype=torch.int32, device=dev)
+    refused(rgc, lambda: rgc.rgc_token_logprobs(ctx, S(wide, t, top_idx=many, top_logprob=many.float())))   # more than RGC_TOP_MAX
+    refused(rgc, lambda: rgc.rgc_distill_loss(ctx, D(wide, many, many.float(), loss=f)))
+    for weights in ((-1.0, 0.0), (0.0, math.nan), (math.inf, 0.0)):
+        refused(rgc, lambda: rgc.rgc_distill_loss(ctx, D(z, idx, val, loss=f, soft_weight=weights[0], label_weight=weights[1])))
+    scored = S(z, t, logprob=f, entropy=f.clone(), stats=torch.zeros(4, 2, device=dev))
+    refused(rgc, lambda: rgc.rgc_token_logprobs_backward(ctx, S(z, t, logprob=f), torch.empty_like(z), f))   # no stats
+    refused(rgc, lambda: rgc.rgc_token_logprobs_backward(ctx, scored, torch.empty_like(z)[:, :9], f))
+    refused(rgc, lambda: rgc.rgc_token_logprobs_backward(ctx, S(z, t, stats=torch.zeros(4, 2, device=dev)), torch.empty_like(z), f, f))
+    lib = rgc.load_library()
+    d = S(z, t, logprob=f)
+    for change in ({"row_stride": 9}, {"rows": -1}, {"rows": 2 ** 31}, {"vocab": 0}, {"dtype": 3}, {"dtype": -1}, {"logits": None},
+                   {"logits": z.data_ptr() + 2}, {"logprob": f.data_ptr() + 1}, {"targets": t.data_ptr() + 2}, {"top": -1}):
+        d = S(z, t, logprob=f)
+        for k, v in change.items():
+            setattr(d.desc, k, v)
+        assert lib.rgc_token_logprobs(ctx.handle, ctypes.byref(d.desc), None) == -1, change
+    assert lib.rgc_token_logprobs(None, ctypes.byref(d.desc), None) == -1
+    assert lib.rgc_token_logprobs(ctx.handle, None, None) == -1
+    assert lib.rgc_distill_loss(ctx.handle, None, None) == -1
+    # nothing to do is no error
+    none = torch.zeros(0, 10, device=dev)
+    rgc.rgc_token_logprobs(ctx, S(none, t[:0], logprob=f[:0], stats=torch.zeros(0, 2, device=dev)))
+    rgc.rgc_token_logprobs_backward(ctx, S(none, t[:0], logprob=f[:0], stats=torch.zeros(0, 2, device=dev)), none)
+    rgc.rgc_distill_loss(ctx, D(none, idx[:0], val[:0], loss=f[:0], grad_logits=none))
+    torch.cuda.synchronize()
