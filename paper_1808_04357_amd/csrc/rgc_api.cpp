@@ -259,6 +259,7 @@ struct rgc_ctx {
   DevBuf<float> d_slots_u;                 // the velocity of every listed element (first use)
   DevBuf<unsigned long long> d_members2;   // member pool of the dense layers (first use)
   DevBuf<uint32_t> d_shards;               // their sub-list counters (first use)
+  DevBuf<unsigned long long> d_lm;         // scratch of the language model's operators (first use, grows)
   CompressPlan plans[kPlanCache];
   uint64_t tick = 0;
   int64_t optional_scratch_cap = -1;       // bytes the dense layers' lists may take (diagnostics); negative: no cap
@@ -597,6 +598,7 @@ int rgc_destroy(rgc_ctx* ctx) {
   ctx->d_norm_part.release();
   ctx->d_mean_part.release();
   ctx->d_moments.release();
+  ctx->d_lm.release();
   ctx->missing.release();                  // (the frees above have waited for the kernels that may write to it)
   for (auto* v : {&ctx->ev_compress, &ctx->ev_decompress, &ctx->ev_pool})
     for (hipEvent_t e : *v) (void)hipEventDestroy(e);
@@ -1342,6 +1344,17 @@ bool recurrence_fits(const rgc_recurrence* r) {
          (!r->out_gate.data || sequence_fits(r->out_gate, r, false));
 }
 
+// Room for `words` in the operators' scratch.  (Replacing it waits for what still uses the old one: hipFree does.)
+int lm_scratch(rgc_ctx* ctx, uint64_t words) {
+  if (words <= ctx->d_lm.n) return RGC_OK;
+  const hipError_t e = ctx->d_lm.alloc(words);
+  if (e == hipErrorOutOfMemory) {
+    (void)hipGetLastError();
+    return RGC_ENOMEM;
+  }
+  return e == hipSuccess ? RGC_OK : fail_hip(e, "scratch of the language model's operators");
+}
+
 SequenceView view_of(const rgc_sequence& v) { return SequenceView{v.data, v.batch_stride, v.step_stride}; }
 
 RecurrenceArgs recurrence_args(const rgc_recurrence* r) {
@@ -1453,7 +1466,10 @@ int rgc_gated_recurrence(rgc_ctx* ctx, const rgc_recurrence* r, void* hip_stream
   if (r->batch == 0) return RGC_OK;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
-  RGC_HIP(launch_recurrence(recurrence_args(r), r->dtype, static_cast<hipStream_t>(hip_stream)));
+  const RecurrenceArgs A = recurrence_args(r);
+  const int rc = lm_scratch(ctx, recurrence_scratch_words(A, r->dtype, false));
+  if (rc != RGC_OK) return rc;
+  RGC_HIP(launch_recurrence(A, r->dtype, ctx->d_lm.p, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 
@@ -1473,7 +1489,10 @@ int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* r, const r
   G.dout_gate = view_of(g->dout_gate);
   G.dh_last = g->dh_last;
   G.dh0 = g->dh0;
-  RGC_HIP(launch_recurrence_backward(recurrence_args(r), G, r->dtype, static_cast<hipStream_t>(hip_stream)));
+  const RecurrenceArgs A = recurrence_args(r);
+  const int rc = lm_scratch(ctx, recurrence_scratch_words(A, r->dtype, true));
+  if (rc != RGC_OK) return rc;
+  RGC_HIP(launch_recurrence_backward(A, G, r->dtype, ctx->d_lm.p, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 

@@ -72,10 +72,18 @@ struct RecurrenceGradArgs {
   float* dh0;
 };
 
+// How a recurrence is cut into tiles (workgroups), and what they tell each other.
+struct TileArgs {
+  uint32_t across, tiles;        // chains a sequence has (stretches of channels), tiles a chain has
+  unsigned long long* words;     // [chains][tiles][channels of a tile]
+  uint32_t* ticket;
+};
+
 hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, hipStream_t s);
 hipError_t launch_token_logprobs_backward(const ScoreGradArgs& a, int dtype, hipStream_t s);
 hipError_t launch_distill(const DistillArgs& a, int dtype, hipStream_t s);
-hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, hipStream_t s);
-hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, hipStream_t s);
+uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backward);      // 64-bit words of `scratch`
+hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, hipStream_t s);
+hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s);
 
 }  // namespace rgc
