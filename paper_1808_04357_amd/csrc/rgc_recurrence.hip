@@ -58,17 +58,59 @@ struct alignas(sizeof(T)) Raw {
   T v[kVec];
 };
 
+// A tensor's rows from a step on: an address that is the same for the whole wave, which a step moves on, and a lane's offset from it.
+template <typename T>
+struct Rows {
+  char* p;
+  int64_t step;                       // bytes
+  __device__ Rows(const SequenceView& v, uint32_t b, uint32_t t)
+      : p(reinterpret_cast<char*>(static_cast<T*>(v.data) + (b * v.batch_stride + t * v.step_stride))), step(v.step_stride * static_cast<int64_t>(sizeof(T))) {}
+};
+
 template <typename T, int kVec>
-__device__ __forceinline__ Raw<T, kVec> read(const T* p) {
+__device__ __forceinline__ Raw<T, kVec> read(const char* row, uint32_t offset) {
+  Raw<T, kVec> r;
   if constexpr (sizeof(T) * kVec == 4) {
-    const uint32_t w = *reinterpret_cast<const word*>(p);
-    Raw<T, kVec> r;
+    const uint32_t w = *reinterpret_cast<const word*>(row + offset);
     __builtin_memcpy(&r, &w, 4);
-    return r;
   } else {
-    return *reinterpret_cast<const Raw<T, kVec>*>(p);
+    r = *reinterpret_cast<const Raw<T, kVec>*>(row + offset);
+  }
+  return r;
+}
+
+template <typename T, int kVec>
+__device__ __forceinline__ void write(char* row, uint32_t offset, const float (&v)[kVec]) {
+  Raw<T, kVec> r;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) r.v[i] = static_cast<T>(v[i]);
+  if constexpr (sizeof(T) * kVec == 4) {
+    uint32_t w;
+    __builtin_memcpy(&w, &r, 4);
+    *reinterpret_cast<word*>(row + offset) = w;
+  } else {
+    *reinterpret_cast<Raw<T, kVec>*>(row + offset) = r;
   }
 }
+
+// A wave's steps of one tensor, all asked for at once.  Steps at `end` and beyond are read as the last one before: a branch around every
+// read makes the compiler wait for one before it asks for the next.
+template <typename T, int kVec, int kSteps, bool kWhole>
+__device__ __forceinline__ void read_steps(Raw<T, kVec> (&to)[kSteps], const SequenceView& v, uint32_t b, uint32_t first, uint32_t end, uint32_t offset) {
+  Rows<T> rows(v, b, first);
+#pragma unroll
+  for (uint32_t r = 0; r < kSteps; ++r) {
+    to[r] = read<T, kVec>(rows.p, offset);
+    if (kWhole || first + r + 1u < end) rows.p += rows.step;
+  }
+}
+
+struct Yes {
+  constexpr operator bool() const { return true; }
+};
+struct No {
+  constexpr operator bool() const { return false; }
+};
 
 // Where a lane's channels lie.  The last lane of a row with an odd number of channels takes the two last ones and stores the second only; lanes
 // behind the row's end work on the last channels too, so that all lanes do the same, and store nothing.
@@ -84,22 +126,10 @@ struct Lane {
   }
 };
 
-template <typename T, int kVec>
-__device__ __forceinline__ void store(T* row, const Lane<kVec>& lane, const float (&v)[kVec]) {
-  if (lane.all) {
-    Raw<T, kVec> r;
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) r.v[i] = static_cast<T>(v[i]);
-    if constexpr (sizeof(T) * kVec == 4) {
-      uint32_t w;
-      __builtin_memcpy(&w, &r, 4);
-      *reinterpret_cast<word*>(row + lane.c) = w;
-    } else {
-      *reinterpret_cast<Raw<T, kVec>*>(row + lane.c) = r;
-    }
-  } else if (lane.last) {
-    row[lane.c + kVec - 1] = static_cast<T>(v[kVec - 1]);
-  }
+template <typename T, int kVec, bool kWhole>
+__device__ __forceinline__ void store(char* row, const Lane<kVec>& lane, const float (&v)[kVec]) {
+  if (kWhole || lane.all) write<T, kVec>(row, lane.c * static_cast<uint32_t>(sizeof(T)), v);
+  else if (lane.last) reinterpret_cast<T*>(row)[lane.c + kVec - 1] = static_cast<T>(v[kVec - 1]);
 }
 template <int kVec>
 __device__ __forceinline__ void store_state(float* row, const Lane<kVec>& lane, const float (&v)[kVec]) {
@@ -123,11 +153,6 @@ __device__ __forceinline__ uint32_t resets_of(const RecurrenceArgs& A, uint32_t 
   const uint32_t t = first + (threadIdx.x & 63u);
   const bool anew = (threadIdx.x & 63u) < kSteps && t < end && A.resets[static_cast<uint64_t>(b) * A.steps + t] != 0;
   return static_cast<uint32_t>(__ballot(anew));
-}
-
-template <typename T>
-__device__ __forceinline__ T* row_at(const SequenceView& v, uint32_t b, uint32_t t) {
-  return static_cast<T*>(v.data) + (b * v.batch_stride + t * v.step_stride);
 }
 
 // Which tile this workgroup works on: by ticket where tiles wait for each other.
@@ -190,6 +215,7 @@ __device__ __forceinline__ void look_back(const TileArgs& G, const Place& at, ui
     bool open = false;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
+#pragma unroll 4
       for (uint32_t j = 0; j < kWaves && j < next; ++j) seen[i] = both(lds[j][lane * kVec + i], seen[i]);
       open |= !cut(seen[i].p);
     }
@@ -202,55 +228,61 @@ __device__ __forceinline__ void look_back(const TileArgs& G, const Place& at, ui
   for (int i = 0; i < kVec; ++i) carry[i] = seen[i].h;
 }
 
-template <typename T, int kVec, int kWaves, int kSteps>
-__global__ void __launch_bounds__(64 * kWaves) recurrence_kernel(RecurrenceArgs A, TileArgs G) {
+template <int kVec, int kWaves>
+struct Shared {
+  Stretch parts[kWaves][64 * kVec], earlier[kWaves][64 * kVec];
+  uint32_t ticket;
+};
+
+// kWhole: all the tile's steps are there, and all its channels.  Otherwise steps behind the row's end become steps that change nothing (f = 1, u = 0).
+// What depends on a state starting anew stands in loops of its own, in two forms: the one without is taken by the waves that have none.
+template <typename T, int kVec, int kWaves, int kSteps, bool kGated, bool kWhole>
+__device__ __forceinline__ void forward_tile(const RecurrenceArgs& A, const TileArgs& G, const Place& at, uint32_t n, Shared<kVec, kWaves>& lds) {
   constexpr uint32_t kTile = kWaves * kSteps;
-  __shared__ Stretch parts[kWaves][64 * kVec];
-  __shared__ Stretch earlier[kWaves][64 * kVec];
-  __shared__ uint32_t lds_ticket;
-  const Place at = take_place(A, G, &lds_ticket);
+  auto& parts = lds.parts;
   const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, b = at.b;
   const Lane<kVec> mine(at.block, A.width);
-  const uint32_t n = length_of(A, b);
+  const uint32_t offset = mine.c * static_cast<uint32_t>(sizeof(T));
   const uint32_t first = at.order * kTile + wave * kSteps;           // this wave's steps
-  const uint32_t valid = n > first ? min(n - first, static_cast<uint32_t>(kSteps)) : 0u;
-  const uint32_t anew = resets_of<kSteps>(A, b, first, n);
-
+  const uint32_t valid = kWhole ? kSteps : n > first ? min(n - first, static_cast<uint32_t>(kSteps)) : 0u;
   Raw<T, kVec> x[kSteps], v[kSteps], w[kSteps];
-#pragma unroll
-  for (uint32_t r = 0; r < kSteps; ++r)
-    if (r < valid) {
-      v[r] = read<T, kVec>(row_at<T>(A.gate, b, first + r) + mine.c);
-      x[r] = read<T, kVec>(row_at<T>(A.x, b, first + r) + mine.c);
-    }
-  if (A.out_gate.data) {
-#pragma unroll
-    for (uint32_t r = 0; r < kSteps; ++r)
-      if (r < valid) w[r] = read<T, kVec>(row_at<T>(A.out_gate, b, first + r) + mine.c);
+  if (kWhole || valid > 0u) {
+    read_steps<T, kVec, kSteps, kWhole>(v, A.gate, b, first, n, offset);
+    read_steps<T, kVec, kSteps, kWhole>(x, A.x, b, first, n, offset);
+    if constexpr (kGated) read_steps<T, kVec, kSteps, kWhole>(w, A.out_gate, b, first, n, offset);
   }
+  const uint32_t anew = resets_of<kSteps>(A, b, first, n);
   float carry[kVec];
 #pragma unroll
   for (int i = 0; i < kVec; ++i) carry[i] = at.order == 0u && A.h0 ? A.h0[static_cast<uint64_t>(b) * A.width + mine.c + i] : 0.0f;
-
   float f[kSteps][kVec], u[kSteps][kVec];
+#pragma unroll
+  for (uint32_t r = 0; r < kSteps; ++r) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      float take;
+      gate_of(static_cast<float>(v[r].v[i]), f[r][i], take);
+      u[r][i] = take * static_cast<float>(x[r].v[i]);
+      if (!kWhole && r >= valid) f[r][i] = 1.0f, u[r][i] = 0.0f;
+    }
+  }
   Stretch own[kVec];
+  auto scan = [&](auto with_resets) __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) own[i] = Stretch{1.0f, 0.0f};
+    for (int i = 0; i < kVec; ++i) own[i] = Stretch{1.0f, 0.0f};
 #pragma unroll
-  for (uint32_t r = 0; r < kSteps; ++r)
-    if (r < valid) {
-      const bool starts = (anew >> r) & 1u;
+    for (uint32_t r = 0; r < kSteps; ++r) {
+      const bool starts = with_resets && ((anew >> r) & 1u) != 0u;
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        float take;
-        gate_of(static_cast<float>(v[r].v[i]), f[r][i], take);
-        u[r][i] = take * static_cast<float>(x[r].v[i]);
         if (starts) own[i] = Stretch{-0.0f, 0.0f};
         own[i].h = __fmaf_rn(f[r][i], own[i].h, u[r][i]);
         own[i].p *= f[r][i];
       }
     }
+  };
   if constexpr (kWaves > 1) {
+    if (anew == 0u) scan(No{}); else scan(Yes{});
 #pragma unroll
     for (int i = 0; i < kVec; ++i) parts[wave][lane * kVec + i] = own[i];
     __syncthreads();
@@ -261,111 +293,143 @@ __global__ void __launch_bounds__(64 * kWaves) recurrence_kernel(RecurrenceArgs 
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         whole[i] = own[i];
+#pragma unroll 4
         for (uint32_t j = 1; j < kWaves; ++j) whole[i] = both(whole[i], parts[j][lane * kVec + i]);
       }
       if (at.order > 0u && at.order + 1u < G.tiles) publish<kVec>(words_of<kVec>(G, at.chain, at.order), whole);
     }
-    if (at.order > 0u) look_back<kVec, kWaves>(G, at, wave, earlier, carry);
+    if (at.order > 0u) look_back<kVec, kWaves>(G, at, wave, lds.earlier, carry);
     if (wave == 0u && at.order + 1u < G.tiles) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) whole[i] = Stretch{-0.0f, after(whole[i], carry[i])};
       publish<kVec>(words_of<kVec>(G, at.chain, at.order), whole);
     }
   }
-  if (A.states && A.steps > 0u && wave == 0u && (at.order * kTile) % kChunk == 0u) {
+  if (A.states && wave == 0u && at.order * kTile < A.steps && (at.order * kTile) % kChunk == 0u) {
     const uint32_t chunks = (A.steps + kChunk - 1u) / kChunk;
     store_state<kVec>(A.states + (static_cast<uint64_t>(b) * chunks + at.order * kTile / kChunk) * A.width, mine, carry);
   }
 #pragma unroll
-  for (int i = 0; i < kVec; ++i)
+  for (int i = 0; i < kVec; ++i) {
+#pragma unroll 4
     for (uint32_t j = 0; j < wave; ++j) carry[i] = after(parts[j][lane * kVec + i], carry[i]);
+  }
+  // the states take the place of u, step by step
+  auto run = [&](auto with_resets) __attribute__((always_inline)) {
 #pragma unroll
-  for (uint32_t r = 0; r < kSteps; ++r) {
-    if (r < valid) {
-      float y[kVec];
-      const bool starts = (anew >> r) & 1u;
+    for (uint32_t r = 0; r < kSteps; ++r) {
+      const bool starts = with_resets && ((anew >> r) & 1u) != 0u;
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        if (starts) carry[i] = 0.0f;
-        carry[i] = __fmaf_rn(f[r][i], carry[i], u[r][i]);
-        y[i] = carry[i];
-        if (A.out_gate.data) {
-          float open, shut;
-          gate_of(static_cast<float>(w[r].v[i]), open, shut);
-          y[i] *= open;
-        }
-      }
-      store<T, kVec>(row_at<T>(A.y, b, first + r), mine, y);
-    } else if (first + r < A.steps) {
-      const float zero[kVec] = {};
-      store<T, kVec>(row_at<T>(A.y, b, first + r), mine, zero);
+      for (int i = 0; i < kVec; ++i) u[r][i] = carry[i] = __fmaf_rn(f[r][i], starts ? 0.0f : carry[i], u[r][i]);
     }
+  };
+  if (anew == 0u) run(No{}); else run(Yes{});
+  const uint32_t behind = kWhole ? kSteps : A.steps > first ? min(A.steps - first, static_cast<uint32_t>(kSteps)) : 0u;
+  Rows<T> to(A.y, b, first);
+#pragma unroll
+  for (uint32_t r = 0; r < kSteps; ++r, to.p += to.step) {
+    if (!kWhole && r >= behind) continue;
+    float y[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      y[i] = u[r][i];
+      if constexpr (kGated) {
+        float open, shut;
+        gate_of(static_cast<float>(w[r].v[i]), open, shut);
+        y[i] *= open;
+      }
+      if (!kWhole && r >= valid) y[i] = 0.0f;
+    }
+    store<T, kVec, kWhole>(to.p, mine, y);
   }
   if (A.h_last && at.order + 1u == G.tiles && wave + 1u == kWaves) store_state<kVec>(A.h_last + static_cast<uint64_t>(b) * A.width, mine, carry);
 }
 
-template <typename T, int kWaves, int kSteps>
-__global__ void __launch_bounds__(64 * kWaves) recurrence_backward_kernel(RecurrenceArgs A, RecurrenceGradArgs D, TileArgs G) {
+template <typename T, int kVec, int kWaves, int kSteps, bool kGated>
+__global__ void __launch_bounds__(64 * kWaves) recurrence_kernel(RecurrenceArgs A, TileArgs G) {
+  __shared__ Shared<kVec, kWaves> lds;
+  const Place at = take_place(A, G, &lds.ticket);
+  const uint32_t n = length_of(A, at.b);
+  if ((at.order + 1u) * (kWaves * kSteps) <= n && (at.block + 1u) * 64u * kVec <= A.width)
+    forward_tile<T, kVec, kWaves, kSteps, kGated, true>(A, G, at, n, lds);
+  else
+    forward_tile<T, kVec, kWaves, kSteps, kGated, false>(A, G, at, n, lds);
+}
+
+template <int kWaves>
+struct SharedBackward {
+  Stretch parts[kWaves][64], back[kWaves][64], earlier[kWaves][64];
+  uint32_t ticket;
+};
+
+template <typename T, int kWaves, int kSteps, bool kGated, bool kWhole>
+__device__ __forceinline__ void backward_tile(const RecurrenceArgs& A, const RecurrenceGradArgs& D, const TileArgs& G, const Place& at, uint32_t n,
+                                              SharedBackward<kWaves>& lds) {
   constexpr uint32_t kTile = kWaves * kSteps;
-  static_assert(kTile <= kChunk, "a tile begins with a kept state");
-  __shared__ Stretch parts[kWaves][64], back[kWaves][64];
-  __shared__ Stretch earlier[kWaves][64];
-  __shared__ uint32_t lds_ticket;
-  const Place at = take_place(A, G, &lds_ticket);
+  static_assert(kTile == kChunk || kTile <= 64u, "a tile begins with a kept state, the first one of a short sequence with the first");
+  auto& parts = lds.parts;
+  auto& back = lds.back;
   const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, b = at.b;
   const Lane<1> mine(at.block, A.width);
-  const uint32_t n = length_of(A, b);
+  const uint32_t offset = mine.c * static_cast<uint32_t>(sizeof(T));
   const uint32_t tile = G.tiles - 1u - at.order;                     // the last tile first
   const uint32_t first = tile * kTile + wave * kSteps;
-  const uint32_t valid = n > first ? min(n - first, static_cast<uint32_t>(kSteps)) : 0u;
-  const uint32_t anew = resets_of<kSteps>(A, b, first, n);
+  const uint32_t valid = kWhole ? kSteps : n > first ? min(n - first, static_cast<uint32_t>(kSteps)) : 0u;
   const uint64_t state_at = static_cast<uint64_t>(b) * A.width + mine.c;
-
-  T x[kSteps], v[kSteps], w[kSteps], dy[kSteps];
-#pragma unroll
-  for (uint32_t r = 0; r < kSteps; ++r)
-    if (r < valid) {
-      v[r] = row_at<T>(A.gate, b, first + r)[mine.c];
-      x[r] = row_at<T>(A.x, b, first + r)[mine.c];
-    }
-#pragma unroll
-  for (uint32_t r = 0; r < kSteps; ++r)
-    if (r < valid) dy[r] = row_at<T>(D.dy, b, first + r)[mine.c];
-  if (A.out_gate.data) {
-#pragma unroll
-    for (uint32_t r = 0; r < kSteps; ++r)
-      if (r < valid) w[r] = row_at<T>(A.out_gate, b, first + r)[mine.c];
+  Raw<T, 1> read_x[kSteps], v[kSteps], w[kSteps], dy[kSteps];
+  if (kWhole || valid > 0u) {
+    read_steps<T, 1, kSteps, kWhole>(v, A.gate, b, first, n, offset);
+    read_steps<T, 1, kSteps, kWhole>(read_x, A.x, b, first, n, offset);
+    if constexpr (kGated) read_steps<T, 1, kSteps, kWhole>(w, A.out_gate, b, first, n, offset);
+    read_steps<T, 1, kSteps, kWhole>(dy, D.dy, b, first, n, offset);
   }
+  const uint32_t anew = resets_of<kSteps>(A, b, first, n);
   const uint32_t chunks = (A.steps + kChunk - 1u) / kChunk;
   float h = chunks > 0u ? A.states[(static_cast<uint64_t>(b) * chunks + tile) * A.width + mine.c] : 0.0f;
   float carry[1] = {at.order == 0u && D.dh_last ? D.dh_last[state_at] : 0.0f};
 
   // e: the gradient that y brings to the state; shut: 1 - o
-  float f[kSteps], take[kSteps], e[kSteps], shut[kSteps];
-  Stretch own{1.0f, 0.0f};
+  float f[kSteps], take[kSteps], x[kSteps], e[kSteps], shut[kSteps];
 #pragma unroll
-  for (uint32_t r = 0; r < kSteps; ++r)
-    if (r < valid) {
-      gate_of(static_cast<float>(v[r]), f[r], take[r]);
-      if ((anew >> r) & 1u) own = Stretch{-0.0f, 0.0f};
-      own.h = __fmaf_rn(f[r], own.h, take[r] * static_cast<float>(x[r]));
-      own.p *= f[r];
-      e[r] = static_cast<float>(dy[r]);
-      if (A.out_gate.data) {
-        float open;
-        gate_of(static_cast<float>(w[r]), open, shut[r]);
-        e[r] *= open;
-      }
+  for (uint32_t r = 0; r < kSteps; ++r) {
+    gate_of(static_cast<float>(v[r].v[0]), f[r], take[r]);
+    x[r] = static_cast<float>(read_x[r].v[0]);
+    if (!kWhole && r >= valid) f[r] = 1.0f, take[r] = 0.0f, x[r] = 0.0f;
+  }
+#pragma unroll
+  for (uint32_t r = 0; r < kSteps; ++r) {
+    e[r] = static_cast<float>(dy[r].v[0]);
+    if constexpr (kGated) {
+      float open;
+      gate_of(static_cast<float>(w[r].v[0]), open, shut[r]);
+      e[r] *= open;
     }
-  Stretch rear{1.0f, 0.0f};                                          // from the gradient that comes in behind the steps to the one that leaves before them
+    if (!kWhole && r >= valid) e[r] = 0.0f;
+  }
+  // (Held as they are: the compiler would rather keep each one's power and reciprocal for later, which is twice the registers.)
 #pragma unroll
-  for (uint32_t r = kSteps; r-- > 0u;)
-    if (r < valid) {
+  for (uint32_t r = 0; r < kSteps; ++r) {
+    asm volatile("" : "+v"(f[r]), "+v"(take[r]), "+v"(x[r]), "+v"(e[r]));
+    if constexpr (kGated) asm volatile("" : "+v"(shut[r]));
+  }
+  Stretch own, rear;                 // rear: from the gradient that comes in behind the steps to the one that leaves before them
+  auto scan = [&](auto with_resets) __attribute__((always_inline)) {
+    own = rear = Stretch{1.0f, 0.0f};
+#pragma unroll
+    for (uint32_t r = 0; r < kSteps; ++r) {
+      if (with_resets && ((anew >> r) & 1u) != 0u) own = Stretch{-0.0f, 0.0f};
+      own.h = __fmaf_rn(f[r], own.h, take[r] * x[r]);
+      own.p *= f[r];
+    }
+#pragma unroll
+    for (uint32_t r = kSteps; r-- > 0u;) {
       rear.h = f[r] * (e[r] + rear.h);
       rear.p *= f[r];
-      if ((anew >> r) & 1u) rear = Stretch{-0.0f, 0.0f};
+      if (with_resets && ((anew >> r) & 1u) != 0u) rear = Stretch{-0.0f, 0.0f};
     }
+  };
   if constexpr (kWaves > 1) {
+    if (anew == 0u) scan(No{}); else scan(Yes{});
     parts[wave][lane] = own;
     back[wave][lane] = rear;
     __syncthreads();
@@ -374,43 +438,63 @@ __global__ void __launch_bounds__(64 * kWaves) recurrence_backward_kernel(Recurr
     Stretch whole[1];
     if (wave == 0u) {
       whole[0] = back[kWaves - 1][lane];
+#pragma unroll 4
       for (uint32_t j = kWaves - 1u; j-- > 0u;) whole[0] = both(whole[0], back[j][lane]);
       if (at.order > 0u && at.order + 1u < G.tiles) publish<1>(words_of<1>(G, at.chain, at.order), whole);
     }
-    if (at.order > 0u) look_back<1, kWaves>(G, at, wave, earlier, carry);
+    if (at.order > 0u) look_back<1, kWaves>(G, at, wave, lds.earlier, carry);
     if (wave == 0u && at.order + 1u < G.tiles) {
       whole[0] = Stretch{-0.0f, after(whole[0], carry[0])};
       publish<1>(words_of<1>(G, at.chain, at.order), whole);
     }
   }
+#pragma unroll 4
   for (uint32_t j = 0; j < wave; ++j) h = after(parts[j][lane], h);
   float g = carry[0];
+#pragma unroll 4
   for (uint32_t j = kWaves - 1u; j > wave; --j) g = after(back[j][lane], g);
-  float before[kSteps];
+  float before[kSteps];              // the state before the step
+  const uint32_t behind = kWhole ? kSteps : A.steps > first ? min(A.steps - first, static_cast<uint32_t>(kSteps)) : 0u;
+  Rows<T> to_out(D.dout_gate, b, first), to_x(D.dx, b, first + kSteps - 1u), to_gate(D.dgate, b, first + kSteps - 1u);
 #pragma unroll
-  for (uint32_t r = 0; r < kSteps; ++r)
-    if (r < valid) {
-      if ((anew >> r) & 1u) h = 0.0f;
+  for (uint32_t r = 0; r < kSteps; ++r) asm volatile("" : "+v"(x[r]));      // (keeps take * x from being held in sixteen more registers)
+  auto finish = [&](auto with_resets) __attribute__((always_inline)) {
+#pragma unroll
+    for (uint32_t r = 0; r < kSteps; ++r, to_out.p += to_out.step) {
+      if (with_resets && ((anew >> r) & 1u) != 0u) h = 0.0f;
       before[r] = h;
-      h = __fmaf_rn(f[r], h, take[r] * static_cast<float>(x[r]));
+      h = __fmaf_rn(f[r], h, take[r] * x[r]);
+      if constexpr (kGated) {
+        const float dout[1] = {kWhole || r < valid ? shut[r] * e[r] * h : 0.0f};
+        if (kWhole || r < behind) store<T, 1, kWhole>(to_out.p, mine, dout);
+      }
     }
 #pragma unroll
-  for (uint32_t r = kSteps; r-- > 0u;) {
-    float dx[1] = {0.0f}, dgate[1] = {0.0f}, dout[1] = {0.0f};
-    if (r < valid) {
-      const float d = e[r] + g, xr = static_cast<float>(x[r]);
-      dx[0] = d * take[r];
-      dgate[0] = dx[0] * (before[r] - xr) * f[r];
-      if (A.out_gate.data) dout[0] = e[r] * shut[r] * __fmaf_rn(f[r], before[r], take[r] * xr);
-      g = (anew >> r) & 1u ? 0.0f : f[r] * d;
+    for (uint32_t r = kSteps; r-- > 0u; to_x.p -= to_x.step, to_gate.p -= to_gate.step) {
+      const float d = e[r] + g;      // the gradient of the state after the step
+      float dx[1] = {d * take[r]}, dgate[1] = {d * take[r] * (before[r] - x[r]) * f[r]};
+      if (!kWhole && r >= valid) dx[0] = dgate[0] = 0.0f;
+      g = f[r] * d;
+      if (with_resets && ((anew >> r) & 1u) != 0u) g = 0.0f;
+      if (kWhole || r < behind) {
+        store<T, 1, kWhole>(to_x.p, mine, dx);
+        store<T, 1, kWhole>(to_gate.p, mine, dgate);
+      }
     }
-    if (first + r < A.steps) {
-      store<T, 1>(row_at<T>(D.dx, b, first + r), mine, dx);
-      store<T, 1>(row_at<T>(D.dgate, b, first + r), mine, dgate);
-      if (A.out_gate.data) store<T, 1>(row_at<T>(D.dout_gate, b, first + r), mine, dout);
-    }
-  }
+  };
+  if (anew == 0u) finish(No{}); else finish(Yes{});
   if (D.dh0 && tile == 0u && wave == 0u && mine.all) D.dh0[state_at] = g;
+}
+
+template <typename T, int kWaves, int kSteps, bool kGated>
+__global__ void __launch_bounds__(64 * kWaves) recurrence_backward_kernel(RecurrenceArgs A, RecurrenceGradArgs D, TileArgs G) {
+  __shared__ SharedBackward<kWaves> lds;
+  const Place at = take_place(A, G, &lds.ticket);
+  const uint32_t n = length_of(A, at.b);
+  if ((G.tiles - at.order) * (kWaves * kSteps) <= n && (at.block + 1u) * 64u <= A.width)
+    backward_tile<T, kWaves, kSteps, kGated, true>(A, D, G, at, n, lds);
+  else
+    backward_tile<T, kWaves, kSteps, kGated, false>(A, D, G, at, n, lds);
 }
 
 __global__ void __launch_bounds__(256) clear_words_kernel(TileArgs G, uint64_t words) {
@@ -419,22 +503,34 @@ __global__ void __launch_bounds__(256) clear_words_kernel(TileArgs G, uint64_t w
   if (i == 0u) *G.ticket = 0u;
 }
 
-struct Cut {
-  uint32_t vec, waves, steps;      // channels a lane, waves a workgroup, steps a wave
+// How a sequence is cut: the same constants make the tiles and choose the kernel.
+struct Shape {
+  uint32_t waves, steps;           // waves a workgroup, steps a wave
+  constexpr uint32_t tile() const { return waves * steps; }
 };
+constexpr Shape kOneWave{1, 4}, kShort{4, 16}, kLong{4, 16}, kLongBackward{16, 16};
+enum class Kind { kOneWave, kShort, kLong };
+
+struct Cut {
+  Kind kind;
+  uint32_t vec;                    // channels a lane
+};
+
+constexpr Shape shape_of(Kind kind, bool backward) {
+  return kind == Kind::kOneWave ? kOneWave : kind == Kind::kShort ? kShort : backward ? kLongBackward : kLong;
+}
 
 Cut cut_of(const RecurrenceArgs& a, int dtype, bool backward) {
   Cut c;
   c.vec = !backward && dtype != 0 && a.width > 64u ? 2u : 1u;
-  c.waves = a.steps <= 4u ? 1u : a.steps <= 64u ? 4u : backward ? 16u : 8u;
-  c.steps = a.steps <= 16u ? 4u : 16u;
+  c.kind = a.steps <= kOneWave.tile() ? Kind::kOneWave : a.steps <= kShort.tile() ? Kind::kShort : Kind::kLong;
   return c;
 }
 
-TileArgs tiles_of(const RecurrenceArgs& a, const Cut& c) {
+TileArgs tiles_of(const RecurrenceArgs& a, const Cut& c, bool backward) {
   TileArgs G{};
   G.across = (a.width + 64u * c.vec - 1u) / (64u * c.vec);
-  const uint32_t tile = c.waves * c.steps;
+  const uint32_t tile = shape_of(c.kind, backward).tile();
   G.tiles = a.steps == 0u ? 1u : (a.steps + tile - 1u) / tile;
   return G;
 }
@@ -457,55 +553,74 @@ hipError_t clear_words(TileArgs& G, uint64_t words, unsigned long long* scratch,
   return hipGetLastError();
 }
 
-template <typename T, int kVec>
+template <typename T, int kVec, bool kGated, uint32_t kWaves, uint32_t kSteps>
+void launch_forward(const RecurrenceArgs& a, const TileArgs& G, uint32_t wgs, hipStream_t s) {
+  recurrence_kernel<T, kVec, kWaves, kSteps, kGated><<<dim3(wgs), dim3(64u * kWaves), 0, s>>>(a, G);
+}
+template <typename T, int kVec, bool kGated>
 void launch_forward(const RecurrenceArgs& a, const Cut& c, const TileArgs& G, uint32_t wgs, hipStream_t s) {
-  if (c.waves == 1u) recurrence_kernel<T, kVec, 1, 4><<<dim3(wgs), dim3(64), 0, s>>>(a, G);
-  else if (c.steps == 4u) recurrence_kernel<T, kVec, 4, 4><<<dim3(wgs), dim3(256), 0, s>>>(a, G);
-  else if (c.waves == 4u) recurrence_kernel<T, kVec, 4, 16><<<dim3(wgs), dim3(256), 0, s>>>(a, G);
-  else recurrence_kernel<T, kVec, 8, 16><<<dim3(wgs), dim3(512), 0, s>>>(a, G);
+  if (c.kind == Kind::kOneWave) launch_forward<T, kVec, kGated, kOneWave.waves, kOneWave.steps>(a, G, wgs, s);
+  else if (c.kind == Kind::kShort) launch_forward<T, kVec, kGated, kShort.waves, kShort.steps>(a, G, wgs, s);
+  else launch_forward<T, kVec, kGated, kLong.waves, kLong.steps>(a, G, wgs, s);
 }
 
-template <typename T>
+template <typename T, bool kGated, uint32_t kWaves, uint32_t kSteps>
+void launch_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& d, const TileArgs& G, uint32_t wgs, hipStream_t s) {
+  recurrence_backward_kernel<T, kWaves, kSteps, kGated><<<dim3(wgs), dim3(64u * kWaves), 0, s>>>(a, d, G);
+}
+template <typename T, bool kGated>
 void launch_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& d, const Cut& c, const TileArgs& G, uint32_t wgs, hipStream_t s) {
-  if (c.waves == 1u) recurrence_backward_kernel<T, 1, 4><<<dim3(wgs), dim3(64), 0, s>>>(a, d, G);
-  else if (c.steps == 4u) recurrence_backward_kernel<T, 4, 4><<<dim3(wgs), dim3(256), 0, s>>>(a, d, G);
-  else if (c.waves == 4u) recurrence_backward_kernel<T, 4, 16><<<dim3(wgs), dim3(256), 0, s>>>(a, d, G);
-  else recurrence_backward_kernel<T, 16, 16><<<dim3(wgs), dim3(1024), 0, s>>>(a, d, G);
+  if (c.kind == Kind::kOneWave) launch_backward<T, kGated, kOneWave.waves, kOneWave.steps>(a, d, G, wgs, s);
+  else if (c.kind == Kind::kShort) launch_backward<T, kGated, kShort.waves, kShort.steps>(a, d, G, wgs, s);
+  else launch_backward<T, kGated, kLongBackward.waves, kLongBackward.steps>(a, d, G, wgs, s);
+}
+
+// One of the two template arguments a run decides.
+template <typename T, typename F>
+void by_gate(const RecurrenceArgs& a, F&& f) {
+  if (a.out_gate.data) f(T{}, Yes{}); else f(T{}, No{});
 }
 
 }  // namespace
 
 uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backward) {
   const Cut c = cut_of(a, dtype, backward);
-  const uint64_t words = words_for(a, c, tiles_of(a, c));
+  const uint64_t words = words_for(a, c, tiles_of(a, c, backward));
   return words ? words + 1u : 0u;
 }
 
 hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, hipStream_t s) {
   const Cut c = cut_of(a, dtype, false);
-  TileArgs G = tiles_of(a, c);
+  TileArgs G = tiles_of(a, c, false);
   const uint32_t wgs = workgroups(a, G);
   if (wgs == 0u) return hipErrorInvalidValue;
   const hipError_t e = clear_words(G, words_for(a, c, G), scratch, s);
   if (e != hipSuccess) return e;
-  if (dtype == 0) launch_forward<float, 1>(a, c, G, wgs, s);
-  else if (dtype == 1 && c.vec == 2u) launch_forward<__bf16, 2>(a, c, G, wgs, s);
-  else if (dtype == 1) launch_forward<__bf16, 1>(a, c, G, wgs, s);
-  else if (c.vec == 2u) launch_forward<_Float16, 2>(a, c, G, wgs, s);
-  else launch_forward<_Float16, 1>(a, c, G, wgs, s);
+  auto launch = [&](auto type, auto gated) {
+    using T = decltype(type);
+    constexpr bool kGated = decltype(gated){};
+    if constexpr (sizeof(T) == 2) {
+      if (c.vec == 2u) return launch_forward<T, 2, kGated>(a, c, G, wgs, s);
+    }
+    launch_forward<T, 1, kGated>(a, c, G, wgs, s);
+  };
+  if (dtype == 0) by_gate<float>(a, launch);
+  else if (dtype == 1) by_gate<__bf16>(a, launch);
+  else by_gate<_Float16>(a, launch);
   return hipGetLastError();
 }
 
 hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s) {
   const Cut c = cut_of(a, dtype, true);
-  TileArgs G = tiles_of(a, c);
+  TileArgs G = tiles_of(a, c, true);
   const uint32_t wgs = workgroups(a, G);
   if (wgs == 0u) return hipErrorInvalidValue;
   const hipError_t e = clear_words(G, words_for(a, c, G), scratch, s);
   if (e != hipSuccess) return e;
-  if (dtype == 0) launch_backward<float>(a, g, c, G, wgs, s);
-  else if (dtype == 1) launch_backward<__bf16>(a, g, c, G, wgs, s);
-  else launch_backward<_Float16>(a, g, c, G, wgs, s);
+  auto launch = [&](auto type, auto gated) { launch_backward<decltype(type), bool(decltype(gated){})>(a, g, c, G, wgs, s); };
+  if (dtype == 0) by_gate<float>(a, launch);
+  else if (dtype == 1) by_gate<__bf16>(a, launch);
+  else by_gate<_Float16>(a, launch);
   return hipGetLastError();
 }
 
