@@ -155,7 +155,9 @@ __device__ __forceinline__ uint32_t resets_of(const RecurrenceArgs& A, uint32_t 
   return static_cast<uint32_t>(__ballot(anew));
 }
 
-// Which tile this workgroup works on: by ticket where tiles wait for each other.
+// Which tile this workgroup works on: by ticket where tiles wait for each other.  (Stretches of channels side by side share cache lines where rows do not
+// begin on one.  Handing them to workgroups of one die, eight tiles of each chain side by side, took longer: one prompt 135 instead of 129 us, the backward
+// kernel of 8 x 4096 x 2048 246 instead of 234: tiles that begin together wait for each other.)
 struct Place {
   uint32_t chain, b, block, order;      // order: how many tiles of the chain come before it
 };
@@ -190,25 +192,35 @@ __device__ __forceinline__ void publish(unsigned long long* w, const Stretch (&s
   }
 }
 
-// What comes into the tile, from the published words of the chain's earlier tiles: kWaves of them at a time, a wave each.
-// (A word carries all there is to know, so no other memory needs ordering.)  lds: as `parts` of the kernels.
+// What comes into the tile, from the published words of the chain's earlier tiles: kWindow of them at a time, the same number by each wave, which
+// asks for all of its own before it looks at one.  (A word carries all there is to know, so no other memory needs ordering.)
+constexpr uint32_t kWindow = 8;
+
 template <int kVec, int kWaves>
 __device__ __forceinline__ void look_back(const TileArgs& G, const Place& at, uint32_t wave, Stretch (*lds)[64 * kVec], float (&carry)[kVec]) {
+  constexpr uint32_t kEach = kWindow > kWaves ? kWindow / kWaves : 1u, kSeen = kEach * kWaves;
   const uint32_t lane = threadIdx.x & 63u;
   Stretch seen[kVec];
 #pragma unroll
   for (int i = 0; i < kVec; ++i) seen[i] = Stretch{1.0f, 0.0f};
   for (uint32_t next = at.order; next > 0u;) {                       // tiles next - 1, next - 2, ..
-    if (wave < next) {
-      const unsigned long long* w = words_of<kVec>(G, at.chain, next - 1u - wave);
+    unsigned long long v[kEach][kVec];
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) {
+      const uint32_t back = min(wave * kEach + j, next - 1u);        // (the first tile again, where there are no more)
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[j][i] = __hip_atomic_load(words_of<kVec>(G, at.chain, next - 1u - back) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) {
+      const uint32_t back = min(wave * kEach + j, next - 1u);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        unsigned long long v = __hip_atomic_load(w + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        while (v == kUnset) {
+        while (v[j][i] == kUnset) {
           __builtin_amdgcn_s_sleep(1);
-          v = __hip_atomic_load(w + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          v[j][i] = __hip_atomic_load(words_of<kVec>(G, at.chain, next - 1u - back) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
-        lds[wave][lane * kVec + i] = Stretch{__uint_as_float(static_cast<uint32_t>(v >> 32)), __uint_as_float(static_cast<uint32_t>(v))};
+        lds[wave * kEach + j][lane * kVec + i] = Stretch{__uint_as_float(static_cast<uint32_t>(v[j][i] >> 32)), __uint_as_float(static_cast<uint32_t>(v[j][i]))};
       }
     }
     __syncthreads();
@@ -216,12 +228,12 @@ __device__ __forceinline__ void look_back(const TileArgs& G, const Place& at, ui
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
 #pragma unroll 4
-      for (uint32_t j = 0; j < kWaves && j < next; ++j) seen[i] = both(lds[j][lane * kVec + i], seen[i]);
+      for (uint32_t j = 0; j < kSeen && j < next; ++j) seen[i] = both(lds[j][lane * kVec + i], seen[i]);
       open |= !cut(seen[i].p);
     }
     // the same in every wave, which all have the same words (the first tile's word is a state, so it ends there at the latest)
     if (!__any(open)) break;
-    next = next > kWaves ? next - kWaves : 0u;
+    next = next > kSeen ? next - kSeen : 0u;
     __syncthreads();
   }
 #pragma unroll
@@ -230,7 +242,7 @@ __device__ __forceinline__ void look_back(const TileArgs& G, const Place& at, ui
 
 template <int kVec, int kWaves>
 struct Shared {
-  Stretch parts[kWaves][64 * kVec], earlier[kWaves][64 * kVec];
+  Stretch parts[kWaves][64 * kVec], earlier[kWaves > kWindow ? kWaves : kWindow][64 * kVec];
   uint32_t ticket;
 };
 
@@ -346,7 +358,7 @@ __device__ __forceinline__ void forward_tile(const RecurrenceArgs& A, const Tile
 }
 
 template <typename T, int kVec, int kWaves, int kSteps, bool kGated>
-__global__ void __launch_bounds__(64 * kWaves) recurrence_kernel(RecurrenceArgs A, TileArgs G) {
+__global__ void __launch_bounds__(64 * kWaves, 4) recurrence_kernel(RecurrenceArgs A, TileArgs G) {
   __shared__ Shared<kVec, kWaves> lds;
   const Place at = take_place(A, G, &lds.ticket);
   const uint32_t n = length_of(A, at.b);
@@ -358,7 +370,7 @@ __global__ void __launch_bounds__(64 * kWaves) recurrence_kernel(RecurrenceArgs 
 
 template <int kWaves>
 struct SharedBackward {
-  Stretch parts[kWaves][64], back[kWaves][64], earlier[kWaves][64];
+  Stretch parts[kWaves][64], back[kWaves][64], earlier[kWaves > kWindow ? kWaves : kWindow][64];
   uint32_t ticket;
 };
 
@@ -498,9 +510,11 @@ __global__ void __launch_bounds__(64 * kWaves) recurrence_backward_kernel(Recurr
 }
 
 __global__ void __launch_bounds__(256) clear_words_kernel(TileArgs G, uint64_t words) {
-  const uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256u + threadIdx.x;
-  if (i < words) G.words[i] = kUnset;
-  if (i == 0u) *G.ticket = 0u;
+  typedef unsigned long long two __attribute__((ext_vector_type(2)));
+  two* to = reinterpret_cast<two*>(G.words);                         // (scratch begins on 256 bytes, and a chain has an even number of words)
+  const uint64_t pairs = words / 2u, threads = static_cast<uint64_t>(gridDim.x) * 256u;
+  for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256u + threadIdx.x; i < pairs; i += threads) to[i] = two{kUnset, kUnset};
+  if (blockIdx.x == 0u && threadIdx.x == 0u) *G.ticket = 0u;
 }
 
 // How a sequence is cut: the same constants make the tiles and choose the kernel.
@@ -508,7 +522,7 @@ struct Shape {
   uint32_t waves, steps;           // waves a workgroup, steps a wave
   constexpr uint32_t tile() const { return waves * steps; }
 };
-constexpr Shape kOneWave{1, 4}, kShort{4, 16}, kLong{4, 16}, kLongBackward{16, 16};
+constexpr Shape kOneWave{1, 4}, kShort{4, 16}, kLong{8, 16}, kLongBackward{16, 16};
 enum class Kind { kOneWave, kShort, kLong };
 
 struct Cut {
@@ -547,9 +561,10 @@ uint32_t workgroups(const RecurrenceArgs& a, const TileArgs& G) {
 
 hipError_t clear_words(TileArgs& G, uint64_t words, unsigned long long* scratch, hipStream_t s) {
   if (words == 0u) return hipSuccess;
-  G.words = scratch + 1;
-  G.ticket = reinterpret_cast<uint32_t*>(scratch);
-  clear_words_kernel<<<dim3(static_cast<uint32_t>((words + 255u) / 256u)), dim3(256), 0, s>>>(G, words);
+  G.words = scratch;
+  G.ticket = reinterpret_cast<uint32_t*>(scratch + words);
+  const uint64_t wgs = (words / 2u + 1023u) / 1024u;                  // four pairs a thread, up to a grid that fills the device twice over
+  clear_words_kernel<<<dim3(static_cast<uint32_t>(wgs < 2048u ? wgs : 2048u)), dim3(256), 0, s>>>(G, words);
   return hipGetLastError();
 }
 
