@@ -270,6 +270,7 @@ int rgc_last_error(rgc_ctx* ctx, void* hip_stream);
 #define RGC_BF16 1
 #define RGC_F16  2
 #define RGC_TOP_MAX 128 /* alternatives, or teacher entries, a row can have */
+#define RGC_VOCAB_MAX 4194304
 
 /* Log probabilities of given tokens, with the entropy of their distribution and its top alternatives.  For every row of
  * logits z:  log p_j = z_j / T - ln sum_i exp(z_i / T),  entropy = -sum_j p_j log p_j  (0 where p_j = 0).
@@ -279,7 +280,7 @@ int rgc_last_error(rgc_ctx* ctx, void* hip_stream);
  *    NaN ranks above +Inf).
  *  - A logit of -inf has log probability -inf; so has every logit of a row of nothing else, whose entropy is 0.  A NaN or
  *    +inf makes the row's log probabilities and entropy NaN.
- * Limits: 0 <= rows < 2^31, 1 <= vocab < 2^31, 0 <= top <= min(RGC_TOP_MAX, vocab), T > 0. */
+ * Limits: 0 <= rows, rows * ceil(vocab / 4096) < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 0 <= top <= min(RGC_TOP_MAX, vocab), T > 0. */
 typedef struct {
   const void*    logits;      /* [rows][vocab], row r at logits + r * row_stride elements           */
   int64_t        row_stride;  /* >= vocab                                                           */

@@ -1302,7 +1302,7 @@ float exponent_scale(float temperature) {
 
 // A [rows][vocab] tensor of logits or of their gradient.
 bool rows_fit(const void* data, int64_t rows, int32_t vocab, int64_t row_stride, int32_t dtype) {
-  if (rows < 0 || rows > kInt32Most || vocab < 1 || dtype < RGC_F32 || dtype > RGC_F16) return false;
+  if (rows < 0 || rows > kInt32Most || vocab < 1 || vocab > RGC_VOCAB_MAX || dtype < RGC_F32 || dtype > RGC_F16) return false;
   if (row_stride < vocab || row_stride > (int64_t(1) << 40)) return false;
   return rows == 0 || (data && aligned_to(data, element_size(dtype)));
 }
@@ -1397,7 +1397,16 @@ int rgc_token_logprobs(rgc_ctx* ctx, const rgc_token_scores* a, void* hip_stream
   A.stats = a->stats;
   A.top_idx = a->top_idx;
   A.top_logprob = a->top_logprob;
-  RGC_HIP(launch_token_logprobs(A, a->dtype, static_cast<hipStream_t>(hip_stream)));
+  SplitArgs P = split_of(A.vocab, a->dtype);
+  if (static_cast<uint64_t>(A.rows) * P.segments > kInt32Most) return RGC_EINVAL;
+  if (P.segments > 1u) {
+    const uint64_t parts = static_cast<uint64_t>(A.rows) * P.segments;
+    const int rc = lm_scratch(ctx, parts * (2u + A.top));
+    if (rc != RGC_OK) return rc;
+    P.sums = reinterpret_cast<float*>(ctx->d_lm.p);
+    P.entries = reinterpret_cast<uint64_t*>(ctx->d_lm.p + 2u * parts);
+  }
+  RGC_HIP(launch_token_logprobs(A, a->dtype, P, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 
@@ -1406,6 +1415,7 @@ int rgc_token_logprobs_backward(rgc_ctx* ctx, const rgc_token_scores* a, const f
                                 void* hip_stream) {
   if (!ctx || !a || !scores_fit(a) || !rows_fit(grad_logits, a->rows, a->vocab, grad_row_stride, a->dtype)) return RGC_EINVAL;
   if (!words_aligned({grad_logprob, grad_entropy})) return RGC_EINVAL;
+  if (a->rows * ((a->vocab + 4095) / 4096) > kInt32Most) return RGC_EINVAL;
   if (a->rows == 0) return RGC_OK;
   if (!a->stats || (grad_logprob && !a->targets) || (grad_entropy && !a->entropy)) return RGC_EINVAL;
   DeviceGuard guard(ctx->device);
@@ -1445,18 +1455,31 @@ int rgc_distill_loss(rgc_ctx* ctx, const rgc_distill* a, void* hip_stream) {
   A.vocab = static_cast<uint32_t>(a->vocab);
   A.teacher_idx = a->teacher_idx;
   A.teacher_logits = a->teacher_logits;
-  A.k = static_cast<uint32_t>(a->k);
-  A.targets = a->targets;
+  // a part whose weight is 0 is off, and so is one without entries or targets
+  const bool soft = a->soft_weight > 0.0f && a->k > 0, label = a->label_weight > 0.0f && a->targets;
+  A.k = soft ? static_cast<uint32_t>(a->k) : 0u;
+  A.targets = label ? a->targets : nullptr;
   A.temperature = a->temperature;
-  A.scale = exponent_scale(a->temperature);
   A.inv_t = 1.0f / a->temperature;
+  A.other_scale = exponent_scale(1.0f);
+  A.scale = soft ? exponent_scale(a->temperature) : A.other_scale;
+  A.temperatures = !soft || !label || a->temperature == 1.0f ? Temperatures::kOne : a->temperature == 2.0f ? Temperatures::kSquared : Temperatures::kTwo;
   A.soft_weight = a->soft_weight;
   A.label_weight = a->label_weight;
   A.grad_loss = a->grad_loss;
   A.loss = a->loss;
   A.grad_logits = a->grad_logits;
   A.grad_row_stride = a->grad_row_stride;
-  RGC_HIP(launch_distill(A, a->dtype, static_cast<hipStream_t>(hip_stream)));
+  SplitArgs P = split_of(A.vocab, a->dtype);
+  if (static_cast<uint64_t>(A.rows) * P.segments > kInt32Most) return RGC_EINVAL;
+  if (P.segments > 1u) {
+    const uint64_t parts = static_cast<uint64_t>(A.rows) * P.segments;
+    const int rc = lm_scratch(ctx, parts * 2u + (static_cast<uint64_t>(A.rows) * (RGC_TOP_MAX + 1) + 1u) / 2u);
+    if (rc != RGC_OK) return rc;
+    P.sums = reinterpret_cast<float*>(ctx->d_lm.p);
+    P.logits = reinterpret_cast<float*>(ctx->d_lm.p + 2u * parts);
+  }
+  RGC_HIP(launch_distill(A, a->dtype, P, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 

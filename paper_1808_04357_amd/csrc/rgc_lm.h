@@ -35,21 +35,36 @@ struct ScoreGradArgs {
   int64_t grad_row_stride;
 };
 
+// Which softmaxes of a row a distillation needs: one (T = 1, or only one of the two parts is on); at T = 2 and 1, the weights of the second being the squares of
+// the first's; at another T and 1.
+enum class Temperatures { kOne, kSquared, kTwo };
+
 struct DistillArgs {
   const void* logits;
   int64_t row_stride;
   uint32_t rows, vocab;
   const int32_t* teacher_idx;
   const float* teacher_logits;
-  uint32_t k;
+  uint32_t k;                // 0: no soft part
   const int32_t* targets;    // null: no labels
-  float temperature, scale, inv_t;
+  float temperature, inv_t;
+  float scale, other_scale;  // of the first softmax, log2(e) / T or log2(e), and of the second
+  Temperatures temperatures;
   float soft_weight, label_weight;
   const float* grad_loss;
   float* loss;
   void* grad_logits;
   int64_t grad_row_stride;
 };
+
+// How rows are cut into segments (workgroups), and what those leave for each other where there are several.
+struct SplitArgs {
+  uint32_t segments, length;
+  float* sums;               // [rows][segments][4]
+  uint64_t* entries;         // [rows][segments][top]: scores
+  float* logits;             // [rows][RGC_TOP_MAX + 1]: distillation
+};
+SplitArgs split_of(uint32_t vocab, int dtype);
 
 struct SequenceView {
   void* data;
@@ -79,9 +94,9 @@ struct TileArgs {
   uint32_t* ticket;
 };
 
-hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, hipStream_t s);
+hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, const SplitArgs& p, hipStream_t s);
 hipError_t launch_token_logprobs_backward(const ScoreGradArgs& a, int dtype, hipStream_t s);
-hipError_t launch_distill(const DistillArgs& a, int dtype, hipStream_t s);
+hipError_t launch_distill(const DistillArgs& a, int dtype, const SplitArgs& p, hipStream_t s);
 uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backward);      // 64-bit words of `scratch`
 hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, hipStream_t s);
 hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s);

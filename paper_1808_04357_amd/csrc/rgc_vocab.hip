@@ -2,289 +2,856 @@
 // gradient, and the distillation loss with its gradient (include/rgc.h has the formulas).
 //
 // A softmax is computed in powers of two: with c = log2(e) / T and M the row's largest logit, a_j = (z_j - M) c, S = sum 2^a_j,
-//   log p_j = ln 2 * (a_j - log2 S),   entropy = ln 2 * (log2 S - sum 2^a_j a_j / S).
+//   p_j = 2^a_j / S,   ln p_j = (z_j - M) / T - ln S,   entropy = ln S - ln 2 * sum 2^a_j a_j / S.
 // The difference is taken before the scaling: z_j c overflows for logits near the type's lowest value, with which masks are written.
+//
+// All of it is bound by reading (and, for gradients, writing) the logits once.  A workgroup holds a row, or a segment of one, in registers as it
+// lies in memory: all its 16-byte reads are in flight at once, and the later passes (exponentials again for the gradient, a look for
+// the top alternatives) cost no traffic.  Several such workgroups share a compute unit, so that one's reads overlap another's arithmetic.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
+#include "rgc_device.h"
 #include "rgc_lm.h"
 
 namespace rgc {
 namespace {
 
-constexpr uint32_t kThreads = 256, kWaves = kThreads / 64u;
 constexpr float kLn2 = 0.693147180559945309f;
-constexpr uint32_t kTopMost = 128;
+constexpr uint32_t kTopMost = 128;         // RGC_TOP_MAX
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }   // 1 ulp; a result below 2^-126 is 0
 __device__ __forceinline__ float log2_of(float x) { return __builtin_amdgcn_logf(x); }    // 1 ulp; log2(0) = -inf
 
-// (z - m) c; a row of nothing but -inf has m = -inf, and every element has probability 0.
-__device__ __forceinline__ float exponent(float z, float m, float c) { return m == -INFINITY ? -INFINITY : (z - m) * c; }
+// What is subtracted from the logits: their largest, but 0 where that is -inf (a row of nothing else, whose weights are all 0 then).
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
 
 // ln of a logit's probability, given ln S; -inf for every logit of a row of nothing but -inf.
 __device__ __forceinline__ float log_probability(float z, float m, float inv_t, float log_sum) {
   return m == -INFINITY ? m : (z - m) * inv_t - log_sum;
 }
 
-// Sums over the elements seen so far: m the largest, s = sum 2^a, e = sum 2^a a.
+// An exponent as a factor beside its power: 2^-200 is 0 in fp32, and 0 * -inf is not.
+__device__ __forceinline__ float as_factor(float a) { return fmaxf(a, -200.0f); }
+
+__device__ __forceinline__ bool is_token(int32_t t, uint32_t vocab) { return static_cast<uint32_t>(t) < vocab; }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ float dpp(float old, float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(x), kCtrl, kRowMask, 0xF, false));
+}
+__device__ __forceinline__ float last_lane(float x) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63)); }
+__device__ __forceinline__ float wave_sum(float x) {
+  x += dpp<0x111, 0xF>(0.0f, x);
+  x += dpp<0x112, 0xF>(0.0f, x);
+  x += dpp<0x114, 0xF>(0.0f, x);
+  x += dpp<0x118, 0xF>(0.0f, x);
+  x += dpp<0x142, 0xA>(0.0f, x);
+  x += dpp<0x143, 0xC>(0.0f, x);
+  return last_lane(x);
+}
+__device__ __forceinline__ float wave_max(float x) {
+  x = fmaxf(x, dpp<0x111, 0xF>(x, x));
+  x = fmaxf(x, dpp<0x112, 0xF>(x, x));
+  x = fmaxf(x, dpp<0x114, 0xF>(x, x));
+  x = fmaxf(x, dpp<0x118, 0xF>(x, x));
+  x = fmaxf(x, dpp<0x142, 0xA>(x, x));
+  x = fmaxf(x, dpp<0x143, 0xC>(x, x));
+  return last_lane(x);
+}
+
+// What a softmax needs of a set of logits: m the largest (NaN passed over), s = sum 2^a with a = (z - m) c, and a third sum that
+// goes along: of 2^a a (scores) or of the weights at another temperature (distillation).  A NaN or +inf among the logits makes s a NaN.
+enum class Third { kNone, kEntropy, kOther };      // kOther: of 2^((z - m) c1)
 struct Sums {
   float m, s, e;
 };
+constexpr Sums kNothing{-INFINITY, 0.0f, 0.0f};
 
-__device__ __forceinline__ float finite_or_zero_weight(float a) { return fmaxf(a, -200.0f); }   // 2^-200 is 0 in fp32, and 0 * -inf is not
-
-// The two sets of elements as one: the one with the smaller maximum is scaled down.
-__device__ __forceinline__ Sums join(const Sums& x, const Sums& y, float c) {
-  const float m = fmaxf(x.m, y.m);
-  if (m == -INFINITY) return Sums{m, x.s + y.s, x.e + y.e};        // (nothing but -inf on either side: zeros, or NaN)
-  const float ax = finite_or_zero_weight((x.m - m) * c), ay = finite_or_zero_weight((y.m - m) * c);
-  const float wx = exp2_of((x.m - m) * c), wy = exp2_of((y.m - m) * c);
-  return Sums{m, x.s * wx + y.s * wy, wx * (x.e + x.s * ax) + wy * (y.e + y.s * ay)};
-}
-
-__device__ __forceinline__ void add(Sums& t, float z, float c) {
-  t = join(t, Sums{z, z == -INFINITY ? 0.0f : 1.0f + (z - z), 0.0f}, c);      // z - z: NaN for a NaN or an infinity
-}
-
-__device__ __forceinline__ Sums wave_join(Sums t, float c) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const Sums o{__shfl_xor(t.m, d), __shfl_xor(t.s, d), __shfl_xor(t.e, d)};
-    t = join(t, o, c);
-  }
-  return t;
-}
-
-// The same value in all threads of the workgroup; lds: 3 * kWaves floats.
-__device__ __forceinline__ Sums block_join(Sums t, float c, float* lds) {
-  t = wave_join(t, c);
-  const uint32_t wave = threadIdx.x >> 6;
-  __syncthreads();
-  if ((threadIdx.x & 63u) == 0u) {
-    lds[3u * wave] = t.m;
-    lds[3u * wave + 1u] = t.s;
-    lds[3u * wave + 2u] = t.e;
-  }
-  __syncthreads();
-  Sums r{lds[0], lds[1], lds[2]};
-  for (uint32_t w = 1; w < kWaves; ++w) r = join(r, Sums{lds[3u * w], lds[3u * w + 1u], lds[3u * w + 2u]}, c);
-  if (r.s != r.s) r.m = r.s;       // a NaN or +inf: everything that is made of the row is NaN (fmaxf passes NaN over)
+template <Third kThird>
+__device__ __forceinline__ Sums rebased(const Sums& t, float m, float c, float c1) {
+  const float d = t.m - base_of(m), a = d * c, w = exp2_of(a);
+  Sums r{m, t.s * w, 0.0f};
+  if constexpr (kThird == Third::kEntropy) r.e = w * (t.e + t.s * as_factor(a));
+  if constexpr (kThird == Third::kOther) r.e = t.e * exp2_of(d * c1);
   return r;
 }
 
-__device__ __forceinline__ bool is_token(int32_t t, uint32_t vocab) { return static_cast<uint32_t>(t) < vocab; }
+// The same in every lane.
+template <Third kThird>
+__device__ __forceinline__ Sums wave_join(const Sums& t, float c, float c1) {
+  Sums r = rebased<kThird>(t, wave_max(t.m), c, c1);
+  r.s = wave_sum(r.s);
+  if constexpr (kThird != Third::kNone) r.e = wave_sum(r.e);
+  return r;
+}
 
-// Larger for a larger logit, the same for +0 and -0, largest for a NaN.
+// The same in every thread; lds: 3 floats a wave.  Holds one barrier, which callers rely on.
+template <Third kThird, uint32_t kWaves>
+__device__ __forceinline__ Sums block_join(const Sums& t, float c, float c1, float* lds) {
+  const Sums own = wave_join<kThird>(t, c, c1);
+  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+  if (lane == 0u) {
+    lds[3u * wave] = own.m;
+    lds[3u * wave + 1u] = own.s;
+    lds[3u * wave + 2u] = own.e;
+  }
+  __syncthreads();
+  if constexpr (kWaves == 1) return own;
+  Sums o = kNothing;
+  if (lane < kWaves) o = Sums{lds[3u * lane], lds[3u * lane + 1u], lds[3u * lane + 2u]};
+  return wave_join<kThird>(o, c, c1);
+}
+
+// Everything that is made of a row with a NaN or +inf is NaN.
+__device__ __forceinline__ Sums spoiled(Sums t) {
+  if (t.s != t.s) t.m = t.s;
+  return t;
+}
+
+// ---------------------------------------------------------------- a row's segment in registers
+
+template <typename T>
+struct Vector {
+  static constexpr uint32_t kElems = 16u / sizeof(T);
+  typedef uint32_t Words __attribute__((ext_vector_type(4)));
+  // aligned to an element only: a row of an odd vocabulary starts anywhere, and gfx950 reads and writes 16 bytes at any address
+  typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
+
+  static __device__ __forceinline__ Words load(const T* p) { return *reinterpret_cast<const Unaligned*>(p); }
+  static __device__ __forceinline__ void store(T* p, const float (&v)[kElems]) {
+    T t[kElems];
+#pragma unroll
+    for (uint32_t i = 0; i < kElems; ++i) t[i] = static_cast<T>(v[i]);
+    Words w;
+    __builtin_memcpy(&w, t, 16);
+    *reinterpret_cast<Unaligned*>(p) = w;
+  }
+  static __device__ __forceinline__ void unpack(const Words& w, float (&v)[kElems]) {
+    T t[kElems];
+    __builtin_memcpy(t, &w, 16);
+#pragma unroll
+    for (uint32_t i = 0; i < kElems; ++i) v[i] = static_cast<float>(t[i]);
+  }
+};
+
+// n elements from z on, by a workgroup of kThreads: vector i * kThreads + thread in raw[i], the up to kElems - 1 elements behind the last whole
+// vector one each by the first threads.  What is beyond the segment reads as -inf.
+template <typename T, uint32_t kThreads, uint32_t kVectors>
+struct Held {
+  using V = Vector<T>;
+  static constexpr uint32_t kElems = V::kElems, kCapacity = kThreads * kVectors * kElems;
+  mutable typename V::Words raw[kVectors];
+  float rest;
+  uint32_t n, vectors, wave0;      // wave0: the wave's first thread
+
+  __device__ __forceinline__ Held(const T* z, uint32_t n_) : n(n_), vectors(n_ / kElems), wave0(uniform(threadIdx.x & ~63u)) {
+    if (vectors > 0u) {
+      // (no branches between the reads, or the compiler waits for each: behind the end, the last vector again)
+#pragma unroll
+      for (uint32_t i = 0; i < kVectors; ++i) raw[i] = V::load(z + static_cast<uint64_t>(min(i * kThreads + threadIdx.x, vectors - 1u)) * kElems);
+    }
+    rest = has_rest() ? static_cast<float>(z[vectors * kElems + threadIdx.x]) : -INFINITY;
+  }
+  __device__ __forceinline__ bool has_rest() const { return threadIdx.x < n - vectors * kElems; }
+  __device__ __forceinline__ bool any() const { return threadIdx.x < vectors || has_rest(); }
+  __device__ __forceinline__ uint32_t index(uint32_t i) const { return (i * kThreads + threadIdx.x) * kElems; }
+  __device__ __forceinline__ bool mine(uint32_t i) const { return i * kThreads + threadIdx.x < vectors; }
+  // f(i, values): for the vectors of which the wave has any
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll
+    for (uint32_t i = 0; i < kVectors; ++i) {
+      if (i * kThreads + wave0 >= vectors) break;
+      // (Another pass's unpacked values are not to be kept for this one: they take two registers where the packed ones take one.)
+      asm volatile("" : "+v"(raw[i]));
+      float v[kElems];
+      V::unpack(raw[i], v);
+      if (i * kThreads + wave0 + 64u > vectors) {
+#pragma unroll
+        for (uint32_t j = 0; j < kElems; ++j) v[j] = mine(i) ? v[j] : -INFINITY;
+      }
+      f(i, v);
+    }
+  }
+  // Which thread holds element `at` of the segment.
+  __device__ __forceinline__ static uint32_t owner(uint32_t at, uint32_t n) {
+    const uint32_t whole = n / kElems;
+    return at / kElems < whole ? at / kElems % kThreads : at - whole * kElems;
+  }
+};
+
+__device__ __forceinline__ float weigh(float z, float base, float c) { return exp2_of((z - base) * c); }
+
+// Sums of what a thread holds, the largest rescaling those before it, vector by vector as they arrive.  kSquared: the other temperature's weights are the squares
+// of these (T = 2).
+template <Third kThird, bool kSquared, typename H>
+__device__ __forceinline__ Sums sums_of(const H& held, float c, float c1) {
+  Sums t{held.rest, 0.0f, 0.0f};
+  {
+    const float base = base_of(t.m), w = weigh(held.rest, base, c);      // 1, 0 for -inf, NaN for NaN and +inf
+    t.s = w;
+    if constexpr (kThird == Third::kOther) t.e = w;
+  }
+  held.each([&](uint32_t, const float (&v)[H::kElems]) __attribute__((always_inline)) {
+    float m = t.m;
+#pragma unroll
+    for (uint32_t j = 0; j < H::kElems; ++j) m = fmaxf(m, v[j]);
+    const float base = base_of(m);
+    {
+      const float d = t.m - base, a = d * c, w = exp2_of(a);
+      if constexpr (kThird == Third::kEntropy) t.e = w * (t.e + t.s * as_factor(a));
+      if constexpr (kThird == Third::kOther) t.e *= kSquared ? w * w : exp2_of(d * c1);
+      t.s *= w;
+    }
+    t.m = m;
+#pragma unroll
+    for (uint32_t j = 0; j < H::kElems; ++j) {
+      const float d = v[j] - base, a = d * c, w = exp2_of(a);
+      t.s += w;
+      if constexpr (kThird == Third::kEntropy) t.e = __fmaf_rn(w, as_factor(a), t.e);
+      if constexpr (kThird == Third::kOther) t.e = kSquared ? __fmaf_rn(w, w, t.e) : t.e + exp2_of(d * c1);
+    }
+  });
+  return t;
+}
+
+// ---------------------------------------------------------------- the top alternatives of a segment
+
+// Larger for a larger logit, the same for +0 and -0, largest for a NaN; 0 is no logit's.
 __device__ __forceinline__ uint32_t order_of(float z) {
   const uint32_t b = __float_as_uint(z + 0.0f);
   if (z != z) return 0xFFFFFFFFu;
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float logit_of(uint32_t order) {
+  if (order == 0xFFFFFFFFu) return NAN;
+  return __uint_as_float((order & 0x80000000u) ? order & 0x7FFFFFFFu : ~order);
+}
+// Orders entries: larger logits first, then lower indices.
+__device__ __forceinline__ uint64_t entry_of(float z, uint32_t index) { return (static_cast<uint64_t>(order_of(z)) << 32) | (0xFFFFFFFFu - index); }
 
-__device__ __forceinline__ uint64_t block_max(uint64_t v, uint64_t* lds) {
+constexpr uint32_t kListed = 1024;      // candidates a workgroup can list
+
+template <uint32_t kThreads>
+struct TopShared {
+  uint64_t list[kListed];
+  uint32_t largest[kThreads];           // of every thread, by order
+  uint32_t count, line, scan[kThreads / 64u];
+};
+
+// The largest number, looked at from bit `from` down to bit `to`, that at least k of the wave's values (kEach a lane) reach.
+template <uint32_t kEach>
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&v)[kEach], uint32_t k, uint32_t line, int from, int to) {
+  for (int bit = from; bit >= to; --bit) {
+    const uint32_t higher = line | (1u << bit);
+    uint32_t n = 0;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t o = __shfl_xor(v, d);
-    v = o > v ? o : v;
+    for (uint32_t i = 0; i < kEach; ++i) n += popc64(__ballot(v[i] >= higher));
+    if (n >= k) line = higher;
+  }
+  return line;
+}
+
+// f(index, logit) for every logit of a segment, read (again) from memory.
+template <typename T, uint32_t kThreads, typename F>
+__device__ __forceinline__ void read_again(const T* z, uint32_t n, F&& f) {
+  using V = Vector<T>;
+  const uint32_t vectors = n / V::kElems;
+#pragma unroll 1
+  for (uint32_t i = threadIdx.x; i < vectors; i += kThreads) {
+    float v[V::kElems];
+    V::unpack(V::load(z + i * V::kElems), v);
+#pragma unroll
+    for (uint32_t j = 0; j < V::kElems; ++j) f(i * V::kElems + j, v[j]);
+  }
+  const uint32_t rest = vectors * V::kElems + threadIdx.x;
+  if (rest < n) f(rest, static_cast<float>(z[rest]));
+}
+
+// How many of the segment's logits have an order above `line`; the same in every thread.  Holds barriers.
+template <typename T, uint32_t kThreads>
+__device__ __forceinline__ uint32_t count_above(const T* z, uint32_t n, uint32_t line, TopShared<kThreads>& lds) {
+  uint32_t mine = 0, total = 0;
+  read_again<T, kThreads>(z, n, [&](uint32_t, float v) { mine += order_of(v) > line ? 1u : 0u; });
+  (void)block_excl_scan<kThreads / 64u>(mine, lds.scan, total);
+  return total;
+}
+
+// lds.list: the k largest, where more logits than it holds reach a line, `line` not above the k-th largest.  Those above the k-th largest, and
+// then those equal to it in the order of their indices.
+template <typename T, uint32_t kThreads>
+__device__ __noinline__ void list_exactly(const T* z, uint32_t n, uint32_t line, uint32_t k, uint32_t first, TopShared<kThreads>& lds) {
+  uint32_t above = count_above<T, kThreads>(z, n, line, lds);
+  if (above >= k) {                                        // the k-th largest is higher: bit by bit
+    uint32_t found = 0u;
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t higher = found | (1u << bit);
+      if (count_above<T, kThreads>(z, n, higher - 1u, lds) >= k) found = higher;
+    }
+    line = found;
+    above = count_above<T, kThreads>(z, n, line, lds);
+  }
+  if (threadIdx.x == 0u) lds.count = 0u;
+  __syncthreads();
+  read_again<T, kThreads>(z, n, [&](uint32_t i, float v) {
+    if (order_of(v) > line) lds.list[atomicAdd(&lds.count, 1u)] = entry_of(v, first + i);
+  });
+  constexpr uint32_t kElems = Vector<T>::kElems;
+  const uint32_t vectors = n / kElems;
+  uint32_t before = above;
+  for (uint32_t from = 0; from < n && before < k;) {
+    // a vector a thread, at last the elements behind the last whole one
+    const bool whole = from < vectors * kElems;
+    const uint32_t at = from + (whole ? threadIdx.x * kElems : threadIdx.x), each = whole ? kElems : 1u, end = whole ? vectors * kElems : n;
+    uint32_t equal = 0;
+    if (at < end)
+      for (uint32_t j = 0; j < each; ++j) equal |= order_of(static_cast<float>(z[at + j])) == line ? 1u << j : 0u;
+    uint32_t total = 0;
+    uint32_t place = before + block_excl_scan<kThreads / 64u>(static_cast<uint32_t>(__popc(equal)), lds.scan, total);
+    for (; equal != 0u && place < k; equal &= equal - 1u) lds.list[place++] = entry_of(logit_of(line), first + at + static_cast<uint32_t>(__ffs(static_cast<int>(equal)) - 1));
+    before += total;
+    from = whole ? min(from + kThreads * kElems, end) : n;
   }
   __syncthreads();
-  if ((threadIdx.x & 63u) == 0u) lds[threadIdx.x >> 6] = v;
+}
+
+// The k largest (k <= the segment's length), put(rank, entry) each.  `t`: the thread's largest; `spoilt`: there is a NaN or +inf among them.
+//  A line under the k-th largest of all comes cheap: the k-th largest of the threads' largest.  Few logits reach it (with 256 threads some
+// 1.02 k for k = 10, 1.4 k for k = 128, where they lie anywhere); they are listed and ranked.  Where more do than the list holds, as with many equal ones
+// (a mask that leaves fewer than k), list_exactly reads the segment again.
+template <typename T, uint32_t kThreads, typename H, typename Put>
+__device__ __forceinline__ void top_of(const H& held, const T* z, float t, bool spoilt, uint32_t k, uint32_t first, TopShared<kThreads>& lds, Put&& put) {
+  constexpr uint32_t kEach = kThreads >= 256u ? 4u : kThreads / 64u;      // groups of threads a lane of the first wave stands for
+  const uint32_t lane = threadIdx.x & 63u;
+  lds.largest[threadIdx.x] = held.any() ? order_of(t) : 0u;
+  if (threadIdx.x == 0u) lds.count = 0u;
   __syncthreads();
-  uint64_t r = lds[0];
-  for (uint32_t w = 1; w < kWaves; ++w) r = lds[w] > r ? lds[w] : r;
-  return r;
+  uint32_t group[kEach];
+  uint32_t line = 0u;
+  if (threadIdx.x < 64u) {
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) {
+      group[i] = 0u;
+      for (uint32_t j = lane + 64u * i; j < kThreads; j += 64u * kEach) group[i] = max(group[i], lds.largest[j]);
+    }
+    // (sixteen bits of it will do: a line a little lower lets a few more through)
+    line = reached_by<kEach>(group, k, 0u, 31, 16);
+    if (lane == 0u) lds.line = line;
+  }
+  __syncthreads();
+  line = uniform(lds.line);
+  if (!spoilt) {
+    auto list = [&](float v, uint32_t index) __attribute__((always_inline)) {
+      const uint32_t at = atomicAdd(&lds.count, 1u);
+      if (at < kListed) lds.list[at] = entry_of(v, first + index);
+    };
+    const float least = line <= 0x007FFFFFu ? -INFINITY : logit_of(line);      // (below the order of -inf all are taken)
+    held.each([&](uint32_t i, const float (&v)[H::kElems]) __attribute__((always_inline)) {
+      float most = v[0];
+#pragma unroll
+      for (uint32_t j = 1; j < H::kElems; ++j) most = fmaxf(most, v[j]);
+      if (!(most >= least) || !held.mine(i)) return;
+#pragma unroll
+      for (uint32_t j = 0; j < H::kElems; ++j)
+        if (v[j] >= least) list(v[j], held.index(i) + j);
+    });
+    if (held.has_rest() && held.rest >= least) list(held.rest, held.vectors * H::kElems + threadIdx.x);
+  }
+  __syncthreads();
+  uint32_t listed = uniform(lds.count);
+  if (spoilt || listed > kListed) {
+    if (threadIdx.x < 64u) {
+      const uint32_t exact = spoilt ? 0u : reached_by<kEach>(group, k, line, 15, 0);
+      if (lane == 0u) lds.line = exact;
+    }
+    __syncthreads();
+    list_exactly<T, kThreads>(z, held.n, uniform(lds.line), k, first, lds);
+    listed = k;
+  }
+  for (uint32_t i = threadIdx.x; i < listed; i += kThreads) {
+    const uint64_t e = lds.list[i];
+    uint32_t rank = 0;
+    for (uint32_t j = 0; j < listed; ++j) rank += lds.list[j] > e ? 1u : 0u;
+    if (rank < k) put(rank, e);
+  }
+}
+
+// ---------------------------------------------------------------- scores
+
+__device__ __forceinline__ void put_alternative(const ScoreArgs& A, uint32_t r, uint32_t rank, uint64_t entry, const Sums& t, float log_sum) {
+  const uint64_t at = static_cast<uint64_t>(r) * A.top + rank;
+  A.top_idx[at] = static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(entry));
+  A.top_logprob[at] = log_probability(logit_of(static_cast<uint32_t>(entry >> 32)), t.m, A.inv_t, log_sum);
+}
+
+__device__ __forceinline__ void put_left_out(const ScoreArgs& A, uint32_t r) {
+  if (threadIdx.x == 0u) {
+    if (A.logprob) A.logprob[r] = 0.0f;
+    if (A.entropy) A.entropy[r] = 0.0f;
+    if (A.stats) A.stats[2ull * r] = A.stats[2ull * r + 1u] = 0.0f;
+  }
+  for (uint32_t i = threadIdx.x; i < A.top; i += blockDim.x) {
+    A.top_idx[static_cast<uint64_t>(r) * A.top + i] = -1;
+    A.top_logprob[static_cast<uint64_t>(r) * A.top + i] = -INFINITY;
+  }
+}
+
+// By one thread; at_target: the target's logit.
+__device__ __forceinline__ void put_scores(const ScoreArgs& A, uint32_t r, const Sums& t, float log_sum, float at_target) {
+  if (A.logprob) A.logprob[r] = log_probability(at_target, t.m, A.inv_t, log_sum);
+  if (A.entropy) A.entropy[r] = t.s == 0.0f ? 0.0f : log_sum - kLn2 * (t.e / t.s);
+  if (A.stats) {
+    A.stats[2ull * r] = t.m;
+    A.stats[2ull * r + 1u] = log_sum;
+  }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) score_kernel(ScoreArgs A) {
-  __shared__ float lds[3 * kWaves];
-  __shared__ uint64_t lds_key[kWaves];
-  const uint32_t r = blockIdx.x;
-  const T* z = static_cast<const T*>(A.logits) + static_cast<int64_t>(r) * A.row_stride;
+__device__ __forceinline__ const T* row_of(const void* p, int64_t stride, uint32_t r) {
+  return static_cast<const T*>(p) + static_cast<int64_t>(r) * stride;
+}
+
+// A workgroup a segment.  One segment a row: its results; several: its sums and its top entries for score_join_kernel.
+template <typename T, uint32_t kThreads, uint32_t kVectors>
+__global__ void __launch_bounds__(kThreads) score_kernel(ScoreArgs A, SplitArgs P) {
+  __shared__ float lds[3 * kThreads / 64u];
+  __shared__ TopShared<kThreads> top;
+  const uint32_t r = blockIdx.x / P.segments, segment = blockIdx.x - r * P.segments;
+  const uint32_t first = segment * P.length, n = min(A.vocab - first, P.length);
+  const int32_t target = A.targets ? A.targets[r] : 0;
+  const T* z = row_of<T>(A.logits, A.row_stride, r);
+  if (!is_token(target, A.vocab)) {
+    if (P.segments == 1u) put_left_out(A, r);
+    return;
+  }
+  const Held<T, kThreads, kVectors> held(z + first, n);
+  const Sums own = sums_of<Third::kEntropy, false>(held, A.scale, 0.0f);
+  const Sums raw = block_join<Third::kEntropy, kThreads / 64u>(own, A.scale, 0.0f, lds);
+  const Sums t = spoiled(raw);
+  const float log_sum = kLn2 * log2_of(t.s);
+  if (P.segments == 1u) {
+    if (threadIdx.x == 0u) put_scores(A, r, t, log_sum, static_cast<float>(z[target]));
+    if (A.top > 0u)
+      top_of<T, kThreads>(held, z + first, own.m, t.s != t.s, A.top, 0u, top, [&](uint32_t rank, uint64_t e) { put_alternative(A, r, rank, e, t, log_sum); });
+  } else {
+    if (threadIdx.x == 0u) {
+      float* to = P.sums + 4ull * blockIdx.x;
+      to[0] = raw.m;
+      to[1] = raw.s;
+      to[2] = raw.e;
+    }
+    const uint32_t k = min(A.top, n);
+    if (k > 0u)
+      top_of<T, kThreads>(held, z + first, own.m, t.s != t.s, k, first, top, [&](uint32_t rank, uint64_t e) { P.entries[static_cast<uint64_t>(blockIdx.x) * A.top + rank] = e; });
+  }
+}
+
+// A row of several segments (64 at most): their sums joined, their entries, which stand in order, merged.
+constexpr uint32_t kJoinThreads = 256;
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) score_join_kernel(ScoreArgs A, SplitArgs P) {
+  extern __shared__ uint64_t entries[];                    // [segments][top]
+  const uint32_t r = blockIdx.x, lane = threadIdx.x & 63u, last = A.vocab - (P.segments - 1u) * P.length;
   const int32_t target = A.targets ? A.targets[r] : 0;
   if (!is_token(target, A.vocab)) {
-    if (threadIdx.x == 0u) {
-      if (A.logprob) A.logprob[r] = 0.0f;
-      if (A.entropy) A.entropy[r] = 0.0f;
-      if (A.stats) A.stats[2ull * r] = A.stats[2ull * r + 1u] = 0.0f;
-    }
-    for (uint32_t i = threadIdx.x; i < A.top; i += kThreads) {
-      A.top_idx[static_cast<uint64_t>(r) * A.top + i] = -1;
-      A.top_logprob[static_cast<uint64_t>(r) * A.top + i] = -INFINITY;
-    }
+    put_left_out(A, r);
     return;
   }
-  Sums t{-INFINITY, 0.0f, 0.0f};
-  for (uint64_t i = threadIdx.x; i < A.vocab; i += kThreads) add(t, static_cast<float>(z[i]), A.scale);
-  t = block_join(t, A.scale, lds);
-  const float log2s = log2_of(t.s);
+  Sums own = kNothing;
+  if (lane < P.segments) {
+    const float* from = P.sums + 4ull * (static_cast<uint64_t>(r) * P.segments + lane);
+    own = Sums{from[0], from[1], from[2]};
+  }
+  const uint32_t all = P.segments * A.top;
+  auto length = [&](uint32_t s) { return s + 1u == P.segments ? min(A.top, last) : A.top; };      // (a segment but the last has more than RGC_TOP_MAX logits)
+  for (uint32_t i = threadIdx.x; i < all; i += kJoinThreads)
+    if (i % A.top < length(i / A.top)) entries[i] = P.entries[static_cast<uint64_t>(r) * all + i];
+  const Sums t = spoiled(wave_join<Third::kEntropy>(own, A.scale, 0.0f));
+  const float log_sum = kLn2 * log2_of(t.s);
+  if (threadIdx.x == 0u) put_scores(A, r, t, log_sum, static_cast<float>(row_of<T>(A.logits, A.row_stride, r)[target]));
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < all; i += kJoinThreads) {
+    const uint32_t segment = i / A.top;
+    if (i - segment * A.top >= length(segment)) continue;
+    const uint64_t e = entries[i];
+    uint32_t rank = i - segment * A.top;
+    for (uint32_t s = 0; s < P.segments && rank < A.top; ++s) {
+      if (s == segment) continue;
+      uint32_t low = 0, high = length(s);                  // how many of that segment's entries come before e
+      while (low < high) {
+        const uint32_t mid = (low + high) / 2u;
+        if (entries[s * A.top + mid] > e) low = mid + 1u; else high = mid;
+      }
+      rank += low;
+    }
+    if (rank < A.top) put_alternative(A, r, rank, e, t, log_sum);
+  }
+}
+
+// dz_j = g (1{j = target} - p_j) - h p_j (log p_j + entropy), g and h divided by T: no sums, so any part of a row by any workgroup.
+constexpr uint32_t kGradThreads = 256, kGradVectors = 4;
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs A, uint32_t parts) {
+  using V = Vector<T>;
+  constexpr uint32_t kPart = kGradThreads * kGradVectors * V::kElems;
+  const uint32_t r = blockIdx.x / parts, first = (blockIdx.x - r * parts) * kPart, n = min(A.vocab - first, kPart);
+  const T* z = row_of<T>(A.logits, A.row_stride, r) + first;
+  T* dz = static_cast<T*>(A.grad_logits) + static_cast<int64_t>(r) * A.grad_row_stride + first;
+  const int32_t target = A.targets ? A.targets[r] : -1;
+  const float m = A.stats[2ull * r], log_sum = A.stats[2ull * r + 1u];
+  const bool nothing = (A.targets && !is_token(target, A.vocab)) || log_sum == -INFINITY;
+  const Held<T, kGradThreads, kGradVectors> held(z, n);
+  const uint32_t whole = n / V::kElems;
+  if (nothing) {
+    const float zeros[V::kElems] = {};
+    for (uint32_t i = threadIdx.x; i < whole; i += kGradThreads) V::store(dz + i * V::kElems, zeros);
+    if (held.has_rest()) dz[whole * V::kElems + threadIdx.x] = static_cast<T>(0.0f);
+    return;
+  }
+  const float g = A.grad_logprob ? A.grad_logprob[r] * A.inv_t : 0.0f, h = A.grad_entropy ? A.grad_entropy[r] * A.inv_t : 0.0f;
+  const float entropy = A.grad_entropy ? A.entropy[r] : 0.0f, log2s = log_sum * (1.0f / kLn2);
+  // p (g + h (ln p + entropy)) = p (u + w a), a = log2 p
+  const float u = g + h * entropy, w = h * kLn2;
+  auto slope = [&](float v) {
+    const float a = __fmaf_rn(v - m, A.scale, -log2s);
+    return -exp2_of(a) * __fmaf_rn(w, as_factor(a), u);
+  };
+  const uint32_t at = static_cast<uint32_t>(target) - first;       // of the target in this part, if it is
+  const bool here = target >= 0 && at < n && Held<T, kGradThreads, kGradVectors>::owner(at, n) == threadIdx.x;
+  const float at_target = here ? static_cast<float>(z[at]) : 0.0f;
+  held.each([&](uint32_t i, const float (&v)[V::kElems]) __attribute__((always_inline)) {
+    float d[V::kElems];
+#pragma unroll
+    for (uint32_t j = 0; j < V::kElems; ++j) d[j] = slope(v[j]);
+    if (held.mine(i)) V::store(dz + held.index(i), d);
+  });
+  if (held.has_rest()) dz[whole * V::kElems + threadIdx.x] = static_cast<T>(slope(held.rest));
+  if (here) dz[at] = static_cast<T>(g + slope(at_target));         // over what the same thread has just stored
+}
+
+// ---------------------------------------------------------------- distillation
+
+// A row's teacher entries and label, made by the first wave.
+struct Teacher {
+  int32_t at[kTopMost + 1];             // an index, once; the label's last unless it is one of the others; -1: none
+  float off[kTopMost + 1], z[kTopMost + 1];      // what is subtracted there, and the student's logit
+  float soft;                           // sum of the weights q: 0 if there are none
+};
+
+// Two entries a lane.
+struct TeacherLane {
+  float q[2], log_q[2], z[2];
+  int32_t at[2];
+  float at_label;
+};
+
+__device__ __forceinline__ float lane_of(float x, uint32_t lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), static_cast<int>(lane))); }
+
+// gather(index): the student's logit.
+template <typename Gather>
+__device__ __forceinline__ TeacherLane teach(const DistillArgs& A, uint32_t r, int32_t label, Gather&& gather, Teacher& to) {
+  const uint32_t lane = threadIdx.x;
+  TeacherLane t;
+  float z[2], largest = -INFINITY;
+  t.at_label = label >= 0 ? gather(kTopMost, label) : 0.0f;
+#pragma unroll
+  for (uint32_t u = 0; u < 2u; ++u) {
+    const uint32_t i = lane + 64u * u;
+    t.at[u] = i < A.k ? A.teacher_idx[static_cast<uint64_t>(r) * A.k + i] : -1;
+    if (!is_token(t.at[u], A.vocab)) t.at[u] = -1;
+    z[u] = t.at[u] >= 0 ? A.teacher_logits[static_cast<uint64_t>(r) * A.k + i] : -INFINITY;
+    t.z[u] = t.at[u] >= 0 ? gather(i, t.at[u]) : 0.0f;
+    largest = fmaxf(largest, z[u]);
+  }
+  largest = wave_max(largest);
+  float w[2], sum = 0.0f;
+#pragma unroll
+  for (uint32_t u = 0; u < 2u; ++u) {
+    w[u] = weigh(z[u], base_of(largest), A.scale);
+    sum += w[u];
+  }
+  sum = wave_sum(sum);
+  const float log_sum = kLn2 * log2_of(sum);
+  float off[2] = {0.0f, 0.0f};
+  bool again[2] = {false, false};
+#pragma unroll
+  for (uint32_t u = 0; u < 2u; ++u) {
+    t.q[u] = sum == 0.0f ? 0.0f : w[u] / sum;
+    t.log_q[u] = log_probability(z[u], largest, A.inv_t, log_sum);
+  }
+  bool label_listed = false;
+  for (uint32_t j = 0; j < A.k; ++j) {
+    const uint32_t from = j & 63u;
+    const int32_t at = __builtin_amdgcn_readlane(j < 64u ? t.at[0] : t.at[1], static_cast<int>(from));
+    const float q = lane_of(j < 64u ? t.q[0] : t.q[1], from);
+    label_listed |= at == label;
+#pragma unroll
+    for (uint32_t u = 0; u < 2u; ++u)
+      if (at == t.at[u]) {
+        off[u] += q;
+        again[u] |= j < lane + 64u * u;
+      }
+  }
+  const float soft = A.soft_weight * A.temperature;
+#pragma unroll
+  for (uint32_t u = 0; u < 2u; ++u) {
+    const uint32_t i = lane + 64u * u;
+    to.at[i] = again[u] ? -1 : t.at[u];
+    to.off[i] = soft * off[u] + (t.at[u] == label ? A.label_weight : 0.0f);
+    to.z[i] = t.z[u];
+  }
+  if (lane == 0u) {
+    to.at[kTopMost] = label_listed ? -1 : label;
+    to.off[kTopMost] = A.label_weight;
+    to.z[kTopMost] = t.at_label;
+    to.soft = sum;
+  }
+  return t;
+}
+
+// The row's loss, by the first wave.  t: the sums at temperature T (m, s), s1 the sum at 1.
+__device__ __forceinline__ void put_loss(const DistillArgs& A, uint32_t r, const TeacherLane& l, bool softened, bool labelled, const Sums& t, float s1) {
+  float part = 0.0f;
+  const float log_sum = kLn2 * log2_of(t.s);
+#pragma unroll
+  for (uint32_t u = 0; u < 2u; ++u)
+    if (softened && l.at[u] >= 0 && !(l.q[u] == 0.0f)) part += l.q[u] * (l.log_q[u] - log_probability(l.z[u], t.m, A.inv_t, log_sum));
+  part = wave_sum(part);
   if (threadIdx.x == 0u) {
-    if (A.logprob) A.logprob[r] = log_probability(static_cast<float>(z[target]), t.m, A.inv_t, kLn2 * log2s);
-    if (A.entropy) A.entropy[r] = t.s == 0.0f ? 0.0f : kLn2 * (log2s - t.e / t.s);
-    if (A.stats) {
-      A.stats[2ull * r] = t.m;
-      A.stats[2ull * r + 1u] = kLn2 * log2s;
-    }
-  }
-  uint64_t last = ~0ull;
-  for (uint32_t i = 0; i < A.top; ++i) {
-    uint64_t best = 0;
-    for (uint64_t j = threadIdx.x; j < A.vocab; j += kThreads) {
-      const uint64_t key = (static_cast<uint64_t>(order_of(static_cast<float>(z[j]))) << 32) | (0xFFFFFFFFu - static_cast<uint32_t>(j));
-      if (key < last && key > best) best = key;
-    }
-    last = block_max(best, lds_key);
-    if (threadIdx.x == 0u) {
-      const uint32_t j = 0xFFFFFFFFu - static_cast<uint32_t>(last);
-      A.top_idx[static_cast<uint64_t>(r) * A.top + i] = static_cast<int32_t>(j);
-      A.top_logprob[static_cast<uint64_t>(r) * A.top + i] =
-          log_probability(static_cast<float>(z[j]), t.m, A.inv_t, kLn2 * log2s);
-    }
+    float loss = softened ? A.soft_weight * A.temperature * A.temperature * part : 0.0f;
+    if (labelled) loss -= A.label_weight * log_probability(l.at_label, t.m, 1.0f, kLn2 * log2_of(s1));
+    A.loss[r] = loss;
   }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) score_grad_kernel(ScoreGradArgs A) {
-  const uint32_t r = blockIdx.x;
-  const T* z = static_cast<const T*>(A.logits) + static_cast<int64_t>(r) * A.row_stride;
-  T* dz = static_cast<T*>(A.grad_logits) + static_cast<int64_t>(r) * A.grad_row_stride;
-  const int32_t target = A.targets ? A.targets[r] : 0;
-  const float m = A.stats[2ull * r], log2s = A.stats[2ull * r + 1u] * (1.0f / kLn2);
-  const bool nothing = !is_token(target, A.vocab) || m == -INFINITY;
-  const float g = A.grad_logprob ? A.grad_logprob[r] * A.inv_t : 0.0f;
-  const float h = A.grad_entropy ? A.grad_entropy[r] * A.inv_t : 0.0f;
-  const float entropy = A.grad_entropy ? A.entropy[r] : 0.0f;
-  for (uint64_t j = threadIdx.x; j < A.vocab; j += kThreads) {
-    if (nothing) {
-      dz[j] = static_cast<T>(0.0f);
-      continue;
-    }
-    const float a = (static_cast<float>(z[j]) - m) * A.scale - log2s;
-    const float p = exp2_of(a);
-    const float one = A.targets && j == static_cast<uint64_t>(target) ? g : 0.0f;
-    dz[j] = static_cast<T>(one - p * (g + h * (kLn2 * finite_or_zero_weight(a) + entropy)));
+// g [soft part of p^T + label part of p]: w = 2^((z - M) c) times (a + b w), or a w + b 2^((z - M) c1).
+template <Temperatures kTemps>
+struct Slope {
+  float base, c, c1, a, b;
+  __device__ __forceinline__ Slope(const DistillArgs& A, const Sums& t, float s1, bool softened, bool labelled, float g) : base(base_of(t.m)), c(A.scale), c1(A.other_scale) {
+    const float soft = softened && !(t.s == 0.0f) ? g * A.soft_weight * A.temperature / t.s : 0.0f;
+    const float label = labelled && !(s1 == 0.0f) ? g * A.label_weight / s1 : 0.0f;
+    a = kTemps == Temperatures::kOne ? soft + label : soft;
+    b = label;
+  }
+  __device__ __forceinline__ float operator()(float z) const {
+    const float d = z - base, w = exp2_of(d * c);
+    if constexpr (kTemps == Temperatures::kOne) return a * w;
+    if constexpr (kTemps == Temperatures::kSquared) return w * __fmaf_rn(b, w, a);
+    return __fmaf_rn(b, exp2_of(d * c1), a * w);
+  }
+};
+
+template <typename T, uint32_t kThreads, uint32_t kVectors>
+__device__ __forceinline__ void fill_zeros(T* dz, uint32_t n) {
+  using V = Vector<T>;
+  const uint32_t whole = n / V::kElems;
+  const float zeros[V::kElems] = {};
+  for (uint32_t i = threadIdx.x; i < whole; i += kThreads) V::store(dz + i * V::kElems, zeros);
+  if (threadIdx.x < n - whole * V::kElems) dz[whole * V::kElems + threadIdx.x] = static_cast<T>(0.0f);
+}
+
+// The gradient of a held segment; then the entries of the teacher and the label over what was stored for them, each by the wave that
+// stored it (a wave's stores to one address are done in order).
+template <typename T, uint32_t kThreads, uint32_t kVectors, typename S>
+__device__ __forceinline__ void put_gradient(const Held<T, kThreads, kVectors>& held, T* dz, uint32_t first, const Teacher& teacher, const S& slope, float g) {
+  using V = Vector<T>;
+  held.each([&](uint32_t i, const float (&v)[V::kElems]) __attribute__((always_inline)) {
+    float d[V::kElems];
+#pragma unroll
+    for (uint32_t j = 0; j < V::kElems; ++j) d[j] = slope(v[j]);
+    if (held.mine(i)) V::store(dz + held.index(i), d);
+  });
+  if (held.has_rest()) dz[held.vectors * V::kElems + threadIdx.x] = static_cast<T>(slope(held.rest));
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  for (uint32_t i = threadIdx.x & 63u; i <= kTopMost; i += 64u) {
+    const uint32_t at = static_cast<uint32_t>(teacher.at[i]) - first;
+    if (teacher.at[i] < 0 || at >= held.n) continue;
+    if (Held<T, kThreads, kVectors>::owner(at, held.n) / 64u != threadIdx.x / 64u) continue;
+    dz[at] = static_cast<T>(slope(teacher.z[i]) - g * teacher.off[i]);
   }
 }
 
-template <typename T>
+template <Temperatures kTemps, typename H>
+__device__ __forceinline__ Sums distill_sums(const H& held, const DistillArgs& A) {
+  if constexpr (kTemps == Temperatures::kOne) return sums_of<Third::kNone, false>(held, A.scale, 0.0f);
+  return sums_of<Third::kOther, kTemps == Temperatures::kSquared>(held, A.scale, A.other_scale);
+}
+template <Temperatures kTemps>
+constexpr Third third_of() { return kTemps == Temperatures::kOne ? Third::kNone : Third::kOther; }
+
+// A workgroup a row: loss and gradient.
+template <typename T, uint32_t kThreads, uint32_t kVectors, Temperatures kTemps>
 __global__ void __launch_bounds__(kThreads) distill_kernel(DistillArgs A) {
-  __shared__ float lds[3 * kWaves];
-  __shared__ float q[kTopMost], q_log[kTopMost], z_at[kTopMost + 1];
-  __shared__ int32_t at[kTopMost + 1];
+  __shared__ float lds[3 * kThreads / 64u];
+  __shared__ Teacher teacher;
   const uint32_t r = blockIdx.x;
-  const T* z = static_cast<const T*>(A.logits) + static_cast<int64_t>(r) * A.row_stride;
+  const T* z = row_of<T>(A.logits, A.row_stride, r);
   T* dz = static_cast<T*>(A.grad_logits) + static_cast<int64_t>(r) * A.grad_row_stride;
   const int32_t target = A.targets ? A.targets[r] : -1;
-  const bool labelled = A.label_weight > 0.0f && is_token(target, A.vocab);
-  // the teacher's softmax, by the first wave (two entries a lane)
-  if (threadIdx.x < 64u) {
-    float t[2], largest = -INFINITY;
-    for (uint32_t u = 0; u < 2u; ++u) {
-      const uint32_t i = threadIdx.x + 64u * u;
-      int32_t index = -1;
-      t[u] = -INFINITY;
-      if (i < A.k && A.soft_weight > 0.0f) {
-        index = A.teacher_idx[static_cast<uint64_t>(r) * A.k + i];
-        if (!is_token(index, A.vocab)) index = -1;
-        if (index >= 0) t[u] = A.teacher_logits[static_cast<uint64_t>(r) * A.k + i];
-      }
-      at[i] = index;
-      largest = fmaxf(largest, t[u]);
-    }
-    for (int d = 1; d < 64; d <<= 1) largest = fmaxf(largest, __shfl_xor(largest, d));
-    float w[2], sum = 0.0f;
-    for (uint32_t u = 0; u < 2u; ++u) {
-      w[u] = t[u] != t[u] ? t[u] : exp2_of(exponent(t[u], largest, A.scale));
-      sum += w[u];
-    }
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    for (uint32_t u = 0; u < 2u; ++u) {
-      const uint32_t i = threadIdx.x + 64u * u;
-      q[i] = sum == 0.0f ? 0.0f : w[u] / sum;
-      q_log[i] = log_probability(t[u], largest, A.inv_t, kLn2 * log2_of(sum));
-      z_at[i] = at[i] >= 0 ? static_cast<float>(z[at[i]]) : 0.0f;
-    }
-    if (threadIdx.x == 0u) {
-      at[kTopMost] = labelled ? target : -1;
-      z_at[kTopMost] = labelled ? static_cast<float>(z[target]) : 0.0f;
-      lds[0] = sum;
-    }
-  }
-  __syncthreads();
-  const bool softened = A.soft_weight > 0.0f && !(lds[0] == 0.0f);
-  if (!softened && !labelled) {
+  const bool labelled = is_token(target, A.vocab);
+  if (!labelled && A.k == 0u) {
     if (threadIdx.x == 0u && A.loss) A.loss[r] = 0.0f;
-    if (A.grad_logits)
-      for (uint64_t j = threadIdx.x; j < A.vocab; j += kThreads) dz[j] = static_cast<T>(0.0f);
+    if (A.grad_logits) fill_zeros<T, kThreads, kVectors>(dz, A.vocab);
     return;
   }
-  const float c1 = A.scale * A.temperature;                      // the label's softmax has T = 1
-  Sums t{-INFINITY, 0.0f, 0.0f}, t1{-INFINITY, 0.0f, 0.0f};
-  for (uint64_t i = threadIdx.x; i < A.vocab; i += kThreads) {
-    add(t, static_cast<float>(z[i]), A.scale);
-    add(t1, static_cast<float>(z[i]), c1);
-  }
-  t = block_join(t, A.scale, lds);
-  t1 = block_join(t1, c1, lds);
-  const float m = t.m, log2s = m == -INFINITY ? 0.0f : log2_of(t.s), log2s1 = m == -INFINITY ? 0.0f : log2_of(t1.s);
-  const float T1 = A.temperature;
-  if (threadIdx.x < 64u && A.loss) {
-    float part = 0.0f;
-    if (softened)
-      for (uint32_t i = threadIdx.x; i < A.k; i += 64u)
-        if (!(q[i] == 0.0f)) part += q[i] * (q_log[i] - log_probability(z_at[i], m, A.inv_t, kLn2 * log2s));
-    for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d);
-    if (threadIdx.x == 0u) {
-      float loss = softened ? A.soft_weight * T1 * T1 * part : 0.0f;
-      if (labelled) loss -= A.label_weight * log_probability(z_at[kTopMost], m, 1.0f, kLn2 * log2s1);
-      A.loss[r] = loss;
-    }
-  }
-  if (!A.grad_logits) return;
+  const Held<T, kThreads, kVectors> held(z, A.vocab);
   const float g = A.grad_loss ? A.grad_loss[r] : 1.0f;
-  const float gs = softened ? A.soft_weight * T1 : 0.0f, gl = labelled ? A.label_weight : 0.0f;
-  auto smooth = [&](float v) {
-    float d = 0.0f;
-    if (softened) d += gs * exp2_of(exponent(v, m, A.scale) - log2s);
-    if (labelled) d += gl * exp2_of(exponent(v, m, c1) - log2s1);
-    return d;
-  };
-  for (uint64_t j = threadIdx.x; j < A.vocab; j += kThreads) dz[j] = static_cast<T>(g * smooth(static_cast<float>(z[j])));
-  __syncthreads();
-  // the teacher's entries and the label, over what was stored for them
-  for (uint32_t i = threadIdx.x; i <= kTopMost; i += kThreads) {
-    if (at[i] < 0) continue;
-    float off = labelled && at[i] == target ? gl : 0.0f;
-    if (softened)
-      for (uint32_t j = 0; j < A.k; ++j)
-        if (at[j] == at[i]) off += gs * q[j];
-    dz[at[i]] = static_cast<T>(g * (smooth(z_at[i]) - off));
+  TeacherLane lane{};
+  if (threadIdx.x < 64u) lane = teach(A, r, labelled ? target : -1, [&](uint32_t, int32_t i) { return static_cast<float>(z[i]); }, teacher);
+  const Sums t = spoiled(block_join<third_of<kTemps>(), kThreads / 64u>(distill_sums<kTemps>(held, A), A.scale, A.other_scale, lds));
+  const float s1 = kTemps == Temperatures::kOne ? t.s : t.e;
+  const bool softened = A.k > 0u && !(teacher.soft == 0.0f);
+  if (A.loss && threadIdx.x < 64u) put_loss(A, r, lane, softened, labelled, t, s1);
+  if (!A.grad_logits) return;
+  if (!softened && !labelled) fill_zeros<T, kThreads, kVectors>(dz, A.vocab);
+  else put_gradient(held, dz, 0u, teacher, Slope<kTemps>(A, t, s1, softened, labelled, g), g);
+}
+
+// Rows of several segments: the sums of each (and, by a row's first, the student's logits that the loss and the entries need, before
+// a gradient can take their place), then the gradient of each with all of them.
+template <typename T, uint32_t kThreads, uint32_t kVectors, Temperatures kTemps>
+__global__ void __launch_bounds__(kThreads) distill_sums_kernel(DistillArgs A, SplitArgs P) {
+  __shared__ float lds[3 * kThreads / 64u];
+  const uint32_t r = blockIdx.x / P.segments, segment = blockIdx.x - r * P.segments;
+  const uint32_t first = segment * P.length, n = min(A.vocab - first, P.length);
+  const T* z = row_of<T>(A.logits, A.row_stride, r);
+  const int32_t target = A.targets ? A.targets[r] : -1;
+  const Held<T, kThreads, kVectors> held(z + first, n);
+  if (segment == 0u && threadIdx.x < 64u) {
+    float* to = P.logits + static_cast<uint64_t>(r) * (kTopMost + 1u);
+    for (uint32_t i = threadIdx.x; i < A.k; i += 64u) {
+      const int32_t at = A.teacher_idx[static_cast<uint64_t>(r) * A.k + i];
+      if (is_token(at, A.vocab)) to[i] = static_cast<float>(z[at]);
+    }
+    if (threadIdx.x == 0u && is_token(target, A.vocab)) to[kTopMost] = static_cast<float>(z[target]);
+  }
+  const Sums t = block_join<third_of<kTemps>(), kThreads / 64u>(distill_sums<kTemps>(held, A), A.scale, A.other_scale, lds);
+  if (threadIdx.x == 0u) {
+    float* to = P.sums + 4ull * blockIdx.x;
+    to[0] = t.m;
+    to[1] = t.s;
+    to[2] = t.e;
   }
 }
+
+template <typename T, uint32_t kThreads, uint32_t kVectors, Temperatures kTemps>
+__global__ void __launch_bounds__(kThreads) distill_gradient_kernel(DistillArgs A, SplitArgs P) {
+  __shared__ Teacher teacher;
+  const uint32_t r = blockIdx.x / P.segments, segment = blockIdx.x - r * P.segments, lane_id = threadIdx.x & 63u;
+  const uint32_t first = segment * P.length, n = min(A.vocab - first, P.length);
+  const T* z = row_of<T>(A.logits, A.row_stride, r) + first;
+  T* dz = static_cast<T*>(A.grad_logits) + static_cast<int64_t>(r) * A.grad_row_stride + first;
+  const int32_t target = A.targets ? A.targets[r] : -1;
+  const bool labelled = is_token(target, A.vocab);
+  const Held<T, kThreads, kVectors> held(z, A.grad_logits ? n : 0u);
+  const float g = A.grad_loss ? A.grad_loss[r] : 1.0f;
+  Sums own = kNothing;
+  if (lane_id < P.segments) {
+    const float* from = P.sums + 4ull * (static_cast<uint64_t>(r) * P.segments + lane_id);
+    own = Sums{from[0], from[1], from[2]};
+  }
+  const Sums t = spoiled(wave_join<third_of<kTemps>()>(own, A.scale, A.other_scale));
+  const float s1 = kTemps == Temperatures::kOne ? t.s : t.e;
+  TeacherLane lane{};
+  const float* kept = P.logits + static_cast<uint64_t>(r) * (kTopMost + 1u);
+  if (threadIdx.x < 64u) lane = teach(A, r, labelled ? target : -1, [&](uint32_t i, int32_t) { return kept[i]; }, teacher);
+  __syncthreads();
+  const bool softened = A.k > 0u && !(teacher.soft == 0.0f);
+  if (A.loss && segment == 0u && threadIdx.x < 64u) put_loss(A, r, lane, softened, labelled, t, s1);
+  if (!A.grad_logits) return;
+  if (!softened && !labelled) fill_zeros<T, kThreads, kVectors>(dz, n);
+  else put_gradient(held, dz, first, teacher, Slope<kTemps>(A, t, s1, softened, labelled, g), g);
+}
+
+// ---------------------------------------------------------------- launches
+
+template <typename T, uint32_t kThreads_, uint32_t kVectors_>
+struct Shape {
+  using Type = T;
+  static constexpr uint32_t kThreads = kThreads_, kVectors = kVectors_, kCapacity = Held<T, kThreads_, kVectors_>::kCapacity;
+};
+
+// f(shape): of the workgroups that hold `length` logits, the one of fewest threads.  (More alternatives than threads make a poor line: see top_of.)
+template <typename T, typename F>
+void by_length(uint32_t length, uint32_t top, F&& f) {
+  if (length <= Shape<T, 64, 4>::kCapacity && top <= 64u) f(Shape<T, 64, 4>{});
+  else if (length <= Shape<T, 256, 4>::kCapacity) f(Shape<T, 256, 4>{});
+  else if (length <= Shape<T, 256, 8>::kCapacity) f(Shape<T, 256, 8>{});
+  else if (length <= Shape<T, 256, 16>::kCapacity) f(Shape<T, 256, 16>{});
+  else if (length <= Shape<T, 512, 16>::kCapacity) f(Shape<T, 512, 16>{});
+  else f(Shape<T, 1024, 16>{});
+}
+template <typename F>
+void by_type(int dtype, F&& f) {
+  if (dtype == 0) f(float{});
+  else if (dtype == 1) f(__bf16{});
+  else f(_Float16{});
+}
+
+// Logits that one workgroup holds at most, as Shape<T, 1024, 16>.
+uint32_t most_held(int dtype) { return dtype == 0 ? Shape<float, 1024, 16>::kCapacity : Shape<__bf16, 1024, 16>::kCapacity; }
 
 }  // namespace
 
-#define RGC_BY_TYPE(dtype, launch)                      \
-  do {                                                  \
-    if ((dtype) == 0) { using T = float; launch; }      \
-    else if ((dtype) == 1) { using T = __bf16; launch; } \
-    else { using T = _Float16; launch; }                \
-  } while (0)
+// Segments of whole vectors of either type, as few as hold the row.
+SplitArgs split_of(uint32_t vocab, int dtype) {
+  SplitArgs P{};
+  const uint32_t most = most_held(dtype);
+  P.segments = (vocab + most - 1u) / most;
+  P.length = P.segments == 1u ? vocab : ((vocab + P.segments - 1u) / P.segments + 7u) / 8u * 8u;
+  P.segments = (vocab + P.length - 1u) / P.length;
+  return P;
+}
 
-hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, hipStream_t s) {
-  RGC_BY_TYPE(dtype, (score_kernel<T><<<dim3(a.rows), dim3(kThreads), 0, s>>>(a)));
+hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, const SplitArgs& P, hipStream_t s) {
+  by_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    by_length<T>(P.length, a.top, [&](auto shape) {
+      using S = decltype(shape);
+      score_kernel<T, S::kThreads, S::kVectors><<<dim3(a.rows * P.segments), dim3(S::kThreads), 0, s>>>(a, P);
+    });
+    if (P.segments > 1u) score_join_kernel<T><<<dim3(a.rows), dim3(kJoinThreads), P.segments * a.top * sizeof(uint64_t), s>>>(a, P);
+  });
   return hipGetLastError();
 }
 
 hipError_t launch_token_logprobs_backward(const ScoreGradArgs& a, int dtype, hipStream_t s) {
-  RGC_BY_TYPE(dtype, (score_grad_kernel<T><<<dim3(a.rows), dim3(kThreads), 0, s>>>(a)));
+  by_type(dtype, [&](auto type) {
+    using T = decltype(type);
+    const uint32_t part = kGradThreads * kGradVectors * Vector<T>::kElems, parts = (a.vocab + part - 1u) / part;
+    score_grad_kernel<T><<<dim3(a.rows * parts), dim3(kGradThreads), 0, s>>>(a, parts);
+  });
   return hipGetLastError();
 }
 
-hipError_t launch_distill(const DistillArgs& a, int dtype, hipStream_t s) {
-  RGC_BY_TYPE(dtype, (distill_kernel<T><<<dim3(a.rows), dim3(kThreads), 0, s>>>(a)));
+hipError_t launch_distill(const DistillArgs& a, int dtype, const SplitArgs& P, hipStream_t s) {
+  auto launch = [&](auto temps) {
+    constexpr Temperatures kTemps = decltype(temps)::value;
+    by_type(dtype, [&](auto type) {
+      using T = decltype(type);
+      by_length<T>(P.length, 0u, [&](auto shape) {
+        using S = decltype(shape);
+        const dim3 threads(S::kThreads);
+        if (P.segments == 1u) {
+          distill_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(a.rows), threads, 0, s>>>(a);
+        } else if constexpr (S::kThreads == 1024u) {       // (a row of several segments has long ones)
+          distill_sums_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(a.rows * P.segments), threads, 0, s>>>(a, P);
+          distill_gradient_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(a.rows * P.segments), threads, 0, s>>>(a, P);
+        }
+      });
+    });
+  };
+  switch (a.temperatures) {
+    case Temperatures::kOne: launch(std::integral_constant<Temperatures, Temperatures::kOne>{}); break;
+    case Temperatures::kSquared: launch(std::integral_constant<Temperatures, Temperatures::kSquared>{}); break;
+    default: launch(std::integral_constant<Temperatures, Temperatures::kTwo>{}); break;
+  }
   return hipGetLastError();
 }
 
