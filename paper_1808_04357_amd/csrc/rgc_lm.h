@@ -64,7 +64,7 @@ struct SplitArgs {
   uint64_t* entries;         // [rows][segments][top]: scores
   float* logits;             // [rows][RGC_TOP_MAX + 1]: distillation
 };
-SplitArgs split_of(uint32_t vocab, int dtype);
+SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype);
 
 struct SequenceView {
   void* data;

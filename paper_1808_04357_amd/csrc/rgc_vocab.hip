@@ -118,10 +118,11 @@ template <typename T>
 struct Vector {
   static constexpr uint32_t kElems = 16u / sizeof(T);
   typedef uint32_t Words __attribute__((ext_vector_type(4)));
-  // aligned to an element only: a row of an odd vocabulary starts anywhere, and gfx950 reads and writes 16 bytes at any address
+  // aligned to an element only: gfx950 reads and writes 16 bytes at any address
   typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
 
-  static __device__ __forceinline__ Words load(const T* p) { return *reinterpret_cast<const Unaligned*>(p); }
+  static __device__ __forceinline__ Words load(const T* p) { return *reinterpret_cast<const Words*>(p); }
+  static __device__ __forceinline__ Words load_anywhere(const T* p) { return *reinterpret_cast<const Unaligned*>(p); }
   static __device__ __forceinline__ void store(T* p, const float (&v)[kElems]) {
     T t[kElems];
 #pragma unroll
@@ -138,27 +139,31 @@ struct Vector {
   }
 };
 
-// n elements from z on, by a workgroup of kThreads: vector i * kThreads + thread in raw[i], the up to kElems - 1 elements behind the last whole
-// vector one each by the first threads.  What is beyond the segment reads as -inf.
+// n elements from z on, by a workgroup of kThreads: vector i * kThreads + thread in raw[i].  Vectors begin on 16 bytes (an odd vocabulary's rows read at two bytes
+// off took 42 us more of 104); the few elements before the first and behind the last are held one each by the first threads.  What is beyond the segment
+// reads as -inf.
 template <typename T, uint32_t kThreads, uint32_t kVectors>
 struct Held {
   using V = Vector<T>;
   static constexpr uint32_t kElems = V::kElems, kCapacity = kThreads * kVectors * kElems;
   mutable typename V::Words raw[kVectors];
-  float rest;
-  uint32_t n, vectors, wave0;      // wave0: the wave's first thread
+  float single;
+  uint32_t n, head, vectors, wave0;      // wave0: the wave's first thread
 
-  __device__ __forceinline__ Held(const T* z, uint32_t n_) : n(n_), vectors(n_ / kElems), wave0(uniform(threadIdx.x & ~63u)) {
+  __device__ __forceinline__ Held(const T* z, uint32_t n_) : n(n_), wave0(uniform(threadIdx.x & ~63u)) {
+    head = min((16u - (static_cast<uint32_t>(reinterpret_cast<uintptr_t>(z)) & 15u)) % 16u / static_cast<uint32_t>(sizeof(T)), n);
+    vectors = (n - head) / kElems;
     if (vectors > 0u) {
+      const T* from = z + head;
       // (no branches between the reads, or the compiler waits for each: behind the end, the last vector again)
 #pragma unroll
-      for (uint32_t i = 0; i < kVectors; ++i) raw[i] = V::load(z + static_cast<uint64_t>(min(i * kThreads + threadIdx.x, vectors - 1u)) * kElems);
+      for (uint32_t i = 0; i < kVectors; ++i) raw[i] = V::load(from + static_cast<uint64_t>(min(i * kThreads + threadIdx.x, vectors - 1u)) * kElems);
     }
-    rest = has_rest() ? static_cast<float>(z[vectors * kElems + threadIdx.x]) : -INFINITY;
+    single = has_single() ? static_cast<float>(z[single_index()]) : -INFINITY;
   }
-  __device__ __forceinline__ bool has_rest() const { return threadIdx.x < n - vectors * kElems; }
-  __device__ __forceinline__ bool any() const { return threadIdx.x < vectors || has_rest(); }
-  __device__ __forceinline__ uint32_t index(uint32_t i) const { return (i * kThreads + threadIdx.x) * kElems; }
+  __device__ __forceinline__ bool has_single() const { return threadIdx.x < n - vectors * kElems; }
+  __device__ __forceinline__ uint32_t single_index() const { return threadIdx.x < head ? threadIdx.x : threadIdx.x + vectors * kElems; }
+  __device__ __forceinline__ uint32_t index(uint32_t i) const { return head + (i * kThreads + threadIdx.x) * kElems; }
   __device__ __forceinline__ bool mine(uint32_t i) const { return i * kThreads + threadIdx.x < vectors; }
   // f(i, values): for the vectors of which the wave has any
   template <typename F>
@@ -178,9 +183,10 @@ struct Held {
     }
   }
   // Which thread holds element `at` of the segment.
-  __device__ __forceinline__ static uint32_t owner(uint32_t at, uint32_t n) {
-    const uint32_t whole = n / kElems;
-    return at / kElems < whole ? at / kElems % kThreads : at - whole * kElems;
+  __device__ __forceinline__ uint32_t owner(uint32_t at) const {
+    if (at < head) return at;
+    const uint32_t vector = (at - head) / kElems;
+    return vector < vectors ? vector % kThreads : at - vectors * kElems;
   }
 };
 
@@ -190,9 +196,9 @@ __device__ __forceinline__ float weigh(float z, float base, float c) { return ex
 // of these (T = 2).
 template <Third kThird, bool kSquared, typename H>
 __device__ __forceinline__ Sums sums_of(const H& held, float c, float c1) {
-  Sums t{held.rest, 0.0f, 0.0f};
+  Sums t{held.single, 0.0f, 0.0f};
   {
-    const float base = base_of(t.m), w = weigh(held.rest, base, c);      // 1, 0 for -inf, NaN for NaN and +inf
+    const float base = base_of(t.m), w = weigh(held.single, base, c);      // 1, 0 for -inf, NaN for NaN and +inf
     t.s = w;
     if constexpr (kThird == Third::kOther) t.e = w;
   }
@@ -239,21 +245,31 @@ constexpr uint32_t kListed = 1024;      // candidates a workgroup can list
 template <uint32_t kThreads>
 struct TopShared {
   uint64_t list[kListed];
-  uint32_t largest[kThreads];           // of every thread, by order
-  uint32_t count, line, scan[kThreads / 64u];
+  uint32_t line[kThreads / 64u];        // of every wave
+  uint32_t count, scan[kThreads / 64u];
 };
 
-// The largest number, looked at from bit `from` down to bit `to`, that at least k of the wave's values (kEach a lane) reach.
-template <uint32_t kEach>
-__device__ __forceinline__ uint32_t reached_by(const uint32_t (&v)[kEach], uint32_t k, uint32_t line, int from, int to) {
+// The largest number, looked for from bit `from` down to bit `to`, that at least k of the wave's lanes reach.
+__device__ __forceinline__ uint32_t reached_by(uint32_t v, uint32_t k, uint32_t line, int from, int to) {
   for (int bit = from; bit >= to; --bit) {
     const uint32_t higher = line | (1u << bit);
-    uint32_t n = 0;
-#pragma unroll
-    for (uint32_t i = 0; i < kEach; ++i) n += popc64(__ballot(v[i] >= higher));
-    if (n >= k) line = higher;
+    if (popc64(__ballot(v >= higher)) >= k) line = higher;
   }
   return line;
+}
+
+// How many of n entries come before e.
+__device__ __forceinline__ uint32_t rank_in(const uint64_t* list, uint32_t n, uint64_t e) {
+  uint32_t rank = 0, j = 0;
+  for (; j + 8u <= n; j += 8u) {      // (eight reads in flight)
+    uint64_t v[8];
+#pragma unroll
+    for (uint32_t i = 0; i < 8u; ++i) v[i] = list[j + i];
+#pragma unroll
+    for (uint32_t i = 0; i < 8u; ++i) rank += v[i] > e ? 1u : 0u;
+  }
+  for (; j < n; ++j) rank += list[j] > e ? 1u : 0u;
+  return rank;
 }
 
 // f(index, logit) for every logit of a segment, read (again) from memory.
@@ -264,7 +280,7 @@ __device__ __forceinline__ void read_again(const T* z, uint32_t n, F&& f) {
 #pragma unroll 1
   for (uint32_t i = threadIdx.x; i < vectors; i += kThreads) {
     float v[V::kElems];
-    V::unpack(V::load(z + i * V::kElems), v);
+    V::unpack(V::load_anywhere(z + i * V::kElems), v);
 #pragma unroll
     for (uint32_t j = 0; j < V::kElems; ++j) f(i * V::kElems + j, v[j]);
   }
@@ -284,7 +300,7 @@ __device__ __forceinline__ uint32_t count_above(const T* z, uint32_t n, uint32_t
 // lds.list: the k largest, where more logits than it holds reach a line, `line` not above the k-th largest.  Those above the k-th largest, and
 // then those equal to it in the order of their indices.
 template <typename T, uint32_t kThreads>
-__device__ __noinline__ void list_exactly(const T* z, uint32_t n, uint32_t line, uint32_t k, uint32_t first, TopShared<kThreads>& lds) {
+__device__ __forceinline__ void list_exactly(const T* z, uint32_t n, uint32_t line, uint32_t k, uint32_t first, TopShared<kThreads>& lds) {
   uint32_t above = count_above<T, kThreads>(z, n, line, lds);
   if (above >= k) {                                        // the k-th largest is higher: bit by bit
     uint32_t found = 0u;
@@ -319,63 +335,82 @@ __device__ __noinline__ void list_exactly(const T* z, uint32_t n, uint32_t line,
   __syncthreads();
 }
 
-// The k largest (k <= the segment's length), put(rank, entry) each.  `t`: the thread's largest; `spoilt`: there is a NaN or +inf among them.
-//  A line under the k-th largest of all comes cheap: the k-th largest of the threads' largest.  Few logits reach it (with 256 threads some
-// 1.02 k for k = 10, 1.4 k for k = 128, where they lie anywhere); they are listed and ranked.  Where more do than the list holds, as with many equal ones
-// (a mask that leaves fewer than k), list_exactly reads the segment again.
-template <typename T, uint32_t kThreads, typename H, typename Put>
-__device__ __forceinline__ void top_of(const H& held, const T* z, float t, bool spoilt, uint32_t k, uint32_t first, TopShared<kThreads>& lds, Put&& put) {
-  constexpr uint32_t kEach = kThreads >= 256u ? 4u : kThreads / 64u;      // groups of threads a lane of the first wave stands for
-  const uint32_t lane = threadIdx.x & 63u;
-  lds.largest[threadIdx.x] = held.any() ? order_of(t) : 0u;
+//  A line under the k-th largest of a segment comes cheap: with q = ceil(k / waves), every wave's q-th largest of its lanes' largest is reached by q logits
+// of that wave, so the lowest of these is reached by k.  (Of the waves all of whose lanes have a vector, that is; without one all logits reach it.)  Few more reach it (where the logits lie anywhere: some 20 with four waves and k = 8, 100 with k = 64,
+// 55 with sixteen waves and k = 8); they are listed and ranked.  Where more do than the list holds, as with many equal ones (a mask that leaves
+// fewer than k), list_exactly reads the segment again.
+template <uint32_t kThreads, typename H>
+__device__ __forceinline__ uint32_t line_of(const H& held, float t, uint32_t k, uint32_t line, int from, int to) {
+  const uint32_t full = min(kThreads, held.vectors) / 64u;
+  if (full == 0u) return 0u;
+  if (threadIdx.x / 64u >= full) return 0xFFFFFFFFu;
+  return reached_by(order_of(t), (k + full - 1u) / full, line, from, to);
+}
+// Before the barrier of the sums' join; t: the thread's largest.
+template <uint32_t kThreads, typename H>
+__device__ __forceinline__ uint32_t put_line(const H& held, float t, uint32_t k, TopShared<kThreads>& lds) {
+  // (sixteen bits of it will do: a line a little lower lets a few more through)
+  const uint32_t line = line_of<kThreads>(held, t, k, 0u, 31, 16);
+  if ((threadIdx.x & 63u) == 0u) lds.line[threadIdx.x >> 6] = line;
   if (threadIdx.x == 0u) lds.count = 0u;
-  __syncthreads();
-  uint32_t group[kEach];
-  uint32_t line = 0u;
-  if (threadIdx.x < 64u) {
+  return line;
+}
+template <uint32_t kThreads>
+__device__ __forceinline__ uint32_t lowest_line(const TopShared<kThreads>& lds) {
+  uint32_t line = lds.line[0];
 #pragma unroll
-    for (uint32_t i = 0; i < kEach; ++i) {
-      group[i] = 0u;
-      for (uint32_t j = lane + 64u * i; j < kThreads; j += 64u * kEach) group[i] = max(group[i], lds.largest[j]);
-    }
-    // (sixteen bits of it will do: a line a little lower lets a few more through)
-    line = reached_by<kEach>(group, k, 0u, 31, 16);
-    if (lane == 0u) lds.line = line;
-  }
-  __syncthreads();
-  line = uniform(lds.line);
+  for (uint32_t w = 1; w < kThreads / 64u; ++w) line = min(line, lds.line[w]);
+  return uniform(line);
+}
+
+// Behind that barrier: the k largest (k <= the segment's length), put(rank, entry) each.  `own`: what put_line gave; `spoilt`: there is a NaN or +inf among them.
+template <typename T, uint32_t kThreads, typename H, typename Put>
+__device__ __forceinline__ void top_of(const H& held, const T* z, float t, uint32_t own, bool spoilt, uint32_t k, uint32_t first, TopShared<kThreads>& lds, Put&& put) {
   if (!spoilt) {
-    auto list = [&](float v, uint32_t index) __attribute__((always_inline)) {
-      const uint32_t at = atomicAdd(&lds.count, 1u);
-      if (at < kListed) lds.list[at] = entry_of(v, first + index);
-    };
+    const uint32_t line = lowest_line<kThreads>(lds);
     const float least = line <= 0x007FFFFFu ? -INFINITY : logit_of(line);      // (below the order of -inf all are taken)
+    // (a wave's hits of one vector take their places in the list together)
+    auto list = [&](uint32_t bits, const float* v, uint32_t index) __attribute__((always_inline)) {
+      const uint32_t n = static_cast<uint32_t>(__popc(bits)), incl = wave_incl_scan(n);
+      uint32_t base = 0u;
+      if ((threadIdx.x & 63u) == 0u) base = atomicAdd(&lds.count, wave_total(incl));
+      uint32_t at = uniform(base) + incl - n;
+#pragma unroll
+      for (uint32_t j = 0; j < H::kElems; ++j)
+        if ((bits >> j) & 1u) {
+          if (at < kListed) lds.list[at] = entry_of(v[j], first + index + j);
+          ++at;
+        }
+    };
     held.each([&](uint32_t i, const float (&v)[H::kElems]) __attribute__((always_inline)) {
       float most = v[0];
 #pragma unroll
       for (uint32_t j = 1; j < H::kElems; ++j) most = fmaxf(most, v[j]);
-      if (!(most >= least) || !held.mine(i)) return;
+      const bool hit = most >= least && held.mine(i);
+      if (!__any(hit)) return;
+      uint32_t bits = 0;
 #pragma unroll
-      for (uint32_t j = 0; j < H::kElems; ++j)
-        if (v[j] >= least) list(v[j], held.index(i) + j);
+      for (uint32_t j = 0; j < H::kElems; ++j) bits |= v[j] >= least ? 1u << j : 0u;
+      list(hit ? bits : 0u, v, held.index(i));
     });
-    if (held.has_rest() && held.rest >= least) list(held.rest, held.vectors * H::kElems + threadIdx.x);
+    const bool hit = held.has_single() && held.single >= least;
+    if (__any(hit)) {
+      const float v[H::kElems] = {held.single};
+      list(hit ? 1u : 0u, v, held.single_index());
+    }
   }
   __syncthreads();
   uint32_t listed = uniform(lds.count);
   if (spoilt || listed > kListed) {
-    if (threadIdx.x < 64u) {
-      const uint32_t exact = spoilt ? 0u : reached_by<kEach>(group, k, line, 15, 0);
-      if (lane == 0u) lds.line = exact;
-    }
+    const uint32_t exact = line_of<kThreads>(held, t, k, own, 15, 0);
+    if ((threadIdx.x & 63u) == 0u) lds.line[threadIdx.x >> 6] = spoilt ? 0u : exact;
     __syncthreads();
-    list_exactly<T, kThreads>(z, held.n, uniform(lds.line), k, first, lds);
+    list_exactly<T, kThreads>(z, held.n, lowest_line<kThreads>(lds), k, first, lds);
     listed = k;
   }
   for (uint32_t i = threadIdx.x; i < listed; i += kThreads) {
     const uint64_t e = lds.list[i];
-    uint32_t rank = 0;
-    for (uint32_t j = 0; j < listed; ++j) rank += lds.list[j] > e ? 1u : 0u;
+    const uint32_t rank = rank_in(lds.list, listed, e);
     if (rank < k) put(rank, e);
   }
 }
@@ -410,6 +445,39 @@ __device__ __forceinline__ void put_scores(const ScoreArgs& A, uint32_t r, const
   }
 }
 
+// A row whose largest logit has nearly all the weight has S = 1 + x with a small x, of which fp32 keeps little beside the 1, and its log probability is
+// -ln(1 + x).  Up to this S, x is added up by itself.
+constexpr float kNearlyOne = 1.25f;
+__device__ __forceinline__ float log_of_sum(float s, float x) { return s >= 1.0f && s < kNearlyOne ? log1pf(x) : kLn2 * log2_of(s); }
+
+// The weights of all logits but one of the largest, t.m; the same in every thread.  Only the thread that holds that one has the loss: it adds its own up again.
+// join: what block_join left (three floats a wave); lds: a float a wave.  Holds a barrier.
+template <uint32_t kThreads, typename H>
+__device__ __forceinline__ float others_of(const H& held, const Sums& own, const Sums& t, float c, const float* join, float* lds) {
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
+  uint32_t holder = 0u;
+  while (holder + 1u < kThreads / 64u && join[3u * holder] != t.m) ++holder;
+  float x = rebased<Third::kNone>(own, t.m, c, 0.0f).s;
+  if (wave == uniform(holder)) {
+    const uint32_t first = static_cast<uint32_t>(__ffsll(__ballot(own.m == t.m)) - 1);
+    float rest = 0.0f, equal = 0.0f;
+    auto add = [&](float v) __attribute__((always_inline)) {
+      rest += v == t.m ? 0.0f : weigh(v, t.m, c);
+      equal += v == t.m ? 1.0f : 0.0f;
+    };
+    add(held.single);
+    held.each([&](uint32_t, const float (&v)[H::kElems]) __attribute__((always_inline)) {
+#pragma unroll
+      for (uint32_t j = 0; j < H::kElems; ++j) add(v[j]);
+    });
+    if (lane == first) x = rest + (equal - 1.0f);
+  }
+  x = wave_sum(x);
+  if (lane == 0u) lds[wave] = x;
+  __syncthreads();
+  return wave_sum(lane < kThreads / 64u ? lds[lane] : 0.0f);
+}
+
 template <typename T>
 __device__ __forceinline__ const T* row_of(const void* p, int64_t stride, uint32_t r) {
   return static_cast<const T*>(p) + static_cast<int64_t>(r) * stride;
@@ -418,7 +486,7 @@ __device__ __forceinline__ const T* row_of(const void* p, int64_t stride, uint32
 // A workgroup a segment.  One segment a row: its results; several: its sums and its top entries for score_join_kernel.
 template <typename T, uint32_t kThreads, uint32_t kVectors>
 __global__ void __launch_bounds__(kThreads) score_kernel(ScoreArgs A, SplitArgs P) {
-  __shared__ float lds[3 * kThreads / 64u];
+  __shared__ float lds[3 * kThreads / 64u], lds_others[kThreads / 64u];
   __shared__ TopShared<kThreads> top;
   const uint32_t r = blockIdx.x / P.segments, segment = blockIdx.x - r * P.segments;
   const uint32_t first = segment * P.length, n = min(A.vocab - first, P.length);
@@ -429,24 +497,29 @@ __global__ void __launch_bounds__(kThreads) score_kernel(ScoreArgs A, SplitArgs 
     return;
   }
   const Held<T, kThreads, kVectors> held(z + first, n);
+  const float at_target = P.segments == 1u && threadIdx.x == 0u ? static_cast<float>(z[target]) : 0.0f;
   const Sums own = sums_of<Third::kEntropy, false>(held, A.scale, 0.0f);
+  const uint32_t k = min(A.top, n), line = k > 0u ? put_line<kThreads>(held, own.m, k, top) : 0u;
   const Sums raw = block_join<Third::kEntropy, kThreads / 64u>(own, A.scale, 0.0f, lds);
+  float x = raw.s - 1.0f;
+  if (raw.s >= 1.0f && raw.s < kNearlyOne) x = others_of<kThreads>(held, own, raw, A.scale, lds, lds_others);
   const Sums t = spoiled(raw);
-  const float log_sum = kLn2 * log2_of(t.s);
   if (P.segments == 1u) {
-    if (threadIdx.x == 0u) put_scores(A, r, t, log_sum, static_cast<float>(z[target]));
-    if (A.top > 0u)
-      top_of<T, kThreads>(held, z + first, own.m, t.s != t.s, A.top, 0u, top, [&](uint32_t rank, uint64_t e) { put_alternative(A, r, rank, e, t, log_sum); });
+    const float log_sum = log_of_sum(t.s, x);
+    if (threadIdx.x == 0u) put_scores(A, r, t, log_sum, at_target);
+    if (k > 0u)
+      top_of<T, kThreads>(held, z, own.m, line, t.s != t.s, k, 0u, top, [&](uint32_t rank, uint64_t e) { put_alternative(A, r, rank, e, t, log_sum); });
   } else {
     if (threadIdx.x == 0u) {
       float* to = P.sums + 4ull * blockIdx.x;
       to[0] = raw.m;
       to[1] = raw.s;
       to[2] = raw.e;
+      to[3] = x;
     }
-    const uint32_t k = min(A.top, n);
     if (k > 0u)
-      top_of<T, kThreads>(held, z + first, own.m, t.s != t.s, k, first, top, [&](uint32_t rank, uint64_t e) { P.entries[static_cast<uint64_t>(blockIdx.x) * A.top + rank] = e; });
+      top_of<T, kThreads>(held, z + first, own.m, line, t.s != t.s, k, first, top,
+                          [&](uint32_t rank, uint64_t e) { P.entries[static_cast<uint64_t>(blockIdx.x) * A.top + rank] = e; });
   }
 }
 
@@ -461,27 +534,38 @@ __global__ void __launch_bounds__(kJoinThreads) score_join_kernel(ScoreArgs A, S
     put_left_out(A, r);
     return;
   }
+  const float at_target = static_cast<float>(row_of<T>(A.logits, A.row_stride, r)[target]);
   Sums own = kNothing;
+  float x = 0.0f;                                          // of the segment's weights, without one of its largest
   if (lane < P.segments) {
     const float* from = P.sums + 4ull * (static_cast<uint64_t>(r) * P.segments + lane);
     own = Sums{from[0], from[1], from[2]};
+    x = from[3];
   }
-  const uint32_t all = P.segments * A.top;
-  auto length = [&](uint32_t s) { return s + 1u == P.segments ? min(A.top, last) : A.top; };      // (a segment but the last has more than RGC_TOP_MAX logits)
-  for (uint32_t i = threadIdx.x; i < all; i += kJoinThreads)
-    if (i % A.top < length(i / A.top)) entries[i] = P.entries[static_cast<uint64_t>(r) * all + i];
+  // (every segment but the last has more than RGC_TOP_MAX logits)
+  const uint32_t all = (P.segments - 1u) * A.top + min(A.top, last);
+  for (uint32_t i = threadIdx.x; i < all; i += kJoinThreads) entries[i] = P.entries[static_cast<uint64_t>(r) * P.segments * A.top + i];
   const Sums t = spoiled(wave_join<Third::kEntropy>(own, A.scale, 0.0f));
-  const float log_sum = kLn2 * log2_of(t.s);
-  if (threadIdx.x == 0u) put_scores(A, r, t, log_sum, static_cast<float>(row_of<T>(A.logits, A.row_stride, r)[target]));
+  // the first segment that has the largest logit counts without it
+  const unsigned long long holders = __ballot(own.m == t.m);
+  x = wave_sum(holders != 0ull && lane == static_cast<uint32_t>(__ffsll(holders) - 1) ? x : rebased<Third::kNone>(own, t.m, A.scale, 0.0f).s);
+  const float log_sum = log_of_sum(t.s, x);
+  if (threadIdx.x == 0u) put_scores(A, r, t, log_sum, at_target);
   __syncthreads();
+  if (all <= 2u * kJoinThreads) {
+    for (uint32_t i = threadIdx.x; i < all; i += kJoinThreads) {
+      const uint32_t rank = rank_in(entries, all, entries[i]);
+      if (rank < A.top) put_alternative(A, r, rank, entries[i], t, log_sum);
+    }
+    return;
+  }
   for (uint32_t i = threadIdx.x; i < all; i += kJoinThreads) {
     const uint32_t segment = i / A.top;
-    if (i - segment * A.top >= length(segment)) continue;
     const uint64_t e = entries[i];
     uint32_t rank = i - segment * A.top;
     for (uint32_t s = 0; s < P.segments && rank < A.top; ++s) {
       if (s == segment) continue;
-      uint32_t low = 0, high = length(s);                  // how many of that segment's entries come before e
+      uint32_t low = 0, high = s + 1u == P.segments ? min(A.top, last) : A.top;      // how many of that segment's entries come before e
       while (low < high) {
         const uint32_t mid = (low + high) / 2u;
         if (entries[s * A.top + mid] > e) low = mid + 1u; else high = mid;
@@ -505,11 +589,12 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs 
   const float m = A.stats[2ull * r], log_sum = A.stats[2ull * r + 1u];
   const bool nothing = (A.targets && !is_token(target, A.vocab)) || log_sum == -INFINITY;
   const Held<T, kGradThreads, kGradVectors> held(z, n);
-  const uint32_t whole = n / V::kElems;
   if (nothing) {
-    const float zeros[V::kElems] = {};
-    for (uint32_t i = threadIdx.x; i < whole; i += kGradThreads) V::store(dz + i * V::kElems, zeros);
-    if (held.has_rest()) dz[whole * V::kElems + threadIdx.x] = static_cast<T>(0.0f);
+    held.each([&](uint32_t i, const float (&)[V::kElems]) __attribute__((always_inline)) {
+      const float zeros[V::kElems] = {};
+      if (held.mine(i)) V::store(dz + held.index(i), zeros);
+    });
+    if (held.has_single()) dz[held.single_index()] = static_cast<T>(0.0f);
     return;
   }
   const float g = A.grad_logprob ? A.grad_logprob[r] * A.inv_t : 0.0f, h = A.grad_entropy ? A.grad_entropy[r] * A.inv_t : 0.0f;
@@ -521,7 +606,7 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs 
     return -exp2_of(a) * __fmaf_rn(w, as_factor(a), u);
   };
   const uint32_t at = static_cast<uint32_t>(target) - first;       // of the target in this part, if it is
-  const bool here = target >= 0 && at < n && Held<T, kGradThreads, kGradVectors>::owner(at, n) == threadIdx.x;
+  const bool here = target >= 0 && at < n && held.owner(at) == threadIdx.x;
   const float at_target = here ? static_cast<float>(z[at]) : 0.0f;
   held.each([&](uint32_t i, const float (&v)[V::kElems]) __attribute__((always_inline)) {
     float d[V::kElems];
@@ -529,17 +614,19 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs 
     for (uint32_t j = 0; j < V::kElems; ++j) d[j] = slope(v[j]);
     if (held.mine(i)) V::store(dz + held.index(i), d);
   });
-  if (held.has_rest()) dz[whole * V::kElems + threadIdx.x] = static_cast<T>(slope(held.rest));
+  if (held.has_single()) dz[held.single_index()] = static_cast<T>(slope(held.single));
   if (here) dz[at] = static_cast<T>(g + slope(at_target));         // over what the same thread has just stored
 }
 
 // ---------------------------------------------------------------- distillation
 
 // A row's teacher entries and label, made by the first wave.
+constexpr uint32_t kSeenBits = 65536;
 struct Teacher {
   int32_t at[kTopMost + 1];             // an index, once; the label's last unless it is one of the others; -1: none
   float off[kTopMost + 1], z[kTopMost + 1];      // what is subtracted there, and the student's logit
   float soft;                           // sum of the weights q: 0 if there are none
+  uint32_t seen[kSeenBits / 32u];
 };
 
 // Two entries a lane.
@@ -576,32 +663,44 @@ __device__ __forceinline__ TeacherLane teach(const DistillArgs& A, uint32_t r, i
   }
   sum = wave_sum(sum);
   const float log_sum = kLn2 * log2_of(sum);
-  float off[2] = {0.0f, 0.0f};
+  float off[2];
   bool again[2] = {false, false};
 #pragma unroll
   for (uint32_t u = 0; u < 2u; ++u) {
-    t.q[u] = sum == 0.0f ? 0.0f : w[u] / sum;
+    off[u] = t.q[u] = sum == 0.0f ? 0.0f : w[u] / sum;
     t.log_q[u] = log_probability(z[u], largest, A.inv_t, log_sum);
   }
-  bool label_listed = false;
-  for (uint32_t j = 0; j < A.k; ++j) {
-    const uint32_t from = j & 63u;
-    const int32_t at = __builtin_amdgcn_readlane(j < 64u ? t.at[0] : t.at[1], static_cast<int>(from));
-    const float q = lane_of(j < 64u ? t.q[0] : t.q[1], from);
-    label_listed |= at == label;
+  // An index that comes twice has both weights, at its first place.  Few rows have any: whether one may come twice is told by a bit for every index (one of
+  // kSeenBits), and those that find theirs set are looked for among all.  (A loop over all entries took 20 us of 108, 2048 rows of 64.)
 #pragma unroll
-    for (uint32_t u = 0; u < 2u; ++u)
-      if (at == t.at[u]) {
-        off[u] += q;
-        again[u] |= j < lane + 64u * u;
-      }
+  for (uint32_t i = 0; i < kSeenBits / 32u / 256u; ++i) reinterpret_cast<uint4*>(to.seen)[i * 64u + lane] = uint4{0u, 0u, 0u, 0u};
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+  for (uint32_t u = 0; u < 2u; ++u) {
+    const uint32_t h = (static_cast<uint32_t>(t.at[u]) * 2654435761u) >> 16;
+    unsigned long long met = __ballot(t.at[u] >= 0 && ((atomicOr(&to.seen[h / 32u], t.at[u] >= 0 ? 1u << (h & 31u) : 0u) >> (h & 31u)) & 1u) != 0u);
+    for (; met != 0ull; met &= met - 1ull) {
+      const int32_t at = __builtin_amdgcn_readlane(t.at[u], __ffsll(met) - 1);
+      const unsigned long long in0 = __ballot(t.at[0] == at), in1 = __ballot(t.at[1] == at);
+      if (__popcll(in0) + __popcll(in1) < 2) continue;
+      const uint32_t place = in0 != 0ull ? static_cast<uint32_t>(__ffsll(in0) - 1) : 64u + static_cast<uint32_t>(__ffsll(in1) - 1);
+      float both = 0.0f;
+      for (unsigned long long m = in0; m != 0ull; m &= m - 1ull) both += lane_of(t.q[0], static_cast<uint32_t>(__ffsll(m) - 1));
+      for (unsigned long long m = in1; m != 0ull; m &= m - 1ull) both += lane_of(t.q[1], static_cast<uint32_t>(__ffsll(m) - 1));
+#pragma unroll
+      for (uint32_t w = 0; w < 2u; ++w)
+        if (t.at[w] == at) {
+          if (lane + 64u * w == place) off[w] = both; else again[w] = true;
+        }
+    }
   }
+  const bool label_listed = label >= 0 && __any(t.at[0] == label || t.at[1] == label);
   const float soft = A.soft_weight * A.temperature;
 #pragma unroll
   for (uint32_t u = 0; u < 2u; ++u) {
     const uint32_t i = lane + 64u * u;
     to.at[i] = again[u] ? -1 : t.at[u];
-    to.off[i] = soft * off[u] + (t.at[u] == label ? A.label_weight : 0.0f);
+    to.off[i] = soft * off[u] + (t.at[u] >= 0 && t.at[u] == label ? A.label_weight : 0.0f);
     to.z[i] = t.z[u];
   }
   if (lane == 0u) {
@@ -666,13 +765,13 @@ __device__ __forceinline__ void put_gradient(const Held<T, kThreads, kVectors>& 
     for (uint32_t j = 0; j < V::kElems; ++j) d[j] = slope(v[j]);
     if (held.mine(i)) V::store(dz + held.index(i), d);
   });
-  if (held.has_rest()) dz[held.vectors * V::kElems + threadIdx.x] = static_cast<T>(slope(held.rest));
+  if (held.has_single()) dz[held.single_index()] = static_cast<T>(slope(held.single));
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
   for (uint32_t i = threadIdx.x & 63u; i <= kTopMost; i += 64u) {
     const uint32_t at = static_cast<uint32_t>(teacher.at[i]) - first;
     if (teacher.at[i] < 0 || at >= held.n) continue;
-    if (Held<T, kThreads, kVectors>::owner(at, held.n) / 64u != threadIdx.x / 64u) continue;
+    if (held.owner(at) / 64u != threadIdx.x / 64u) continue;
     dz[at] = static_cast<T>(slope(teacher.z[i]) - g * teacher.off[i]);
   }
 }
@@ -777,16 +876,21 @@ struct Shape {
   static constexpr uint32_t kThreads = kThreads_, kVectors = kVectors_, kCapacity = Held<T, kThreads_, kVectors_>::kCapacity;
 };
 
+constexpr uint32_t kFewRows = 128, kFewSegments = 2, kWanted = 512, kFewWorkgroups = 256;
+
 // f(shape): of the workgroups that hold `length` logits, the one of fewest threads.  (More alternatives than threads make a poor line: see top_of.)
+// With fewer workgroups than compute units, of sixteen waves: one workgroup's time is all there is.
 template <typename T, typename F>
-void by_length(uint32_t length, uint32_t top, F&& f) {
+void by_length(uint32_t length, uint32_t top, uint32_t workgroups, F&& f) {
   if (length <= Shape<T, 64, 4>::kCapacity && top <= 64u) f(Shape<T, 64, 4>{});
   else if (length <= Shape<T, 256, 4>::kCapacity) f(Shape<T, 256, 4>{});
+  else if (length <= Shape<T, 1024, 4>::kCapacity && workgroups <= kFewWorkgroups) f(Shape<T, 1024, 4>{});
   else if (length <= Shape<T, 256, 8>::kCapacity) f(Shape<T, 256, 8>{});
   else if (length <= Shape<T, 256, 16>::kCapacity) f(Shape<T, 256, 16>{});
   else if (length <= Shape<T, 512, 16>::kCapacity) f(Shape<T, 512, 16>{});
   else f(Shape<T, 1024, 16>{});
 }
+
 template <typename F>
 void by_type(int dtype, F&& f) {
   if (dtype == 0) f(float{});
@@ -794,17 +898,19 @@ void by_type(int dtype, F&& f) {
   else f(_Float16{});
 }
 
-// Logits that one workgroup holds at most, as Shape<T, 1024, 16>.
-uint32_t most_held(int dtype) { return dtype == 0 ? Shape<float, 1024, 16>::kCapacity : Shape<__bf16, 1024, 16>::kCapacity; }
-
 }  // namespace
 
-// Segments of whole vectors of either type, as few as hold the row.
-SplitArgs split_of(uint32_t vocab, int dtype) {
+// One segment where a workgroup holds the row, unless there are few rows of many logits: then as many as give every compute unit two workgroups
+// (each launch more of them takes 3 us, and what comes after the segments another launch).
+SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype) {
   SplitArgs P{};
-  const uint32_t most = most_held(dtype);
-  P.segments = (vocab + most - 1u) / most;
-  P.length = P.segments == 1u ? vocab : ((vocab + P.segments - 1u) / P.segments + 7u) / 8u * 8u;
+  const uint32_t most = dtype == 0 ? Shape<float, 1024, 16>::kCapacity : Shape<__bf16, 1024, 16>::kCapacity;
+  const uint32_t small = dtype == 0 ? Shape<float, 256, 8>::kCapacity : Shape<__bf16, 256, 8>::kCapacity;
+  const uint32_t big = (vocab + most - 1u) / most, many = (vocab + small - 1u) / small;
+  uint32_t segments = big;
+  if (static_cast<uint64_t>(rows) * big < kFewRows && vocab > kFewSegments * small && many <= 64u)
+    segments = min(64u, max(many, min((kWanted + rows - 1u) / rows, 2u * many)));
+  P.length = segments == 1u ? vocab : ((vocab + segments - 1u) / segments + 7u) / 8u * 8u;
   P.segments = (vocab + P.length - 1u) / P.length;
   return P;
 }
@@ -812,7 +918,7 @@ SplitArgs split_of(uint32_t vocab, int dtype) {
 hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, const SplitArgs& P, hipStream_t s) {
   by_type(dtype, [&](auto type) {
     using T = decltype(type);
-    by_length<T>(P.length, a.top, [&](auto shape) {
+    by_length<T>(P.length, a.top, a.rows * P.segments, [&](auto shape) {
       using S = decltype(shape);
       score_kernel<T, S::kThreads, S::kVectors><<<dim3(a.rows * P.segments), dim3(S::kThreads), 0, s>>>(a, P);
     });
@@ -835,12 +941,12 @@ hipError_t launch_distill(const DistillArgs& a, int dtype, const SplitArgs& P, h
     constexpr Temperatures kTemps = decltype(temps)::value;
     by_type(dtype, [&](auto type) {
       using T = decltype(type);
-      by_length<T>(P.length, 0u, [&](auto shape) {
+      by_length<T>(P.length, 0u, a.rows * P.segments, [&](auto shape) {
         using S = decltype(shape);
         const dim3 threads(S::kThreads);
         if (P.segments == 1u) {
           distill_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(a.rows), threads, 0, s>>>(a);
-        } else if constexpr (S::kThreads == 1024u) {       // (a row of several segments has long ones)
+        } else if constexpr (S::kThreads == 1024u || (S::kThreads == 256u && S::kVectors <= 8u)) {       // (as split_of cuts)
           distill_sums_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(a.rows * P.segments), threads, 0, s>>>(a, P);
           distill_gradient_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(a.rows * P.segments), threads, 0, s>>>(a, P);
         }
