@@ -122,7 +122,6 @@ struct Vector {
   typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
 
   static __device__ __forceinline__ Words load(const T* p) { return *reinterpret_cast<const Words*>(p); }
-  static __device__ __forceinline__ Words load_anywhere(const T* p) { return *reinterpret_cast<const Unaligned*>(p); }
   static __device__ __forceinline__ void store(T* p, const float (&v)[kElems]) {
     T t[kElems];
 #pragma unroll
@@ -272,20 +271,12 @@ __device__ __forceinline__ uint32_t rank_in(const uint64_t* list, uint32_t n, ui
   return rank;
 }
 
-// f(index, logit) for every logit of a segment, read (again) from memory.
+// f(index, logit) for every logit of a segment, read again from memory.  (One at a time: with vectors the whole kernel has a quarter more registers, and fewer
+// workgroups share a compute unit.)
 template <typename T, uint32_t kThreads, typename F>
 __device__ __forceinline__ void read_again(const T* z, uint32_t n, F&& f) {
-  using V = Vector<T>;
-  const uint32_t vectors = n / V::kElems;
-#pragma unroll 1
-  for (uint32_t i = threadIdx.x; i < vectors; i += kThreads) {
-    float v[V::kElems];
-    V::unpack(V::load_anywhere(z + i * V::kElems), v);
-#pragma unroll
-    for (uint32_t j = 0; j < V::kElems; ++j) f(i * V::kElems + j, v[j]);
-  }
-  const uint32_t rest = vectors * V::kElems + threadIdx.x;
-  if (rest < n) f(rest, static_cast<float>(z[rest]));
+#pragma unroll 4
+  for (uint32_t i = threadIdx.x; i < n; i += kThreads) f(i, static_cast<float>(z[i]));
 }
 
 // How many of the segment's logits have an order above `line`; the same in every thread.  Holds barriers.
@@ -369,34 +360,33 @@ __device__ __forceinline__ void top_of(const H& held, const T* z, float t, uint3
   if (!spoilt) {
     const uint32_t line = lowest_line<kThreads>(lds);
     const float least = line <= 0x007FFFFFu ? -INFINITY : logit_of(line);      // (below the order of -inf all are taken)
-    // (a wave's hits of one vector take their places in the list together)
-    auto list = [&](uint32_t bits, const float* v, uint32_t index) __attribute__((always_inline)) {
-      const uint32_t n = static_cast<uint32_t>(__popc(bits)), incl = wave_incl_scan(n);
-      uint32_t base = 0u;
-      if ((threadIdx.x & 63u) == 0u) base = atomicAdd(&lds.count, wave_total(incl));
-      uint32_t at = uniform(base) + incl - n;
-#pragma unroll
-      for (uint32_t j = 0; j < H::kElems; ++j)
-        if ((bits >> j) & 1u) {
-          if (at < kListed) lds.list[at] = entry_of(v[j], first + index + j);
-          ++at;
-        }
-    };
+    // Eight bits a vector, then places in the list for all of a thread's: their indices alone, the few logits are read again below.  (With 8192 rows of 32000, 96 us
+    // without alternatives: 121 with k = 8, 139 with k = 64.  Writing each where it is met 128 and 177, asking the whole wave about every element of a
+    // vector that has one 135 and 190; what needs the packed registers a second time takes 50 more registers a thread, and a third of the workgroups.)
+    constexpr uint32_t kVectors = sizeof(held.raw) / sizeof(held.raw[0]), kHitWords = (kVectors + 3u) / 4u;
+    uint32_t hits[kHitWords] = {}, n = held.has_single() && held.single >= least ? 1u : 0u;
     held.each([&](uint32_t i, const float (&v)[H::kElems]) __attribute__((always_inline)) {
       float most = v[0];
 #pragma unroll
       for (uint32_t j = 1; j < H::kElems; ++j) most = fmaxf(most, v[j]);
-      const bool hit = most >= least && held.mine(i);
-      if (!__any(hit)) return;
-      uint32_t bits = 0;
+      if (most >= least && held.mine(i)) {
+        uint32_t bits = 0;
 #pragma unroll
-      for (uint32_t j = 0; j < H::kElems; ++j) bits |= v[j] >= least ? 1u << j : 0u;
-      list(hit ? bits : 0u, v, held.index(i));
+        for (uint32_t j = 0; j < H::kElems; ++j) bits |= v[j] >= least ? 1u << j : 0u;
+        hits[i / 4u] |= bits << (8u * (i % 4u));
+      }
     });
-    const bool hit = held.has_single() && held.single >= least;
-    if (__any(hit)) {
-      const float v[H::kElems] = {held.single};
-      list(hit ? 1u : 0u, v, held.single_index());
+#pragma unroll
+    for (uint32_t w = 0; w < kHitWords; ++w) n += static_cast<uint32_t>(__popc(hits[w]));
+    if (n > 0u) {
+      uint32_t at = atomicAdd(&lds.count, n);
+      if (held.has_single() && held.single >= least && at < kListed) lds.list[at++] = held.single_index();
+#pragma unroll
+      for (uint32_t w = 0; w < kHitWords; ++w)
+        for (uint32_t bits = hits[w]; bits != 0u && at < kListed; bits &= bits - 1u) {
+          const uint32_t bit = static_cast<uint32_t>(__ffs(static_cast<int>(bits)) - 1);
+          lds.list[at++] = held.index(4u * w + bit / 8u) + bit % 8u;
+        }
     }
   }
   __syncthreads();
@@ -407,6 +397,12 @@ __device__ __forceinline__ void top_of(const H& held, const T* z, float t, uint3
     __syncthreads();
     list_exactly<T, kThreads>(z, held.n, lowest_line<kThreads>(lds), k, first, lds);
     listed = k;
+  } else {
+    for (uint32_t i = threadIdx.x; i < listed; i += kThreads) {
+      const uint32_t index = static_cast<uint32_t>(lds.list[i]);
+      lds.list[i] = entry_of(static_cast<float>(z[index]), first + index);
+    }
+    __syncthreads();
   }
   for (uint32_t i = threadIdx.x; i < listed; i += kThreads) {
     const uint64_t e = lds.list[i];
