@@ -26,6 +26,7 @@ namespace rgc {
 namespace {
 
 constexpr uint32_t kChunk = 256;       // steps between kept states (RGC_RECURRENCE_CHUNK)
+constexpr uint32_t kOneTile = 128;     // steps of the sequences that are one tile (kMiddle below)
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr unsigned long long kUnset = ~0ull;      // a word that is not published yet (its upper half would be a NaN as P, which is never published)
 
@@ -378,7 +379,7 @@ template <typename T, int kWaves, int kSteps, bool kGated, bool kWhole>
 __device__ __forceinline__ void backward_tile(const RecurrenceArgs& A, const RecurrenceGradArgs& D, const TileArgs& G, const Place& at, uint32_t n,
                                               SharedBackward<kWaves>& lds) {
   constexpr uint32_t kTile = kWaves * kSteps;
-  static_assert(kTile == kChunk || kTile <= 64u, "a tile begins with a kept state, the first one of a short sequence with the first");
+  static_assert(kTile == kChunk || kTile <= kOneTile, "a tile begins with a kept state, the only one of a short sequence with the first");
   auto& parts = lds.parts;
   auto& back = lds.back;
   const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, b = at.b;
@@ -522,8 +523,9 @@ struct Shape {
   uint32_t waves, steps;           // waves a workgroup, steps a wave
   constexpr uint32_t tile() const { return waves * steps; }
 };
-constexpr Shape kOneWave{1, 4}, kShort{4, 16}, kLong{8, 16}, kLongBackward{16, 16};
-enum class Kind { kOneWave, kShort, kLong };
+constexpr Shape kOneWave{1, 4}, kShort{8, 8}, kMiddle{16, 8}, kLong{8, 16}, kLongBackward{16, 16};
+static_assert(kMiddle.tile() == kOneTile && kLongBackward.tile() == kChunk, "as backward_tile takes its states");
+enum class Kind { kOneWave, kShort, kMiddle, kLong };
 
 struct Cut {
   Kind kind;
@@ -531,13 +533,13 @@ struct Cut {
 };
 
 constexpr Shape shape_of(Kind kind, bool backward) {
-  return kind == Kind::kOneWave ? kOneWave : kind == Kind::kShort ? kShort : backward ? kLongBackward : kLong;
+  return kind == Kind::kOneWave ? kOneWave : kind == Kind::kShort ? kShort : kind == Kind::kMiddle ? kMiddle : backward ? kLongBackward : kLong;
 }
 
 Cut cut_of(const RecurrenceArgs& a, int dtype, bool backward) {
   Cut c;
   c.vec = !backward && dtype != 0 && a.width > 64u ? 2u : 1u;
-  c.kind = a.steps <= kOneWave.tile() ? Kind::kOneWave : a.steps <= kShort.tile() ? Kind::kShort : Kind::kLong;
+  c.kind = a.steps <= kOneWave.tile() ? Kind::kOneWave : a.steps <= kShort.tile() ? Kind::kShort : a.steps <= kMiddle.tile() ? Kind::kMiddle : Kind::kLong;
   return c;
 }
 
@@ -576,6 +578,7 @@ template <typename T, int kVec, bool kGated>
 void launch_forward(const RecurrenceArgs& a, const Cut& c, const TileArgs& G, uint32_t wgs, hipStream_t s) {
   if (c.kind == Kind::kOneWave) launch_forward<T, kVec, kGated, kOneWave.waves, kOneWave.steps>(a, G, wgs, s);
   else if (c.kind == Kind::kShort) launch_forward<T, kVec, kGated, kShort.waves, kShort.steps>(a, G, wgs, s);
+  else if (c.kind == Kind::kMiddle) launch_forward<T, kVec, kGated, kMiddle.waves, kMiddle.steps>(a, G, wgs, s);
   else launch_forward<T, kVec, kGated, kLong.waves, kLong.steps>(a, G, wgs, s);
 }
 
@@ -587,6 +590,7 @@ template <typename T, bool kGated>
 void launch_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& d, const Cut& c, const TileArgs& G, uint32_t wgs, hipStream_t s) {
   if (c.kind == Kind::kOneWave) launch_backward<T, kGated, kOneWave.waves, kOneWave.steps>(a, d, G, wgs, s);
   else if (c.kind == Kind::kShort) launch_backward<T, kGated, kShort.waves, kShort.steps>(a, d, G, wgs, s);
+  else if (c.kind == Kind::kMiddle) launch_backward<T, kGated, kMiddle.waves, kMiddle.steps>(a, d, G, wgs, s);
   else launch_backward<T, kGated, kLongBackward.waves, kLongBackward.steps>(a, d, G, wgs, s);
 }
 
