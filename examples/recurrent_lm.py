@@ -158,7 +158,7 @@ def continue_text(student, tokens=12, top=3):
     said = rgc.TokenScores(run.logits, target, logprob=logprob)
     token, out = 0, []
     for _ in range(tokens):
-        torch.matmul(p["embedding"][token], p["inner"], out=run.inner.view(-1))
+        torch.matmul(p["embedding"][token:token + 1], p["inner"], out=run.inner.view(1, -1))
         rgc.rgc_gated_recurrence(ctx, run.one, stream)
         torch.matmul(run.y.view(-1, width), p["output"], out=run.logits)
         rgc.rgc_token_logprobs(ctx, scores, stream)

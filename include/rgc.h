@@ -280,7 +280,7 @@ int rgc_last_error(rgc_ctx* ctx, void* hip_stream);
  *    NaN ranks above +Inf).
  *  - A logit of -inf has log probability -inf; so has every logit of a row of nothing else, whose entropy is 0.  A NaN or
  *    +inf makes the row's log probabilities and entropy NaN.
- * Limits: 0 <= rows, rows * ceil(vocab / 4096) < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 0 <= top <= min(RGC_TOP_MAX, vocab), T > 0. */
+ * Limits: 0 <= rows < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 0 <= top <= min(RGC_TOP_MAX, vocab), T > 0. */
 typedef struct {
   const void*    logits;      /* [rows][vocab], row r at logits + r * row_stride elements           */
   int64_t        row_stride;  /* >= vocab                                                           */
@@ -347,7 +347,8 @@ int rgc_distill_loss(rgc_ctx* ctx, const rgc_distill* distill, void* hip_stream)
  *  - Steps at lengths[b] and beyond (lengths are read as at least 0 and at most `steps`) are not looked at; y is 0 there.
  *    h_last is the state after the last step of the row, h0 if it has none.
  * One step (steps == 1) is the serving form: h_last may be h0 itself.
- * Limits: batch, steps >= 0, both < 2^31; 1 <= width < 2^31. */
+ * Limits: batch, steps >= 0, both < 2^31; 1 <= width <= 2^29; batch * ceil(width / 64) < 2^26 for one step, and with more steps as many
+ * sequences as a grid of one workgroup for every 128 steps of 64 or 128 channels has (more than the device's memory holds). */
 typedef struct {
   void*   data;         /* element (b, t, c) at data + b * batch_stride + t * step_stride + c       */
   int64_t batch_stride; /* elements, not negative                                                   */

@@ -141,6 +141,7 @@ bool counts_on_long_lists(const rgc_layer* layers, int32_t L, uint64_t total, ui
   return total <= kTiledDenseElems && !tileable(layers, L, kTileSlots) && tileable(layers, L, slots);
 }
 constexpr int kPlanCache = 8;
+constexpr int kLmBuffers = 48;             // each at least twice the one before
 constexpr uint32_t kElectGroupHost = 32;   // = kElectGroup of the kernels (workgroups per election group)
 constexpr int kLaunches = 6;               // streaming pass + at most five phase launches
 
@@ -259,7 +260,10 @@ struct rgc_ctx {
   DevBuf<float> d_slots_u;                 // the velocity of every listed element (first use)
   DevBuf<unsigned long long> d_members2;   // member pool of the dense layers (first use)
   DevBuf<uint32_t> d_shards;               // their sub-list counters (first use)
-  DevBuf<unsigned long long> d_lm;         // scratch of the language model's operators (first use, grows)
+  // Scratch of the language model's operators (first use).  A call that needs more gets a buffer at least twice as large; the smaller ones stay until
+  // the context goes, for a graph that was recorded with one writes to it whenever it is replayed.
+  DevBuf<unsigned long long> d_lm[kLmBuffers];
+  int lm_buffers = 0;
   CompressPlan plans[kPlanCache];
   uint64_t tick = 0;
   int64_t optional_scratch_cap = -1;       // bytes the dense layers' lists may take (diagnostics); negative: no cap
@@ -598,7 +602,7 @@ int rgc_destroy(rgc_ctx* ctx) {
   ctx->d_norm_part.release();
   ctx->d_mean_part.release();
   ctx->d_moments.release();
-  ctx->d_lm.release();
+  for (auto& b : ctx->d_lm) b.release();
   ctx->missing.release();                  // (the frees above have waited for the kernels that may write to it)
   for (auto* v : {&ctx->ev_compress, &ctx->ev_decompress, &ctx->ev_pool})
     for (hipEvent_t e : *v) (void)hipEventDestroy(e);
@@ -1335,7 +1339,7 @@ bool sequence_fits(const rgc_sequence& v, const rgc_recurrence* r, bool written)
 
 // (steps == 0: only h0 and h_last are there; batch == 0: nothing is)
 bool recurrence_fits(const rgc_recurrence* r) {
-  if (r->batch < 0 || r->batch > kInt32Most || r->steps < 0 || r->steps > kInt32Most || r->width < 1) return false;
+  if (r->batch < 0 || r->batch > kInt32Most || r->steps < 0 || r->steps > kInt32Most || r->width < 1 || r->width > (int32_t(1) << 29)) return false;
   if (r->dtype < RGC_F32 || r->dtype > RGC_F16) return false;
   if (r->batch > 0 && (static_cast<int64_t>(r->width) + 63) / 64 > kInt32Most / r->batch) return false;
   if (!words_aligned({r->lengths, r->h0, r->h_last, r->states})) return false;
@@ -1344,15 +1348,23 @@ bool recurrence_fits(const rgc_recurrence* r) {
          (!r->out_gate.data || sequence_fits(r->out_gate, r, false));
 }
 
-// Room for `words` in the operators' scratch.  (Replacing it waits for what still uses the old one: hipFree does.)
-int lm_scratch(rgc_ctx* ctx, uint64_t words) {
-  if (words <= ctx->d_lm.n) return RGC_OK;
-  const hipError_t e = ctx->d_lm.alloc(words);
-  if (e == hipErrorOutOfMemory) {
-    (void)hipGetLastError();
-    return RGC_ENOMEM;
+// Room for `words` in the operators' scratch: *out.
+int lm_scratch(rgc_ctx* ctx, uint64_t words, unsigned long long** out) {
+  *out = nullptr;
+  if (words == 0) return RGC_OK;
+  uint64_t have = ctx->lm_buffers > 0 ? ctx->d_lm[ctx->lm_buffers - 1].n : 0;
+  if (words > have) {
+    if (ctx->lm_buffers >= kLmBuffers) return RGC_ENOMEM;
+    hipError_t e = ctx->d_lm[ctx->lm_buffers].alloc(std::max<uint64_t>(words, 2 * have));
+    if (e == hipErrorOutOfMemory) {
+      (void)hipGetLastError();
+      return RGC_ENOMEM;
+    }
+    if (e != hipSuccess) return fail_hip(e, "scratch of the language model's operators");
+    ++ctx->lm_buffers;
   }
-  return e == hipSuccess ? RGC_OK : fail_hip(e, "scratch of the language model's operators");
+  *out = ctx->d_lm[ctx->lm_buffers - 1].p;
+  return RGC_OK;
 }
 
 SequenceView view_of(const rgc_sequence& v) { return SequenceView{v.data, v.batch_stride, v.step_stride}; }
@@ -1398,13 +1410,13 @@ int rgc_token_logprobs(rgc_ctx* ctx, const rgc_token_scores* a, void* hip_stream
   A.top_idx = a->top_idx;
   A.top_logprob = a->top_logprob;
   SplitArgs P = split_of(A.rows, A.vocab, a->dtype);
-  if (static_cast<uint64_t>(A.rows) * P.segments > kInt32Most) return RGC_EINVAL;
   if (P.segments > 1u) {
     const uint64_t parts = static_cast<uint64_t>(A.rows) * P.segments;
-    const int rc = lm_scratch(ctx, parts * (2u + A.top));
+    unsigned long long* scratch = nullptr;
+    const int rc = lm_scratch(ctx, parts * (2u + A.top), &scratch);
     if (rc != RGC_OK) return rc;
-    P.sums = reinterpret_cast<float*>(ctx->d_lm.p);
-    P.entries = reinterpret_cast<uint64_t*>(ctx->d_lm.p + 2u * parts);
+    P.sums = reinterpret_cast<float*>(scratch);
+    P.entries = reinterpret_cast<uint64_t*>(scratch + 2u * parts);
   }
   RGC_HIP(launch_token_logprobs(A, a->dtype, P, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
@@ -1415,7 +1427,6 @@ int rgc_token_logprobs_backward(rgc_ctx* ctx, const rgc_token_scores* a, const f
                                 void* hip_stream) {
   if (!ctx || !a || !scores_fit(a) || !rows_fit(grad_logits, a->rows, a->vocab, grad_row_stride, a->dtype)) return RGC_EINVAL;
   if (!words_aligned({grad_logprob, grad_entropy})) return RGC_EINVAL;
-  if (a->rows * ((a->vocab + 4095) / 4096) > kInt32Most) return RGC_EINVAL;
   if (a->rows == 0) return RGC_OK;
   if (!a->stats || (grad_logprob && !a->targets) || (grad_entropy && !a->entropy)) return RGC_EINVAL;
   DeviceGuard guard(ctx->device);
@@ -1471,13 +1482,13 @@ int rgc_distill_loss(rgc_ctx* ctx, const rgc_distill* a, void* hip_stream) {
   A.grad_logits = a->grad_logits;
   A.grad_row_stride = a->grad_row_stride;
   SplitArgs P = split_of(A.rows, A.vocab, a->dtype);
-  if (static_cast<uint64_t>(A.rows) * P.segments > kInt32Most) return RGC_EINVAL;
   if (P.segments > 1u) {
     const uint64_t parts = static_cast<uint64_t>(A.rows) * P.segments;
-    const int rc = lm_scratch(ctx, parts * 2u + (static_cast<uint64_t>(A.rows) * (RGC_TOP_MAX + 1) + 1u) / 2u);
+    unsigned long long* scratch = nullptr;
+    const int rc = lm_scratch(ctx, parts * 2u + (static_cast<uint64_t>(A.rows) * (RGC_TOP_MAX + 1) + 1u) / 2u, &scratch);
     if (rc != RGC_OK) return rc;
-    P.sums = reinterpret_cast<float*>(ctx->d_lm.p);
-    P.logits = reinterpret_cast<float*>(ctx->d_lm.p + 2u * parts);
+    P.sums = reinterpret_cast<float*>(scratch);
+    P.logits = reinterpret_cast<float*>(scratch + 2u * parts);
   }
   RGC_HIP(launch_distill(A, a->dtype, P, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
@@ -1490,9 +1501,11 @@ int rgc_gated_recurrence(rgc_ctx* ctx, const rgc_recurrence* r, void* hip_stream
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
   const RecurrenceArgs A = recurrence_args(r);
-  const int rc = lm_scratch(ctx, recurrence_scratch_words(A, r->dtype, false));
+  if (!recurrence_fits_grid(A, r->dtype, false)) return RGC_EINVAL;
+  unsigned long long* scratch = nullptr;
+  const int rc = lm_scratch(ctx, recurrence_scratch_words(A, r->dtype, false), &scratch);
   if (rc != RGC_OK) return rc;
-  RGC_HIP(launch_recurrence(A, r->dtype, ctx->d_lm.p, static_cast<hipStream_t>(hip_stream)));
+  RGC_HIP(launch_recurrence(A, r->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 
@@ -1513,9 +1526,11 @@ int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* r, const r
   G.dh_last = g->dh_last;
   G.dh0 = g->dh0;
   const RecurrenceArgs A = recurrence_args(r);
-  const int rc = lm_scratch(ctx, recurrence_scratch_words(A, r->dtype, true));
+  if (!recurrence_fits_grid(A, r->dtype, true)) return RGC_EINVAL;
+  unsigned long long* scratch = nullptr;
+  const int rc = lm_scratch(ctx, recurrence_scratch_words(A, r->dtype, true), &scratch);
   if (rc != RGC_OK) return rc;
-  RGC_HIP(launch_recurrence_backward(A, G, r->dtype, ctx->d_lm.p, static_cast<hipStream_t>(hip_stream)));
+  RGC_HIP(launch_recurrence_backward(A, G, r->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 

@@ -97,6 +97,7 @@ struct TileArgs {
 hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, const SplitArgs& p, hipStream_t s);
 hipError_t launch_token_logprobs_backward(const ScoreGradArgs& a, int dtype, hipStream_t s);
 hipError_t launch_distill(const DistillArgs& a, int dtype, const SplitArgs& p, hipStream_t s);
+bool recurrence_fits_grid(const RecurrenceArgs& a, int dtype, bool backward);
 uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backward);      // 64-bit words of `scratch`
 hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, hipStream_t s);
 hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s);

@@ -555,11 +555,7 @@ uint64_t words_for(const RecurrenceArgs& a, const Cut& c, const TileArgs& G) {
   return G.tiles > 1u ? static_cast<uint64_t>(a.batch) * G.across * G.tiles * 64u * c.vec : 0u;
 }
 
-// Workgroups, or 0 if there are more than a grid has.
-uint32_t workgroups(const RecurrenceArgs& a, const TileArgs& G) {
-  const uint64_t n = static_cast<uint64_t>(a.batch) * G.across * G.tiles;
-  return n <= 0x7FFFFFFFull ? static_cast<uint32_t>(n) : 0u;
-}
+uint64_t workgroups(const RecurrenceArgs& a, const TileArgs& G) { return static_cast<uint64_t>(a.batch) * G.across * G.tiles; }
 
 hipError_t clear_words(TileArgs& G, uint64_t words, unsigned long long* scratch, hipStream_t s) {
   if (words == 0u) return hipSuccess;
@@ -602,6 +598,12 @@ void by_gate(const RecurrenceArgs& a, F&& f) {
 
 }  // namespace
 
+// A grid has fewer than 2^32 threads (and tickets are 32 bits).
+bool recurrence_fits_grid(const RecurrenceArgs& a, int dtype, bool backward) {
+  const Cut c = cut_of(a, dtype, backward);
+  return workgroups(a, tiles_of(a, c, backward)) <= 0xFFFFFFFFull / (64u * shape_of(c.kind, backward).waves);
+}
+
 uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backward) {
   const Cut c = cut_of(a, dtype, backward);
   const uint64_t words = words_for(a, c, tiles_of(a, c, backward));
@@ -611,8 +613,7 @@ uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backw
 hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, hipStream_t s) {
   const Cut c = cut_of(a, dtype, false);
   TileArgs G = tiles_of(a, c, false);
-  const uint32_t wgs = workgroups(a, G);
-  if (wgs == 0u) return hipErrorInvalidValue;
+  const uint32_t wgs = static_cast<uint32_t>(workgroups(a, G));
   const hipError_t e = clear_words(G, words_for(a, c, G), scratch, s);
   if (e != hipSuccess) return e;
   auto launch = [&](auto type, auto gated) {
@@ -632,8 +633,7 @@ hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long l
 hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s) {
   const Cut c = cut_of(a, dtype, true);
   TileArgs G = tiles_of(a, c, true);
-  const uint32_t wgs = workgroups(a, G);
-  if (wgs == 0u) return hipErrorInvalidValue;
+  const uint32_t wgs = static_cast<uint32_t>(workgroups(a, G));
   const hipError_t e = clear_words(G, words_for(a, c, G), scratch, s);
   if (e != hipSuccess) return e;
   auto launch = [&](auto type, auto gated) { launch_backward<decltype(type), bool(decltype(gated){})>(a, g, c, G, wgs, s); };

@@ -877,7 +877,7 @@ constexpr uint32_t kFewRows = 128, kFewSegments = 2, kWanted = 512, kFewWorkgrou
 // f(shape): of the workgroups that hold `length` logits, the one of fewest threads.  (More alternatives than threads make a poor line: see top_of.)
 // With fewer workgroups than compute units, of sixteen waves: one workgroup's time is all there is.
 template <typename T, typename F>
-void by_length(uint32_t length, uint32_t top, uint32_t workgroups, F&& f) {
+void by_length(uint32_t length, uint32_t top, uint64_t workgroups, F&& f) {
   if (length <= Shape<T, 64, 4>::kCapacity && top <= 64u) f(Shape<T, 64, 4>{});
   else if (length <= Shape<T, 256, 4>::kCapacity) f(Shape<T, 256, 4>{});
   else if (length <= Shape<T, 1024, 4>::kCapacity && workgroups <= kFewWorkgroups) f(Shape<T, 1024, 4>{});
@@ -911,45 +911,96 @@ SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype) {
   return P;
 }
 
-hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, const SplitArgs& P, hipStream_t s) {
+namespace {
+
+// f(first, rows): stretches of rows whose grids have fewer than 2^32 threads each.
+template <typename F>
+void by_rows(uint32_t rows, uint64_t threads_a_row, F&& f) {
+  const uint64_t most = 0xFFFFFFFFull / threads_a_row;
+  for (uint64_t first = 0; first < rows; first += most) f(first, static_cast<uint32_t>(rows - first < most ? rows - first : most));
+}
+template <typename P>
+P* shifted(P* p, uint64_t by) { return p ? p + by : p; }
+// A tensor of rows, by its type's size.
+const void* shifted(const void* p, uint64_t rows, int64_t stride, int dtype) {
+  return p ? static_cast<const char*>(p) + static_cast<int64_t>(rows) * stride * (dtype == 0 ? 4 : 2) : p;
+}
+void* shifted(void* p, uint64_t rows, int64_t stride, int dtype) { return const_cast<void*>(shifted(static_cast<const void*>(p), rows, stride, dtype)); }
+
+}  // namespace
+
+hipError_t launch_token_logprobs(const ScoreArgs& all, int dtype, const SplitArgs& P, hipStream_t s) {
   by_type(dtype, [&](auto type) {
     using T = decltype(type);
-    by_length<T>(P.length, a.top, a.rows * P.segments, [&](auto shape) {
+    by_length<T>(P.length, all.top, uint64_t(all.rows) * P.segments, [&](auto shape) {
       using S = decltype(shape);
-      score_kernel<T, S::kThreads, S::kVectors><<<dim3(a.rows * P.segments), dim3(S::kThreads), 0, s>>>(a, P);
+      by_rows(all.rows, static_cast<uint64_t>(S::kThreads) * P.segments, [&](uint64_t first, uint32_t rows) {
+        ScoreArgs a = all;
+        a.rows = rows;
+        a.logits = shifted(a.logits, first, a.row_stride, dtype);
+        a.targets = shifted(a.targets, first);
+        a.logprob = shifted(a.logprob, first);
+        a.entropy = shifted(a.entropy, first);
+        a.stats = shifted(a.stats, 2u * first);
+        a.top_idx = shifted(a.top_idx, first * a.top);
+        a.top_logprob = shifted(a.top_logprob, first * a.top);
+        score_kernel<T, S::kThreads, S::kVectors><<<dim3(rows * P.segments), dim3(S::kThreads), 0, s>>>(a, P);
+        if (P.segments > 1u) score_join_kernel<T><<<dim3(rows), dim3(kJoinThreads), P.segments * a.top * sizeof(uint64_t), s>>>(a, P);
+      });
     });
-    if (P.segments > 1u) score_join_kernel<T><<<dim3(a.rows), dim3(kJoinThreads), P.segments * a.top * sizeof(uint64_t), s>>>(a, P);
   });
   return hipGetLastError();
 }
 
-hipError_t launch_token_logprobs_backward(const ScoreGradArgs& a, int dtype, hipStream_t s) {
+hipError_t launch_token_logprobs_backward(const ScoreGradArgs& all, int dtype, hipStream_t s) {
   by_type(dtype, [&](auto type) {
     using T = decltype(type);
-    const uint32_t part = kGradThreads * kGradVectors * Vector<T>::kElems, parts = (a.vocab + part - 1u) / part;
-    score_grad_kernel<T><<<dim3(a.rows * parts), dim3(kGradThreads), 0, s>>>(a, parts);
+    const uint32_t part = kGradThreads * kGradVectors * Vector<T>::kElems, parts = (all.vocab + part - 1u) / part;
+    by_rows(all.rows, static_cast<uint64_t>(kGradThreads) * parts, [&](uint64_t first, uint32_t rows) {
+      ScoreGradArgs a = all;
+      a.rows = rows;
+      a.logits = shifted(a.logits, first, a.row_stride, dtype);
+      a.grad_logits = shifted(a.grad_logits, first, a.grad_row_stride, dtype);
+      a.targets = shifted(a.targets, first);
+      a.stats = shifted(a.stats, 2u * first);
+      a.entropy = shifted(a.entropy, first);
+      a.grad_logprob = shifted(a.grad_logprob, first);
+      a.grad_entropy = shifted(a.grad_entropy, first);
+      score_grad_kernel<T><<<dim3(rows * parts), dim3(kGradThreads), 0, s>>>(a, parts);
+    });
   });
   return hipGetLastError();
 }
 
-hipError_t launch_distill(const DistillArgs& a, int dtype, const SplitArgs& P, hipStream_t s) {
+hipError_t launch_distill(const DistillArgs& all, int dtype, const SplitArgs& P, hipStream_t s) {
   auto launch = [&](auto temps) {
     constexpr Temperatures kTemps = decltype(temps)::value;
     by_type(dtype, [&](auto type) {
       using T = decltype(type);
-      by_length<T>(P.length, 0u, a.rows * P.segments, [&](auto shape) {
+      by_length<T>(P.length, 0u, uint64_t(all.rows) * P.segments, [&](auto shape) {
         using S = decltype(shape);
         const dim3 threads(S::kThreads);
-        if (P.segments == 1u) {
-          distill_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(a.rows), threads, 0, s>>>(a);
-        } else if constexpr (S::kThreads == 1024u || (S::kThreads == 256u && S::kVectors <= 8u)) {       // (as split_of cuts)
-          distill_sums_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(a.rows * P.segments), threads, 0, s>>>(a, P);
-          distill_gradient_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(a.rows * P.segments), threads, 0, s>>>(a, P);
-        }
+        by_rows(all.rows, static_cast<uint64_t>(S::kThreads) * P.segments, [&](uint64_t first, uint32_t rows) {
+          DistillArgs a = all;
+          a.rows = rows;
+          a.logits = shifted(a.logits, first, a.row_stride, dtype);
+          a.grad_logits = shifted(a.grad_logits, first, a.grad_row_stride, dtype);
+          a.teacher_idx = shifted(a.teacher_idx, first * a.k);
+          a.teacher_logits = shifted(a.teacher_logits, first * a.k);
+          a.targets = shifted(a.targets, first);
+          a.grad_loss = shifted(a.grad_loss, first);
+          a.loss = shifted(a.loss, first);
+          if (P.segments == 1u) {
+            distill_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(rows), threads, 0, s>>>(a);
+          } else if constexpr (S::kThreads == 1024u || (S::kThreads == 256u && S::kVectors <= 8u)) {       // (as split_of cuts)
+            distill_sums_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(rows * P.segments), threads, 0, s>>>(a, P);
+            distill_gradient_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(rows * P.segments), threads, 0, s>>>(a, P);
+          }
+        });
       });
     });
   };
-  switch (a.temperatures) {
+  switch (all.temperatures) {
     case Temperatures::kOne: launch(std::integral_constant<Temperatures, Temperatures::kOne>{}); break;
     case Temperatures::kSquared: launch(std::integral_constant<Temperatures, Temperatures::kSquared>{}); break;
     default: launch(std::integral_constant<Temperatures, Temperatures::kTwo>{}); break;

@@ -326,6 +326,31 @@ def test_rows_whose_offsets_pass_32_bits(rgc, ctx):
     check_scores(used, got, targets.cpu().numpy(), "bf16", 4, 1.0, (np.ones(3), None))
 
 
+def test_more_rows_than_a_grid_holds(rgc, ctx):
+    """Rows of two words, one more than 2^32 / 64 (a workgroup each): log p_0 = -ln(1 + e^(z_1 - z_0)), and the gradients made of it."""
+    import torch
+    rows = 2 ** 26 + 1_001
+    z = torch.randn(rows, 2, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").to(torch.bfloat16)
+    targets = (torch.arange(rows, device="cuda") % 3 - 1).to(torch.int32)      # left out, the first word, the second
+    out = {k: torch.full((rows,), 5.0, device="cuda") for k in ("logprob", "entropy")}
+    stats, grad = torch.empty(rows, 2, device="cuda"), torch.full_like(z, 5.0)
+    call = rgc.TokenScores(z, targets, stats=stats, **out)
+    rgc.rgc_token_logprobs(ctx, call)
+    weight = torch.ones(rows, device="cuda")
+    rgc.rgc_token_logprobs_backward(ctx, call, grad, weight)
+    index, teacher, loss, dgrad = targets[:, None].contiguous(), torch.zeros(rows, 1, device="cuda"), torch.full((rows,), 5.0, device="cuda"), torch.full_like(z, 5.0)
+    rgc.rgc_distill_loss(ctx, rgc.Distillation(z, index, teacher, loss=loss, grad_loss=weight, grad_logits=dgrad))
+    torch.cuda.synchronize()
+    logp = torch.log_softmax(z.float(), dim=1)
+    there = targets >= 0
+    want = torch.where(there, logp.gather(1, targets.clamp(min=0).long()[:, None])[:, 0], torch.zeros_like(weight))
+    assert float((out["logprob"] - want).abs().max()) < 2e-6
+    assert float((loss + want).abs().max()) < 2e-6                      # one entry of weight 1: the divergence is -log p
+    slope = torch.nn.functional.one_hot(targets.clamp(min=0).long(), 2) - logp.exp()
+    slope = torch.where(there[:, None], slope, torch.zeros_like(slope))
+    assert float((grad.float() - slope).abs().max()) < 2.0 ** -8 and float((dgrad.float() + slope).abs().max()) < 2.0 ** -8
+
+
 # ------------------------------------------------------------------------------------------------ distillation
 
 def distill64(z, index, teacher, targets, T, ws, wl, g):
