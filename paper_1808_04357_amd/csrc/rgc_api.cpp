@@ -1409,7 +1409,7 @@ int rgc_token_logprobs(rgc_ctx* ctx, const rgc_token_scores* a, void* hip_stream
   A.stats = a->stats;
   A.top_idx = a->top_idx;
   A.top_logprob = a->top_logprob;
-  SplitArgs P = split_of(A.rows, A.vocab, a->dtype);
+  SplitArgs P = split_of(A.rows, A.vocab, a->dtype, Use::kScores, A.top);
   if (P.segments > 1u) {
     const uint64_t parts = static_cast<uint64_t>(A.rows) * P.segments;
     unsigned long long* scratch = nullptr;
@@ -1481,7 +1481,7 @@ int rgc_distill_loss(rgc_ctx* ctx, const rgc_distill* a, void* hip_stream) {
   A.loss = a->loss;
   A.grad_logits = a->grad_logits;
   A.grad_row_stride = a->grad_row_stride;
-  SplitArgs P = split_of(A.rows, A.vocab, a->dtype);
+  SplitArgs P = split_of(A.rows, A.vocab, a->dtype, Use::kDistillation, 0u);
   if (P.segments > 1u) {
     const uint64_t parts = static_cast<uint64_t>(A.rows) * P.segments;
     unsigned long long* scratch = nullptr;

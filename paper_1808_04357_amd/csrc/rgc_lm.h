@@ -64,7 +64,8 @@ struct SplitArgs {
   uint64_t* entries;         // [rows][segments][top]: scores
   float* logits;             // [rows][RGC_TOP_MAX + 1]: distillation
 };
-SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype);
+enum class Use { kScores, kDistillation };
+SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype, Use use, uint32_t top);
 
 struct SequenceView {
   void* data;

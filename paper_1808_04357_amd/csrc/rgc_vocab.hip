@@ -622,7 +622,7 @@ struct Teacher {
   int32_t at[kTopMost + 1];             // an index, once; the label's last unless it is one of the others; -1: none
   float off[kTopMost + 1], z[kTopMost + 1];      // what is subtracted there, and the student's logit
   float soft;                           // sum of the weights q: 0 if there are none
-  uint32_t seen[kSeenBits / 32u];
+  alignas(16) uint32_t seen[kSeenBits / 32u];
 };
 
 // Two entries a lane.
@@ -872,7 +872,7 @@ struct Shape {
   static constexpr uint32_t kThreads = kThreads_, kVectors = kVectors_, kCapacity = Held<T, kThreads_, kVectors_>::kCapacity;
 };
 
-constexpr uint32_t kFewRows = 128, kFewSegments = 2, kWanted = 512, kFewWorkgroups = 256;
+constexpr uint32_t kFewRows = 128, kFewSegments = 2, kWanted = 512, kManyRows = 2048, kFewWorkgroups = 256;
 
 // f(shape): of the workgroups that hold `length` logits, the one of fewest threads.  (More alternatives than threads make a poor line: see top_of.)
 // With fewer workgroups than compute units, of sixteen waves: one workgroup's time is all there is.
@@ -896,16 +896,23 @@ void by_type(int dtype, F&& f) {
 
 }  // namespace
 
-// One segment where a workgroup holds the row, unless there are few rows of many logits: then as many as give every compute unit two workgroups
-// (each launch more of them takes 3 us, and what comes after the segments another launch).
-SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype) {
+// How rows are cut, by what was measured (us; one segment / several).  The launch that joins them takes 3.
+//  - Few rows of many logits: as many segments as give every compute unit two workgroups.  48 rows of 131072 with 20 alternatives 24.3 / 17.1, 4 such 21.4 / 19.2,
+//    64 of 50257 few of whose words are allowed 45.3 / 23.8; 200 of 50257 take 16.8 either way and stay whole.
+//  - Scores of rows of three workgroups of four waves and more: these, for five of them share a compute unit and one's selection is hidden behind the others' reads.
+//    1000 rows of 100003 with 20 alternatives 81.5 / 59.4, without 55.9 / 44.0, 300 of 131072 45.3 / 32.2.  Of two, where there are alternatives and many rows: 6001 of
+//    50257 155 / 140, 4096 of 32000 in fp32 113 / 104 (without alternatives 91 / 99), but 700 of 33278 22.6 / 23.5.
+//  - A gradient after the sums reads its row again if it does not hold it: one segment, as long as a workgroup holds the row.
+SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype, Use use, uint32_t top) {
   SplitArgs P{};
-  const uint32_t most = dtype == 0 ? Shape<float, 1024, 16>::kCapacity : Shape<__bf16, 1024, 16>::kCapacity;
-  const uint32_t small = dtype == 0 ? Shape<float, 256, 8>::kCapacity : Shape<__bf16, 256, 8>::kCapacity;
-  const uint32_t big = (vocab + most - 1u) / most, many = (vocab + small - 1u) / small;
+  const uint32_t of = dtype == 0 ? 1u : 2u;                          // capacities: Shape<T, 256, 8>, <T, 256, 16> and <T, 1024, 16>
+  const uint32_t small = Shape<float, 256, 8>::kCapacity * of, unit = Shape<float, 256, 16>::kCapacity * of, most = Shape<float, 1024, 16>::kCapacity * of;
+  const uint32_t many = (vocab + small - 1u) / small, units = (vocab + unit - 1u) / unit, big = (vocab + most - 1u) / most;
   uint32_t segments = big;
   if (static_cast<uint64_t>(rows) * big < kFewRows && vocab > kFewSegments * small && many <= 64u)
     segments = min(64u, max(many, min((kWanted + rows - 1u) / rows, 2u * many)));
+  else if (units <= 64u && (use == Use::kScores ? units >= 3u || (units == 2u && top > 0u && rows >= kManyRows) : big > 1u))
+    segments = units;
   P.length = segments == 1u ? vocab : ((vocab + segments - 1u) / segments + 7u) / 8u * 8u;
   P.segments = (vocab + P.length - 1u) / P.length;
   return P;
@@ -992,7 +999,7 @@ hipError_t launch_distill(const DistillArgs& all, int dtype, const SplitArgs& P,
           a.loss = shifted(a.loss, first);
           if (P.segments == 1u) {
             distill_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(rows), threads, 0, s>>>(a);
-          } else if constexpr (S::kThreads == 1024u || (S::kThreads == 256u && S::kVectors <= 8u)) {       // (as split_of cuts)
+          } else if constexpr (S::kThreads == 1024u || S::kThreads == 256u) {       // (as split_of cuts)
             distill_sums_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(rows * P.segments), threads, 0, s>>>(a, P);
             distill_gradient_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(rows * P.segments), threads, 0, s>>>(a, P);
           }
