@@ -28,6 +28,24 @@ namespace {
 constexpr uint32_t kChunk = 256;       // steps between kept states (RGC_RECURRENCE_CHUNK)
 constexpr uint32_t kOneTile = 128;     // steps of the sequences that are one tile (kMiddle below)
 constexpr float kLog2e = 1.44269504088896341f;
+
+// How a sequence is cut: the same constants make the tiles and choose the kernel.  What it is bound by: a forward pass moves 4 tensors, a backward one 7, and
+// with 30 and 63 instructions an element the arithmetic takes half of that time.  Forward and backward, us, bf16: 20 x 35 x 1500 with waves of eight steps 5.9 and 8.8, of sixteen
+// 11.4 and 11.1, of four 6.7 and 11.1; 64 x 100 x 1024 in one tile of sixteen waves 18 and 30, in tiles as for long ones 22 and 42.  Long ones forward, one prompt
+// of 32768 x 1500 and 8 x 4096 x 2048, by waves and steps: 8 x 16 129 and 124, 4 x 16 135 and 134, 16 x 8 142 and 154, 8 x 8 149 and 138, 16 x 16 143 and 147 (one or two channels a
+// lane as the registers allow; four channels a lane 240 and 174).  Backward, 16 x 16 (a kept state begins every tile): 234, 4.0 TB/s.
+struct Shape {
+  uint32_t waves, steps;           // waves a workgroup, steps a wave
+  constexpr uint32_t tile() const { return waves * steps; }
+};
+constexpr Shape kOneWave{1, 4}, kShort{8, 8}, kMiddle{16, 8}, kLong{8, 16}, kLongBackward{16, 16};
+static_assert(kMiddle.tile() == kOneTile && kLongBackward.tile() == kChunk, "as backward_tile takes its states");
+enum class Kind { kOneWave, kShort, kMiddle, kLong };
+// Whether tiles of this shape wait for each other (a shorter sequence than those is one tile).
+constexpr bool chained(uint32_t waves, uint32_t steps) {
+  return (waves == kLong.waves && steps == kLong.steps) || (waves == kLongBackward.waves && steps == kLongBackward.steps);
+}
+
 constexpr unsigned long long kUnset = ~0ull;      // a word that is not published yet (its upper half would be a NaN as P, which is never published)
 
 struct Stretch {
@@ -162,9 +180,10 @@ __device__ __forceinline__ uint32_t resets_of(const RecurrenceArgs& A, uint32_t 
 struct Place {
   uint32_t chain, b, block, order;      // order: how many tiles of the chain come before it
 };
+template <bool kChained>
 __device__ __forceinline__ Place take_place(const RecurrenceArgs& A, const TileArgs& G, uint32_t* lds) {
   uint32_t ticket = blockIdx.x;
-  if (G.tiles > 1u) {
+  if (kChained && G.tiles > 1u) {
     if (threadIdx.x == 0u) *lds = atomicAdd(G.ticket, 1u);
     __syncthreads();
     ticket = uniform(*lds);
@@ -195,6 +214,8 @@ __device__ __forceinline__ void publish(unsigned long long* w, const Stretch (&s
 
 // What comes into the tile, from the published words of the chain's earlier tiles: kWindow of them at a time, the same number by each wave, which
 // asks for all of its own before it looks at one.  (A word carries all there is to know, so no other memory needs ordering.)
+// (More at a time are published words that would not have been needed, read past the caches: with 16 and 32 by four waves one prompt of 32768 steps took 141 and
+// 155 us where 4 took 125, 8 x 4096 x 2048 forward 142 and 180 where 4 took 131.)
 constexpr uint32_t kWindow = 8;
 
 template <int kVec, int kWaves>
@@ -241,16 +262,16 @@ __device__ __forceinline__ void look_back(const TileArgs& G, const Place& at, ui
   for (int i = 0; i < kVec; ++i) carry[i] = seen[i].h;
 }
 
-template <int kVec, int kWaves>
+template <int kVec, int kWaves, bool kChained>
 struct Shared {
-  Stretch parts[kWaves][64 * kVec], earlier[kWaves > kWindow ? kWaves : kWindow][64 * kVec];
+  Stretch parts[kWaves][64 * kVec], earlier[kChained ? (kWaves > kWindow ? kWaves : kWindow) : 1][64 * kVec];
   uint32_t ticket;
 };
 
 // kWhole: all the tile's steps are there, and all its channels.  Otherwise steps behind the row's end become steps that change nothing (f = 1, u = 0).
 // What depends on a state starting anew stands in loops of its own, in two forms: the one without is taken by the waves that have none.
 template <typename T, int kVec, int kWaves, int kSteps, bool kGated, bool kWhole>
-__device__ __forceinline__ void forward_tile(const RecurrenceArgs& A, const TileArgs& G, const Place& at, uint32_t n, Shared<kVec, kWaves>& lds) {
+__device__ __forceinline__ void forward_tile(const RecurrenceArgs& A, const TileArgs& G, const Place& at, uint32_t n, Shared<kVec, kWaves, chained(kWaves, kSteps)>& lds) {
   constexpr uint32_t kTile = kWaves * kSteps;
   auto& parts = lds.parts;
   const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, b = at.b;
@@ -300,7 +321,7 @@ __device__ __forceinline__ void forward_tile(const RecurrenceArgs& A, const Tile
     for (int i = 0; i < kVec; ++i) parts[wave][lane * kVec + i] = own[i];
     __syncthreads();
   }
-  if (G.tiles > 1u) {
+  if (chained(kWaves, kSteps) && G.tiles > 1u) {
     Stretch whole[kVec];
     if (wave == 0u) {
 #pragma unroll
@@ -360,8 +381,8 @@ __device__ __forceinline__ void forward_tile(const RecurrenceArgs& A, const Tile
 
 template <typename T, int kVec, int kWaves, int kSteps, bool kGated>
 __global__ void __launch_bounds__(64 * kWaves, 4) recurrence_kernel(RecurrenceArgs A, TileArgs G) {
-  __shared__ Shared<kVec, kWaves> lds;
-  const Place at = take_place(A, G, &lds.ticket);
+  __shared__ Shared<kVec, kWaves, chained(kWaves, kSteps)> lds;
+  const Place at = take_place<chained(kWaves, kSteps)>(A, G, &lds.ticket);
   const uint32_t n = length_of(A, at.b);
   if ((at.order + 1u) * (kWaves * kSteps) <= n && (at.block + 1u) * 64u * kVec <= A.width)
     forward_tile<T, kVec, kWaves, kSteps, kGated, true>(A, G, at, n, lds);
@@ -369,15 +390,15 @@ __global__ void __launch_bounds__(64 * kWaves, 4) recurrence_kernel(RecurrenceAr
     forward_tile<T, kVec, kWaves, kSteps, kGated, false>(A, G, at, n, lds);
 }
 
-template <int kWaves>
+template <int kWaves, bool kChained>
 struct SharedBackward {
-  Stretch parts[kWaves][64], back[kWaves][64], earlier[kWaves > kWindow ? kWaves : kWindow][64];
+  Stretch parts[kWaves][64], back[kWaves][64], earlier[kChained ? (kWaves > kWindow ? kWaves : kWindow) : 1][64];
   uint32_t ticket;
 };
 
 template <typename T, int kWaves, int kSteps, bool kGated, bool kWhole>
 __device__ __forceinline__ void backward_tile(const RecurrenceArgs& A, const RecurrenceGradArgs& D, const TileArgs& G, const Place& at, uint32_t n,
-                                              SharedBackward<kWaves>& lds) {
+                                              SharedBackward<kWaves, chained(kWaves, kSteps)>& lds) {
   constexpr uint32_t kTile = kWaves * kSteps;
   static_assert(kTile == kChunk || kTile <= kOneTile, "a tile begins with a kept state, the only one of a short sequence with the first");
   auto& parts = lds.parts;
@@ -447,7 +468,7 @@ __device__ __forceinline__ void backward_tile(const RecurrenceArgs& A, const Rec
     back[wave][lane] = rear;
     __syncthreads();
   }
-  if (G.tiles > 1u) {
+  if (chained(kWaves, kSteps) && G.tiles > 1u) {
     Stretch whole[1];
     if (wave == 0u) {
       whole[0] = back[kWaves - 1][lane];
@@ -501,8 +522,8 @@ __device__ __forceinline__ void backward_tile(const RecurrenceArgs& A, const Rec
 
 template <typename T, int kWaves, int kSteps, bool kGated>
 __global__ void __launch_bounds__(64 * kWaves) recurrence_backward_kernel(RecurrenceArgs A, RecurrenceGradArgs D, TileArgs G) {
-  __shared__ SharedBackward<kWaves> lds;
-  const Place at = take_place(A, G, &lds.ticket);
+  __shared__ SharedBackward<kWaves, chained(kWaves, kSteps)> lds;
+  const Place at = take_place<chained(kWaves, kSteps)>(A, G, &lds.ticket);
   const uint32_t n = length_of(A, at.b);
   if ((G.tiles - at.order) * (kWaves * kSteps) <= n && (at.block + 1u) * 64u <= A.width)
     backward_tile<T, kWaves, kSteps, kGated, true>(A, D, G, at, n, lds);
@@ -517,15 +538,6 @@ __global__ void __launch_bounds__(256) clear_words_kernel(TileArgs G, uint64_t w
   for (uint64_t i = static_cast<uint64_t>(blockIdx.x) * 256u + threadIdx.x; i < pairs; i += threads) to[i] = two{kUnset, kUnset};
   if (blockIdx.x == 0u && threadIdx.x == 0u) *G.ticket = 0u;
 }
-
-// How a sequence is cut: the same constants make the tiles and choose the kernel.
-struct Shape {
-  uint32_t waves, steps;           // waves a workgroup, steps a wave
-  constexpr uint32_t tile() const { return waves * steps; }
-};
-constexpr Shape kOneWave{1, 4}, kShort{8, 8}, kMiddle{16, 8}, kLong{8, 16}, kLongBackward{16, 16};
-static_assert(kMiddle.tile() == kOneTile && kLongBackward.tile() == kChunk, "as backward_tile takes its states");
-enum class Kind { kOneWave, kShort, kMiddle, kLong };
 
 struct Cut {
   Kind kind;
