@@ -8,6 +8,8 @@
  *   decompress (Section 2.3, last paragraph before the cost model): the N gathered sparse
  *              messages are added into a dense array.
  *
+ * and, further down, the operators that the step of a recurrent language model runs around them.
+ *
  * Every function returns an int status (RGC_OK = 0, negative = error) unless stated; no C++
  * exception crosses this boundary.  All tensor and message pointers are DEVICE pointers into
  * memory owned by the caller (hipMalloc / a PyTorch-ROCm tensor); descriptor arrays

@@ -1,7 +1,8 @@
 """MI355X-native Residual Gradient Compression hot path (RedSync, arXiv 1808.04357).
 
 The package is a thin ctypes binding over ``librgc.so`` (hand-written HIP for gfx950, C ABI in
-``include/rgc.h``).  It only marshals arguments: every step of the path runs in the library's
+``include/rgc.h``): compression, decompression, and the operators that a recurrent language model's
+step runs around them.  It only marshals arguments: every step of the path runs in the library's
 kernels.  PyTorch-ROCm tensors are used for device memory and streams.  There is no CPU
 fallback: if the library is missing, importing the binding's entry points raises.
 """
