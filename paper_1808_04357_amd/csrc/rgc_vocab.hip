@@ -122,13 +122,15 @@ struct Vector {
   typedef uint32_t Unaligned __attribute__((ext_vector_type(4), aligned(2)));
 
   static __device__ __forceinline__ Words load(const T* p) { return *reinterpret_cast<const Words*>(p); }
+  template <bool kStream = false>
   static __device__ __forceinline__ void store(T* p, const float (&v)[kElems]) {
     T t[kElems];
 #pragma unroll
     for (uint32_t i = 0; i < kElems; ++i) t[i] = static_cast<T>(v[i]);
     Words w;
     __builtin_memcpy(&w, t, 16);
-    *reinterpret_cast<Unaligned*>(p) = w;
+    if constexpr (kStream) __builtin_nontemporal_store(static_cast<Unaligned>(w), reinterpret_cast<Unaligned*>(p));
+    else *reinterpret_cast<Unaligned*>(p) = w;
   }
   static __device__ __forceinline__ void unpack(const Words& w, float (&v)[kElems]) {
     T t[kElems];
@@ -326,10 +328,10 @@ __device__ __forceinline__ void list_exactly(const T* z, uint32_t n, uint32_t li
   __syncthreads();
 }
 
-//  A line under the k-th largest of a segment comes cheap: with q = ceil(k / waves), every wave's q-th largest of its lanes' largest is reached by q logits
-// of that wave, so the lowest of these is reached by k.  (Of the waves all of whose lanes have a vector, that is; without one all logits reach it.)  Few more reach it (where the logits lie anywhere: some 20 with four waves and k = 8, 100 with k = 64,
-// 55 with sixteen waves and k = 8); they are listed and ranked.  Where more do than the list holds, as with many equal ones (a mask that leaves
-// fewer than k), list_exactly reads the segment again.
+// A line under the k-th largest of a segment comes cheap: with q = ceil(k / waves), every wave's q-th largest of its lanes' largest is reached by q logits
+// of that wave, so the lowest of these is reached by k.  (Of the waves all of whose lanes have a vector, that is; without one all logits reach it.)  Few more
+// reach it (where the logits lie anywhere: some 20 with four waves and k = 8, 100 with k = 64, 55 with sixteen waves and k = 8); they are listed and ranked.
+// Where more do than the list holds, as with many equal ones (a mask that leaves fewer than k), list_exactly reads the segment again.
 template <uint32_t kThreads, typename H>
 __device__ __forceinline__ uint32_t line_of(const H& held, float t, uint32_t k, uint32_t line, int from, int to) {
   const uint32_t full = min(kThreads, held.vectors) / 64u;
@@ -573,8 +575,14 @@ __global__ void __launch_bounds__(kJoinThreads) score_join_kernel(ScoreArgs A, S
 }
 
 // dz_j = g (1{j = target} - p_j) - h p_j (log p_j + entropy), g and h divided by T: no sums, so any part of a row by any workgroup.
+// A gradient of more than kStreamFrom bytes is stored past the caches (kStream).  Stored the common way, what of it was still in them was written out while
+// the next pass read its logits.  Loss and gradient of 4096 x 32000 bf16 in turn, common -> past the caches: 165 -> 140 us, and 258 -> 240 with a copy of the
+// gradient right behind them; 2000 x 50257 bf16 124 -> 109 and 199 -> 186; 4000 x 10000 bf16 (80 MB) 58 -> 52 and 82 -> 81.  Under the bound a reader finds
+// the gradient in the caches, and loses more than the call gains: 1300 x 10000 f32 (52 MB) 32.0 -> 31.5 and 49.7 -> 52.1.  (The distillation's gradient has no
+// second reading of the logits to disturb; past the caches its reader lost all that it gained: 2048 x 128000 213 -> 207 and 412 -> 420.)
 constexpr uint32_t kGradThreads = 256, kGradVectors = 4;
-template <typename T>
+constexpr uint64_t kStreamFrom = 64ull << 20;
+template <typename T, bool kStream>
 __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs A, uint32_t parts) {
   using V = Vector<T>;
   constexpr uint32_t kPart = kGradThreads * kGradVectors * V::kElems;
@@ -588,7 +596,7 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs 
   if (nothing) {
     held.each([&](uint32_t i, const float (&)[V::kElems]) __attribute__((always_inline)) {
       const float zeros[V::kElems] = {};
-      if (held.mine(i)) V::store(dz + held.index(i), zeros);
+      if (held.mine(i)) V::template store<kStream>(dz + held.index(i), zeros);
     });
     if (held.has_single()) dz[held.single_index()] = static_cast<T>(0.0f);
     return;
@@ -608,7 +616,7 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs 
     float d[V::kElems];
 #pragma unroll
     for (uint32_t j = 0; j < V::kElems; ++j) d[j] = slope(v[j]);
-    if (held.mine(i)) V::store(dz + held.index(i), d);
+    if (held.mine(i)) V::template store<kStream>(dz + held.index(i), d);
   });
   if (held.has_single()) dz[held.single_index()] = static_cast<T>(slope(held.single));
   if (here) dz[at] = static_cast<T>(g + slope(at_target));         // over what the same thread has just stored
@@ -963,6 +971,7 @@ hipError_t launch_token_logprobs_backward(const ScoreGradArgs& all, int dtype, h
   by_type(dtype, [&](auto type) {
     using T = decltype(type);
     const uint32_t part = kGradThreads * kGradVectors * Vector<T>::kElems, parts = (all.vocab + part - 1u) / part;
+    const bool stream = uint64_t(all.rows) * all.vocab * sizeof(T) > kStreamFrom;
     by_rows(all.rows, static_cast<uint64_t>(kGradThreads) * parts, [&](uint64_t first, uint32_t rows) {
       ScoreGradArgs a = all;
       a.rows = rows;
@@ -973,7 +982,8 @@ hipError_t launch_token_logprobs_backward(const ScoreGradArgs& all, int dtype, h
       a.entropy = shifted(a.entropy, first);
       a.grad_logprob = shifted(a.grad_logprob, first);
       a.grad_entropy = shifted(a.grad_entropy, first);
-      score_grad_kernel<T><<<dim3(rows * parts), dim3(kGradThreads), 0, s>>>(a, parts);
+      if (stream) score_grad_kernel<T, true><<<dim3(rows * parts), dim3(kGradThreads), 0, s>>>(a, parts);
+      else score_grad_kernel<T, false><<<dim3(rows * parts), dim3(kGradThreads), 0, s>>>(a, parts);
     });
   });
   return hipGetLastError();

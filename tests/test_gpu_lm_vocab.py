@@ -302,6 +302,40 @@ def test_scores_gradient_against_differences(rgc, ctx):
         assert np.allclose((value(up) - value(down)) / (2 * step), got["grad"][:, j], rtol=1e-5, atol=2e-6)
 
 
+@pytest.mark.parametrize("dtype,rows", [("f32", 530), ("bf16", 1_060), ("f16", 1_060)])
+@pytest.mark.parametrize("pad,shift,in_place", [(0, 0, False), (5, 3, False), (0, 1, True)])
+def test_gradient_of_more_bytes_than_the_caches_take(rgc, ctx, dtype, rows, pad, shift, in_place):
+    """Gradients of 68 MB are stored another way than small ones: the same bits as row by row, nothing beside the rows, and right."""
+    import torch
+    vocab = 32_011
+    g = torch.Generator(device="cuda").manual_seed(rows + pad)
+    flat = torch.full((rows * (vocab + pad) + shift,), math.nan, dtype=dtype_of(dtype), device="cuda")
+    logits = flat[shift:].view(rows, vocab + pad)[:, :vocab]
+    logits.copy_(2 * torch.randn(rows, vocab, generator=g, device="cuda"))
+    targets = torch.randint(0, vocab, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    targets[3::7] = -1
+    weight, bonus = torch.randn(rows, generator=g, device="cuda"), torch.randn(rows, generator=g, device="cuda")
+    out = {"logprob": torch.empty(rows, device="cuda"), "entropy": torch.empty(rows, device="cuda"), "stats": torch.empty(rows, 2, device="cuda")}
+    rgc.rgc_token_logprobs(ctx, rgc.TokenScores(logits, targets, **out))
+    parts = torch.empty(rows, vocab, dtype=logits.dtype, device="cuda")
+    for r in range(0, rows, 100):
+        part = {k: v[r:r + 100] for k, v in out.items()}
+        rgc.rgc_token_logprobs_backward(ctx, rgc.TokenScores(logits[r:r + 100], targets[r:r + 100], **part), parts[r:r + 100],
+                                        weight[r:r + 100], bonus[r:r + 100])
+    some = [0, 1, 3, rows // 2, rows - 1]
+    used = as64(logits[some])
+    whole = flat if in_place else torch.full_like(flat, math.nan)
+    grad = whole[shift:].view(rows, vocab + pad)[:, :vocab]
+    rgc.rgc_token_logprobs_backward(ctx, rgc.TokenScores(logits, targets, **out), grad, weight, bonus)
+    read = grad.clone()                                                 # by the next kernel of the stream
+    torch.cuda.synchronize()
+    assert torch.equal(read, parts) and torch.equal(grad, parts)
+    assert bool(whole[:shift].isnan().all()) and bool(whole[shift:].view(rows, vocab + pad)[:, vocab:].isnan().all())
+    got = {k: as64(v[some]) for k, v in out.items()}
+    got["grad"] = as64(grad[some])
+    check_scores(used, got, targets[some].cpu().numpy(), dtype, grads=(weight[some].cpu().numpy(), bonus[some].cpu().numpy()))
+
+
 def test_rows_whose_offsets_pass_32_bits(rgc, ctx):
     """Rows 2^31 + 64 elements apart: the third one starts beyond 2^32 elements and 2^33 bytes."""
     import torch
