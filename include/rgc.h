@@ -316,7 +316,7 @@ int rgc_token_logprobs_backward(rgc_ctx* ctx, const rgc_token_scores* scores, co
  *   soft = T^2 sum_i q_i (ln q_i - ln p^T_i),   label = -ln p_target,   loss = soft_weight * soft + label_weight * label
  *   dz_j = grad_loss * [ soft_weight * T * (p^T_j - q_j) + label_weight * (p_j - 1{j = target}) ]
  *  - Teacher entries whose index is outside [0, vocab) are left out (rows with fewer than k); an index that comes twice
- *    stands for the sum of both.  A row without entries, or with all its teacher logits -inf, has soft = 0.
+ *    stands for the sum of both (in the loss as in the gradient: the sums run over words).  A row without entries, or with all its teacher logits -inf, has soft = 0.
  *  - A target outside [0, vocab) (or targets == NULL) has label = 0.  A row with neither has loss 0 and gradient 0,
  *    whatever its logits hold.
  *  - Where every logit of a row is -inf, p = 0: the loss is +inf.

@@ -667,15 +667,15 @@ __device__ __forceinline__ TeacherLane teach(const DistillArgs& A, uint32_t r, i
   }
   sum = wave_sum(sum);
   const float log_sum = kLn2 * log2_of(sum);
-  float off[2];
   bool again[2] = {false, false};
 #pragma unroll
   for (uint32_t u = 0; u < 2u; ++u) {
-    off[u] = t.q[u] = sum == 0.0f ? 0.0f : w[u] / sum;
+    t.q[u] = sum == 0.0f ? 0.0f : w[u] / sum;
     t.log_q[u] = log_probability(z[u], largest, A.inv_t, log_sum);
   }
-  // An index that comes twice has both weights, at its first place.  Few rows have any: whether one may come twice is told by a bit for every index (one of
-  // kSeenBits), and those that find theirs set are looked for among all.  (A loop over all entries took 20 us of 108, 2048 rows of 64.)
+  // An index that comes twice has both weights, at its first place, in the loss as in the gradient (q ln q of a sum is not the sum of its parts').  Few
+  // rows have any: whether one may come twice is told by a bit for every index (one of kSeenBits), and those that find theirs set are looked for among
+  // all.  (A loop over all entries took 20 us of 108, 2048 rows of 64.)
 #pragma unroll
   for (uint32_t i = 0; i < kSeenBits / 32u / 256u; ++i) reinterpret_cast<uint4*>(to.seen)[i * 64u + lane] = uint4{0u, 0u, 0u, 0u};
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -689,13 +689,16 @@ __device__ __forceinline__ TeacherLane teach(const DistillArgs& A, uint32_t r, i
       if (__popcll(in0) + __popcll(in1) < 2) continue;
       const uint32_t place = in0 != 0ull ? static_cast<uint32_t>(__ffsll(in0) - 1) : 64u + static_cast<uint32_t>(__ffsll(in1) - 1);
       float both = 0.0f;
-      for (unsigned long long m = in0; m != 0ull; m &= m - 1ull) both += lane_of(t.q[0], static_cast<uint32_t>(__ffsll(m) - 1));
-      for (unsigned long long m = in1; m != 0ull; m &= m - 1ull) both += lane_of(t.q[1], static_cast<uint32_t>(__ffsll(m) - 1));
+      for (unsigned long long m = in0; m != 0ull; m &= m - 1ull) both += lane_of(w[0], static_cast<uint32_t>(__ffsll(m) - 1));
+      for (unsigned long long m = in1; m != 0ull; m &= m - 1ull) both += lane_of(w[1], static_cast<uint32_t>(__ffsll(m) - 1));
 #pragma unroll
-      for (uint32_t w = 0; w < 2u; ++w)
-        if (t.at[w] == at) {
-          if (lane + 64u * w == place) off[w] = both; else again[w] = true;
-        }
+      for (uint32_t v = 0; v < 2u; ++v) {
+        if (t.at[v] != at) continue;
+        const bool here = lane + 64u * v == place;
+        t.q[v] = here && sum != 0.0f ? both / sum : 0.0f;
+        t.log_q[v] = kLn2 * log2_of(both) - log_sum;
+        again[v] = !here;
+      }
     }
   }
   const bool label_listed = label >= 0 && __any(t.at[0] == label || t.at[1] == label);
@@ -704,7 +707,7 @@ __device__ __forceinline__ TeacherLane teach(const DistillArgs& A, uint32_t r, i
   for (uint32_t u = 0; u < 2u; ++u) {
     const uint32_t i = lane + 64u * u;
     to.at[i] = again[u] ? -1 : t.at[u];
-    to.off[i] = soft * off[u] + (t.at[u] >= 0 && t.at[u] == label ? A.label_weight : 0.0f);
+    to.off[i] = soft * t.q[u] + (t.at[u] >= 0 && t.at[u] == label ? A.label_weight : 0.0f);
     to.z[i] = t.z[u];
   }
   if (lane == 0u) {
