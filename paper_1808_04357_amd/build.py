@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librgc.so")
 SOURCES = ["rgc_api.cpp", "rgc_compress.hip", "rgc_decompress.hip", "rgc_threshold.hip", "rgc_yardstick.hip",
            "rgc_vocab.hip", "rgc_recurrence.hip"]
-HEADERS = ["rgc_internal.h", "rgc_device.h", "rgc_exact.h", "rgc_tickets.h", "rgc_tiles.h", "rgc_lm.h", os.path.join("..", "..", "include", "rgc.h"),
+HEADERS = ["rgc_internal.h", "rgc_device.h", "rgc_exact.h", "rgc_tickets.h", "rgc_tiles.h", "rgc_lm.h", "rgc_stretch.h", os.path.join("..", "..", "include", "rgc.h"),
            os.path.join("..", "..", "include", "rgc_diag.h")]
 
 FLAGS = [

@@ -91,7 +91,8 @@ struct RecurrenceGradArgs {
 // How a recurrence is cut into tiles (workgroups), and what they tell each other.
 struct TileArgs {
   uint32_t across, tiles;        // chains a sequence has (stretches of channels), tiles a chain has
-  unsigned long long* words;     // [chains][tiles][channels of a tile]
+  uint32_t groups;               // groups of tiles with another behind them
+  unsigned long long* words;     // [chains][tiles, then groups][channels of a tile]
   uint32_t* ticket;
 };
 

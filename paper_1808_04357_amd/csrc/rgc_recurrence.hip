@@ -8,19 +8,22 @@
 // with g the gradient that leaves a step towards the one before it, d = e + g', g = f d.
 //
 // Tiles of one chain (a sequence's 64 kVec channels) follow each other in time, and a tile needs the state that the one before it ends with.
-// Tiles are handed out by a ticket, all chains' first tiles, then all second ones: a tile publishes its (P, H) as soon as it has it, and the
-// state it ends with (which is a stretch with P = 0) when it knows that, and looks back over the published ones until it has come to such a
-// state.  It waits for tiles of smaller tickets only, and a ticket is taken by a workgroup that runs, so the smallest ticket not done
+// Tiles are handed out by a ticket, all chains' first tiles, then all second ones: a tile publishes its (P, H) as soon as it has it, the last one of a group of
+// tiles the group's, and the state behind the group (which is a stretch with P = 0) when it knows that; and a tile looks back over the published ones until it has come to
+// a state.  It waits for tiles of smaller tickets only, and a ticket is taken by a workgroup that runs, so the smallest ticket not done
 // waits for nothing: every wait ends, however few workgroups run at a time.
 //
-// The sign bit of P says that nothing from before enters at all (a state that started anew, a published state): P h is not even formed there, h may be NaN.
+// Which words were states already when a tile looked is a matter of time, what it makes of them is not: stretches are joined in the same order whatever
+// was met, to the last bit (rgc_stretch.h).
 //
 // 1 - sigmoid(v) is computed as sigmoid(-v), which keeps its precision where the gate is nearly open.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "rgc_lm.h"
+#include "rgc_stretch.h"
 
 namespace rgc {
 namespace {
@@ -44,19 +47,6 @@ enum class Kind { kOneWave, kShort, kMiddle, kLong };
 // Whether tiles of this shape wait for each other (a shorter sequence than those is one tile).
 constexpr bool chained(uint32_t waves, uint32_t steps) {
   return (waves == kLong.waves && steps == kLong.steps) || (waves == kLongBackward.waves && steps == kLongBackward.steps);
-}
-
-constexpr unsigned long long kUnset = ~0ull;      // a word that is not published yet (its upper half would be a NaN as P, which is never published)
-
-struct Stretch {
-  float p, h;
-};
-
-__device__ __forceinline__ bool cut(float p) { return __float_as_int(p) < 0; }
-__device__ __forceinline__ float after(const Stretch& s, float h) { return cut(s.p) ? s.h : __fmaf_rn(s.p, h, s.h); }
-// `first`, then `second`.
-__device__ __forceinline__ Stretch both(const Stretch& first, const Stretch& second) {
-  return Stretch{cut(first.p) || cut(second.p) ? -0.0f : first.p * second.p, after(second, first.h)};
 }
 
 // sigmoid(v) and sigmoid(-v) with one power and one reciprocal.  Below -87 the power may be infinite, and infinity times 0 is not 1.
@@ -198,73 +188,151 @@ __device__ __forceinline__ Place take_place(const RecurrenceArgs& A, const TileA
 }
 
 template <int kVec>
-__device__ __forceinline__ unsigned long long* words_of(const TileArgs& G, uint32_t chain, uint32_t order) {
-  return G.words + (static_cast<uint64_t>(chain) * G.tiles + order) * (64u * kVec) + (threadIdx.x & 63u) * kVec;
+__device__ __forceinline__ unsigned long long* words_of(const TileArgs& G, uint32_t chain, uint32_t at) {
+  return G.words + (static_cast<uint64_t>(chain) * (G.tiles + G.groups) + at) * (64u * kVec) + (threadIdx.x & 63u) * kVec;
 }
 
 template <int kVec>
 __device__ __forceinline__ void publish(unsigned long long* w, const Stretch (&s)[kVec]) {
 #pragma unroll
+  for (int i = 0; i < kVec; ++i) __hip_atomic_store(w + i, word_of(s[i]), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <int kVec>
+struct Words {
+  unsigned long long v[kVec];
+};
+template <int kVec>
+__device__ __forceinline__ Words<kVec> ask(const unsigned long long* w) {
+  Words<kVec> r;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) r.v[i] = __hip_atomic_load(w + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return r;
+}
+// Asks again until they are published.
+template <int kVec>
+__device__ __forceinline__ void settle(Words<kVec>& r, const unsigned long long* w, Stretch* to) {
+#pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    const bool broken = s[i].p != s[i].p;                            // a NaN among the gates: NaN whatever comes before
-    const uint32_t p = __float_as_uint(broken ? -0.0f : s[i].p), h = __float_as_uint(broken ? s[i].p : s[i].h);
-    __hip_atomic_store(w + i, (static_cast<unsigned long long>(p) << 32) | h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    while (r.v[i] == kUnset) {
+      __builtin_amdgcn_s_sleep(1);
+      r.v[i] = __hip_atomic_load(w + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    to[i] = stretch_of(r.v[i]);
   }
 }
 
-// What comes into the tile, from the published words of the chain's earlier tiles: kWindow of them at a time, the same number by each wave, which
-// asks for all of its own before it looks at one.  (A word carries all there is to know, so no other memory needs ordering.)
-// (More at a time are published words that would not have been needed, read past the caches: with 16 and 32 by four waves one prompt of 32768 steps took 141 and
-// 155 us where 4 took 125, 8 x 4096 x 2048 forward 142 and 180 where 4 took 131.)
-constexpr uint32_t kWindow = 8;
+// The state that comes into the tile, from published words.  (A word carries all there is to know, so no other memory needs ordering.)  kGroup tiles that follow each other
+// are a group; what is told:
+//  - every tile's stretch, to the later ones of its group;
+//  - by the group's last tile, the group's stretch, joined from those; and in its place, as soon as that tile knows what came before, the state behind the group.
+// A tile goes back over the earlier groups' words until it comes to a state, kWaves of them at a time, one by each wave, applies the groups' stretches behind it one after the
+// other, and then its own group's tiles'.  It waits for tiles that wait for nothing themselves, or for the stretches of their group alone; only where none of kKept
+// groups' words is a state, it asks for the oldest of them again until one is.
+// In us, one prompt of 32768 x 1500, 8 x 4096 x 2048 forward and backward, 1 x 32768 x 64 forward: groups of 16 123, 121, 238, 13.6; of 8 126, 122, 246, 13.5;
+// no groups, but every tile's state in the place of its stretch, 133, 125, 234, 23.  (The stretches joined to one on the way back, whichever were met as
+// states, 127, 120, 234, 16.4: its last bits were a matter of time.)
+constexpr uint32_t kGroup = 16, kKept = 16;
 
 template <int kVec, int kWaves>
-__device__ __forceinline__ void look_back(const TileArgs& G, const Place& at, uint32_t wave, Stretch (*lds)[64 * kVec], float (&carry)[kVec]) {
-  constexpr uint32_t kEach = kWindow > kWaves ? kWindow / kWaves : 1u, kSeen = kEach * kWaves;
-  const uint32_t lane = threadIdx.x & 63u;
-  Stretch seen[kVec];
+struct Before {
+  Stretch tiles[kGroup][64 * kVec], groups[kKept][64 * kVec];      // groups[j]: the group j + 1 before this one
+  uint32_t is_state[kKept];
+  float group_state[64 * kVec], state[64 * kVec];                  // what comes into the group, and into the tile (with two channels a lane)
+};
+struct Nothing {};
+
+// `whole`: the tile's own stretch, in wave 0; carry: what comes into the first tile.
+template <int kVec, int kWaves>
+__device__ __forceinline__ void come_in(const TileArgs& G, const Place& at, uint32_t wave, Stretch (&whole)[kVec], Before<kVec, kWaves>& lds, float (&carry)[kVec]) {
+  constexpr uint32_t kEach = (kGroup + kWaves - 1u) / kWaves, kMine = 64u * kVec / kWaves;
+  static_assert(kKept % kWaves == 0u, "whole rounds");
+  const uint32_t lane = threadIdx.x & 63u, group = at.order / kGroup, place = at.order % kGroup;
+  const bool followed = at.order + 1u < G.tiles, ends = followed && place + 1u == kGroup;
+  if (wave == 0u && followed && !ends) {
+    if (at.order == 0u) {
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) seen[i] = Stretch{1.0f, 0.0f};
-  for (uint32_t next = at.order; next > 0u;) {                       // tiles next - 1, next - 2, ..
-    unsigned long long v[kEach][kVec];
-#pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) {
-      const uint32_t back = min(wave * kEach + j, next - 1u);        // (the first tile again, where there are no more)
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) v[j][i] = __hip_atomic_load(words_of<kVec>(G, at.chain, next - 1u - back) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      for (int i = 0; i < kVec; ++i) whole[i] = state_of(after(whole[i], carry[i]));
     }
+    publish<kVec>(words_of<kVec>(G, at.chain, at.order), whole);
+  }
+  if (at.order == 0u) return;
+  // the nearest groups' words are asked for together with the tiles'; the group's last tile tells the group's stretch before it waits for them
+  const unsigned long long *const from = words_of<kVec>(G, at.chain, group * kGroup), *const groups = words_of<kVec>(G, at.chain, G.tiles);
+  auto group_at = [&](uint32_t first) { return groups + static_cast<uint64_t>(group - 1u - (first + wave)) * (64u * kVec); };
+  Words<kVec> near = {}, tile[kEach] = {};
+  if (wave < group) near = ask<kVec>(group_at(0u));
 #pragma unroll
-    for (uint32_t j = 0; j < kEach; ++j) {
-      const uint32_t back = min(wave * kEach + j, next - 1u);
+  for (uint32_t j = 0; j < kEach; ++j)
+    if (wave + j * kWaves < place) tile[j] = ask<kVec>(from + (wave + j * kWaves) * (64u * kVec));
+#pragma unroll
+  for (uint32_t j = 0; j < kEach; ++j)
+    if (wave + j * kWaves < place) settle<kVec>(tile[j], from + (wave + j * kWaves) * (64u * kVec), &lds.tiles[wave + j * kWaves][lane * kVec]);
+  if (ends) {
+    __syncthreads();
+    if (wave == 0u) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        while (v[j][i] == kUnset) {
-          __builtin_amdgcn_s_sleep(1);
-          v[j][i] = __hip_atomic_load(words_of<kVec>(G, at.chain, next - 1u - back) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        lds[wave * kEach + j][lane * kVec + i] = Stretch{__uint_as_float(static_cast<uint32_t>(v[j][i] >> 32)), __uint_as_float(static_cast<uint32_t>(v[j][i]))};
-      }
-    }
-    __syncthreads();
-    bool open = false;
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
+        Stretch s = lds.tiles[0][lane * kVec + i];
 #pragma unroll 4
-      for (uint32_t j = 0; j < kSeen && j < next; ++j) seen[i] = both(lds[j][lane * kVec + i], seen[i]);
-      open |= !cut(seen[i].p);
+        for (uint32_t j = 1; j + 1u < kGroup; ++j) s = both(s, lds.tiles[j][lane * kVec + i]);
+        whole[i] = both(s, whole[i]);
+      }
+      publish<kVec>(words_of<kVec>(G, at.chain, G.tiles + group), whole);
     }
-    // the same in every wave, which all have the same words (the first tile's word is a state, so it ends there at the latest)
-    if (!__any(open)) break;
-    next = next > kSeen ? next - kSeen : 0u;
-    __syncthreads();
   }
+  uint32_t n = 0u;                                                   // groups back to the nearest state
+  for (uint32_t first = 0;;) {
+    if (first + wave < group) {
+      Stretch* to = &lds.groups[first + wave][lane * kVec];
+      settle<kVec>(near, group_at(first), to);
+      bool open = false;
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) carry[i] = seen[i].h;
+      for (int i = 0; i < kVec; ++i) open |= !cut(stretch_of(near.v[i]).p);
+      const bool state = !__any(open);                               // (of all lanes)
+      if (lane == 0u) lds.is_state[first + wave] = state ? 1u : 0u;
+    }
+    __syncthreads();
+    if (group == 0u) break;
+    const uint32_t seen = min(group - first, static_cast<uint32_t>(kWaves));
+    const unsigned long long states = __ballot(lane < seen && lds.is_state[first + min(lane, seen - 1u)] != 0u);
+    if (states != 0ull) {
+      n = first + static_cast<uint32_t>(__ffsll(states));
+      break;
+    }
+    if (first + kWaves < kKept) first += kWaves;
+    else __syncthreads();                                            // (before the same words are replaced)
+    if (first + wave < group) near = ask<kVec>(group_at(first));
+  }
+  auto into_group = [&](uint32_t c) { return state_behind<4>(n, [&](uint32_t j) { return lds.groups[j][c]; }); };
+  auto into_tile = [&](uint32_t c, float h) { return state_behind<4>(place, [&](uint32_t j) { return lds.tiles[place - 1u - j][c]; }, h); };
+  float into[kVec];
+  if constexpr (kVec == 1) {
+    into[0] = into_group(lane);
+    carry[0] = into_tile(lane, into[0]);
+  } else {
+    // each wave for some of the channels: eight waves that read all words for all of them keep the shared memory busy for half a microsecond
+    const uint32_t c = wave * kMine + min(lane, kMine - 1u);
+    const float of_group = into_group(c), of_tile = into_tile(c, of_group);
+    if (lane < kMine) {
+      lds.group_state[c] = of_group;
+      lds.state[c] = of_tile;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) into[i] = lds.group_state[lane * kVec + i], carry[i] = lds.state[lane * kVec + i];
+  }
+  if (ends && wave == 0u && group > 0u) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) whole[i] = state_of(after(whole[i], into[i]));
+    publish<kVec>(words_of<kVec>(G, at.chain, G.tiles + group), whole);
+  }
 }
 
 template <int kVec, int kWaves, bool kChained>
 struct Shared {
-  Stretch parts[kWaves][64 * kVec], earlier[kChained ? (kWaves > kWindow ? kWaves : kWindow) : 1][64 * kVec];
+  Stretch parts[kWaves][64 * kVec];
+  std::conditional_t<kChained, Before<kVec, kWaves>, Nothing> before;
   uint32_t ticket;
 };
 
@@ -321,22 +389,18 @@ __device__ __forceinline__ void forward_tile(const RecurrenceArgs& A, const Tile
     for (int i = 0; i < kVec; ++i) parts[wave][lane * kVec + i] = own[i];
     __syncthreads();
   }
-  if (chained(kWaves, kSteps) && G.tiles > 1u) {
-    Stretch whole[kVec];
-    if (wave == 0u) {
+  if constexpr (chained(kWaves, kSteps)) {
+    if (G.tiles > 1u) {
+      Stretch whole[kVec];
+      if (wave == 0u) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        whole[i] = own[i];
+        for (int i = 0; i < kVec; ++i) {
+          whole[i] = own[i];
 #pragma unroll 4
-        for (uint32_t j = 1; j < kWaves; ++j) whole[i] = both(whole[i], parts[j][lane * kVec + i]);
+          for (uint32_t j = 1; j < kWaves; ++j) whole[i] = both(whole[i], parts[j][lane * kVec + i]);
+        }
       }
-      if (at.order > 0u && at.order + 1u < G.tiles) publish<kVec>(words_of<kVec>(G, at.chain, at.order), whole);
-    }
-    if (at.order > 0u) look_back<kVec, kWaves>(G, at, wave, lds.earlier, carry);
-    if (wave == 0u && at.order + 1u < G.tiles) {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) whole[i] = Stretch{-0.0f, after(whole[i], carry[i])};
-      publish<kVec>(words_of<kVec>(G, at.chain, at.order), whole);
+      come_in<kVec, kWaves>(G, at, wave, whole, lds.before, carry);
     }
   }
   if (A.states && wave == 0u && at.order * kTile < A.steps && (at.order * kTile) % kChunk == 0u) {
@@ -392,7 +456,8 @@ __global__ void __launch_bounds__(64 * kWaves, 4) recurrence_kernel(RecurrenceAr
 
 template <int kWaves, bool kChained>
 struct SharedBackward {
-  Stretch parts[kWaves][64], back[kWaves][64], earlier[kChained ? (kWaves > kWindow ? kWaves : kWindow) : 1][64];
+  Stretch parts[kWaves][64], back[kWaves][64];
+  std::conditional_t<kChained, Before<1, kWaves>, Nothing> before;
   uint32_t ticket;
 };
 
@@ -468,18 +533,15 @@ __device__ __forceinline__ void backward_tile(const RecurrenceArgs& A, const Rec
     back[wave][lane] = rear;
     __syncthreads();
   }
-  if (chained(kWaves, kSteps) && G.tiles > 1u) {
-    Stretch whole[1];
-    if (wave == 0u) {
-      whole[0] = back[kWaves - 1][lane];
+  if constexpr (chained(kWaves, kSteps)) {
+    if (G.tiles > 1u) {
+      Stretch whole[1];
+      if (wave == 0u) {
+        whole[0] = back[kWaves - 1][lane];
 #pragma unroll 4
-      for (uint32_t j = kWaves - 1u; j-- > 0u;) whole[0] = both(whole[0], back[j][lane]);
-      if (at.order > 0u && at.order + 1u < G.tiles) publish<1>(words_of<1>(G, at.chain, at.order), whole);
-    }
-    if (at.order > 0u) look_back<1, kWaves>(G, at, wave, lds.earlier, carry);
-    if (wave == 0u && at.order + 1u < G.tiles) {
-      whole[0] = Stretch{-0.0f, after(whole[0], carry[0])};
-      publish<1>(words_of<1>(G, at.chain, at.order), whole);
+        for (uint32_t j = kWaves - 1u; j-- > 0u;) whole[0] = both(whole[0], back[j][lane]);
+      }
+      come_in<1, kWaves>(G, at, wave, whole, lds.before, carry);
     }
   }
 #pragma unroll 4
@@ -560,11 +622,12 @@ TileArgs tiles_of(const RecurrenceArgs& a, const Cut& c, bool backward) {
   G.across = (a.width + 64u * c.vec - 1u) / (64u * c.vec);
   const uint32_t tile = shape_of(c.kind, backward).tile();
   G.tiles = a.steps == 0u ? 1u : (a.steps + tile - 1u) / tile;
+  G.groups = (G.tiles - 1u) / kGroup;
   return G;
 }
 
 uint64_t words_for(const RecurrenceArgs& a, const Cut& c, const TileArgs& G) {
-  return G.tiles > 1u ? static_cast<uint64_t>(a.batch) * G.across * G.tiles * 64u * c.vec : 0u;
+  return G.tiles > 1u ? static_cast<uint64_t>(a.batch) * G.across * (uint64_t(G.tiles) + G.groups) * 64u * c.vec : 0u;
 }
 
 uint64_t workgroups(const RecurrenceArgs& a, const TileArgs& G) { return static_cast<uint64_t>(a.batch) * G.across * G.tiles; }
