@@ -604,14 +604,19 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs 
   const float g = A.grad_logprob ? A.grad_logprob[r] * A.inv_t : 0.0f, h = A.grad_entropy ? A.grad_entropy[r] * A.inv_t : 0.0f;
   const float entropy = A.grad_entropy ? A.entropy[r] : 0.0f, log2s = log_sum * (1.0f / kLn2);
   // p (g + h (ln p + entropy)) = p (u + w a), a = log2 p
-  const float u = g + h * entropy, w = h * kLn2;
+  const float hh = h * entropy, u = g + hh, w = h * kLn2;
   auto slope = [&](float v) {
     const float a = __fmaf_rn(v - m, A.scale, -log2s);
     return -exp2_of(a) * __fmaf_rn(w, as_factor(a), u);
   };
   const uint32_t at = static_cast<uint32_t>(target) - first;       // of the target in this part, if it is
   const bool here = target >= 0 && at < n && held.owner(at) == threadIdx.x;
-  const float at_target = here ? static_cast<float>(z[at]) : 0.0f;
+  // there g (1 - p) - h p (ln p + entropy); 1 - p is made of ln p, for of a probability near 1 fp32 keeps little beside the 1
+  float at_target = 0.0f;
+  if (here) {
+    const float v = static_cast<float>(z[at]), a = __fmaf_rn(v - m, A.scale, -log2s);
+    at_target = -g * expm1f(log_probability(v, m, A.inv_t, log_sum)) - exp2_of(a) * __fmaf_rn(w, as_factor(a), hh);
+  }
   held.each([&](uint32_t i, const float (&v)[V::kElems]) __attribute__((always_inline)) {
     float d[V::kElems];
 #pragma unroll
@@ -619,7 +624,7 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs 
     if (held.mine(i)) V::template store<kStream>(dz + held.index(i), d);
   });
   if (held.has_single()) dz[held.single_index()] = static_cast<T>(slope(held.single));
-  if (here) dz[at] = static_cast<T>(g + slope(at_target));         // over what the same thread has just stored
+  if (here) dz[at] = static_cast<T>(at_target);                    // over what the same thread has just stored
 }
 
 // ---------------------------------------------------------------- distillation
