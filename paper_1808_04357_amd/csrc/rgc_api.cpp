@@ -1485,10 +1485,10 @@ int rgc_distill_loss(rgc_ctx* ctx, const rgc_distill* a, void* hip_stream) {
   if (P.segments > 1u) {
     const uint64_t parts = static_cast<uint64_t>(A.rows) * P.segments;
     unsigned long long* scratch = nullptr;
-    const int rc = lm_scratch(ctx, parts * 2u + (static_cast<uint64_t>(A.rows) * (RGC_TOP_MAX + 1) + 1u) / 2u, &scratch);
+    const int rc = lm_scratch(ctx, parts * (kDistillSums / 2u) + (static_cast<uint64_t>(A.rows) * (RGC_TOP_MAX + 1) + 1u) / 2u, &scratch);
     if (rc != RGC_OK) return rc;
     P.sums = reinterpret_cast<float*>(scratch);
-    P.logits = reinterpret_cast<float*>(scratch + 2u * parts);
+    P.logits = reinterpret_cast<float*>(scratch + (kDistillSums / 2u) * parts);
   }
   RGC_HIP(launch_distill(A, a->dtype, P, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;

@@ -60,10 +60,11 @@ struct DistillArgs {
 // How rows are cut into segments (workgroups), and what those leave for each other where there are several.
 struct SplitArgs {
   uint32_t segments, length;
-  float* sums;               // [rows][segments][4]
+  float* sums;               // [rows][segments][4], distillation [rows][segments][kDistillSums]
   uint64_t* entries;         // [rows][segments][top]: scores
   float* logits;             // [rows][RGC_TOP_MAX + 1]: distillation
 };
+constexpr uint64_t kDistillSums = 6;
 enum class Use { kScores, kDistillation };
 SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype, Use use, uint32_t top);
 

@@ -89,23 +89,6 @@ __device__ __forceinline__ Sums wave_join(const Sums& t, float c, float c1) {
   return r;
 }
 
-// The same in every thread; lds: 3 floats a wave.  Holds one barrier, which callers rely on.
-template <Third kThird, uint32_t kWaves>
-__device__ __forceinline__ Sums block_join(const Sums& t, float c, float c1, float* lds) {
-  const Sums own = wave_join<kThird>(t, c, c1);
-  const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-  if (lane == 0u) {
-    lds[3u * wave] = own.m;
-    lds[3u * wave + 1u] = own.s;
-    lds[3u * wave + 2u] = own.e;
-  }
-  __syncthreads();
-  if constexpr (kWaves == 1) return own;
-  Sums o = kNothing;
-  if (lane < kWaves) o = Sums{lds[3u * lane], lds[3u * lane + 1u], lds[3u * lane + 2u]};
-  return wave_join<kThird>(o, c, c1);
-}
-
 // Everything that is made of a row with a NaN or +inf is NaN.
 __device__ __forceinline__ Sums spoiled(Sums t) {
   if (t.s != t.s) t.m = t.s;
@@ -224,6 +207,106 @@ __device__ __forceinline__ Sums sums_of(const H& held, float c, float c1) {
     }
   });
   return t;
+}
+
+// A row whose largest logit has nearly all the weight has S = 1 + x with a small x, of which fp32 keeps little beside the 1, and its log probability is
+// -ln(1 + x).  Up to this S, x is added up by itself.
+constexpr float kNearlyOne = 1.25f;
+__device__ __forceinline__ bool nearly_one(float s) { return s >= 1.0f && s < kNearlyOne; }
+// ln(1 + x) for -1 + 1 / kNearlyOne <= x <= kNearlyOne - 1: 2 artanh(t) with t = x / (2 + x), |t| <= 1/9, by its series up to t^9 (the next term is below 2^-34 of it).
+__device__ __forceinline__ float log1p_of(float x) {
+  const float t = x * __builtin_amdgcn_rcpf(2.0f + x), t2 = t * t;
+  return 2.0f * t * __fmaf_rn(t2, __fmaf_rn(t2, __fmaf_rn(t2, __fmaf_rn(t2, 1.0f / 9.0f, 1.0f / 7.0f), 1.0f / 5.0f), 1.0f / 3.0f), 1.0f);
+}
+__device__ __forceinline__ float log_of_sum(float s, float x) { return nearly_one(s) ? log1p_of(x) : kLn2 * log2_of(s); }
+
+// The weights of all logits but one of the largest, and the same at the other temperature (kOther).
+struct Others {
+  float x, x1;
+};
+template <Third kThird>
+__device__ __forceinline__ bool others_wanted(const Sums& t) { return nearly_one(t.s) || (kThird == Third::kOther && nearly_one(t.e)); }
+
+// Of several sets (a row's waves or segments) joined to t: own and x are the lane's set's.
+template <Third kThird>
+__device__ __forceinline__ Others others_join(const Sums& own, const Others& x, const Sums& t, float c, float c1) {
+  // the first set that has the largest logit counts without it
+  const unsigned long long holders = __ballot(own.m == t.m);
+  const bool holds = holders != 0ull && (threadIdx.x & 63u) == static_cast<uint32_t>(__ffsll(holders) - 1);
+  const Sums moved = rebased<kThird == Third::kOther ? Third::kOther : Third::kNone>(own, t.m, c, c1);
+  Others o{wave_sum(holds ? x.x : moved.s), 0.0f};
+  if constexpr (kThird == Third::kOther) o.x1 = wave_sum(holds ? x.x1 : moved.e);
+  return o;
+}
+
+template <uint32_t kThreads, uint32_t kVectors>
+struct JoinShared {
+  float sums[kThreads / 64u][5];
+  uint4 raw[kThreads / 64u][kVectors];                               // of one thread of each wave
+};
+
+// What a wave holds; t: its sums.  Only the lane that holds the one left out has the loss: what it holds is added up again, by the whole wave (by that
+// lane alone it took 3 us of 17, 700 rows of 10000 in fp32).
+template <Third kThird, bool kSquared, typename T, uint32_t kThreads, uint32_t kVectors>
+__device__ __forceinline__ Others others_of(const Held<T, kThreads, kVectors>& held, const Sums& own, const Sums& t, float c, float c1, uint4 (&raw)[kVectors]) {
+  constexpr bool kTwo = kThird == Third::kOther;
+  const uint32_t lane = threadIdx.x & 63u, first = static_cast<uint32_t>(__ffsll(__ballot(own.m == t.m)) - 1), thread = held.wave0 + first;
+  if (lane == first) {
+#pragma unroll
+    for (uint32_t i = 0; i < kVectors; ++i) __builtin_memcpy(&raw[i], &held.raw[i], 16);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const uint32_t n = thread < held.vectors ? ((held.vectors - 1u - thread) / kThreads + 1u) * Vector<T>::kElems : 0u;
+  // (element n: the single one)
+  const float single = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(held.single), static_cast<int>(first)));
+  const Sums moved = rebased<kTwo ? Third::kOther : Third::kNone>(own, t.m, c, c1);
+  Others x{lane == first ? 0.0f : moved.s, lane == first ? 0.0f : moved.e};
+  uint32_t equal = 0u;
+  for (uint32_t from = 0; from <= n; from += 64u) {
+    const uint32_t i = from + lane;
+    const float v = i < n ? static_cast<float>(reinterpret_cast<const T*>(raw)[i]) : i == n ? single : -INFINITY;
+    const bool largest = v == t.m;
+    const float w = largest ? 0.0f : weigh(v, t.m, c);
+    x.x += w;
+    if constexpr (kTwo) x.x1 += kSquared ? w * w : largest ? 0.0f : weigh(v, t.m, c1);
+    equal += static_cast<uint32_t>(__popcll(__ballot(largest)));
+  }
+  x.x = wave_sum(x.x) + static_cast<float>(equal - 1u);
+  if constexpr (kTwo) x.x1 = wave_sum(x.x1) + static_cast<float>(equal - 1u);
+  return x;
+}
+
+// The same in every thread.  Holds one barrier, which callers rely on.
+struct Joined {
+  Sums t;
+  Others x;
+};
+template <Third kThird, bool kSquared, typename T, uint32_t kThreads, uint32_t kVectors>
+__device__ __forceinline__ Joined block_join(const Held<T, kThreads, kVectors>& held, const Sums& own, float c, float c1, JoinShared<kThreads, kVectors>& lds) {
+  constexpr uint32_t kWaves = kThreads / 64u;
+  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
+  auto others = [](const Sums& t) { return Others{t.s - 1.0f, t.e - 1.0f}; };
+  Joined j;
+  j.t = wave_join<kThird>(own, c, c1);
+  j.x = others_wanted<kThird>(j.t) ? others_of<kThird, kSquared>(held, own, j.t, c, c1, lds.raw[wave]) : others(j.t);
+  if (kWaves > 1 && lane == 0u) {
+    float(&to)[5] = lds.sums[wave];
+    to[0] = j.t.m, to[1] = j.t.s, to[2] = j.t.e, to[3] = j.x.x, to[4] = j.x.x1;
+  }
+  __syncthreads();
+  if constexpr (kWaves > 1) {
+    Sums of = kNothing;
+    Others x{};
+    if (lane < kWaves) {
+      const float(&from)[5] = lds.sums[lane];
+      of = Sums{from[0], from[1], from[2]};
+      x = Others{from[3], from[4]};
+    }
+    j.t = wave_join<kThird>(of, c, c1);
+    j.x = others_wanted<kThird>(j.t) ? others_join<kThird>(of, x, j.t, c, c1) : others(j.t);
+  }
+  return j;
 }
 
 // ---------------------------------------------------------------- the top alternatives of a segment
@@ -443,39 +526,6 @@ __device__ __forceinline__ void put_scores(const ScoreArgs& A, uint32_t r, const
   }
 }
 
-// A row whose largest logit has nearly all the weight has S = 1 + x with a small x, of which fp32 keeps little beside the 1, and its log probability is
-// -ln(1 + x).  Up to this S, x is added up by itself.
-constexpr float kNearlyOne = 1.25f;
-__device__ __forceinline__ float log_of_sum(float s, float x) { return s >= 1.0f && s < kNearlyOne ? log1pf(x) : kLn2 * log2_of(s); }
-
-// The weights of all logits but one of the largest, t.m; the same in every thread.  Only the thread that holds that one has the loss: it adds its own up again.
-// join: what block_join left (three floats a wave); lds: a float a wave.  Holds a barrier.
-template <uint32_t kThreads, typename H>
-__device__ __forceinline__ float others_of(const H& held, const Sums& own, const Sums& t, float c, const float* join, float* lds) {
-  const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
-  uint32_t holder = 0u;
-  while (holder + 1u < kThreads / 64u && join[3u * holder] != t.m) ++holder;
-  float x = rebased<Third::kNone>(own, t.m, c, 0.0f).s;
-  if (wave == uniform(holder)) {
-    const uint32_t first = static_cast<uint32_t>(__ffsll(__ballot(own.m == t.m)) - 1);
-    float rest = 0.0f, equal = 0.0f;
-    auto add = [&](float v) __attribute__((always_inline)) {
-      rest += v == t.m ? 0.0f : weigh(v, t.m, c);
-      equal += v == t.m ? 1.0f : 0.0f;
-    };
-    add(held.single);
-    held.each([&](uint32_t, const float (&v)[H::kElems]) __attribute__((always_inline)) {
-#pragma unroll
-      for (uint32_t j = 0; j < H::kElems; ++j) add(v[j]);
-    });
-    if (lane == first) x = rest + (equal - 1.0f);
-  }
-  x = wave_sum(x);
-  if (lane == 0u) lds[wave] = x;
-  __syncthreads();
-  return wave_sum(lane < kThreads / 64u ? lds[lane] : 0.0f);
-}
-
 template <typename T>
 __device__ __forceinline__ const T* row_of(const void* p, int64_t stride, uint32_t r) {
   return static_cast<const T*>(p) + static_cast<int64_t>(r) * stride;
@@ -484,7 +534,7 @@ __device__ __forceinline__ const T* row_of(const void* p, int64_t stride, uint32
 // A workgroup a segment.  One segment a row: its results; several: its sums and its top entries for score_join_kernel.
 template <typename T, uint32_t kThreads, uint32_t kVectors>
 __global__ void __launch_bounds__(kThreads) score_kernel(ScoreArgs A, SplitArgs P) {
-  __shared__ float lds[3 * kThreads / 64u], lds_others[kThreads / 64u];
+  __shared__ JoinShared<kThreads, kVectors> lds;
   __shared__ TopShared<kThreads> top;
   const uint32_t r = blockIdx.x / P.segments, segment = blockIdx.x - r * P.segments;
   const uint32_t first = segment * P.length, n = min(A.vocab - first, P.length);
@@ -498,22 +548,20 @@ __global__ void __launch_bounds__(kThreads) score_kernel(ScoreArgs A, SplitArgs 
   const float at_target = P.segments == 1u && threadIdx.x == 0u ? static_cast<float>(z[target]) : 0.0f;
   const Sums own = sums_of<Third::kEntropy, false>(held, A.scale, 0.0f);
   const uint32_t k = min(A.top, n), line = k > 0u ? put_line<kThreads>(held, own.m, k, top) : 0u;
-  const Sums raw = block_join<Third::kEntropy, kThreads / 64u>(own, A.scale, 0.0f, lds);
-  float x = raw.s - 1.0f;
-  if (raw.s >= 1.0f && raw.s < kNearlyOne) x = others_of<kThreads>(held, own, raw, A.scale, lds, lds_others);
-  const Sums t = spoiled(raw);
+  const Joined raw = block_join<Third::kEntropy, false>(held, own, A.scale, 0.0f, lds);
+  const Sums t = spoiled(raw.t);
   if (P.segments == 1u) {
-    const float log_sum = log_of_sum(t.s, x);
+    const float log_sum = log_of_sum(t.s, raw.x.x);
     if (threadIdx.x == 0u) put_scores(A, r, t, log_sum, at_target);
     if (k > 0u)
       top_of<T, kThreads>(held, z, own.m, line, t.s != t.s, k, 0u, top, [&](uint32_t rank, uint64_t e) { put_alternative(A, r, rank, e, t, log_sum); });
   } else {
     if (threadIdx.x == 0u) {
       float* to = P.sums + 4ull * blockIdx.x;
-      to[0] = raw.m;
-      to[1] = raw.s;
-      to[2] = raw.e;
-      to[3] = x;
+      to[0] = raw.t.m;
+      to[1] = raw.t.s;
+      to[2] = raw.t.e;
+      to[3] = raw.x.x;
     }
     if (k > 0u)
       top_of<T, kThreads>(held, z + first, own.m, line, t.s != t.s, k, first, top,
@@ -544,10 +592,7 @@ __global__ void __launch_bounds__(kJoinThreads) score_join_kernel(ScoreArgs A, S
   const uint32_t all = (P.segments - 1u) * A.top + min(A.top, last);
   for (uint32_t i = threadIdx.x; i < all; i += kJoinThreads) entries[i] = P.entries[static_cast<uint64_t>(r) * P.segments * A.top + i];
   const Sums t = spoiled(wave_join<Third::kEntropy>(own, A.scale, 0.0f));
-  // the first segment that has the largest logit counts without it
-  const unsigned long long holders = __ballot(own.m == t.m);
-  x = wave_sum(holders != 0ull && lane == static_cast<uint32_t>(__ffsll(holders) - 1) ? x : rebased<Third::kNone>(own, t.m, A.scale, 0.0f).s);
-  const float log_sum = log_of_sum(t.s, x);
+  const float log_sum = log_of_sum(t.s, others_join<Third::kEntropy>(own, Others{x, 0.0f}, t, A.scale, 0.0f).x);
   if (threadIdx.x == 0u) put_scores(A, r, t, log_sum, at_target);
   __syncthreads();
   if (all <= 2u * kJoinThreads) {
@@ -632,9 +677,11 @@ __global__ void __launch_bounds__(kGradThreads) score_grad_kernel(ScoreGradArgs 
 // A row's teacher entries and label, made by the first wave.
 constexpr uint32_t kSeenBits = 65536;
 struct Teacher {
-  int32_t at[kTopMost + 1];             // an index, once; the label's last unless it is one of the others; -1: none
-  float off[kTopMost + 1], z[kTopMost + 1];      // what is subtracted there, and the student's logit
-  float soft;                           // sum of the weights q: 0 if there are none
+  int32_t at[kTopMost + 1];             // k entries, an index once, and the label's unless it is one of them; -1: none
+  float q[kTopMost + 1], z[kTopMost + 1];        // the teacher's probability there, and the student's logit
+  float soft;                           // sum of the weights: 0 if there are none
+  int32_t heavy;                        // the index of nearly all of the teacher's probability, -1: none; and the others' probability
+  float rest;
   alignas(16) uint32_t seen[kSeenBits / 32u];
 };
 
@@ -706,35 +753,61 @@ __device__ __forceinline__ TeacherLane teach(const DistillArgs& A, uint32_t r, i
       }
     }
   }
+  // What is made of 1 - q where q is nearly one is made of the others' weights.
+  int32_t heavy = -1;
+  float rest = 0.0f;
+  const unsigned long long heavy0 = __ballot(t.q[0] > 1.0f / kNearlyOne), heavy1 = __ballot(t.q[1] > 1.0f / kNearlyOne);
+  if ((heavy0 | heavy1) != 0ull) {
+    heavy = heavy0 != 0ull ? __builtin_amdgcn_readlane(t.at[0], __ffsll(heavy0) - 1) : __builtin_amdgcn_readlane(t.at[1], __ffsll(heavy1) - 1);
+    rest = wave_sum((t.at[0] == heavy ? 0.0f : w[0]) + (t.at[1] == heavy ? 0.0f : w[1])) / sum;
+#pragma unroll
+    for (uint32_t u = 0; u < 2u; ++u)
+      if (t.at[u] == heavy) t.log_q[u] = log1p_of(-rest);
+  }
   const bool label_listed = label >= 0 && __any(t.at[0] == label || t.at[1] == label);
-  const float soft = A.soft_weight * A.temperature;
 #pragma unroll
   for (uint32_t u = 0; u < 2u; ++u) {
     const uint32_t i = lane + 64u * u;
+    if (i >= A.k) continue;
     to.at[i] = again[u] ? -1 : t.at[u];
-    to.off[i] = soft * t.q[u] + (t.at[u] >= 0 && t.at[u] == label ? A.label_weight : 0.0f);
+    to.q[i] = t.q[u];
     to.z[i] = t.z[u];
   }
   if (lane == 0u) {
-    to.at[kTopMost] = label_listed ? -1 : label;
-    to.off[kTopMost] = A.label_weight;
-    to.z[kTopMost] = t.at_label;
+    to.at[A.k] = label_listed ? -1 : label;
+    to.q[A.k] = 0.0f;
+    to.z[A.k] = t.at_label;
     to.soft = sum;
+    to.heavy = heavy;
+    to.rest = rest;
   }
   return t;
 }
 
-// The row's loss, by the first wave.  t: the sums at temperature T (m, s), s1 the sum at 1.
-__device__ __forceinline__ void put_loss(const DistillArgs& A, uint32_t r, const TeacherLane& l, bool softened, bool labelled, const Sums& t, float s1) {
+// A row's sums as loss and gradient need them, at temperature T and at 1.
+struct Softmaxes {
+  float m, s, s1;
+  Others others;
+  __device__ __forceinline__ float log_s() const { return log_of_sum(s, others.x); }
+  __device__ __forceinline__ float log_s1() const { return log_of_sum(s1, others.x1); }
+};
+template <Temperatures kTemps>
+__device__ __forceinline__ Softmaxes softmaxes_of(const Sums& t, const Others& x) {
+  if constexpr (kTemps == Temperatures::kOne) return Softmaxes{t.m, t.s, t.s, Others{x.x, x.x}};
+  return Softmaxes{t.m, t.s, t.e, x};
+}
+
+// The row's loss, by the first wave.
+__device__ __forceinline__ void put_loss(const DistillArgs& A, uint32_t r, const TeacherLane& l, bool softened, bool labelled, const Softmaxes& t) {
   float part = 0.0f;
-  const float log_sum = kLn2 * log2_of(t.s);
+  const float log_s = t.log_s();
 #pragma unroll
   for (uint32_t u = 0; u < 2u; ++u)
-    if (softened && l.at[u] >= 0 && !(l.q[u] == 0.0f)) part += l.q[u] * (l.log_q[u] - log_probability(l.z[u], t.m, A.inv_t, log_sum));
+    if (softened && l.at[u] >= 0 && !(l.q[u] == 0.0f)) part += l.q[u] * (l.log_q[u] - log_probability(l.z[u], t.m, A.inv_t, log_s));
   part = wave_sum(part);
   if (threadIdx.x == 0u) {
     float loss = softened ? A.soft_weight * A.temperature * A.temperature * part : 0.0f;
-    if (labelled) loss -= A.label_weight * log_probability(l.at_label, t.m, 1.0f, kLn2 * log2_of(s1));
+    if (labelled) loss -= A.label_weight * log_probability(l.at_label, t.m, 1.0f, t.log_s1());
     A.loss[r] = loss;
   }
 }
@@ -743,9 +816,9 @@ __device__ __forceinline__ void put_loss(const DistillArgs& A, uint32_t r, const
 template <Temperatures kTemps>
 struct Slope {
   float base, c, c1, a, b;
-  __device__ __forceinline__ Slope(const DistillArgs& A, const Sums& t, float s1, bool softened, bool labelled, float g) : base(base_of(t.m)), c(A.scale), c1(A.other_scale) {
+  __device__ __forceinline__ Slope(const DistillArgs& A, const Softmaxes& t, bool softened, bool labelled, float g) : base(base_of(t.m)), c(A.scale), c1(A.other_scale) {
     const float soft = softened && !(t.s == 0.0f) ? g * A.soft_weight * A.temperature / t.s : 0.0f;
-    const float label = labelled && !(s1 == 0.0f) ? g * A.label_weight / s1 : 0.0f;
+    const float label = labelled && !(t.s1 == 0.0f) ? g * A.label_weight / t.s1 : 0.0f;
     a = kTemps == Temperatures::kOne ? soft + label : soft;
     b = label;
   }
@@ -756,6 +829,19 @@ struct Slope {
     return __fmaf_rn(b, exp2_of(d * c1), a * w);
   }
 };
+
+// The whole gradient at the label, and where the teacher has nearly all of its probability.  Of a probability near 1 fp32 keeps little beside the 1:
+// 1 - p of a largest logit is the others' weights over the sum (of any other p is a half at most), and p^T - q is (1 - q) - (1 - p^T).
+template <Temperatures kTemps>
+__device__ __forceinline__ float slope_at(const DistillArgs& A, const Softmaxes& t, const Teacher& teacher, uint32_t i, int32_t label, bool softened, float g) {
+  const float z = teacher.z[i], d = z - base_of(t.m), w = exp2_of(d * A.scale);
+  const float w1 = kTemps == Temperatures::kOne ? w : kTemps == Temperatures::kSquared ? w * w : exp2_of(d * A.other_scale);
+  const bool largest = z == t.m && !(t.s == 0.0f);
+  const float of_s = t.s == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(t.s), of_s1 = t.s1 == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(t.s1);
+  const float p = w * of_s, p1 = w1 * of_s1, not_p = largest ? t.others.x * of_s : 1.0f - p, not_p1 = largest ? t.others.x1 * of_s1 : 1.0f - p1;
+  const float soft = teacher.at[i] == teacher.heavy ? teacher.rest - not_p : p - teacher.q[i], hard = teacher.at[i] == label ? -not_p1 : p1;
+  return (softened ? g * A.soft_weight * A.temperature * soft : 0.0f) + (label >= 0 ? g * A.label_weight * hard : 0.0f);
+}
 
 template <typename T, uint32_t kThreads, uint32_t kVectors>
 __device__ __forceinline__ void fill_zeros(T* dz, uint32_t n) {
@@ -768,8 +854,11 @@ __device__ __forceinline__ void fill_zeros(T* dz, uint32_t n) {
 
 // The gradient of a held segment; then the entries of the teacher and the label over what was stored for them, each by the wave that
 // stored it (a wave's stores to one address are done in order).
-template <typename T, uint32_t kThreads, uint32_t kVectors, typename S>
-__device__ __forceinline__ void put_gradient(const Held<T, kThreads, kVectors>& held, T* dz, uint32_t first, const Teacher& teacher, const S& slope, float g) {
+template <Temperatures kTemps, typename T, uint32_t kThreads, uint32_t kVectors>
+__device__ __forceinline__ void put_gradient(const DistillArgs& A, const Held<T, kThreads, kVectors>& held, T* dz, uint32_t first, const Teacher& teacher, const Softmaxes& t,
+                                             int32_t label, bool softened, float g) {
+  const Slope<kTemps> slope(A, t, softened, label >= 0, g);
+  const float of_teacher = softened ? g * A.soft_weight * A.temperature : 0.0f;
   using V = Vector<T>;
   held.each([&](uint32_t i, const float (&v)[V::kElems]) __attribute__((always_inline)) {
     float d[V::kElems];
@@ -780,12 +869,21 @@ __device__ __forceinline__ void put_gradient(const Held<T, kThreads, kVectors>& 
   if (held.has_single()) dz[held.single_index()] = static_cast<T>(slope(held.single));
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
   __builtin_amdgcn_wave_barrier();
-  for (uint32_t i = threadIdx.x & 63u; i <= kTopMost; i += 64u) {
+  for (uint32_t i = threadIdx.x & 63u; i <= A.k; i += 64u) {
     const uint32_t at = static_cast<uint32_t>(teacher.at[i]) - first;
     if (teacher.at[i] < 0 || at >= held.n) continue;
     if (held.owner(at) / 64u != threadIdx.x / 64u) continue;
-    dz[at] = static_cast<T>(slope(teacher.z[i]) - g * teacher.off[i]);
+    float d;
+    if (teacher.at[i] == label || teacher.at[i] == teacher.heavy) d = slope_at<kTemps>(A, t, teacher, i, label, softened, g);
+    else d = slope(teacher.z[i]) - of_teacher * teacher.q[i];
+    dz[at] = static_cast<T>(d);
   }
+}
+
+// The row's label, -1: none.
+__device__ __forceinline__ int32_t label_of(const DistillArgs& A, uint32_t r) {
+  const int32_t target = A.targets ? A.targets[r] : -1;
+  return is_token(target, A.vocab) ? target : -1;
 }
 
 template <Temperatures kTemps, typename H>
@@ -799,13 +897,13 @@ constexpr Third third_of() { return kTemps == Temperatures::kOne ? Third::kNone 
 // A workgroup a row: loss and gradient.
 template <typename T, uint32_t kThreads, uint32_t kVectors, Temperatures kTemps>
 __global__ void __launch_bounds__(kThreads) distill_kernel(DistillArgs A) {
-  __shared__ float lds[3 * kThreads / 64u];
+  __shared__ JoinShared<kThreads, kVectors> lds;
   __shared__ Teacher teacher;
   const uint32_t r = blockIdx.x;
   const T* z = row_of<T>(A.logits, A.row_stride, r);
   T* dz = static_cast<T*>(A.grad_logits) + static_cast<int64_t>(r) * A.grad_row_stride;
-  const int32_t target = A.targets ? A.targets[r] : -1;
-  const bool labelled = is_token(target, A.vocab);
+  const int32_t label = label_of(A, r);
+  const bool labelled = label >= 0;
   if (!labelled && A.k == 0u) {
     if (threadIdx.x == 0u && A.loss) A.loss[r] = 0.0f;
     if (A.grad_logits) fill_zeros<T, kThreads, kVectors>(dz, A.vocab);
@@ -814,25 +912,25 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(DistillArgs A) {
   const Held<T, kThreads, kVectors> held(z, A.vocab);
   const float g = A.grad_loss ? A.grad_loss[r] : 1.0f;
   TeacherLane lane{};
-  if (threadIdx.x < 64u) lane = teach(A, r, labelled ? target : -1, [&](uint32_t, int32_t i) { return static_cast<float>(z[i]); }, teacher);
-  const Sums t = spoiled(block_join<third_of<kTemps>(), kThreads / 64u>(distill_sums<kTemps>(held, A), A.scale, A.other_scale, lds));
-  const float s1 = kTemps == Temperatures::kOne ? t.s : t.e;
+  if (threadIdx.x < 64u) lane = teach(A, r, label, [&](uint32_t, int32_t i) { return static_cast<float>(z[i]); }, teacher);
+  const Joined raw = block_join<third_of<kTemps>(), kTemps == Temperatures::kSquared>(held, distill_sums<kTemps>(held, A), A.scale, A.other_scale, lds);
+  const Softmaxes t = softmaxes_of<kTemps>(spoiled(raw.t), raw.x);
   const bool softened = A.k > 0u && !(teacher.soft == 0.0f);
-  if (A.loss && threadIdx.x < 64u) put_loss(A, r, lane, softened, labelled, t, s1);
+  if (A.loss && threadIdx.x < 64u) put_loss(A, r, lane, softened, labelled, t);
   if (!A.grad_logits) return;
   if (!softened && !labelled) fill_zeros<T, kThreads, kVectors>(dz, A.vocab);
-  else put_gradient(held, dz, 0u, teacher, Slope<kTemps>(A, t, s1, softened, labelled, g), g);
+  else put_gradient<kTemps>(A, held, dz, 0u, teacher, t, label, softened, g);
 }
 
 // Rows of several segments: the sums of each (and, by a row's first, the student's logits that the loss and the entries need, before
 // a gradient can take their place), then the gradient of each with all of them.
 template <typename T, uint32_t kThreads, uint32_t kVectors, Temperatures kTemps>
 __global__ void __launch_bounds__(kThreads) distill_sums_kernel(DistillArgs A, SplitArgs P) {
-  __shared__ float lds[3 * kThreads / 64u];
+  __shared__ JoinShared<kThreads, kVectors> lds;
   const uint32_t r = blockIdx.x / P.segments, segment = blockIdx.x - r * P.segments;
   const uint32_t first = segment * P.length, n = min(A.vocab - first, P.length);
   const T* z = row_of<T>(A.logits, A.row_stride, r);
-  const int32_t target = A.targets ? A.targets[r] : -1;
+  const int32_t label = label_of(A, r);
   const Held<T, kThreads, kVectors> held(z + first, n);
   if (segment == 0u && threadIdx.x < 64u) {
     float* to = P.logits + static_cast<uint64_t>(r) * (kTopMost + 1u);
@@ -840,14 +938,16 @@ __global__ void __launch_bounds__(kThreads) distill_sums_kernel(DistillArgs A, S
       const int32_t at = A.teacher_idx[static_cast<uint64_t>(r) * A.k + i];
       if (is_token(at, A.vocab)) to[i] = static_cast<float>(z[at]);
     }
-    if (threadIdx.x == 0u && is_token(target, A.vocab)) to[kTopMost] = static_cast<float>(z[target]);
+    if (threadIdx.x == 0u && label >= 0) to[kTopMost] = static_cast<float>(z[label]);
   }
-  const Sums t = block_join<third_of<kTemps>(), kThreads / 64u>(distill_sums<kTemps>(held, A), A.scale, A.other_scale, lds);
+  const Joined raw = block_join<third_of<kTemps>(), kTemps == Temperatures::kSquared>(held, distill_sums<kTemps>(held, A), A.scale, A.other_scale, lds);
   if (threadIdx.x == 0u) {
-    float* to = P.sums + 4ull * blockIdx.x;
-    to[0] = t.m;
-    to[1] = t.s;
-    to[2] = t.e;
+    float* to = P.sums + kDistillSums * blockIdx.x;
+    to[0] = raw.t.m;
+    to[1] = raw.t.s;
+    to[2] = raw.t.e;
+    to[3] = raw.x.x;
+    to[4] = raw.x.x1;
   }
 }
 
@@ -858,26 +958,29 @@ __global__ void __launch_bounds__(kThreads) distill_gradient_kernel(DistillArgs 
   const uint32_t first = segment * P.length, n = min(A.vocab - first, P.length);
   const T* z = row_of<T>(A.logits, A.row_stride, r) + first;
   T* dz = static_cast<T*>(A.grad_logits) + static_cast<int64_t>(r) * A.grad_row_stride + first;
-  const int32_t target = A.targets ? A.targets[r] : -1;
-  const bool labelled = is_token(target, A.vocab);
+  const int32_t label = label_of(A, r);
+  const bool labelled = label >= 0;
   const Held<T, kThreads, kVectors> held(z, A.grad_logits ? n : 0u);
   const float g = A.grad_loss ? A.grad_loss[r] : 1.0f;
   Sums own = kNothing;
+  Others x{};
   if (lane_id < P.segments) {
-    const float* from = P.sums + 4ull * (static_cast<uint64_t>(r) * P.segments + lane_id);
+    const float* from = P.sums + kDistillSums * (static_cast<uint64_t>(r) * P.segments + lane_id);
     own = Sums{from[0], from[1], from[2]};
+    x = Others{from[3], from[4]};
   }
-  const Sums t = spoiled(wave_join<third_of<kTemps>()>(own, A.scale, A.other_scale));
-  const float s1 = kTemps == Temperatures::kOne ? t.s : t.e;
+  const Sums raw = wave_join<third_of<kTemps>()>(own, A.scale, A.other_scale);
+  x = others_wanted<third_of<kTemps>()>(raw) ? others_join<third_of<kTemps>()>(own, x, raw, A.scale, A.other_scale) : Others{raw.s - 1.0f, raw.e - 1.0f};
+  const Softmaxes t = softmaxes_of<kTemps>(spoiled(raw), x);
   TeacherLane lane{};
   const float* kept = P.logits + static_cast<uint64_t>(r) * (kTopMost + 1u);
-  if (threadIdx.x < 64u) lane = teach(A, r, labelled ? target : -1, [&](uint32_t i, int32_t) { return kept[i]; }, teacher);
+  if (threadIdx.x < 64u) lane = teach(A, r, label, [&](uint32_t i, int32_t) { return kept[i]; }, teacher);
   __syncthreads();
   const bool softened = A.k > 0u && !(teacher.soft == 0.0f);
-  if (A.loss && segment == 0u && threadIdx.x < 64u) put_loss(A, r, lane, softened, labelled, t, s1);
+  if (A.loss && segment == 0u && threadIdx.x < 64u) put_loss(A, r, lane, softened, labelled, t);
   if (!A.grad_logits) return;
   if (!softened && !labelled) fill_zeros<T, kThreads, kVectors>(dz, n);
-  else put_gradient(held, dz, first, teacher, Slope<kTemps>(A, t, s1, softened, labelled, g), g);
+  else put_gradient<kTemps>(A, held, dz, first, teacher, t, label, softened, g);
 }
 
 // ---------------------------------------------------------------- launches
