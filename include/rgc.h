@@ -266,8 +266,9 @@ int rgc_last_error(rgc_ctx* ctx, void* hip_stream);
  * sequence may be strided; the innermost dimension is contiguous.  Tensors hold one of three types; sums, softmax
  * statistics and states are fp32 throughout, and each result is rounded to its type once.  The results do not depend on
  * scheduling, and nothing is kept from one call for the next except scratch of the context (grown at the first call that needs
- * more: after one eager call of the same sizes the calls may be captured into a HIP graph).  The tensors of one call must not
- * overlap except where stated.  Errors of all of them (nothing is enqueued): RGC_EINVAL, RGC_ENOMEM, RGC_EHIP. */
+ * more: after one eager call of the same sizes the calls may be captured into a HIP graph).  Calls on one context, graphs
+ * recorded with it among them, share that scratch: ones that overlap on the device, which the caller has to rule out (see the
+ * top of this file), end, with wrong results or NaN.  The tensors of one call must not overlap except where stated.  Errors of all of them (nothing is enqueued): RGC_EINVAL, RGC_ENOMEM, RGC_EHIP. */
 #define RGC_F32  0
 #define RGC_BF16 1
 #define RGC_F16  2

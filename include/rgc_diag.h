@@ -24,6 +24,11 @@ int rgc_poison_hints(rgc_ctx* ctx, int mode, void* hip_stream);
  * the cap (after a device synchronisation). */
 int rgc_limit_optional_scratch(rgc_ctx* ctx, int64_t max_bytes);
 
+/* A workgroup of a long recurrence looks for what the workgroups before it publish at most `looks` times (>= 1; negative: the library's own
+ * limit, which is seconds), and goes on with NaN where it has not come by then.  With the library's own limit that happens only where
+ * the words are lost, because calls on one context overlap (see rgc.h).  For the test that such a wait ends. */
+int rgc_limit_looks(rgc_ctx* ctx, int32_t looks);
+
 /* Runs a one-workgroup kernel that checks the wave64 primitives the kernels rely on (DPP
  * prefix scan, ballot ranks) against values computed on the host.  Synchronises `hip_stream`.
  * Returns RGC_OK, RGC_EINTERNAL on a mismatch, or RGC_EHIP. */

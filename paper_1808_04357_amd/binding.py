@@ -41,7 +41,7 @@ EXPORTS = ["rgc_create", "rgc_destroy", "rgc_k_for_density", "rgc_compress_layer
            "rgc_compress_layers_threshold",
            "rgc_token_logprobs", "rgc_token_logprobs_backward", "rgc_distill_loss", "rgc_gated_recurrence",
            "rgc_gated_recurrence_backward",
-           "rgc_decompress_accumulate", "rgc_reset_hints", "rgc_poison_hints", "rgc_limit_optional_scratch", "rgc_selftest",
+           "rgc_decompress_accumulate", "rgc_reset_hints", "rgc_poison_hints", "rgc_limit_optional_scratch", "rgc_limit_looks", "rgc_selftest",
            "rgc_last_paths", "rgc_last_stats", "rgc_last_error", "rgc_decompress_status", "rgc_profile_enable", "rgc_profile_read", "rgc_stream_yardstick", "rgc_strerror"]
 
 
@@ -159,6 +159,8 @@ def load_library() -> ctypes.CDLL:
                                                 ctypes.POINTER(rgc_recurrence_grads), ctypes.c_void_p]
     L.rgc_reset_hints.restype = ctypes.c_int
     L.rgc_reset_hints.argtypes = [ctypes.c_void_p]
+    L.rgc_limit_looks.restype = ctypes.c_int
+    L.rgc_limit_looks.argtypes = [ctypes.c_void_p, ctypes.c_int32]
     L.rgc_limit_optional_scratch.restype = ctypes.c_int
     L.rgc_limit_optional_scratch.argtypes = [ctypes.c_void_p, ctypes.c_int64]
     L.rgc_poison_hints.restype = ctypes.c_int
@@ -233,6 +235,9 @@ class Context:
 
     def limit_optional_scratch(self, max_bytes: int) -> None:
         _check(self._lib.rgc_limit_optional_scratch(self._h, int(max_bytes)))
+
+    def limit_looks(self, looks: int) -> None:
+        _check(self._lib.rgc_limit_looks(self._h, int(looks)))
 
     def poison_hints(self, mode: int, stream=None) -> None:
         _check(self._lib.rgc_poison_hints(self._h, int(mode), _stream(stream)))

@@ -264,6 +264,7 @@ struct rgc_ctx {
   // the context goes, for a graph that was recorded with one writes to it whenever it is replayed.
   DevBuf<unsigned long long> d_lm[kLmBuffers];
   int lm_buffers = 0;
+  uint32_t lm_looks = kMostLooks;
   CompressPlan plans[kPlanCache];
   uint64_t tick = 0;
   int64_t optional_scratch_cap = -1;       // bytes the dense layers' lists may take (diagnostics); negative: no cap
@@ -627,6 +628,12 @@ int rgc_limit_optional_scratch(rgc_ctx* ctx, int64_t max_bytes) {
     ctx->d_slots_u.release();
     ctx->d_members2.release();
   }
+  return RGC_OK;
+}
+
+int rgc_limit_looks(rgc_ctx* ctx, int32_t looks) {
+  if (!ctx || looks == 0) return RGC_EINVAL;
+  ctx->lm_looks = looks < 0 ? kMostLooks : static_cast<uint32_t>(looks);
   return RGC_OK;
 }
 
@@ -1505,7 +1512,7 @@ int rgc_gated_recurrence(rgc_ctx* ctx, const rgc_recurrence* r, void* hip_stream
   unsigned long long* scratch = nullptr;
   const int rc = lm_scratch(ctx, recurrence_scratch_words(A, r->dtype, false), &scratch);
   if (rc != RGC_OK) return rc;
-  RGC_HIP(launch_recurrence(A, r->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
+  RGC_HIP(launch_recurrence(A, r->dtype, scratch, ctx->lm_looks, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 
@@ -1530,7 +1537,7 @@ int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* r, const r
   unsigned long long* scratch = nullptr;
   const int rc = lm_scratch(ctx, recurrence_scratch_words(A, r->dtype, true), &scratch);
   if (rc != RGC_OK) return rc;
-  RGC_HIP(launch_recurrence_backward(A, G, r->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
+  RGC_HIP(launch_recurrence_backward(A, G, r->dtype, scratch, ctx->lm_looks, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 

@@ -89,11 +89,15 @@ struct RecurrenceGradArgs {
   float* dh0;
 };
 
+// Looks of a few hundred nanoseconds each: seconds, where a tile in its turn waits for microseconds.
+constexpr uint32_t kMostLooks = 1u << 23;
+
 // How a recurrence is cut into tiles (workgroups), and what they tell each other.
 struct TileArgs {
   uint32_t across, tiles;        // chains a sequence has (stretches of channels), tiles a chain has
   uint32_t groups;               // groups of tiles with another behind them
   unsigned long long* words;     // [chains][tiles, then groups][channels of a tile]
+  uint32_t looks;                // how many times a tile looks for a word at most
   uint32_t* ticket;
 };
 
@@ -102,7 +106,7 @@ hipError_t launch_token_logprobs_backward(const ScoreGradArgs& a, int dtype, hip
 hipError_t launch_distill(const DistillArgs& a, int dtype, const SplitArgs& p, hipStream_t s);
 bool recurrence_fits_grid(const RecurrenceArgs& a, int dtype, bool backward);
 uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backward);      // 64-bit words of `scratch`
-hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, hipStream_t s);
-hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s);
+hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, uint32_t looks, hipStream_t s);
+hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, unsigned long long* scratch, uint32_t looks, hipStream_t s);
 
 }  // namespace rgc

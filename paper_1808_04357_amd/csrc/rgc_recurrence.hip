@@ -182,6 +182,7 @@ __device__ __forceinline__ Place take_place(const RecurrenceArgs& A, const TileA
   Place p;
   p.order = ticket / chains;
   p.chain = ticket - p.order * chains;
+  if (kChained) p.order = min(p.order, G.tiles - 1u);                // (a ticket may be anything where another call has written over it, see settle)
   p.b = p.chain / G.across;
   p.block = p.chain - p.b * G.across;
   return p;
@@ -209,15 +210,24 @@ __device__ __forceinline__ Words<kVec> ask(const unsigned long long* w) {
   for (int i = 0; i < kVec; ++i) r.v[i] = __hip_atomic_load(w + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return r;
 }
-// Asks again until they are published.
 template <int kVec>
-__device__ __forceinline__ void settle(Words<kVec>& r, const unsigned long long* w, Stretch* to) {
+__device__ __forceinline__ Words<kVec> lost_words() {
+  Words<kVec> r;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) r.v[i] = kLost;
+  return r;
+}
+// Asks again until they are published.  They are, unless another call on the same context runs at the same time, which the caller is to rule out, and clears them; then
+// the kernel ends all the same, with NaN.
+template <int kVec>
+__device__ __forceinline__ void settle(const TileArgs& G, Words<kVec>& r, const unsigned long long* w, Stretch* to) {
 #pragma unroll
   for (int i = 0; i < kVec; ++i) {
-    while (r.v[i] == kUnset) {
+    for (uint32_t looks = 1u; __any(r.v[i] == kUnset) && looks < G.looks; ++looks) {
       __builtin_amdgcn_s_sleep(1);
-      r.v[i] = __hip_atomic_load(w + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (r.v[i] == kUnset) r.v[i] = __hip_atomic_load(w + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+    if (r.v[i] == kUnset) r.v[i] = kLost;
     to[i] = stretch_of(r.v[i]);
   }
 }
@@ -267,7 +277,7 @@ __device__ __forceinline__ void come_in(const TileArgs& G, const Place& at, uint
     if (wave + j * kWaves < place) tile[j] = ask<kVec>(from + (wave + j * kWaves) * (64u * kVec));
 #pragma unroll
   for (uint32_t j = 0; j < kEach; ++j)
-    if (wave + j * kWaves < place) settle<kVec>(tile[j], from + (wave + j * kWaves) * (64u * kVec), &lds.tiles[wave + j * kWaves][lane * kVec]);
+    if (wave + j * kWaves < place) settle<kVec>(G, tile[j], from + (wave + j * kWaves) * (64u * kVec), &lds.tiles[wave + j * kWaves][lane * kVec]);
   if (ends) {
     __syncthreads();
     if (wave == 0u) {
@@ -282,10 +292,10 @@ __device__ __forceinline__ void come_in(const TileArgs& G, const Place& at, uint
     }
   }
   uint32_t n = 0u;                                                   // groups back to the nearest state
-  for (uint32_t first = 0;;) {
+  for (uint32_t first = 0, looks = 1u;; ++looks) {
     if (first + wave < group) {
       Stretch* to = &lds.groups[first + wave][lane * kVec];
-      settle<kVec>(near, group_at(first), to);
+      settle<kVec>(G, near, group_at(first), to);
       bool open = false;
 #pragma unroll
       for (int i = 0; i < kVec; ++i) open |= !cut(stretch_of(near.v[i]).p);
@@ -302,7 +312,7 @@ __device__ __forceinline__ void come_in(const TileArgs& G, const Place& at, uint
     }
     if (first + kWaves < kKept) first += kWaves;
     else __syncthreads();                                            // (before the same words are replaced)
-    if (first + wave < group) near = ask<kVec>(group_at(first));
+    if (first + wave < group) near = looks < G.looks ? ask<kVec>(group_at(first)) : lost_words<kVec>();
   }
   auto into_group = [&](uint32_t c) { return state_behind<4>(n, [&](uint32_t j) { return lds.groups[j][c]; }); };
   auto into_tile = [&](uint32_t c, float h) { return state_behind<4>(place, [&](uint32_t j) { return lds.tiles[place - 1u - j][c]; }, h); };
@@ -685,9 +695,10 @@ uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backw
   return words ? words + 1u : 0u;
 }
 
-hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, hipStream_t s) {
+hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, uint32_t looks, hipStream_t s) {
   const Cut c = cut_of(a, dtype, false);
   TileArgs G = tiles_of(a, c, false);
+  G.looks = looks;
   const uint32_t wgs = static_cast<uint32_t>(workgroups(a, G));
   const hipError_t e = clear_words(G, words_for(a, c, G), scratch, s);
   if (e != hipSuccess) return e;
@@ -705,9 +716,10 @@ hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long l
   return hipGetLastError();
 }
 
-hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s) {
+hipError_t launch_recurrence_backward(const RecurrenceArgs& a, const RecurrenceGradArgs& g, int dtype, unsigned long long* scratch, uint32_t looks, hipStream_t s) {
   const Cut c = cut_of(a, dtype, true);
   TileArgs G = tiles_of(a, c, true);
+  G.looks = looks;
   const uint32_t wgs = static_cast<uint32_t>(workgroups(a, G));
   const hipError_t e = clear_words(G, words_for(a, c, G), scratch, s);
   if (e != hipSuccess) return e;

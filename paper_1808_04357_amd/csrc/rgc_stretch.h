@@ -23,6 +23,7 @@ constexpr Stretch both(const Stretch& first, const Stretch& second) {
 constexpr Stretch state_of(float h) { return Stretch{-0.0f, h}; }
 
 constexpr uint64_t kUnset = ~0ull;      // a word that is not published yet (its upper half would be a NaN as P, which is never published)
+constexpr uint64_t kLost = 0x800000007FC00000ull;       // in the place of one that never came: the state is a NaN
 
 // A NaN among the gates or states: NaN whatever comes before, and one NaN as good as another.
 constexpr uint64_t word_of(const Stretch& s) {
