@@ -21,7 +21,8 @@ int rgc_poison_hints(rgc_ctx* ctx, int mode, void* hip_stream);
  * their elements (their candidate lists; see rgc.h, "Stream capture"): a call that would need more than
  * `max_bytes` does not ask for it, as if the device were short of memory, and those layers take the
  * hint-free path.  Results do not change.  A negative value lifts the cap.  Frees what is held beyond
- * the cap (after a device synchronisation). */
+ * the cap (after a device synchronisation).  The language model's operators ask for no buffer of more than `max_bytes` either;
+ * a call that needs a larger one than it has returns RGC_ENOMEM (what they hold stays). */
 int rgc_limit_optional_scratch(rgc_ctx* ctx, int64_t max_bytes);
 
 /* A workgroup of a long recurrence looks for what the workgroups before it publish at most `looks` times (>= 1; negative: the library's own

@@ -141,7 +141,7 @@ bool counts_on_long_lists(const rgc_layer* layers, int32_t L, uint64_t total, ui
   return total <= kTiledDenseElems && !tileable(layers, L, kTileSlots) && tileable(layers, L, slots);
 }
 constexpr int kPlanCache = 8;
-constexpr int kLmBuffers = 48;             // each at least twice the one before
+constexpr int kLmBuffers = 48;             // each larger than the one before, twice as large where the device can spare it
 constexpr uint32_t kElectGroupHost = 32;   // = kElectGroup of the kernels (workgroups per election group)
 constexpr int kLaunches = 6;               // streaming pass + at most five phase launches
 
@@ -260,7 +260,7 @@ struct rgc_ctx {
   DevBuf<float> d_slots_u;                 // the velocity of every listed element (first use)
   DevBuf<unsigned long long> d_members2;   // member pool of the dense layers (first use)
   DevBuf<uint32_t> d_shards;               // their sub-list counters (first use)
-  // Scratch of the language model's operators (first use).  A call that needs more gets a buffer at least twice as large; the smaller ones stay until
+  // Scratch of the language model's operators (first use).  A call that needs more gets another buffer (lm_scratch); the smaller ones stay until
   // the context goes, for a graph that was recorded with one writes to it whenever it is replayed.
   DevBuf<unsigned long long> d_lm[kLmBuffers];
   int lm_buffers = 0;
@@ -1355,18 +1355,23 @@ bool recurrence_fits(const rgc_recurrence* r) {
          (!r->out_gate.data || sequence_fits(r->out_gate, r, false));
 }
 
-// Room for `words` in the operators' scratch: *out.
+// Room for `words` in the operators' scratch: *out.  Twice the buffer before, so that calls of growing sizes do not allocate each time, but no more than
+// needed where the device cannot spare that.
 int lm_scratch(rgc_ctx* ctx, uint64_t words, unsigned long long** out) {
   *out = nullptr;
   if (words == 0) return RGC_OK;
   uint64_t have = ctx->lm_buffers > 0 ? ctx->d_lm[ctx->lm_buffers - 1].n : 0;
   if (words > have) {
     if (ctx->lm_buffers >= kLmBuffers) return RGC_ENOMEM;
-    hipError_t e = ctx->d_lm[ctx->lm_buffers].alloc(std::max<uint64_t>(words, 2 * have));
-    if (e == hipErrorOutOfMemory) {
+    auto& buffer = ctx->d_lm[ctx->lm_buffers];
+    hipError_t e = hipErrorOutOfMemory;
+    for (const uint64_t want : {std::max<uint64_t>(words, 2 * have), words}) {
+      const bool capped = ctx->optional_scratch_cap >= 0 && want > static_cast<uint64_t>(ctx->optional_scratch_cap) / sizeof(unsigned long long);
+      e = capped ? hipErrorOutOfMemory : buffer.alloc(want);
+      if (e != hipErrorOutOfMemory) break;
       (void)hipGetLastError();
-      return RGC_ENOMEM;
     }
+    if (e == hipErrorOutOfMemory) return RGC_ENOMEM;
     if (e != hipSuccess) return fail_hip(e, "scratch of the language model's operators");
     ++ctx->lm_buffers;
   }
