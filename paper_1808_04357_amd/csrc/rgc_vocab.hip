@@ -995,15 +995,20 @@ constexpr uint32_t kFewRows = 128, kFewSegments = 2, kWanted = 512, kManyRows = 
 
 // f(shape): of the workgroups that hold `length` logits, the one of fewest threads.  (More alternatives than threads make a poor line: see top_of.)
 // With fewer workgroups than compute units, of sixteen waves: one workgroup's time is all there is.
-template <typename T, typename F>
+// kSegments: for segments as split_of cuts them, of which none is so short or just of that length; the last one holds any.
+template <typename T, bool kSegments = false, typename F>
 void by_length(uint32_t length, uint32_t top, uint64_t workgroups, F&& f) {
-  if (length <= Shape<T, 64, 4>::kCapacity && top <= 64u) f(Shape<T, 64, 4>{});
-  else if (length <= Shape<T, 256, 4>::kCapacity) f(Shape<T, 256, 4>{});
-  else if (length <= Shape<T, 1024, 4>::kCapacity && workgroups <= kFewWorkgroups) f(Shape<T, 1024, 4>{});
-  else if (length <= Shape<T, 256, 8>::kCapacity) f(Shape<T, 256, 8>{});
-  else if (length <= Shape<T, 256, 16>::kCapacity) f(Shape<T, 256, 16>{});
-  else if (length <= Shape<T, 512, 16>::kCapacity) f(Shape<T, 512, 16>{});
-  else f(Shape<T, 1024, 16>{});
+  if constexpr (!kSegments) {
+    if (length <= Shape<T, 64, 4>::kCapacity && top <= 64u) return f(Shape<T, 64, 4>{});
+  }
+  if (length <= Shape<T, 256, 4>::kCapacity) return f(Shape<T, 256, 4>{});
+  if (length <= Shape<T, 1024, 4>::kCapacity && workgroups <= kFewWorkgroups) return f(Shape<T, 1024, 4>{});
+  if (length <= Shape<T, 256, 8>::kCapacity) return f(Shape<T, 256, 8>{});
+  if (length <= Shape<T, 256, 16>::kCapacity) return f(Shape<T, 256, 16>{});
+  if constexpr (!kSegments) {
+    if (length <= Shape<T, 512, 16>::kCapacity) return f(Shape<T, 512, 16>{});
+  }
+  f(Shape<T, 1024, 16>{});
 }
 
 template <typename F>
@@ -1105,7 +1110,7 @@ hipError_t launch_distill(const DistillArgs& all, int dtype, const SplitArgs& P,
     constexpr Temperatures kTemps = decltype(temps)::value;
     by_type(dtype, [&](auto type) {
       using T = decltype(type);
-      by_length<T>(P.length, 0u, uint64_t(all.rows) * P.segments, [&](auto shape) {
+      auto run = [&](auto shape, auto split) {
         using S = decltype(shape);
         const dim3 threads(S::kThreads);
         by_rows(all.rows, static_cast<uint64_t>(S::kThreads) * P.segments, [&](uint64_t first, uint32_t rows) {
@@ -1118,14 +1123,17 @@ hipError_t launch_distill(const DistillArgs& all, int dtype, const SplitArgs& P,
           a.targets = shifted(a.targets, first);
           a.grad_loss = shifted(a.grad_loss, first);
           a.loss = shifted(a.loss, first);
-          if (P.segments == 1u) {
+          if constexpr (!decltype(split)::value) {
             distill_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(rows), threads, 0, s>>>(a);
-          } else if constexpr (S::kThreads == 1024u || S::kThreads == 256u) {       // (as split_of cuts)
+          } else {
             distill_sums_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(rows * P.segments), threads, 0, s>>>(a, P);
             distill_gradient_kernel<T, S::kThreads, S::kVectors, kTemps><<<dim3(rows * P.segments), threads, 0, s>>>(a, P);
           }
         });
-      });
+      };
+      const uint64_t workgroups = uint64_t(all.rows) * P.segments;
+      if (P.segments == 1u) by_length<T>(P.length, 0u, workgroups, [&](auto shape) { run(shape, std::false_type{}); });
+      else by_length<T, true>(P.length, 0u, workgroups, [&](auto shape) { run(shape, std::true_type{}); });
     });
   };
   switch (all.temperatures) {
