@@ -307,7 +307,8 @@ int rgc_token_logprobs(rgc_ctx* ctx, const rgc_token_scores* scores, void* hip_s
  *   dz_j = [ g (1{j = target} - p_j) - h p_j (log p_j + entropy) ] / T,  g = grad_logprob[r], h = grad_entropy[r]
  * for the rows of a forward call with the same descriptor, whose `stats` (and `entropy`, with grad_entropy) it reads.
  * Either of grad_logprob, grad_entropy ([rows], DEVICE) may be NULL: zeros.  Rows left out, and rows of -inf only, get zeros.
- * grad_logits: [rows][vocab] of the logits' type, rows grad_row_stride elements apart; it may be the logits themselves. */
+ * grad_logits: [rows][vocab] of the logits' type, rows grad_row_stride elements apart; it may be the logits themselves
+ * (with their row_stride). */
 int rgc_token_logprobs_backward(rgc_ctx* ctx, const rgc_token_scores* scores, const float* grad_logprob,
                                 const float* grad_entropy, void* grad_logits, int64_t grad_row_stride,
                                 void* hip_stream);
@@ -337,7 +338,8 @@ typedef struct {
   float          label_weight;
   const float*   grad_loss;      /* [rows] or NULL: ones                                           */
   float*         loss;           /* [rows] or NULL                                                 */
-  void*          grad_logits;    /* [rows][vocab] or NULL; may be the logits themselves            */
+  void*          grad_logits;    /* [rows][vocab] or NULL; may be the logits themselves
+                                     (with their row_stride)                                       */
   int64_t        grad_row_stride;
 } rgc_distill;
 

@@ -1318,6 +1318,11 @@ bool rows_fit(const void* data, int64_t rows, int32_t vocab, int64_t row_stride,
   return rows == 0 || (data && aligned_to(data, element_size(dtype)));
 }
 
+// The gradient's rows where the logits are, or elsewhere.  (In their place but further apart or closer together, one row's gradient lies over another's logits.)
+bool grad_fits(const void* grad, int64_t grad_row_stride, const void* logits, int64_t row_stride, int64_t rows, int32_t vocab, int32_t dtype) {
+  return rows_fit(grad, rows, vocab, grad_row_stride, dtype) && (grad != logits || rows <= 1 || grad_row_stride == row_stride);
+}
+
 bool scores_fit(const rgc_token_scores* a) {
   if (!rows_fit(a->logits, a->rows, a->vocab, a->row_stride, a->dtype) || exponent_scale(a->temperature) == 0.0f) return false;
   if (a->top < 0 || a->top > RGC_TOP_MAX || a->top > a->vocab) return false;
@@ -1437,7 +1442,8 @@ int rgc_token_logprobs(rgc_ctx* ctx, const rgc_token_scores* a, void* hip_stream
 int rgc_token_logprobs_backward(rgc_ctx* ctx, const rgc_token_scores* a, const float* grad_logprob,
                                 const float* grad_entropy, void* grad_logits, int64_t grad_row_stride,
                                 void* hip_stream) {
-  if (!ctx || !a || !scores_fit(a) || !rows_fit(grad_logits, a->rows, a->vocab, grad_row_stride, a->dtype)) return RGC_EINVAL;
+  if (!ctx || !a || !scores_fit(a)) return RGC_EINVAL;
+  if (!grad_fits(grad_logits, grad_row_stride, a->logits, a->row_stride, a->rows, a->vocab, a->dtype)) return RGC_EINVAL;
   if (!words_aligned({grad_logprob, grad_entropy})) return RGC_EINVAL;
   if (a->rows == 0) return RGC_OK;
   if (!a->stats || (grad_logprob && !a->targets) || (grad_entropy && !a->entropy)) return RGC_EINVAL;
@@ -1463,7 +1469,7 @@ int rgc_token_logprobs_backward(rgc_ctx* ctx, const rgc_token_scores* a, const f
 
 int rgc_distill_loss(rgc_ctx* ctx, const rgc_distill* a, void* hip_stream) {
   if (!ctx || !a || !rows_fit(a->logits, a->rows, a->vocab, a->row_stride, a->dtype)) return RGC_EINVAL;
-  if (a->grad_logits && !rows_fit(a->grad_logits, a->rows, a->vocab, a->grad_row_stride, a->dtype)) return RGC_EINVAL;
+  if (a->grad_logits && !grad_fits(a->grad_logits, a->grad_row_stride, a->logits, a->row_stride, a->rows, a->vocab, a->dtype)) return RGC_EINVAL;
   if (exponent_scale(a->temperature) == 0.0f || a->k < 0 || a->k > RGC_TOP_MAX) return RGC_EINVAL;
   if (!std::isfinite(a->soft_weight) || !std::isfinite(a->label_weight) || a->soft_weight < 0.0f || a->label_weight < 0.0f) return RGC_EINVAL;
   if (!words_aligned({a->teacher_idx, a->teacher_logits, a->targets, a->grad_loss, a->loss})) return RGC_EINVAL;

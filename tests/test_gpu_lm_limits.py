@@ -76,3 +76,22 @@ def test_gradient_without_targets(rgc, ctx, dtype, vocab):      # noqa: F811
     used, got = plain.run_scores(rgc, ctx, z, dtype, None, 6, 0.5, grads=grads)
     plain.check_scores(used, got, None, dtype, 6, 0.5, grads)
     assert np.all(got["grad"][2] == 0) and np.any(got["grad"][0] != 0)
+
+
+def test_gradient_in_the_logits_place_with_other_rows_is_refused(rgc, ctx):      # noqa: F811
+    """Its rows would lie over other rows' logits."""
+    import torch
+    flat = torch.zeros(4 * 16, device="cuda")
+    logits, closer = flat.view(4, 16)[:, :10], flat.as_strided((4, 10), (10, 1))
+    t, f = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, device="cuda")
+    scores = rgc.TokenScores(logits, t, logprob=f, stats=torch.zeros(4, 2, device="cuda"))
+    idx, val = torch.zeros(4, 3, dtype=torch.int32, device="cuda"), torch.zeros(4, 3, device="cuda")
+    for call in (lambda: rgc.rgc_token_logprobs_backward(ctx, scores, closer, f),
+                 lambda: rgc.rgc_distill_loss(ctx, rgc.Distillation(logits, idx, val, grad_logits=closer)),
+                 lambda: rgc.rgc_distill_loss(ctx, rgc.Distillation(closer, idx, val, grad_logits=logits))):
+        with pytest.raises(rgc.RgcError) as e:
+            call()
+        assert e.value.status == -1
+    # one row has no stride
+    rgc.rgc_distill_loss(ctx, rgc.Distillation(logits[:1], idx[:1], val[:1], grad_logits=closer[:1]))
+    torch.cuda.synchronize()
