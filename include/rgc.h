@@ -349,6 +349,7 @@ int rgc_distill_loss(rgc_ctx* ctx, const rgc_distill* distill, void* hip_stream)
  *   h_t = f_t * h_{t-1} + (1 - f_t) * x_t,   y_t = o_t * h_t      (o = 1 without out_gate)
  *  - h before the first step is h0 (0 without one); a reset at step t puts 0 in the place of h_{t-1} there, as between texts
  *    packed into one row.
+ *  - A state that is infinite makes the later ones infinite or NaN, until one starts anew.
  *  - Steps at lengths[b] and beyond (lengths are read as at least 0 and at most `steps`) are not looked at; y is 0 there.
  *    h_last is the state after the last step of the row, h0 if it has none.
  * One step (steps == 1) is the serving form: h_last may be h0 itself.

@@ -33,10 +33,13 @@ constexpr uint32_t kOneTile = 128;     // steps of the sequences that are one ti
 constexpr float kLog2e = 1.44269504088896341f;
 
 // How a sequence is cut: the same constants make the tiles and choose the kernel.  What it is bound by: a forward pass moves 4 tensors, a backward one 7, and
-// with 30 and 63 instructions an element the arithmetic takes half of that time.  Forward and backward, us, bf16: 20 x 35 x 1500 with waves of eight steps 5.9 and 8.8, of sixteen
-// 11.4 and 11.1, of four 6.7 and 11.1; 64 x 100 x 1024 in one tile of sixteen waves 18 and 30, in tiles as for long ones 22 and 42.  Long ones forward, one prompt
+// with 29 and 61 instructions an element the arithmetic takes half of that time.  Forward and backward, us, bf16: 20 x 35 x 1500 with waves of eight steps 5.9 and 8.8, of sixteen
+// 11.4 and 11.1, of four 6.7 and 11.1; 64 x 100 x 1024 in one tile of sixteen waves 17 and 28.5, in tiles as for long ones 22 and 42.  Long ones forward, one prompt
 // of 32768 x 1500 and 8 x 4096 x 2048, by waves and steps: 8 x 16 129 and 124, 4 x 16 135 and 134, 16 x 8 142 and 154, 8 x 8 149 and 138, 16 x 16 143 and 147 (one or two channels a
-// lane as the registers allow; four channels a lane 240 and 174).  Backward, 16 x 16 (a kept state begins every tile): 234, 4.0 TB/s.
+// lane as the registers allow; four channels a lane 240 and 174), all with the stretches joined as come_in says of earlier; 8 x 16 now 123 and 122.  Backward, 16 x 16 (a kept
+// state begins every tile): 235, 4.0 TB/s.
+// With an output gate the long kernels of 16 bits have no registers left: of 128 a lane the forward one spills 12 to 14, the backward one 11 (7 in fp32); without a gate
+// they have 115 and 114, in fp32 forward 75.
 struct Shape {
   uint32_t waves, steps;           // waves a workgroup, steps a wave
   constexpr uint32_t tile() const { return waves * steps; }

@@ -445,9 +445,9 @@ __device__ __forceinline__ void top_of(const H& held, const T* z, float t, uint3
   if (!spoilt) {
     const uint32_t line = lowest_line<kThreads>(lds);
     const float least = line <= 0x007FFFFFu ? -INFINITY : logit_of(line);      // (below the order of -inf all are taken)
-    // Eight bits a vector, then places in the list for all of a thread's: their indices alone, the few logits are read again below.  (With 8192 rows of 32000, 96 us
-    // without alternatives: 121 with k = 8, 139 with k = 64.  Writing each where it is met 128 and 177, asking the whole wave about every element of a
-    // vector that has one 135 and 190; what needs the packed registers a second time takes 50 more registers a thread, and a third of the workgroups.)
+    // Eight bits a vector, then places in the list for all of a thread's: their indices alone, the few logits are read again below.  (With 8192 rows of 32000, 91 us
+    // without alternatives: 108 with k = 8, 122 with k = 64.  When these were 96, 121 and 139: writing each where it is met 128 and 177, asking the whole wave about
+    // every element of a vector that has one 135 and 190; what needs the packed registers a second time takes 50 more registers a thread, and a third of the workgroups.)
     constexpr uint32_t kVectors = sizeof(held.raw) / sizeof(held.raw[0]), kHitWords = (kVectors + 3u) / 4u;
     uint32_t hits[kHitWords] = {}, n = held.has_single() && held.single >= least ? 1u : 0u;
     held.each([&](uint32_t i, const float (&v)[H::kElems]) __attribute__((always_inline)) {
@@ -1021,12 +1021,13 @@ void by_type(int dtype, F&& f) {
 }  // namespace
 
 // How rows are cut, by what was measured (us; one segment / several).  The launch that joins them takes 3.
-//  - Few rows of many logits: as many segments as give every compute unit two workgroups.  48 rows of 131072 with 20 alternatives 24.3 / 17.1, 4 such 21.4 / 19.2,
-//    64 of 50257 few of whose words are allowed 45.3 / 23.8; 200 of 50257 take 16.8 either way and stay whole.
+//  - Few rows of many logits: as many segments as give every compute unit two workgroups.  48 rows of 131072 with 20 alternatives 20.3 / 15.7, 4 such 18.9 / 18.3,
+//    64 of 50257 few of whose words are allowed 43.3 / 22.3; 200 of 50257 take 14.2, in two 16.5, and stay whole.
 //  - Scores of rows of three workgroups of four waves and more: these, for five of them share a compute unit and one's selection is hidden behind the others' reads.
-//    1000 rows of 100003 with 20 alternatives 81.5 / 59.4, without 55.9 / 44.0, 300 of 131072 45.3 / 32.2.  Of two, where there are alternatives and many rows: 6001 of
-//    50257 155 / 140, 4096 of 32000 in fp32 113 / 104 (without alternatives 91 / 99), but 700 of 33278 22.6 / 23.5.
-//  - A gradient after the sums reads its row again if it does not hold it: one segment, as long as a workgroup holds the row.
+//    1000 rows of 100003 with 20 alternatives 76.2 / 53.8, without 50.7 / 41.4, 300 of 131072 42.4 / 28.6.  Of two, where there are alternatives and many rows: 6001 of
+//    50257 140 / 123, 4096 of 32000 in fp32 108 / 99 (without alternatives 87 / 95), but 700 of 33278 19.8 / 21.0.
+//  - A gradient after the sums reads its row again if it does not hold it: one segment, as long as a workgroup holds the row.  (2048 rows of 131072 bf16 220, of 151936, which
+//    none holds, 357; the floors are 211 and 245.)
 SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype, Use use, uint32_t top) {
   SplitArgs P{};
   const uint32_t of = dtype == 0 ? 1u : 2u;                          // capacities: Shape<T, 256, 8>, <T, 256, 16> and <T, 1024, 16>
