@@ -8,39 +8,34 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librgc.so")
+OBJECTS = os.path.join(HERE, "_build")
 SOURCES = ["rgc_api.cpp", "rgc_compress.hip", "rgc_decompress.hip", "rgc_threshold.hip", "rgc_yardstick.hip",
            "rgc_vocab.hip", "rgc_recurrence.hip"]
 HEADERS = ["rgc_internal.h", "rgc_device.h", "rgc_exact.h", "rgc_tickets.h", "rgc_tiles.h", "rgc_lm.h", "rgc_stretch.h", os.path.join("..", "..", "include", "rgc.h"),
            os.path.join("..", "..", "include", "rgc_diag.h")]
 
 FLAGS = [
-    "-O3", "-std=c++17", "-fPIC", "-shared", "--offload-arch=gfx950",
+    "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
     "-ffp-contract=off",                       # the oracle is built the same way: no silent fma
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-Wall", "-Wno-unused-function",
 ]
 
 
+def _newest(paths) -> float:
+    return max(os.path.getmtime(os.path.join(CSRC, f)) for f in paths)
+
+
 def needs_build() -> bool:
-    if not os.path.exists(LIB):
-        return True
-    t = os.path.getmtime(LIB)
-    for f in SOURCES + HEADERS:
-        if os.path.getmtime(os.path.join(CSRC, f)) > t:
-            return True
-    return False
+    return not os.path.exists(LIB) or _newest(SOURCES + HEADERS) > os.path.getmtime(LIB)
 
 
-def build(force: bool = True, verbose: bool = False) -> str:
-    if not force and not needs_build():
-        return LIB
-    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    extra = os.environ.get("RGC_EXTRA_FLAGS", "").split()      # tuning experiments only
-    cmd = [hipcc] + FLAGS + extra + ["-x", "hip"] + [os.path.join(CSRC, s) for s in SOURCES] + ["-o", LIB]
+def _run(cmd, verbose: bool) -> None:
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -50,10 +45,30 @@ def build(force: bool = True, verbose: bool = False) -> str:
         raise RuntimeError("hipcc failed:\n" + out)
     if verbose and out.strip():
         print(out)
+
+
+def build(force: bool = True, verbose: bool = False) -> str:
+    """Compiles the sources side by side and links them.  Without `force`: those only that changed since their object was made."""
+    if not force and not needs_build():
+        return LIB
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    extra = os.environ.get("RGC_EXTRA_FLAGS", "").split()      # tuning experiments only
+    os.makedirs(OBJECTS, exist_ok=True)
+
+    def compile_one(source: str) -> str:
+        target = os.path.join(OBJECTS, source + (".extra.o" if extra else ".o"))
+        if force or extra or not os.path.exists(target) or _newest([source] + HEADERS) > os.path.getmtime(target):
+            _run([hipcc] + FLAGS + extra + ["-x", "hip", "-c", os.path.join(CSRC, source), "-o", target], verbose)
+        return target
+
+    jobs = int(os.environ.get("MAX_JOBS", 0)) or min(16, os.cpu_count() or 1)
+    with ThreadPoolExecutor(jobs) as pool:
+        objects = list(pool.map(compile_one, SOURCES))
+    _run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950"] + objects + ["-o", LIB], verbose)
     return LIB
 
 
 if __name__ == "__main__":
-    build(force=True, verbose=True)
+    build(force="--changed" not in sys.argv[1:], verbose=True)
     print("built", LIB)
     sys.exit(0)
