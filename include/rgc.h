@@ -262,7 +262,7 @@ int rgc_last_error(rgc_ctx* ctx, void* hip_stream);
 
 /* ---- the language model's own operators ----------------------------------------------------
  * What the step of a recurrent language model (the paper's LSTM workloads) runs around the compression of its gradients:
- * the recurrent layer, the loss, and the scoring of tokens, each with its gradient.  Rows of logits and steps of a
+ * the embedding, the recurrent layer, the loss, and the scoring of tokens, each with its gradient.  Rows of logits and steps of a
  * sequence may be strided; the innermost dimension is contiguous.  Tensors hold one of three types; sums, softmax
  * statistics and states are fp32 throughout, and each result is rounded to its type once.  The results do not depend on
  * scheduling, and nothing is kept from one call for the next except scratch of the context (grown at the first call that needs
@@ -392,6 +392,34 @@ typedef struct {
 
 int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* recurrence, const rgc_recurrence_grads* grads,
                                   void* hip_stream);
+
+/* Rows of an embedding table, scaled:  out[r] = scale * table[tokens[r]], rounded to its type once.
+ * A token outside [0, vocab) is left out: its row is 0, and no row of the table is looked at for it.  A token may come as often as it likes.
+ * Limits: 0 <= rows < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 1 <= width <= RGC_EMBEDDING_WIDTH_MAX; strides not negative, that of out at least width. */
+#define RGC_EMBEDDING_WIDTH_MAX 1048576
+
+typedef struct {
+  const void*    table;        /* [vocab][width], row v at table + v * table_stride elements        */
+  int64_t        table_stride;
+  int32_t        vocab, width;
+  int32_t        table_dtype;  /* RGC_F32, RGC_BF16, RGC_F16                                        */
+  int32_t        dtype;        /* of out and of its gradient                                        */
+  const int32_t* tokens;       /* [rows]                                                            */
+  int64_t        rows;
+  float          scale;
+  void*          out;          /* [rows][width], row r at out + r * out_stride elements             */
+  int64_t        out_stride;
+} rgc_embedding;
+
+int rgc_embed_tokens(rgc_ctx* ctx, const rgc_embedding* embedding, void* hip_stream);
+
+/* The table's gradient, dense, as compression takes it:  s[v] = scale * sum of dout[r] over the rows whose token is v,
+ *   RGC_OVERWRITE : dtable = s (0 where a token does not occur);   RGC_ADD_TO_DST: dtable = dtable + s
+ * table and out are not read.  Rows left out have no part in it, whatever dout holds there.  The order of a sum's additions is made of the tokens alone: the
+ * same tokens give the same result to the last bit.  dout: [rows][width] of `dtype`, rows dout_stride elements apart; dtable: [vocab][width].
+ * flags: exactly one of the two. */
+int rgc_embed_tokens_backward(rgc_ctx* ctx, const rgc_embedding* embedding, const void* dout, int64_t dout_stride,
+                              float* dtable, uint32_t flags, void* hip_stream);
 
 /* Text for a status code; for RGC_EHIP the text of the last HIP error seen by this thread. */
 const char* rgc_strerror(int status);

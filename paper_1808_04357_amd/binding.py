@@ -94,6 +94,12 @@ class rgc_recurrence_grads(ctypes.Structure):
                 ("dh_last", ctypes.c_void_p), ("dh0", ctypes.c_void_p)]
 
 
+class rgc_embedding(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("vocab", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("table_dtype", ctypes.c_int32), ("dtype", ctypes.c_int32), ("tokens", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -157,6 +163,11 @@ def load_library() -> ctypes.CDLL:
     L.rgc_gated_recurrence_backward.restype = ctypes.c_int
     L.rgc_gated_recurrence_backward.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_recurrence),
                                                 ctypes.POINTER(rgc_recurrence_grads), ctypes.c_void_p]
+    L.rgc_embed_tokens.restype = ctypes.c_int
+    L.rgc_embed_tokens.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_embedding), ctypes.c_void_p]
+    L.rgc_embed_tokens_backward.restype = ctypes.c_int
+    L.rgc_embed_tokens_backward.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_embedding), ctypes.c_void_p, ctypes.c_int64,
+                                            ctypes.c_void_p, ctypes.c_uint32, ctypes.c_void_p]
     L.rgc_reset_hints.restype = ctypes.c_int
     L.rgc_reset_hints.argtypes = [ctypes.c_void_p]
     L.rgc_limit_looks.restype = ctypes.c_int
@@ -540,3 +551,40 @@ def rgc_gated_recurrence(ctx: Context, recurrence: Recurrence, stream=None) -> N
 
 def rgc_gated_recurrence_backward(ctx: Context, recurrence: Recurrence, grads: RecurrenceGrads, stream=None) -> None:
     _check(load_library().rgc_gated_recurrence_backward(ctx.handle, recurrence._ref, grads._ref, _stream(stream)))
+
+
+def _table(t, name: str) -> int:
+    """Row stride of a [rows, width] tensor whose channels are contiguous."""
+    _require(t.dim() == 2 and str(t.dtype) in _DTYPES, "%s: a [rows, width] tensor of float32, bfloat16 or float16 expected" % name)
+    _require(t.shape[1] >= 1 and (t.shape[1] == 1 or t.stride(1) == 1), "%s: the channels must be contiguous" % name)
+    return int(t.stride(0)) if t.shape[0] > 1 else max(int(t.stride(0)), int(t.shape[1]))
+
+
+class Embedding:
+    """A host ``rgc_embedding`` built once from tensors (keeps them alive).  table: [vocab, width], rows strided as they may be; tokens: int32
+    [rows]; out: [rows, width] of any of the three types, rows strided as they may be."""
+
+    def __init__(self, table, tokens, out, scale: float = 1.0):
+        a = self.desc = rgc_embedding()
+        a.table_stride, a.out_stride = _table(table, "table"), _table(out, "out")
+        rows, width = (int(n) for n in out.shape)
+        _require(int(table.shape[1]) == width and table.device == out.device, "out: width and device of the table expected")
+        a.table, a.vocab, a.width, a.table_dtype = _ptr(table), int(table.shape[0]), width, _DTYPES[str(table.dtype)]
+        a.out, a.rows, a.dtype = _ptr(out), rows, _DTYPES[str(out.dtype)]
+        a.tokens = _plain(tokens, "tokens", (rows,), "int32", table)
+        a.scale = float(scale)
+        self.table, self.out = table, out
+        self._keep = (table, tokens, out)
+        self._ref = ctypes.byref(a)
+
+
+def rgc_embed_tokens(ctx: Context, embedding: Embedding, stream=None) -> None:
+    _check(load_library().rgc_embed_tokens(ctx.handle, embedding._ref, _stream(stream)))
+
+
+def rgc_embed_tokens_backward(ctx: Context, embedding: Embedding, dout, dtable, flags: int = RGC_OVERWRITE, stream=None) -> None:
+    """dout: like the embedding's out; dtable: float32 [vocab, width]."""
+    stride, out = _table(dout, "dout"), embedding.out
+    _require(dout.shape == out.shape and dout.dtype == out.dtype and dout.device == out.device, "dout: shape, type and device of out expected")
+    to = _plain(dtable, "dtable", (embedding.desc.vocab, embedding.desc.width), "float32", out)
+    _check(load_library().rgc_embed_tokens_backward(ctx.handle, embedding._ref, _ptr(dout), stride, to, int(flags), _stream(stream)))

@@ -1403,6 +1403,33 @@ RecurrenceArgs recurrence_args(const rgc_recurrence* r) {
   return A;
 }
 
+bool dtype_fits(int32_t dtype) { return dtype >= RGC_F32 && dtype <= RGC_F16; }
+
+bool embedding_fits(const rgc_embedding* a) {
+  if (a->rows < 0 || a->rows > kInt32Most || a->vocab < 1 || a->vocab > RGC_VOCAB_MAX || a->width < 1 || a->width > RGC_EMBEDDING_WIDTH_MAX) return false;
+  if (!dtype_fits(a->table_dtype) || !dtype_fits(a->dtype) || !std::isfinite(a->scale)) return false;
+  return words_aligned({a->tokens}) && (a->rows == 0 || a->tokens);
+}
+
+// n rows that lie `stride` elements apart.
+bool table_rows_fit(const void* data, int64_t stride, int64_t n, int32_t dtype) {
+  return data && aligned_to(data, element_size(dtype)) && stride >= 0 && stride <= (int64_t(1) << 44) / std::max<int64_t>(n, 1);
+}
+
+EmbedArgs embed_args(const rgc_embedding* a) {
+  EmbedArgs A{};
+  A.table = a->table;
+  A.table_stride = a->table_stride;
+  A.vocab = static_cast<uint32_t>(a->vocab);
+  A.width = static_cast<uint32_t>(a->width);
+  A.tokens = a->tokens;
+  A.rows = static_cast<uint32_t>(a->rows);
+  A.scale = a->scale;
+  A.out = a->out;
+  A.out_stride = a->out_stride;
+  return A;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1549,6 +1576,34 @@ int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* r, const r
   const int rc = lm_scratch(ctx, recurrence_scratch_words(A, r->dtype, true), &scratch);
   if (rc != RGC_OK) return rc;
   RGC_HIP(launch_recurrence_backward(A, G, r->dtype, scratch, ctx->lm_looks, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_embed_tokens(rgc_ctx* ctx, const rgc_embedding* a, void* hip_stream) {
+  if (!ctx || !a || !embedding_fits(a)) return RGC_EINVAL;
+  if (a->rows > 0 && !table_rows_fit(a->table, a->table_stride, a->vocab, a->table_dtype)) return RGC_EINVAL;
+  if (a->rows > 0 && (!table_rows_fit(a->out, a->out_stride, a->rows, a->dtype) || (a->rows > 1 && a->out_stride < a->width))) return RGC_EINVAL;
+  if (a->rows == 0) return RGC_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  RGC_HIP(launch_embed(embed_args(a), a->table_dtype, a->dtype, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_embed_tokens_backward(rgc_ctx* ctx, const rgc_embedding* a, const void* dout, int64_t dout_stride,
+                              float* dtable, uint32_t flags, void* hip_stream) {
+  if (!ctx || !a || !embedding_fits(a) || !dtable || !words_aligned({dtable})) return RGC_EINVAL;
+  if (flags != RGC_OVERWRITE && flags != RGC_ADD_TO_DST) return RGC_EINVAL;
+  if (a->rows > 0 && !table_rows_fit(dout, dout_stride, a->rows, a->dtype)) return RGC_EINVAL;
+  if (a->rows == 0 && flags == RGC_ADD_TO_DST) return RGC_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  const EmbedArgs A = embed_args(a);
+  const EmbedGradArgs G{dout, dout_stride, dtable, flags == RGC_ADD_TO_DST ? 1u : 0u};
+  unsigned long long* scratch = nullptr;
+  const int rc = lm_scratch(ctx, embed_scratch_words(A), &scratch);
+  if (rc != RGC_OK) return rc;
+  RGC_HIP(launch_embed_backward(A, G, a->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 

@@ -1,4 +1,4 @@
-// Arguments of the language-model operators' kernels (rgc_vocab.hip, rgc_recurrence.hip), as the host side fills them.
+// Arguments of the language-model operators' kernels (rgc_vocab.hip, rgc_recurrence.hip, rgc_embed.hip), as the host side fills them.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -68,6 +68,24 @@ constexpr uint64_t kDistillSums = 6;
 enum class Use { kScores, kDistillation };
 SplitArgs split_of(uint32_t rows, uint32_t vocab, int dtype, Use use, uint32_t top);
 
+struct EmbedArgs {
+  const void* table;
+  int64_t table_stride;
+  uint32_t vocab, width;
+  const int32_t* tokens;
+  uint32_t rows;
+  float scale;
+  void* out;
+  int64_t out_stride;
+};
+
+struct EmbedGradArgs {
+  const void* dout;
+  int64_t dout_stride;
+  float* dtable;
+  uint32_t add;              // dtable += instead of =
+};
+
 struct SequenceView {
   void* data;
   int64_t batch_stride, step_stride;
@@ -104,6 +122,9 @@ struct TileArgs {
 hipError_t launch_token_logprobs(const ScoreArgs& a, int dtype, const SplitArgs& p, hipStream_t s);
 hipError_t launch_token_logprobs_backward(const ScoreGradArgs& a, int dtype, hipStream_t s);
 hipError_t launch_distill(const DistillArgs& a, int dtype, const SplitArgs& p, hipStream_t s);
+hipError_t launch_embed(const EmbedArgs& a, int table_dtype, int dtype, hipStream_t s);
+uint64_t embed_scratch_words(const EmbedArgs& a);
+hipError_t launch_embed_backward(const EmbedArgs& a, const EmbedGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s);
 bool recurrence_fits_grid(const RecurrenceArgs& a, int dtype, bool backward);
 uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backward);      // 64-bit words of `scratch`
 hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, uint32_t looks, hipStream_t s);

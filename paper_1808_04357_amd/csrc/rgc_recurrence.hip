@@ -23,6 +23,7 @@
 #include <type_traits>
 
 #include "rgc_lm.h"
+#include "rgc_sequence.h"
 #include "rgc_stretch.h"
 
 namespace rgc {
@@ -30,7 +31,6 @@ namespace {
 
 constexpr uint32_t kChunk = 256;       // steps between kept states (RGC_RECURRENCE_CHUNK)
 constexpr uint32_t kOneTile = 128;     // steps of the sequences that are one tile (kMiddle below)
-constexpr float kLog2e = 1.44269504088896341f;
 
 // How a sequence is cut: the same constants make the tiles and choose the kernel.  What it is bound by: a forward pass moves 4 tensors, a backward one 7, and
 // with 29 and 61 instructions an element the arithmetic takes half of that time.  Forward and backward, us, bf16: 20 x 35 x 1500 with waves of eight steps 5.9 and 8.8, of sixteen
@@ -52,59 +52,6 @@ constexpr bool chained(uint32_t waves, uint32_t steps) {
   return (waves == kLong.waves && steps == kLong.steps) || (waves == kLongBackward.waves && steps == kLongBackward.steps);
 }
 
-// sigmoid(v) and sigmoid(-v) with one power and one reciprocal.  Below -87 the power may be infinite, and infinity times 0 is not 1.
-// (Written so that a NaN passes.)
-__device__ __forceinline__ void gate_of(float v, float& keep, float& take) {
-  const float x = -kLog2e * v;
-  const float e = __builtin_amdgcn_exp2f(x);
-  keep = __builtin_amdgcn_rcpf(1.0f + e);
-  take = x > 126.0f ? 1.0f : e * keep;
-}
-
-// kVec neighbouring channels as they lie in memory (aligned to an element only: rows may start anywhere, and gfx950 reads and
-// writes words at any address).
-typedef uint32_t __attribute__((aligned(2))) word;
-
-template <typename T, int kVec>
-struct alignas(sizeof(T)) Raw {
-  T v[kVec];
-};
-
-// A tensor's rows from a step on: an address that is the same for the whole wave, which a step moves on, and a lane's offset from it.
-template <typename T>
-struct Rows {
-  char* p;
-  int64_t step;                       // bytes
-  __device__ Rows(const SequenceView& v, uint32_t b, uint32_t t)
-      : p(reinterpret_cast<char*>(static_cast<T*>(v.data) + (b * v.batch_stride + t * v.step_stride))), step(v.step_stride * static_cast<int64_t>(sizeof(T))) {}
-};
-
-template <typename T, int kVec>
-__device__ __forceinline__ Raw<T, kVec> read(const char* row, uint32_t offset) {
-  Raw<T, kVec> r;
-  if constexpr (sizeof(T) * kVec == 4) {
-    const uint32_t w = *reinterpret_cast<const word*>(row + offset);
-    __builtin_memcpy(&r, &w, 4);
-  } else {
-    r = *reinterpret_cast<const Raw<T, kVec>*>(row + offset);
-  }
-  return r;
-}
-
-template <typename T, int kVec>
-__device__ __forceinline__ void write(char* row, uint32_t offset, const float (&v)[kVec]) {
-  Raw<T, kVec> r;
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) r.v[i] = static_cast<T>(v[i]);
-  if constexpr (sizeof(T) * kVec == 4) {
-    uint32_t w;
-    __builtin_memcpy(&w, &r, 4);
-    *reinterpret_cast<word*>(row + offset) = w;
-  } else {
-    *reinterpret_cast<Raw<T, kVec>*>(row + offset) = r;
-  }
-}
-
 // A wave's steps of one tensor, all asked for at once.  Steps at `end` and beyond are read as the last one before: a branch around every
 // read makes the compiler wait for one before it asks for the next.
 template <typename T, int kVec, int kSteps, bool kWhole>
@@ -117,40 +64,12 @@ __device__ __forceinline__ void read_steps(Raw<T, kVec> (&to)[kSteps], const Seq
   }
 }
 
-struct Yes {
-  constexpr operator bool() const { return true; }
-};
-struct No {
-  constexpr operator bool() const { return false; }
-};
-
-// Where a lane's channels lie.  The last lane of a row with an odd number of channels takes the two last ones and stores the second only; lanes
-// behind the row's end work on the last channels too, so that all lanes do the same, and store nothing.
-template <int kVec>
-struct Lane {
-  uint32_t c;                 // first channel
-  bool all, last;             // stores all its channels / its last one only
-  __device__ Lane(uint32_t block, uint32_t width) {
-    const uint32_t want = (block * 64u + (threadIdx.x & 63u)) * kVec;
-    all = want + kVec <= width;
-    last = kVec > 1 && !all && want < width;
-    c = all ? want : width - kVec;
-  }
-};
-
-template <typename T, int kVec, bool kWhole>
-__device__ __forceinline__ void store(char* row, const Lane<kVec>& lane, const float (&v)[kVec]) {
-  if (kWhole || lane.all) write<T, kVec>(row, lane.c * static_cast<uint32_t>(sizeof(T)), v);
-  else if (lane.last) reinterpret_cast<T*>(row)[lane.c + kVec - 1] = static_cast<T>(v[kVec - 1]);
-}
 template <int kVec>
 __device__ __forceinline__ void store_state(float* row, const Lane<kVec>& lane, const float (&v)[kVec]) {
 #pragma unroll
   for (int i = 0; i < kVec; ++i)
     if (lane.all || (lane.last && i == kVec - 1)) row[lane.c + i] = v[i];
 }
-
-__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
 
 __device__ __forceinline__ uint32_t length_of(const RecurrenceArgs& A, uint32_t b) {
   if (!A.lengths) return A.steps;
