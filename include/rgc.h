@@ -395,8 +395,8 @@ int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* recurrence
 
 /* Rows of an embedding table, scaled:  out[r] = scale * table[tokens[r]], rounded to its type once.
  * A token outside [0, vocab) is left out: its row is 0, and no row of the table is looked at for it.  A token may come as often as it likes.
- * Limits: 0 <= rows < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 1 <= width <= RGC_EMBEDDING_WIDTH_MAX; strides not negative, that of out at least width. */
-#define RGC_EMBEDDING_WIDTH_MAX 1048576
+ * Limits: 0 <= rows < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 1 <= width <= RGC_WIDTH_MAX; strides not negative, that of out at least width. */
+#define RGC_WIDTH_MAX 1048576
 
 typedef struct {
   const void*    table;        /* [vocab][width], row v at table + v * table_stride elements        */
@@ -420,6 +420,47 @@ int rgc_embed_tokens(rgc_ctx* ctx, const rgc_embedding* embedding, void* hip_str
  * flags: exactly one of the two. */
 int rgc_embed_tokens_backward(rgc_ctx* ctx, const rgc_embedding* embedding, const void* dout, int64_t dout_stride,
                               float* dtable, uint32_t flags, void* hip_stream);
+
+/* Short causal convolution along the steps of sequences, every channel by itself: with K taps
+ *   s_t = bias + sum_j w_j u_{t - K + 1 + j},  j = 0 .. K - 1;   y_t = silu(s_t) = s_t sigmoid(s_t)  (without `silu`: s_t)
+ * u_t is the input x_t.  Before the first step there are the kept inputs `before` (zeros without any); a reset at step t puts zeros in the place of all inputs before t,
+ * for step t and the later ones, as between texts packed into one row.
+ *  - Steps at lengths[b] and beyond (lengths are read as at least 0 and at most `steps`) are not looked at; y is 0 there.
+ *  - `last` takes the K - 1 inputs that end with the row's last step, as the step after it would see them: `before` of the call that goes on from there.
+ * One step (steps == 1) is the serving form: `last` may be `before` itself.
+ * Limits: batch, steps >= 0, both < 2^31; 1 <= width <= RGC_WIDTH_MAX; 1 <= taps <= RGC_TAPS_MAX.  y is not x. */
+#define RGC_TAPS_MAX 8
+
+typedef struct {
+  int64_t        batch, steps;
+  int32_t        width, taps;
+  int32_t        dtype;    /* of x, y, before, last and of their gradients                          */
+  int32_t        silu;     /* 0 or 1                                                                */
+  rgc_sequence   x;        /* read only                                                             */
+  rgc_sequence   y;
+  const float*   weight;   /* [width][taps], the step's own input's last                            */
+  const float*   bias;     /* [width] or NULL                                                       */
+  const int32_t* lengths;  /* [batch] or NULL                                                       */
+  const uint8_t* resets;   /* [batch][steps] or NULL; not zero: a text begins at this step          */
+  const void*    before;   /* [batch][taps - 1][width] or NULL, oldest first                        */
+  void*          last;     /* [batch][taps - 1][width] or NULL                                      */
+} rgc_convolution;
+
+int rgc_causal_convolution(rgc_ctx* ctx, const rgc_convolution* convolution, void* hip_stream);
+
+/* Its backward pass: gradients of x, of the weights and the bias (summed over batch and steps) and of the kept inputs, from those of y and of `last`.
+ * convolution: the descriptor of the forward call; y and last are not read.  Steps beyond a row's length get zeros. */
+typedef struct {
+  rgc_sequence   dy;       /* read only                                                             */
+  rgc_sequence   dx;
+  float*         dweight;  /* [width][taps]                                                         */
+  float*         dbias;    /* [width] or NULL                                                       */
+  const void*    dlast;    /* [batch][taps - 1][width] or NULL: zeros                               */
+  void*          dbefore;  /* [batch][taps - 1][width] or NULL                                      */
+} rgc_convolution_grads;
+
+int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* convolution, const rgc_convolution_grads* grads,
+                                    void* hip_stream);
 
 /* Text for a status code; for RGC_EHIP the text of the last HIP error seen by this thread. */
 const char* rgc_strerror(int status);

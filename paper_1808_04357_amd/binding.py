@@ -100,6 +100,17 @@ class rgc_embedding(ctypes.Structure):
                 ("scale", ctypes.c_float), ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64)]
 
 
+class rgc_convolution(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("steps", ctypes.c_int64), ("width", ctypes.c_int32), ("taps", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("silu", ctypes.c_int32), ("x", rgc_sequence), ("y", rgc_sequence), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("resets", ctypes.c_void_p), ("before", ctypes.c_void_p), ("last", ctypes.c_void_p)]
+
+
+class rgc_convolution_grads(ctypes.Structure):
+    _fields_ = [("dy", rgc_sequence), ("dx", rgc_sequence), ("dweight", ctypes.c_void_p), ("dbias", ctypes.c_void_p), ("dlast", ctypes.c_void_p),
+                ("dbefore", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -168,6 +179,10 @@ def load_library() -> ctypes.CDLL:
     L.rgc_embed_tokens_backward.restype = ctypes.c_int
     L.rgc_embed_tokens_backward.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_embedding), ctypes.c_void_p, ctypes.c_int64,
                                             ctypes.c_void_p, ctypes.c_uint32, ctypes.c_void_p]
+    L.rgc_causal_convolution.restype = ctypes.c_int
+    L.rgc_causal_convolution.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_convolution), ctypes.c_void_p]
+    L.rgc_causal_convolution_backward.restype = ctypes.c_int
+    L.rgc_causal_convolution_backward.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_convolution), ctypes.POINTER(rgc_convolution_grads), ctypes.c_void_p]
     L.rgc_reset_hints.restype = ctypes.c_int
     L.rgc_reset_hints.argtypes = [ctypes.c_void_p]
     L.rgc_limit_looks.restype = ctypes.c_int
@@ -588,3 +603,51 @@ def rgc_embed_tokens_backward(ctx: Context, embedding: Embedding, dout, dtable, 
     _require(dout.shape == out.shape and dout.dtype == out.dtype and dout.device == out.device, "dout: shape, type and device of out expected")
     to = _plain(dtable, "dtable", (embedding.desc.vocab, embedding.desc.width), "float32", out)
     _check(load_library().rgc_embed_tokens_backward(ctx.handle, embedding._ref, _ptr(dout), stride, to, int(flags), _stream(stream)))
+
+
+def _resets(t, shape, like) -> Optional[int]:
+    return _plain(t, "resets", shape, "bool" if str(getattr(t, "dtype", "")) == "torch.bool" else "uint8", like)
+
+
+class Convolution:
+    """A host ``rgc_convolution`` built once from tensors (keeps them alive).  x, y: [batch, steps, width] of one type, the first two dimensions strided
+    as they may be; weight: float32 [width, taps]; bias: float32 [width] or None; lengths: int32 [batch] or None; resets: uint8 or bool
+    [batch, steps] or None; before, last: [batch, taps - 1, width] of x's type or None."""
+
+    def __init__(self, x, weight, y, bias=None, silu: bool = False, lengths=None, resets=None, before=None, last=None):
+        a = self.desc = rgc_convolution()
+        a.x, a.y = _sequence(x, "x"), _sequence(y, "y", x)
+        batch, steps, width = (int(n) for n in x.shape)
+        _require(weight.dim() == 2, "weight: a [width, taps] tensor expected")
+        a.batch, a.steps, a.width, a.taps, a.dtype, a.silu = batch, steps, width, int(weight.shape[1]), _DTYPES[str(x.dtype)], int(bool(silu))
+        a.weight, a.bias = _plain(weight, "weight", (width, a.taps), "float32", x), _plain(bias, "bias", (width,), "float32", x)
+        a.lengths, a.resets = _plain(lengths, "lengths", (batch,), "int32", x), _resets(resets, (batch, steps), x)
+        self.kept, kind = (batch, a.taps - 1, width), str(x.dtype)[len("torch."):]
+        a.before, a.last = _plain(before, "before", self.kept, kind, x), _plain(last, "last", self.kept, kind, x)
+        self.x, self.kind = x, kind
+        self._keep = (x, weight, y, bias, lengths, resets, before, last)
+        self._ref = ctypes.byref(a)
+
+
+class ConvolutionGrads:
+    """A host ``rgc_convolution_grads`` for a Convolution (keeps the tensors alive).  dy, dx: like x; dweight: float32 [width, taps]; dbias: float32 [width]
+    or None; dlast, dbefore: [batch, taps - 1, width] of x's type or None."""
+
+    def __init__(self, convolution: Convolution, dy, dx, dweight, dbias=None, dlast=None, dbefore=None):
+        x, a = convolution.x, rgc_convolution_grads()
+        self.desc = a
+        a.dy, a.dx = _sequence(dy, "dy", x), _sequence(dx, "dx", x)
+        a.dweight = _plain(dweight, "dweight", (x.shape[2], convolution.desc.taps), "float32", x)
+        a.dbias = _plain(dbias, "dbias", (x.shape[2],), "float32", x)
+        a.dlast = _plain(dlast, "dlast", convolution.kept, convolution.kind, x)
+        a.dbefore = _plain(dbefore, "dbefore", convolution.kept, convolution.kind, x)
+        self._keep = (convolution, dy, dx, dweight, dbias, dlast, dbefore)
+        self._ref = ctypes.byref(a)
+
+
+def rgc_causal_convolution(ctx: Context, convolution: Convolution, stream=None) -> None:
+    _check(load_library().rgc_causal_convolution(ctx.handle, convolution._ref, _stream(stream)))
+
+
+def rgc_causal_convolution_backward(ctx: Context, convolution: Convolution, grads: ConvolutionGrads, stream=None) -> None:
+    _check(load_library().rgc_causal_convolution_backward(ctx.handle, convolution._ref, grads._ref, _stream(stream)))

@@ -1331,23 +1331,25 @@ bool scores_fit(const rgc_token_scores* a) {
 }
 
 // A strided sequence; `written`: no two elements of it may be one.
-bool sequence_fits(const rgc_sequence& v, const rgc_recurrence* r, bool written) {
+bool sequence_fits(const rgc_sequence& v, int64_t batch, int64_t steps, int32_t width, int32_t dtype, bool written) {
   constexpr int64_t kMost = int64_t(1) << 44;
-  if (!v.data || !aligned_to(v.data, element_size(r->dtype))) return false;
+  if (!v.data || !aligned_to(v.data, element_size(dtype))) return false;
   if (v.batch_stride < 0 || v.step_stride < 0 || v.batch_stride > kMost || v.step_stride > kMost) return false;
-  if (r->batch > 1 && v.batch_stride > kMost / r->batch) return false;
-  if (r->steps > 1 && v.step_stride > kMost / r->steps) return false;
+  if (batch > 1 && v.batch_stride > kMost / batch) return false;
+  if (steps > 1 && v.step_stride > kMost / steps) return false;
   if (!written) return true;
   const bool by_batch = v.batch_stride >= v.step_stride;
-  const int64_t inner = by_batch ? v.step_stride : v.batch_stride, inner_n = by_batch ? r->steps : r->batch;
-  const int64_t outer = by_batch ? v.batch_stride : v.step_stride, outer_n = by_batch ? r->batch : r->steps;
-  int64_t span = r->width;                             // of the dimensions further in
+  const int64_t inner = by_batch ? v.step_stride : v.batch_stride, inner_n = by_batch ? steps : batch;
+  const int64_t outer = by_batch ? v.batch_stride : v.step_stride, outer_n = by_batch ? batch : steps;
+  int64_t span = width;                                // of the dimensions further in
   if (inner_n > 1) {
     if (inner < span) return false;
     span += inner * (inner_n - 1);
   }
   return outer_n <= 1 || outer >= span;
 }
+bool sequence_fits(const rgc_sequence& v, const rgc_recurrence* r, bool written) { return sequence_fits(v, r->batch, r->steps, r->width, r->dtype, written); }
+bool sequence_fits(const rgc_sequence& v, const rgc_convolution* r, bool written) { return sequence_fits(v, r->batch, r->steps, r->width, r->dtype, written); }
 
 // (steps == 0: only h0 and h_last are there; batch == 0: nothing is)
 bool recurrence_fits(const rgc_recurrence* r) {
@@ -1406,7 +1408,7 @@ RecurrenceArgs recurrence_args(const rgc_recurrence* r) {
 bool dtype_fits(int32_t dtype) { return dtype >= RGC_F32 && dtype <= RGC_F16; }
 
 bool embedding_fits(const rgc_embedding* a) {
-  if (a->rows < 0 || a->rows > kInt32Most || a->vocab < 1 || a->vocab > RGC_VOCAB_MAX || a->width < 1 || a->width > RGC_EMBEDDING_WIDTH_MAX) return false;
+  if (a->rows < 0 || a->rows > kInt32Most || a->vocab < 1 || a->vocab > RGC_VOCAB_MAX || a->width < 1 || a->width > RGC_WIDTH_MAX) return false;
   if (!dtype_fits(a->table_dtype) || !dtype_fits(a->dtype) || !std::isfinite(a->scale)) return false;
   return words_aligned({a->tokens}) && (a->rows == 0 || a->tokens);
 }
@@ -1427,6 +1429,33 @@ EmbedArgs embed_args(const rgc_embedding* a) {
   A.scale = a->scale;
   A.out = a->out;
   A.out_stride = a->out_stride;
+  return A;
+}
+
+// (steps == 0: only the kept inputs are there; batch == 0: nothing is)
+bool convolution_fits(const rgc_convolution* r) {
+  if (r->batch < 0 || r->batch > kInt32Most || r->steps < 0 || r->steps > kInt32Most || r->width < 1 || r->width > RGC_WIDTH_MAX) return false;
+  if (!dtype_fits(r->dtype) || r->taps < 1 || r->taps > RGC_TAPS_MAX || (r->silu & ~1) != 0) return false;
+  if (!r->weight || !words_aligned({r->weight, r->bias, r->lengths})) return false;
+  const size_t size = element_size(r->dtype);
+  if (!aligned_to(r->before, size) || !aligned_to(r->last, size)) return false;
+  return r->batch == 0 || r->steps == 0 || sequence_fits(r->x, r, false);
+}
+
+ConvArgs convolution_args(const rgc_convolution* r) {
+  ConvArgs A{};
+  A.batch = static_cast<uint32_t>(r->batch);
+  A.steps = static_cast<uint32_t>(r->steps);
+  A.width = static_cast<uint32_t>(r->width);
+  A.x = view_of(r->x);
+  A.y = view_of(r->y);
+  A.weight = r->weight;
+  A.bias = r->bias;
+  A.silu = static_cast<uint32_t>(r->silu);
+  A.lengths = r->lengths;
+  A.resets = r->resets;
+  A.before = r->before;
+  A.last = r->last;
   return A;
 }
 
@@ -1604,6 +1633,35 @@ int rgc_embed_tokens_backward(rgc_ctx* ctx, const rgc_embedding* a, const void* 
   const int rc = lm_scratch(ctx, embed_scratch_words(A), &scratch);
   if (rc != RGC_OK) return rc;
   RGC_HIP(launch_embed_backward(A, G, a->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_causal_convolution(rgc_ctx* ctx, const rgc_convolution* r, void* hip_stream) {
+  if (!ctx || !r || !convolution_fits(r)) return RGC_EINVAL;
+  if (r->batch > 0 && r->steps > 0 && (!sequence_fits(r->y, r, true) || r->y.data == r->x.data)) return RGC_EINVAL;
+  if (r->last && r->last == r->before && r->steps > 1 && r->taps > 1) return RGC_EINVAL;
+  if (r->batch == 0) return RGC_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  RGC_HIP(launch_convolution(convolution_args(r), static_cast<uint32_t>(r->taps), r->dtype, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* r, const rgc_convolution_grads* g, void* hip_stream) {
+  if (!ctx || !r || !g || !convolution_fits(r) || !g->dweight || !words_aligned({g->dweight, g->dbias})) return RGC_EINVAL;
+  if (!aligned_to(g->dlast, element_size(r->dtype)) || !aligned_to(g->dbefore, element_size(r->dtype))) return RGC_EINVAL;
+  if (r->batch > 0 && r->steps > 0) {
+    if (!sequence_fits(g->dy, r, false) || !sequence_fits(g->dx, r, true) || g->dx.data == g->dy.data || g->dx.data == r->x.data) return RGC_EINVAL;
+  }
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  const ConvArgs A = convolution_args(r);
+  const ConvGradArgs G{view_of(g->dy), view_of(g->dx), g->dweight, g->dbias, g->dlast, g->dbefore};
+  const uint32_t taps = static_cast<uint32_t>(r->taps);
+  unsigned long long* scratch = nullptr;
+  const int rc = lm_scratch(ctx, convolution_scratch_words(A, taps, r->dtype), &scratch);
+  if (rc != RGC_OK) return rc;
+  RGC_HIP(launch_convolution_backward(A, G, taps, r->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 

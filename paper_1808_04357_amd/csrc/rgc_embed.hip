@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(256) embed_kernel(EmbedArgs A, uint32_t across
     float v[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) v[i] = token < A.vocab ? static_cast<float>(r[j].v[i]) * A.scale : 0.0f;
-    if (lane.mine) write_at<T, kVec>(to + lane.c, v);
+    write_own<T, kVec>(to, lane, v);
   }
 }
 
@@ -206,26 +206,17 @@ __device__ __forceinline__ uint32_t lower_bound(const Pair* sorted, uint32_t row
   return first;
 }
 
-// A row's sums to their place.  (Added to what is there, a channel is its own lane's alone: read again after another lane has stored it, it would have its sum twice.)
+// A row's sums to their place.
 template <int kVec>
 __device__ __forceinline__ void put(float* row, const Channels<kVec>& lane, float (&v)[kVec], float scale, uint32_t add) {
-  if (!lane.mine) return;
 #pragma unroll
   for (int i = 0; i < kVec; ++i) v[i] *= scale;
-  if (lane.c == lane.own) {
-    if (add) {
-      const Raw<float, kVec> old = read_at<float, kVec>(row + lane.c);
+  if (add) {
+    const Raw<float, kVec> old = read_at<float, kVec>(row + lane.c);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) v[i] += old.v[i];
-    }
-    write_at<float, kVec>(row + lane.c, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      if (lane.c + i < lane.own) continue;
-      row[lane.c + i] = add ? row[lane.c + i] + v[i] : v[i];
-    }
+    for (int i = 0; i < kVec; ++i) v[i] += old.v[i];
   }
+  write_own<float, kVec>(row, lane, v);
 }
 
 // Zeros where the table has tokens that do not occur.
@@ -254,7 +245,7 @@ __device__ __forceinline__ void fill(const EmbedArgs& A, const EmbedGradArgs& G,
     for (uint32_t b = 0; b < S.across; ++b) {
       const Channels<kVec> lane(b, A.width);
       const float zero[kVec] = {};
-      if (lane.mine) write_at<float, kVec>(to + lane.c, zero);
+      write_own<float, kVec>(to, lane, zero);
     }
   }
 }
@@ -281,7 +272,7 @@ __global__ void __launch_bounds__(256) sum_kernel(EmbedArgs A, EmbedGradArgs G, 
   auto leave = [&](bool goes_on) {
     if (now >= A.vocab) return;                       // (uniform)
     if (from_before || goes_on) {
-      if (lane.mine) write_at<float, kVec>(S.parts + (static_cast<uint64_t>(segment) * 2u + (from_before ? 0u : 1u)) * A.width + lane.c, sum);
+      write_own<float, kVec>(S.parts + (static_cast<uint64_t>(segment) * 2u + (from_before ? 0u : 1u)) * A.width, lane, sum);
     } else {
       put<kVec>(G.dtable + static_cast<uint64_t>(now) * A.width, lane, sum, A.scale, G.add);
     }
@@ -347,13 +338,6 @@ __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(EmbedArgs A, Embe
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------------- launches
-
-// A grid has fewer than 2^32 threads: more workgroups than that take several launches, each told which its first one is.
-template <typename F>
-void in_grids(uint64_t workgroups, F&& launch) {
-  constexpr uint64_t kMost = uint64_t(1) << 22;
-  for (uint64_t begin = 0; begin < workgroups; begin += kMost) launch(begin, dim3(static_cast<uint32_t>(workgroups - begin < kMost ? workgroups - begin : kMost)));
-}
 
 uint32_t stretches(uint32_t width, uint32_t vec) { return (width + 64u * vec - 1u) / (64u * vec); }
 uint32_t blocks_of(uint32_t rows) { return static_cast<uint32_t>((static_cast<uint64_t>(rows) + kBlock - 1u) / kBlock); }

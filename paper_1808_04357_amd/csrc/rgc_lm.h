@@ -1,4 +1,4 @@
-// Arguments of the language-model operators' kernels (rgc_vocab.hip, rgc_recurrence.hip, rgc_embed.hip), as the host side fills them.
+// Arguments of the language-model operators' kernels (rgc_vocab.hip, rgc_recurrence.hip, rgc_embed.hip, rgc_convolution.hip, rgc_parts.hip), as the host side fills them.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -91,6 +91,34 @@ struct SequenceView {
   int64_t batch_stride, step_stride;
 };
 
+struct ConvArgs {
+  uint32_t batch, steps, width;
+  SequenceView x, y;
+  const float* weight;       // [width][taps]
+  const float* bias;
+  uint32_t silu;
+  const int32_t* lengths;
+  const uint8_t* resets;
+  const void* before;        // [batch][taps - 1][width]
+  void* last;
+};
+
+struct ConvGradArgs {
+  SequenceView dy, dx;
+  float* dweight;
+  float* dbias;
+  const void* dlast;
+  void* dbefore;
+};
+
+// Sums of [count][columns] parts over their rows; the columns are those of up to three outputs, one behind the other (a null one is left out).
+struct PartsArgs {
+  const float* parts;
+  uint64_t count, columns;
+  float* to[3];
+  uint64_t ends[3];          // the column behind each one's last
+};
+
 struct RecurrenceArgs {
   uint32_t batch, steps, width;
   SequenceView x, gate, out_gate, y;
@@ -125,6 +153,10 @@ hipError_t launch_distill(const DistillArgs& a, int dtype, const SplitArgs& p, h
 hipError_t launch_embed(const EmbedArgs& a, int table_dtype, int dtype, hipStream_t s);
 uint64_t embed_scratch_words(const EmbedArgs& a);
 hipError_t launch_embed_backward(const EmbedArgs& a, const EmbedGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s);
+hipError_t launch_sum_parts(const PartsArgs& a, hipStream_t s);
+hipError_t launch_convolution(const ConvArgs& a, uint32_t taps, int dtype, hipStream_t s);
+uint64_t convolution_scratch_words(const ConvArgs& a, uint32_t taps, int dtype);
+hipError_t launch_convolution_backward(const ConvArgs& a, const ConvGradArgs& g, uint32_t taps, int dtype, unsigned long long* scratch, hipStream_t s);
 bool recurrence_fits_grid(const RecurrenceArgs& a, int dtype, bool backward);
 uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backward);      // 64-bit words of `scratch`
 hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, uint32_t looks, hipStream_t s);

@@ -143,7 +143,8 @@ __device__ __forceinline__ void write_at(T* p, const float (&v)[kVec]) {
 }
 
 // Where a lane's kVec channels lie in a row that has at least kVec.  The last lane of a row whose width is no multiple takes the row's last ones, some of which
-// the lane before has too: both come to the same values.  Lanes behind it do as it does (all lanes do the same, so that no branch is needed) and store nothing.
+// the lane before has too, and stores those only that no other lane has (another one's may have been replaced already where a call works in place).  Lanes behind
+// it do as it does, so that all lanes do the same, and store nothing.
 template <int kVec>
 struct Channels {
   uint32_t c, own;             // the first one; the first that no lane before has
@@ -155,7 +156,32 @@ struct Channels {
   }
 };
 
+template <typename T, int kVec>
+__device__ __forceinline__ void write_own(T* row, const Channels<kVec>& lane, const float (&v)[kVec]) {
+  if (lane.c == lane.own) {
+    write_at<T, kVec>(row + lane.c, v);
+  } else if (lane.mine) {
+#pragma unroll
+    for (int i = 1; i < kVec; ++i)
+      if (lane.c + i >= lane.own) row[lane.c + i] = static_cast<T>(v[i]);
+  }
+}
+
+// Steps that a row has.
+__device__ __forceinline__ uint32_t steps_of(const int32_t* lengths, uint32_t b, uint32_t steps) {
+  if (!lengths) return steps;
+  const int32_t n = __builtin_amdgcn_readfirstlane(lengths[b]);
+  return n < 0 ? 0u : min(static_cast<uint32_t>(n), steps);
+}
+
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// A grid has fewer than 2^32 threads: more workgroups (of up to 512 threads) than that take several launches, each told which its first one is.
+template <typename F>
+void in_grids(uint64_t workgroups, F&& launch) {
+  constexpr uint64_t kMost = uint64_t(1) << 22;
+  for (uint64_t begin = 0; begin < workgroups; begin += kMost) launch(begin, dim3(static_cast<uint32_t>(workgroups - begin < kMost ? workgroups - begin : kMost)));
+}
 
 }  // namespace
 }  // namespace rgc
