@@ -262,7 +262,7 @@ int rgc_last_error(rgc_ctx* ctx, void* hip_stream);
 
 /* ---- the language model's own operators ----------------------------------------------------
  * What the step of a recurrent language model (the paper's LSTM workloads) runs around the compression of its gradients:
- * the embedding, the recurrent layer, the loss, and the scoring of tokens, each with its gradient.  Rows of logits and steps of a
+ * the embedding, the recurrent layer (a gated one, or a state space layer with its short convolution), the loss, and the scoring of tokens, each with its gradient.  Rows of logits and steps of a
  * sequence may be strided; the innermost dimension is contiguous.  Tensors hold one of three types; sums, softmax
  * statistics and states are fp32 throughout, and each result is rounded to its type once.  The results do not depend on
  * scheduling, and nothing is kept from one call for the next except scratch of the context (grown at the first call that needs
@@ -461,6 +461,57 @@ typedef struct {
 
 int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* convolution, const rgc_convolution_grads* grads,
                                     void* hip_stream);
+
+/* Selective scan: a state space layer whose step sizes, inputs' and outputs' weights are the sequence's own.  For every sequence and channel c, with N states a channel, z the gate,
+ * B and C those of the channel's group (the channels are `groups` equal groups that follow each other)
+ *   delta_t = softplus(delta[t] + delta_bias)    (without `softplus`: the sum itself; softplus(v) = ln(1 + exp(v)))
+ *   h_t[n] = exp(delta_t a[c][n]) h_{t-1}[n] + delta_t B_t[n] x_t,    y_t = (sum_n C_t[n] h_t[n] + d x_t) silu(z_t)    (silu = 1 without a gate, d = 0 without one)
+ *  - h before the first step is h0 (0 without one); a reset at step t puts 0 in the place of h_{t-1} there, as between texts packed into one row.
+ *  - Steps at lengths[b] and beyond (lengths are read as at least 0 and at most `steps`) are not looked at; y is 0 there.  h_last is the state after the row's last step,
+ *    h0 if it has none.
+ *  - A rate of -inf is read as the lowest finite one.  A state that is infinite or NaN makes the later ones so, until one starts anew.
+ * h_last may be h0 itself; steps == 1 is the serving form.
+ * Limits: batch, steps >= 0, both < 2^31; 1 <= width <= RGC_WIDTH_MAX, a multiple of `groups`; 1 <= states <= RGC_SCAN_STATES_MAX. */
+#define RGC_SCAN_CHUNK 64
+#define RGC_SCAN_STATES_MAX 64
+
+typedef struct {
+  int64_t        batch, steps;
+  int32_t        width, states, groups;
+  int32_t        dtype;      /* of x, delta, gate, b, c, y and of their gradients                     */
+  int32_t        softplus;   /* 0 or 1                                                                */
+  rgc_sequence   x, delta;   /* read only                                                             */
+  rgc_sequence   gate;       /* read only; data == NULL: none                                         */
+  rgc_sequence   b, c;       /* read only, of groups * states channels                                */
+  rgc_sequence   y;
+  const float*   a;          /* [width][states], the rates (negative: decays)                         */
+  const float*   d;          /* [width] or NULL                                                       */
+  const float*   delta_bias; /* [width] or NULL                                                       */
+  const int32_t* lengths;    /* [batch] or NULL                                                       */
+  const uint8_t* resets;     /* [batch][steps] or NULL; not zero: the state starts anew at this step  */
+  const float*   h0;         /* [batch][width][states] or NULL                                        */
+  float*         h_last;     /* [batch][width][states] or NULL                                        */
+  float*         kept;       /* [batch][ceil(steps / RGC_SCAN_CHUNK)][width][states] or NULL: the state before every
+                                RGC_SCAN_CHUNK-th step, for the backward call                         */
+} rgc_scan;
+
+int rgc_selective_scan(rgc_ctx* ctx, const rgc_scan* scan, void* hip_stream);
+
+/* Its backward pass.  scan: the descriptor of the forward call, with `kept` as that call left it; y, h0 and h_last are not read.  Gradients of a, d and delta_bias are
+ * summed over batch and steps, those of B and C over their group's channels, in orders made of the sizes alone.  Steps beyond a row's length get zeros. */
+typedef struct {
+  rgc_sequence   dy;          /* read only                                                            */
+  rgc_sequence   dx, ddelta;
+  rgc_sequence   dgate;       /* with a gate                                                          */
+  rgc_sequence   db, dc;      /* of groups * states channels                                          */
+  float*         da;          /* [width][states]                                                      */
+  float*         dd;          /* [width] or NULL                                                      */
+  float*         ddelta_bias; /* [width] or NULL                                                      */
+  const float*   dh_last;     /* [batch][width][states] or NULL: zeros                                */
+  float*         dh0;         /* [batch][width][states] or NULL                                       */
+} rgc_scan_grads;
+
+int rgc_selective_scan_backward(rgc_ctx* ctx, const rgc_scan* scan, const rgc_scan_grads* grads, void* hip_stream);
 
 /* Text for a status code; for RGC_EHIP the text of the last HIP error seen by this thread. */
 const char* rgc_strerror(int status);

@@ -14,6 +14,7 @@ from .binding import (  # noqa: F401
     rgc_compress_layers_threshold, rgc_decompress_accumulate, rgc_k_for_density, rgc_message_means, rgc_message_means_noalloc, rgc_stream_yardstick,
     RGC_NOALLOC_MAX_LAYERS,
     RGC_BF16, RGC_F16, RGC_F32, RGC_RECURRENCE_CHUNK, RGC_TOP_MAX, Distillation, Recurrence, RecurrenceGrads, TokenScores,
+    RGC_SCAN_CHUNK, RGC_SCAN_STATES_MAX, RGC_TAPS_MAX, Scan, ScanGrads, rgc_selective_scan, rgc_selective_scan_backward,
     Convolution, ConvolutionGrads, rgc_causal_convolution, rgc_causal_convolution_backward,
     Embedding, rgc_embed_tokens, rgc_embed_tokens_backward,
     rgc_distill_loss, rgc_gated_recurrence, rgc_gated_recurrence_backward, rgc_token_logprobs, rgc_token_logprobs_backward,

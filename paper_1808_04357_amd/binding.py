@@ -32,6 +32,9 @@ RGC_BF16 = 1
 RGC_F16 = 2
 RGC_TOP_MAX = 128
 RGC_RECURRENCE_CHUNK = 256
+RGC_SCAN_CHUNK = 64
+RGC_SCAN_STATES_MAX = 64
+RGC_TAPS_MAX = 8
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "librgc.so")
@@ -111,6 +114,18 @@ class rgc_convolution_grads(ctypes.Structure):
                 ("dbefore", ctypes.c_void_p)]
 
 
+class rgc_scan(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("steps", ctypes.c_int64), ("width", ctypes.c_int32), ("states", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("softplus", ctypes.c_int32), ("x", rgc_sequence), ("delta", rgc_sequence), ("gate", rgc_sequence), ("b", rgc_sequence),
+                ("c", rgc_sequence), ("y", rgc_sequence), ("a", ctypes.c_void_p), ("d", ctypes.c_void_p), ("delta_bias", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("resets", ctypes.c_void_p), ("h0", ctypes.c_void_p), ("h_last", ctypes.c_void_p), ("kept", ctypes.c_void_p)]
+
+
+class rgc_scan_grads(ctypes.Structure):
+    _fields_ = [("dy", rgc_sequence), ("dx", rgc_sequence), ("ddelta", rgc_sequence), ("dgate", rgc_sequence), ("db", rgc_sequence), ("dc", rgc_sequence),
+                ("da", ctypes.c_void_p), ("dd", ctypes.c_void_p), ("ddelta_bias", ctypes.c_void_p), ("dh_last", ctypes.c_void_p), ("dh0", ctypes.c_void_p)]
+
+
 _lib = None
 
 
@@ -183,6 +198,10 @@ def load_library() -> ctypes.CDLL:
     L.rgc_causal_convolution.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_convolution), ctypes.c_void_p]
     L.rgc_causal_convolution_backward.restype = ctypes.c_int
     L.rgc_causal_convolution_backward.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_convolution), ctypes.POINTER(rgc_convolution_grads), ctypes.c_void_p]
+    L.rgc_selective_scan.restype = ctypes.c_int
+    L.rgc_selective_scan.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_scan), ctypes.c_void_p]
+    L.rgc_selective_scan_backward.restype = ctypes.c_int
+    L.rgc_selective_scan_backward.argtypes = [ctypes.c_void_p, ctypes.POINTER(rgc_scan), ctypes.POINTER(rgc_scan_grads), ctypes.c_void_p]
     L.rgc_reset_hints.restype = ctypes.c_int
     L.rgc_reset_hints.argtypes = [ctypes.c_void_p]
     L.rgc_limit_looks.restype = ctypes.c_int
@@ -651,3 +670,61 @@ def rgc_causal_convolution(ctx: Context, convolution: Convolution, stream=None) 
 
 def rgc_causal_convolution_backward(ctx: Context, convolution: Convolution, grads: ConvolutionGrads, stream=None) -> None:
     _check(load_library().rgc_causal_convolution_backward(ctx.handle, convolution._ref, grads._ref, _stream(stream)))
+
+
+def _group_sequence(t, name: str, x, channels: int) -> rgc_sequence:
+    """A [batch, steps, channels] tensor of x's type."""
+    s = _sequence(t, name)
+    _require(tuple(t.shape) == tuple(x.shape[:2]) + (channels,) and t.dtype == x.dtype and t.device == x.device,
+             "%s: a [batch, steps, %d] tensor of x's type on its device expected" % (name, channels))
+    return s
+
+
+class Scan:
+    """A host ``rgc_scan`` built once from tensors (keeps them alive).  x, delta, y, gate (or None): [batch, steps, width] of one type; b, c: [batch, steps, groups * N] of that
+    type; the first two dimensions strided as they may be.  a: float32 [width, N]; d, delta_bias: float32 [width] or None; lengths: int32 [batch] or None; resets: uint8 or bool
+    [batch, steps] or None; h0, h_last: float32 [batch, width, N] or None; states: float32 [batch, ceil(steps / RGC_SCAN_CHUNK), width, N], needed for the backward call."""
+
+    def __init__(self, x, delta, a, b, c, y, groups: int = 1, d=None, gate=None, delta_bias=None, softplus: bool = False, lengths=None, resets=None, h0=None, h_last=None,
+                 states=None):
+        s = self.desc = rgc_scan()
+        s.x = _sequence(x, "x")
+        s.delta, s.y, s.gate = _sequence(delta, "delta", x), _sequence(y, "y", x), _sequence(gate, "gate", x)
+        batch, steps, width = (int(n) for n in x.shape)
+        _require(a.dim() == 2, "a: a [width, states] tensor expected")
+        n = int(a.shape[1])
+        _require(int(groups) >= 1 and width % int(groups) == 0, "groups: the width must be a multiple of them")
+        s.batch, s.steps, s.width, s.states, s.groups, s.dtype, s.softplus = batch, steps, width, n, int(groups), _DTYPES[str(x.dtype)], int(bool(softplus))
+        self.channels, self.x, self.has_gate, self.state_shape = int(groups) * n, x, gate is not None, (batch, width, n)
+        s.b, s.c = _group_sequence(b, "b", x, self.channels), _group_sequence(c, "c", x, self.channels)
+        s.a, s.d, s.delta_bias = _plain(a, "a", (width, n), "float32", x), _plain(d, "d", (width,), "float32", x), _plain(delta_bias, "delta_bias", (width,), "float32", x)
+        s.lengths, s.resets = _plain(lengths, "lengths", (batch,), "int32", x), _resets(resets, (batch, steps), x)
+        s.h0, s.h_last = _plain(h0, "h0", self.state_shape, "float32", x), _plain(h_last, "h_last", self.state_shape, "float32", x)
+        s.kept = _plain(states, "states", (batch, -(-steps // RGC_SCAN_CHUNK), width, n), "float32", x)
+        self._keep = (x, delta, a, b, c, y, d, gate, delta_bias, lengths, resets, h0, h_last, states)
+        self._ref = ctypes.byref(s)
+
+
+class ScanGrads:
+    """A host ``rgc_scan_grads`` for a Scan (keeps the tensors alive).  dy, dx, ddelta, dgate (with a gate): like x; db, dc: like b and c; da: float32 [width, N]; dd, ddelta_bias:
+    float32 [width] or None; dh_last, dh0: float32 [batch, width, N] or None."""
+
+    def __init__(self, scan: Scan, dy, dx, ddelta, da, db, dc, dd=None, dgate=None, ddelta_bias=None, dh_last=None, dh0=None):
+        x, g = scan.x, rgc_scan_grads()
+        self.desc = g
+        _require(scan.has_gate == (dgate is not None), "dgate comes with a gate")
+        width, n = int(x.shape[2]), scan.desc.states
+        g.dy, g.dx, g.ddelta, g.dgate = _sequence(dy, "dy", x), _sequence(dx, "dx", x), _sequence(ddelta, "ddelta", x), _sequence(dgate, "dgate", x)
+        g.db, g.dc = _group_sequence(db, "db", x, scan.channels), _group_sequence(dc, "dc", x, scan.channels)
+        g.da, g.dd, g.ddelta_bias = _plain(da, "da", (width, n), "float32", x), _plain(dd, "dd", (width,), "float32", x), _plain(ddelta_bias, "ddelta_bias", (width,), "float32", x)
+        g.dh_last, g.dh0 = _plain(dh_last, "dh_last", scan.state_shape, "float32", x), _plain(dh0, "dh0", scan.state_shape, "float32", x)
+        self._keep = (scan, dy, dx, ddelta, da, db, dc, dd, dgate, ddelta_bias, dh_last, dh0)
+        self._ref = ctypes.byref(g)
+
+
+def rgc_selective_scan(ctx: Context, scan: Scan, stream=None) -> None:
+    _check(load_library().rgc_selective_scan(ctx.handle, scan._ref, _stream(stream)))
+
+
+def rgc_selective_scan_backward(ctx: Context, scan: Scan, grads: ScanGrads, stream=None) -> None:
+    _check(load_library().rgc_selective_scan_backward(ctx.handle, scan._ref, grads._ref, _stream(stream)))

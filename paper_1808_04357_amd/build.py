@@ -16,8 +16,8 @@ LIB = os.path.join(HERE, "librgc.so")
 OBJECTS = os.path.join(HERE, "_build")
 SOURCES = ["rgc_api.cpp", "rgc_compress.hip", "rgc_decompress.hip", "rgc_threshold.hip", "rgc_yardstick.hip",
            "rgc_vocab.hip", "rgc_recurrence.hip", "rgc_embed.hip",
-           "rgc_convolution.hip", "rgc_parts.hip"]
-HEADERS = ["rgc_internal.h", "rgc_device.h", "rgc_exact.h", "rgc_tickets.h", "rgc_tiles.h", "rgc_lm.h", "rgc_sequence.h", "rgc_stretch.h", os.path.join("..", "..", "include", "rgc.h"),
+           "rgc_convolution.hip", "rgc_scan.hip", "rgc_scan_backward.hip", "rgc_parts.hip"]
+HEADERS = ["rgc_internal.h", "rgc_device.h", "rgc_exact.h", "rgc_tickets.h", "rgc_tiles.h", "rgc_lm.h", "rgc_sequence.h", "rgc_scan.h", "rgc_stretch.h", os.path.join("..", "..", "include", "rgc.h"),
            os.path.join("..", "..", "include", "rgc_diag.h")]
 
 FLAGS = [

@@ -1459,6 +1459,43 @@ ConvArgs convolution_args(const rgc_convolution* r) {
   return A;
 }
 
+// (steps == 0: only h0 and h_last are there; batch == 0: nothing is)
+bool scan_fits(const rgc_scan* r) {
+  if (r->batch < 0 || r->batch > kInt32Most || r->steps < 0 || r->steps > kInt32Most || r->width < 1 || r->width > RGC_WIDTH_MAX) return false;
+  if (!dtype_fits(r->dtype) || r->states < 1 || r->states > RGC_SCAN_STATES_MAX || (r->softplus & ~1) != 0) return false;
+  if (r->groups < 1 || r->groups > r->width || r->width % r->groups != 0) return false;
+  if (!r->a || !words_aligned({r->a, r->d, r->delta_bias, r->lengths, r->h0, r->h_last, r->kept})) return false;
+  if (r->batch == 0 || r->steps == 0) return true;
+  const int32_t both = r->groups * r->states;
+  auto fits = [&](const rgc_sequence& v, int32_t width) { return sequence_fits(v, r->batch, r->steps, width, r->dtype, false); };
+  return fits(r->x, r->width) && fits(r->delta, r->width) && fits(r->b, both) && fits(r->c, both) && (!r->gate.data || fits(r->gate, r->width));
+}
+
+ScanArgs scan_args(const rgc_scan* r) {
+  ScanArgs A{};
+  A.batch = static_cast<uint32_t>(r->batch);
+  A.steps = static_cast<uint32_t>(r->steps);
+  A.width = static_cast<uint32_t>(r->width);
+  A.states = static_cast<uint32_t>(r->states);
+  A.groups = static_cast<uint32_t>(r->groups);
+  A.softplus = static_cast<uint32_t>(r->softplus);
+  A.x = view_of(r->x);
+  A.delta = view_of(r->delta);
+  A.gate = view_of(r->gate);
+  A.b = view_of(r->b);
+  A.c = view_of(r->c);
+  A.y = view_of(r->y);
+  A.a = r->a;
+  A.d = r->d;
+  A.delta_bias = r->delta_bias;
+  A.lengths = r->lengths;
+  A.resets = r->resets;
+  A.h0 = r->h0;
+  A.h_last = r->h_last;
+  A.kept = r->kept;
+  return A;
+}
+
 }  // namespace
 
 extern "C" {
@@ -1662,6 +1699,39 @@ int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* r, cons
   const int rc = lm_scratch(ctx, convolution_scratch_words(A, taps, r->dtype), &scratch);
   if (rc != RGC_OK) return rc;
   RGC_HIP(launch_convolution_backward(A, G, taps, r->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_selective_scan(rgc_ctx* ctx, const rgc_scan* r, void* hip_stream) {
+  if (!ctx || !r || !scan_fits(r)) return RGC_EINVAL;
+  if (r->batch > 0 && r->steps > 0 && !sequence_fits(r->y, r->batch, r->steps, r->width, r->dtype, true)) return RGC_EINVAL;
+  if (r->batch == 0) return RGC_OK;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  const ScanArgs A = scan_args(r);
+  unsigned long long* scratch = nullptr;
+  const int rc = lm_scratch(ctx, scan_scratch_words(A), &scratch);
+  if (rc != RGC_OK) return rc;
+  RGC_HIP(launch_scan(A, r->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
+  return RGC_OK;
+}
+
+int rgc_selective_scan_backward(rgc_ctx* ctx, const rgc_scan* r, const rgc_scan_grads* g, void* hip_stream) {
+  if (!ctx || !r || !g || !scan_fits(r) || !g->da || !words_aligned({g->da, g->dd, g->ddelta_bias, g->dh_last, g->dh0})) return RGC_EINVAL;
+  if (r->batch > 0 && r->steps > 0) {
+    const int32_t both = r->groups * r->states;
+    auto fits = [&](const rgc_sequence& v, int32_t width, bool written) { return sequence_fits(v, r->batch, r->steps, width, r->dtype, written); };
+    if (!r->kept || !fits(g->dy, r->width, false) || !fits(g->dx, r->width, true) || !fits(g->ddelta, r->width, true)) return RGC_EINVAL;
+    if (!fits(g->db, both, true) || !fits(g->dc, both, true) || (r->gate.data && !fits(g->dgate, r->width, true))) return RGC_EINVAL;
+  }
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
+  const ScanArgs A = scan_args(r);
+  const ScanGradArgs G{view_of(g->dy), view_of(g->dx), view_of(g->ddelta), view_of(g->dgate), view_of(g->db), view_of(g->dc), g->da, g->dd, g->ddelta_bias, g->dh_last, g->dh0};
+  unsigned long long* scratch = nullptr;
+  const int rc = lm_scratch(ctx, scan_backward_scratch_words(A), &scratch);
+  if (rc != RGC_OK) return rc;
+  RGC_HIP(launch_scan_backward(A, G, r->dtype, scratch, static_cast<hipStream_t>(hip_stream)));
   return RGC_OK;
 }
 

@@ -1,4 +1,5 @@
-// Arguments of the language-model operators' kernels (rgc_vocab.hip, rgc_recurrence.hip, rgc_embed.hip, rgc_convolution.hip, rgc_parts.hip), as the host side fills them.
+// Arguments of the language-model operators' kernels (rgc_vocab.hip, rgc_recurrence.hip, rgc_embed.hip, rgc_convolution.hip, rgc_scan.hip,
+// rgc_scan_backward.hip, rgc_parts.hip), as the host side fills them.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -111,6 +112,38 @@ struct ConvGradArgs {
   void* dbefore;
 };
 
+struct ScanArgs {
+  uint32_t batch, steps, width, states, groups;
+  uint32_t softplus;
+  SequenceView x, delta, gate, b, c, y;
+  const float* a;            // [width][states]
+  const float* d;
+  const float* delta_bias;
+  const int32_t* lengths;
+  const uint8_t* resets;
+  const float* h0;           // [batch][width][states]
+  float* h_last;
+  float* kept;               // [batch][chunks][width][states]
+};
+
+struct ScanGradArgs {
+  SequenceView dy, dx, ddelta, dgate, db, dc;
+  float* da;
+  float* dd;
+  float* ddelta_bias;
+  const float* dh_last;
+  float* dh0;
+};
+
+// How a scan is cut along its steps, and what the pieces tell each other.
+struct ScanCut {
+  uint32_t chunks, stretch, stretches;   // chunks of a sequence, chunks of a stretch, stretches of a sequence
+  uint32_t across;                       // workgroups for a group's channels
+  float* starts;                         // [batch][stretches][width][states]
+  float* sums;                           // [batch][stretches][width]
+  uint32_t* cuts;                        // [batch][stretches]: a text begins in it
+};
+
 // Sums of [count][columns] parts over their rows; the columns are those of up to three outputs, one behind the other (a null one is left out).
 struct PartsArgs {
   const float* parts;
@@ -157,6 +190,10 @@ hipError_t launch_sum_parts(const PartsArgs& a, hipStream_t s);
 hipError_t launch_convolution(const ConvArgs& a, uint32_t taps, int dtype, hipStream_t s);
 uint64_t convolution_scratch_words(const ConvArgs& a, uint32_t taps, int dtype);
 hipError_t launch_convolution_backward(const ConvArgs& a, const ConvGradArgs& g, uint32_t taps, int dtype, unsigned long long* scratch, hipStream_t s);
+hipError_t launch_scan(const ScanArgs& a, int dtype, unsigned long long* scratch, hipStream_t s);
+uint64_t scan_scratch_words(const ScanArgs& a);
+hipError_t launch_scan_backward(const ScanArgs& a, const ScanGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s);
+uint64_t scan_backward_scratch_words(const ScanArgs& a);
 bool recurrence_fits_grid(const RecurrenceArgs& a, int dtype, bool backward);
 uint64_t recurrence_scratch_words(const RecurrenceArgs& a, int dtype, bool backward);      // 64-bit words of `scratch`
 hipError_t launch_recurrence(const RecurrenceArgs& a, int dtype, unsigned long long* scratch, uint32_t looks, hipStream_t s);

@@ -1,0 +1,220 @@
+// rgc_scan.hip -- the selective scan, forward (include/rgc.h has the formulas; rgc_scan.h how a wave is laid out).
+//
+// A step of a state is two products, a power and two fused steps; the tensors are read and written once.  It is bound by that arithmetic.  Each wave walks along its steps with its
+// channels' states in registers.  Where sequences and channels alone are too few waves, a sequence is cut into stretches of whole chunks: one launch takes every stretch from
+// a state of zero to the state H that it ends with and adds up its steps' sizes, the next one makes the states that stretches begin with of those, h -> exp(rate sum) h + H, and the last one is
+// the walk from there.  What a state was before it starts anew is not used: not even multiplied by 0.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "rgc_scan.h"
+
+namespace rgc {
+namespace {
+
+constexpr uint32_t kWaves = 4;         // of a workgroup
+
+// kSummary: what a stretch does to a state, instead of its results.
+template <typename T, int kS, int kQ, bool kSummary>
+__global__ void __launch_bounds__(64 * kWaves) scan_kernel(ScanArgs A, ScanCut K, uint64_t begin) {
+  typedef Spot<kS, kQ> At;
+  constexpr uint32_t kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
+  __shared__ __attribute__((aligned(16))) float rows_b[kChunk * kStates], rows_c[kSummary ? 1 : kChunk * kStates];
+  __shared__ __attribute__((aligned(16))) float sizes[kWaves][kChannels * kTile], feeds[kWaves][kChannels * kTile];
+  uint64_t rest = begin + blockIdx.x;
+  const uint32_t wave = uniform(threadIdx.x >> 6);
+  const uint32_t block = uniform(static_cast<uint32_t>(rest % K.across)) * kWaves + wave;
+  rest /= K.across;
+  const uint32_t g = uniform(static_cast<uint32_t>(rest % A.groups));
+  rest /= A.groups;
+  const uint32_t walked = kSummary ? K.stretches - 1u : K.stretches;                  // (what the last stretch ends with, the walk itself knows)
+  const uint32_t stretch = uniform(static_cast<uint32_t>(rest % walked)), b = uniform(static_cast<uint32_t>(rest / walked));
+  const At at(A, g, block);
+  const uint32_t n = steps_of(A.lengths, b, A.steps);
+  const uint64_t states_of_row = static_cast<uint64_t>(A.width) * A.states;
+  float rate[kS], h[kS] = {};
+  rates_of(A, at, rate);
+  const float through = !kSummary && A.d ? A.d[at.c] : 0.0f, bias = A.delta_bias ? A.delta_bias[at.c] : 0.0f;
+  if constexpr (!kSummary) {
+    if (K.stretches > 1u) read_states(K.starts + (static_cast<uint64_t>(b) * K.stretches + stretch) * states_of_row, A, at, h);
+    else if (A.h0) read_states(A.h0 + b * states_of_row, A, at, h);
+  }
+  float total = 0.0f;                  // of the owner's steps' sizes
+  uint64_t cut = 0u;
+  const uint32_t last_chunk = min((stretch + 1u) * K.stretch, K.chunks);
+  for (uint32_t chunk = stretch * K.stretch; chunk < last_chunk; ++chunk) {
+    const uint32_t first = chunk * kChunk, count = steps_in(first, kChunk, n);
+    if (!kSummary && A.kept) write_states(A.kept + (static_cast<uint64_t>(b) * K.chunks + chunk) * states_of_row, A, at, h);
+    if (count > 0u) {                  // (the same for the whole workgroup)
+      __syncthreads();
+      stage<T, kStates, 64 * kWaves>(rows_b, A.b, A, b, g, first, count);
+      if constexpr (!kSummary) stage<T, kStates, 64 * kWaves>(rows_c, A.c, A, b, g, first, count);
+      __syncthreads();
+    }
+    const uint64_t anew = anew_from(A, b, first, n);
+    cut |= anew;
+    Own<T, kOwn> x, v, z;
+    auto ask = [&](uint32_t t) {
+      if (t + kTile <= n) {
+        x.read(A.x, b, t + at.own, at.c), v.read(A.delta, b, t + at.own, at.c);
+        if (!kSummary && A.gate.data) z.read(A.gate, b, t + at.own, at.c);
+      } else {
+        x.read(A.x, b, t + at.own, n, at.c), v.read(A.delta, b, t + at.own, n, at.c);
+        if (!kSummary && A.gate.data) z.read(A.gate, b, t + at.own, n, at.c);
+      }
+    };
+    if (count > 0u) ask(first);
+    for (uint32_t tile = 0; tile < count; tile += kTile) {
+      const uint32_t t0 = first + tile, valid = min(count - tile, kTile);
+      float input[kOwn], shown[kOwn];
+#pragma unroll
+      for (uint32_t j = 0; j < kOwn; ++j) {
+        float grow, size = size_of(A, static_cast<float>(v.v[j]), bias, grow);
+        if (t0 + at.own + j >= n) size = 0.0f;                                       // (what is not there was read as 0)
+        input[j] = static_cast<float>(x.v[j]);
+        sizes[wave][at.channel * kTile + at.own + j] = size;
+        feeds[wave][at.channel * kTile + at.own + j] = size * input[j];
+        if constexpr (kSummary) {
+          total += size;
+        } else {
+          shown[j] = 1.0f;
+          if (A.gate.data) {
+            const float zj = static_cast<float>(z.v[j]);
+            float open, shut;
+            gate_of(zj, open, shut);
+            shown[j] = zj * open;
+          }
+        }
+      }
+      if (tile + kTile < count) ask(t0 + kTile);
+      wave_sync();
+      float size[kTile], fed[kTile], y[kTile] = {};
+      read_tile(&sizes[wave][at.channel * kTile], size);
+      read_tile(&feeds[wave][at.channel * kTile], fed);
+      const uint32_t starts = static_cast<uint32_t>(anew >> tile) & 0xFFu;
+      auto walk = [&](auto plain) __attribute__((always_inline)) {
+        constexpr bool kPlain = decltype(plain){};
+#pragma unroll
+        for (uint32_t t = 0; t < kTile; ++t) {
+          if (!kPlain && t >= valid) continue;
+          float in[kS], out[kS];
+          read_shared<kS>(&rows_b[(tile + t) * kStates + at.q * kS], in);
+          if constexpr (!kSummary) read_shared<kS>(&rows_c[(tile + t) * kStates + at.q * kS], out);
+#pragma unroll
+          for (uint32_t s = 0; s < kS; ++s) {
+            if (!kPlain && ((starts >> t) & 1u) != 0u) h[s] = 0.0f;
+            h[s] = __fmaf_rn(__builtin_amdgcn_exp2f(size[t] * rate[s]), h[s], fed[t] * in[s]);
+            if constexpr (!kSummary) y[t] = __fmaf_rn(h[s], out[s], y[t]);
+          }
+        }
+      };
+      if (valid == kTile && starts == 0u) walk(Yes{}); else walk(No{});
+      wave_sync();                     // (before the next tile's sizes take their place)
+      if constexpr (!kSummary) {
+        sum_for_owners<kQ>(y, at.lane);
+        T* to = element<T>(A.y, b, t0 + at.own, at.c);
+#pragma unroll
+        for (uint32_t j = 0; j < kOwn; ++j, to += A.y.step_stride)
+          if (at.owner && at.own + j < valid) *to = static_cast<T>(__fmaf_rn(through, input[j], y[j]) * shown[j]);
+      }
+    }
+    if constexpr (!kSummary) {
+      const uint32_t behind = steps_in(first, kChunk, A.steps);
+      for (uint32_t t = count + at.q; t < behind; t += kQ)
+        if (at.mine) *element<T>(A.y, b, first + t, at.c) = static_cast<T>(0.0f);
+    }
+  }
+  if constexpr (kSummary) {
+    const uint64_t slot = static_cast<uint64_t>(b) * K.stretches + stretch;
+    write_states(K.starts + slot * states_of_row, A, at, h);
+    if (kQ == 16 && !at.owner) total = 0.0f;
+#pragma unroll
+    for (uint32_t m = 1; m < kQ; m <<= 1) total += __shfl_xor(total, m);
+    if (at.mine && at.q == 0u) K.sums[slot * A.width + at.c] = total;
+    if (g == 0u && block == 0u && at.lane == 0u) K.cuts[slot] = cut != 0u ? 1u : 0u;
+  } else {
+    if (A.h_last && stretch + 1u == K.stretches) write_states(A.h_last + b * states_of_row, A, at, h);
+  }
+}
+
+// The states that stretches begin with, in the place of those that they end with from 0.
+__global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs A, ScanCut K, uint64_t begin) {
+  constexpr uint32_t kAtOnce = 8;
+  const uint64_t row = static_cast<uint64_t>(A.width) * A.states, i = (begin + blockIdx.x) * 256u + threadIdx.x;
+  if (i >= row * A.batch) return;
+  const uint64_t b = i / row, at = i % row, c = at / A.states;
+  const float r0 = A.a[at] * kLog2e, r1 = r0 > 3.0e38f ? 3.0e38f : r0, rate = r1 < -3.0e38f ? -3.0e38f : r1;
+  float h = A.h0 ? A.h0[i] : 0.0f;
+  float* to = K.starts + b * K.stretches * row + at;
+  const float* sums = K.sums + b * K.stretches * A.width + c;
+  const uint32_t* cuts = K.cuts + b * K.stretches;
+  for (uint32_t k0 = 0; k0 < K.stretches; k0 += kAtOnce) {
+    float ends[kAtOnce], decay[kAtOnce];
+#pragma unroll
+    for (uint32_t j = 0; j < kAtOnce; ++j) {
+      const uint32_t k = min(k0 + j, K.stretches - 1u);                              // (the last one's slot is unset memory, and not used)
+      ends[j] = to[k * row];
+      decay[j] = __builtin_amdgcn_exp2f(rate * sums[static_cast<uint64_t>(k) * A.width]);
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kAtOnce; ++j) {
+      const uint32_t k = k0 + j;
+      if (k >= K.stretches) continue;
+      to[k * row] = h;
+      if (k + 1u < K.stretches) h = cuts[k] != 0u ? ends[j] : __fmaf_rn(decay[j], h, ends[j]);
+    }
+  }
+}
+
+uint64_t workgroups(const ScanArgs& a, const ScanCut& k, uint32_t stretches) { return static_cast<uint64_t>(a.batch) * stretches * a.groups * k.across; }
+
+}  // namespace
+
+// Stretches where sequences and channels are fewer waves than kFew: so many that there are kEnough.
+ScanCut scan_cut(const ScanArgs& a) {
+  constexpr uint64_t kFew = 768, kEnough = 4096;
+  ScanCut K{};
+  K.chunks = (a.steps + kChunk - 1u) / kChunk;
+  const uint32_t channels = kWaves * wave_channels(a.states), each = a.width / a.groups;
+  K.across = (each + channels - 1u) / channels;
+  const uint64_t waves = static_cast<uint64_t>(a.batch) * a.groups * ((each + channels / kWaves - 1u) / (channels / kWaves));
+  K.stretches = 1u;
+  K.stretch = K.chunks > 0u ? K.chunks : 1u;
+  if (waves < kFew && K.chunks > 1u) {
+    const uint64_t want = kEnough / waves;
+    K.stretch = static_cast<uint32_t>((K.chunks + want - 1u) / want);
+    K.stretches = (K.chunks + K.stretch - 1u) / K.stretch;
+  }
+  return K;
+}
+
+uint64_t scan_scratch_words(const ScanArgs& a) {
+  const ScanCut K = scan_cut(a);
+  if (K.stretches <= 1u) return 0u;
+  return (static_cast<uint64_t>(a.batch) * K.stretches * (static_cast<uint64_t>(a.width) * (a.states + 1u) + 1u) + 1u) / 2u;
+}
+
+hipError_t launch_scan(const ScanArgs& a, int dtype, unsigned long long* scratch, hipStream_t s) {
+  ScanCut K = scan_cut(a);
+  if (K.stretches > 1u) {
+    const uint64_t slots = static_cast<uint64_t>(a.batch) * K.stretches;
+    K.starts = reinterpret_cast<float*>(scratch);
+    K.sums = K.starts + slots * a.width * a.states;
+    K.cuts = reinterpret_cast<uint32_t*>(K.sums + slots * a.width);
+  }
+  return by_states(a.states, dtype, [&](auto type, auto states, auto lanes) {
+    using T = decltype(type);
+    constexpr int kS = decltype(states)::value, kQ = decltype(lanes)::value;
+    if (K.stretches > 1u) {
+      in_grids(workgroups(a, K, K.stretches - 1u), [&](uint64_t begin, dim3 grid) { scan_kernel<T, kS, kQ, true><<<grid, dim3(64 * kWaves), 0, s>>>(a, K, begin); });
+      const uint64_t all = static_cast<uint64_t>(a.batch) * a.width * a.states;
+      in_grids((all + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_join_kernel<<<grid, dim3(256), 0, s>>>(a, K, begin); });
+    }
+    in_grids(workgroups(a, K, K.stretches), [&](uint64_t begin, dim3 grid) { scan_kernel<T, kS, kQ, false><<<grid, dim3(64 * kWaves), 0, s>>>(a, K, begin); });
+    return hipGetLastError();
+  });
+}
+
+}  // namespace rgc

@@ -1,0 +1,503 @@
+// rgc_scan_backward.hip -- the selective scan's gradients (include/rgc.h has the formulas; rgc_scan.h how a wave is laid out).
+//
+// With g the gradient that leaves a step towards the state before it and e = the step's output gradient times C, a state's gradient is d = e + g' (g' of the step behind it), and g = a d.
+// So the gradients go through the steps as the states do, the other way.
+//  1. Every chunk but the first from a gradient of zero behind it: what it hands on, and the sum of its steps' sizes (scan_rear_kernel).
+//  2. What comes in behind each chunk, from the last one to the first (scan_rear_join_kernel).  With one chunk neither is needed.
+//  3. A workgroup for each chunk and group of channels (scan_backward_kernel).  Its eight waves take eight steps each, of as many channels as a wave has at a time: each makes its powers,
+//     what its steps do to a state and to a gradient (both from zero), hears from the others what state it begins and what gradient it ends with, and walks its steps in both directions out of
+//     registers: B's and C's gradients, sums over channels, stay in registers over all of the workgroup's channels; those of A, D and delta's bias, sums over steps, are added up over the waves.
+//  4. The workgroups' parts of both are added up in an order made of the sizes alone (scan_rows_kernel, launch_sum_parts).
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "rgc_scan.h"
+
+namespace rgc {
+namespace {
+
+constexpr uint32_t kRearWaves = 4;     // of a workgroup of the first launch
+constexpr uint32_t kWaves = kChunk / kTile;
+
+struct RearCut {
+  uint32_t chunks, across;             // workgroups of the first launch for a group's channels
+  uint32_t splits, blocks;             // workgroups of the third for them, stretches of a wave's channels
+  float* ends;                         // [batch][chunks][width][states]: what a chunk hands on from 0, then what comes in behind it
+  float* sums;                         // [batch][chunks][width]
+  uint32_t* cuts;                      // [batch][chunks]
+  float* parts;                        // [batch][chunks][width * states + width + width]: gradients of A, D and delta's bias
+  float* rows;                         // [splits][batch][steps][2][groups * states]: of B and C
+};
+
+// Gradients that reach the states of a step through its output: the output's, before the gate.
+__device__ __forceinline__ float shown_of(bool gate, float z, float& slope) {
+  if (!gate) {
+    slope = 0.0f;
+    return 1.0f;
+  }
+  float open, shut;
+  gate_of(z, open, shut);
+  slope = open * __fmaf_rn(z, shut, 1.0f);
+  return z * open;
+}
+
+template <typename T, int kS, int kQ>
+__global__ void __launch_bounds__(64 * kRearWaves) scan_rear_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
+  typedef Spot<kS, kQ> At;
+  constexpr uint32_t kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
+  __shared__ __attribute__((aligned(16))) float rows_c[kChunk * kStates], sizes[kRearWaves][kChannels * kTile], grads[kRearWaves][kChannels * kTile];
+  uint64_t rest = begin + blockIdx.x;
+  const uint32_t wave = uniform(threadIdx.x >> 6);
+  const uint32_t block = uniform(static_cast<uint32_t>(rest % K.across)) * kRearWaves + wave;
+  rest /= K.across;
+  const uint32_t group = uniform(static_cast<uint32_t>(rest % A.groups));
+  rest /= A.groups;
+  const uint32_t chunk = 1u + uniform(static_cast<uint32_t>(rest % (K.chunks - 1u))), b = uniform(static_cast<uint32_t>(rest / (K.chunks - 1u)));
+  const At at(A, group, block);
+  const uint32_t n = steps_of(A.lengths, b, A.steps), first = chunk * kChunk, count = steps_in(first, kChunk, n);
+  const bool gate = A.gate.data != nullptr;
+  float rate[kS], g[kS] = {};
+  rates_of(A, at, rate);
+  const float bias = A.delta_bias ? A.delta_bias[at.c] : 0.0f;
+  stage<T, kStates, 64 * kRearWaves>(rows_c, A.c, A, b, group, first, count);
+  __syncthreads();
+  const uint64_t anew = anew_from(A, b, first, n);
+  float total = 0.0f;
+  const uint32_t tiles = (count + kTile - 1u) / kTile;
+  Own<T, kOwn> v, z, dy;
+  auto ask = [&](uint32_t t) {
+    if (t + kTile <= n) {
+      v.read(A.delta, b, t + at.own, at.c), dy.read(G.dy, b, t + at.own, at.c);
+      if (gate) z.read(A.gate, b, t + at.own, at.c);
+    } else {
+      v.read(A.delta, b, t + at.own, n, at.c), dy.read(G.dy, b, t + at.own, n, at.c);
+      if (gate) z.read(A.gate, b, t + at.own, n, at.c);
+    }
+  };
+  if (tiles > 0u) ask(first + (tiles - 1u) * kTile);
+  for (uint32_t i = tiles; i-- > 0u;) {
+    const uint32_t tile = i * kTile, t0 = first + tile, valid = min(count - tile, kTile);
+#pragma unroll
+    for (uint32_t j = 0; j < kOwn; ++j) {
+      float grow, slope, size = size_of(A, static_cast<float>(v.v[j]), bias, grow);
+      if (t0 + at.own + j >= n) size = 0.0f;
+      total += size;
+      sizes[wave][at.channel * kTile + at.own + j] = size;
+      grads[wave][at.channel * kTile + at.own + j] = static_cast<float>(dy.v[j]) * shown_of(gate, gate ? static_cast<float>(z.v[j]) : 0.0f, slope);
+    }
+    if (i > 0u) ask(t0 - kTile);
+    wave_sync();
+    float size[kTile], dinner[kTile];
+    read_tile(&sizes[wave][at.channel * kTile], size);
+    read_tile(&grads[wave][at.channel * kTile], dinner);
+    const uint32_t starts = static_cast<uint32_t>(anew >> tile) & 0xFFu;
+    auto walk = [&](auto plain) __attribute__((always_inline)) {
+      constexpr bool kPlain = decltype(plain){};
+#pragma unroll
+      for (uint32_t t = kTile; t-- > 0u;) {
+        if (!kPlain && t >= valid) continue;
+        float out[kS];
+        read_shared<kS>(&rows_c[(tile + t) * kStates + at.q * kS], out);
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) {
+          g[s] = __builtin_amdgcn_exp2f(size[t] * rate[s]) * __fmaf_rn(dinner[t], out[s], g[s]);
+          if (!kPlain && ((starts >> t) & 1u) != 0u) g[s] = 0.0f;
+        }
+      }
+    };
+    if (valid == kTile && starts == 0u) walk(Yes{}); else walk(No{});
+    wave_sync();
+  }
+  const uint64_t slot = static_cast<uint64_t>(b) * K.chunks + chunk;
+  write_states(K.ends + slot * (static_cast<uint64_t>(A.width) * A.states), A, at, g);
+  if (kQ == 16 && !at.owner) total = 0.0f;
+#pragma unroll
+  for (uint32_t m = 1; m < kQ; m <<= 1) total += __shfl_xor(total, m);
+  if (at.mine && at.q == 0u) K.sums[slot * A.width + at.c] = total;
+  if (group == 0u && block == 0u && at.lane == 0u) K.cuts[slot] = anew != 0u ? 1u : 0u;
+}
+
+__global__ void __launch_bounds__(256) scan_rear_join_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
+  constexpr uint32_t kAtOnce = 8;
+  const uint64_t row = static_cast<uint64_t>(A.width) * A.states, i = (begin + blockIdx.x) * 256u + threadIdx.x;
+  if (i >= row * A.batch) return;
+  const uint64_t b = i / row, at = i % row, c = at / A.states;
+  const float r0 = A.a[at] * kLog2e, r1 = r0 > 3.0e38f ? 3.0e38f : r0, rate = r1 < -3.0e38f ? -3.0e38f : r1;
+  float g = G.dh_last ? G.dh_last[i] : 0.0f;
+  float* to = K.ends + b * K.chunks * row + at;
+  const float* sums = K.sums + b * K.chunks * A.width + c;
+  const uint32_t* cuts = K.cuts + b * K.chunks;
+  for (uint32_t done = 0; done < K.chunks; done += kAtOnce) {
+    const uint32_t upto = K.chunks - done;                                           // chunks left, the last of them first
+    float ends[kAtOnce], decay[kAtOnce];
+#pragma unroll
+    for (uint32_t j = 0; j < kAtOnce; ++j) {
+      const uint32_t k = max(upto, j + 1u) - j - 1u;                                 // (the first one's slot is unset memory, and not used)
+      ends[j] = to[k * row];
+      decay[j] = __builtin_amdgcn_exp2f(rate * sums[static_cast<uint64_t>(k) * A.width]);
+    }
+#pragma unroll
+    for (uint32_t j = 0; j < kAtOnce; ++j) {
+      if (j >= upto) continue;
+      const uint32_t k = upto - j - 1u;
+      to[k * row] = g;
+      if (k > 0u) g = cuts[k] != 0u ? ends[j] : __fmaf_rn(decay[j], g, ends[j]);
+    }
+  }
+}
+
+// Sums over the channels of a wave of kCount numbers a lane: lanes that differ in kBit and above are different channels of the same states.  Every lane is left with some of the sums, those
+// from `base` on; how many, is returned.
+template <int kBit, int kLeast, int kCount>
+__device__ __forceinline__ constexpr int left_of() {
+  if constexpr (kBit < kLeast) return kCount;
+  else return left_of<kBit / 2, kLeast, kCount % 2 == 0 ? kCount / 2 : kCount>();
+}
+template <int kBit, int kLeast, int kCount, int kAll>
+__device__ __forceinline__ void sum_channels(float (&v)[kAll], uint32_t lane, uint32_t& base) {
+  if constexpr (kBit >= kLeast) {
+    if constexpr (kCount % 2 == 0) {
+      const bool upper = (lane & kBit) != 0u;
+#pragma unroll
+      for (int i = 0; i < kCount / 2; ++i) {
+        const float keep = upper ? v[i + kCount / 2] : v[i], give = upper ? v[i] : v[i + kCount / 2];
+        v[i] = keep + __shfl_xor(give, kBit);
+      }
+      base += upper ? kCount / 2 : 0u;
+      sum_channels<kBit / 2, kLeast, kCount / 2>(v, lane, base);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) v[i] += __shfl_xor(v[i], kBit);
+      sum_channels<kBit / 2, kLeast, kCount>(v, lane, base);
+    }
+  }
+}
+
+template <int kS, int kQ>
+struct SharedBackward {
+  static constexpr uint32_t kStates = kS * kQ, kChannels = 64 / kQ;
+  float rows_b[kChunk * kStates], rows_c[kChunk * kStates];
+  float of_step[kWaves][3][kChannels * kTile];     // sizes, size * input, gradient before the gate
+  float parts[2][kWaves][3][64 * kS];              // what a wave's steps do: decay, state, gradient
+  float da[2][kWaves][64 * kS], own[2][kWaves][2][64];
+};
+
+template <typename T, int kS, int kQ>
+__global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
+  typedef Spot<kS, kQ> At;
+  constexpr uint32_t kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
+  __shared__ __attribute__((aligned(16))) SharedBackward<kS, kQ> lds;
+  uint64_t rest = begin + blockIdx.x;
+  const uint32_t split = uniform(static_cast<uint32_t>(rest % K.splits));
+  rest /= K.splits;
+  const uint32_t group = uniform(static_cast<uint32_t>(rest % A.groups));
+  rest /= A.groups;
+  const uint32_t chunk = uniform(static_cast<uint32_t>(rest % K.chunks)), b = uniform(static_cast<uint32_t>(rest / K.chunks));
+  const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, each = A.width / A.groups;
+  const uint32_t n = steps_of(A.lengths, b, A.steps), first = chunk * kChunk, count = steps_in(first, kChunk, n);
+  const uint32_t t0 = first + wave * kTile, valid = steps_in(t0, kTile, n);
+  const bool gate = A.gate.data != nullptr;
+  const uint64_t row = static_cast<uint64_t>(A.width) * A.states, slot = static_cast<uint64_t>(b) * K.chunks + chunk;
+  stage<T, kStates, 64 * kWaves>(lds.rows_b, A.b, A, b, group, first, count);
+  stage<T, kStates, 64 * kWaves>(lds.rows_c, A.c, A, b, group, first, count);
+  __syncthreads();
+  const uint64_t anew = anew_from(A, b, first, n);
+  const uint32_t starts = static_cast<uint32_t>(anew >> (wave * kTile)) & 0xFFu;
+  float sums[2 * kTile * kS] = {};     // of the gradients of B and C
+  // the sums over the waves of what an earlier turn left
+  auto finish = [&](uint32_t block, uint32_t turn) {
+    float* to = K.parts + slot * (row + 2u * A.width);
+    const uint32_t id = threadIdx.x;
+    if (id < 64u * kS) {
+      const uint32_t l = id / kS, state = l % kQ * kS + id % kS, c = block * kChannels + l / kQ;
+      float sum = 0.0f;
+#pragma unroll
+      for (uint32_t w = 0; w < kWaves; ++w) sum += lds.da[turn][w][id];
+      if (c < each && state < A.states) to[static_cast<uint64_t>(group * each + c) * A.states + state] = sum;
+    } else if (id < 64u * kS + 2u * kChannels) {
+      const uint32_t which = (id - 64u * kS) / kChannels, channel = (id - 64u * kS) % kChannels, c = block * kChannels + channel;
+      float sum = 0.0f;
+      for (uint32_t w = 0; w < kWaves; ++w) {
+        for (uint32_t q = 0; q < kQ; ++q) sum += lds.own[turn][w][which][channel * kQ + q];
+      }
+      if (c < each) to[row + which * A.width + group * each + c] = sum;
+    }
+  };
+  const uint32_t per = (K.blocks + K.splits - 1u) / K.splits, from = split * per, upto = min(from + per, K.blocks);
+  Own<T, kOwn> x, v, z, dy;
+  float h_in[kS], g_in[kS];
+  auto ask = [&](uint32_t block) {
+    const At at(A, group, block);
+    if (valid == kTile) {
+      x.read(A.x, b, t0 + at.own, at.c), v.read(A.delta, b, t0 + at.own, at.c), dy.read(G.dy, b, t0 + at.own, at.c);
+      if (gate) z.read(A.gate, b, t0 + at.own, at.c);
+    } else if (valid > 0u) {
+      x.read(A.x, b, t0 + at.own, n, at.c), v.read(A.delta, b, t0 + at.own, n, at.c), dy.read(G.dy, b, t0 + at.own, n, at.c);
+      if (gate) z.read(A.gate, b, t0 + at.own, n, at.c);
+    }
+    read_states(A.kept + slot * row, A, at, h_in);
+    if (K.chunks > 1u) {
+      read_states(K.ends + slot * row, A, at, g_in);
+    } else if (G.dh_last) {
+      read_states(G.dh_last + b * row, A, at, g_in);
+    } else {
+#pragma unroll
+      for (uint32_t s = 0; s < kS; ++s) g_in[s] = 0.0f;
+    }
+  };
+  if (from < upto) ask(from);
+  for (uint32_t block = from; block < upto; ++block) {
+    const uint32_t turn = (block - from) & 1u;
+    const At at(A, group, block);
+    float rate[kS];
+    rates_of(A, at, rate);
+    const float through = A.d ? A.d[at.c] : 0.0f, bias = A.delta_bias ? A.delta_bias[at.c] : 0.0f;
+    float input[kOwn], grow[kOwn], size_own[kOwn], dinner_own[kOwn], dgate_by[kOwn];      // dgate_by: the gate's gradient, without its factor `inner`
+    float h[kS], g[kS];
+    float *const of_size = lds.of_step[wave][0] + at.channel * kTile, *const of_fed = lds.of_step[wave][1] + at.channel * kTile, *const of_grad = lds.of_step[wave][2] + at.channel * kTile;
+#pragma unroll
+    for (uint32_t j = 0; j < kOwn; ++j) {
+      float slope = 0.0f;
+      input[j] = grow[j] = size_own[j] = dinner_own[j] = dgate_by[j] = 0.0f;
+      if (at.mine && valid > 0u && t0 + at.own + j < n) {        // (lanes behind the group have no part in its sums)
+        input[j] = static_cast<float>(x.v[j]);
+        size_own[j] = size_of(A, static_cast<float>(v.v[j]), bias, grow[j]);
+        const float given = static_cast<float>(dy.v[j]);
+        dinner_own[j] = given * shown_of(gate, gate ? static_cast<float>(z.v[j]) : 0.0f, slope);
+        dgate_by[j] = given * slope;
+      }
+      of_size[at.own + j] = size_own[j];
+      of_fed[at.own + j] = size_own[j] * input[j];
+      of_grad[at.own + j] = dinner_own[j];
+    }
+#pragma unroll
+    for (uint32_t s = 0; s < kS; ++s) h[s] = at.mine ? h_in[s] : 0.0f, g[s] = at.mine ? g_in[s] : 0.0f;
+    if (block + 1u < upto) ask(block + 1u);
+    wave_sync();
+    float size[kTile], fed[kTile], dinner[kTile];
+    read_tile(of_size, size);
+    read_tile(of_fed, fed);
+    read_tile(of_grad, dinner);
+    wave_sync();
+    const float *const row_b = lds.rows_b + wave * kTile * kStates + at.q * kS, *const row_c = lds.rows_c + wave * kTile * kStates + at.q * kS;
+    float a[kTile][kS], own_h[kS] = {}, own_g[kS] = {}, whole[kS];
+    auto alone = [&](auto plain) __attribute__((always_inline)) {
+      constexpr bool kPlain = decltype(plain){};
+#pragma unroll
+      for (uint32_t t = 0; t < kTile; ++t) {
+        if (!kPlain && t >= valid) continue;
+        float in[kS];
+        read_shared<kS>(row_b + t * kStates, in);
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) {
+          a[t][s] = __builtin_amdgcn_exp2f(size[t] * rate[s]);
+          if (!kPlain && ((starts >> t) & 1u) != 0u) own_h[s] = 0.0f;
+          own_h[s] = __fmaf_rn(a[t][s], own_h[s], fed[t] * in[s]);
+        }
+      }
+#pragma unroll
+      for (uint32_t t = kTile; t-- > 0u;) {
+        if (!kPlain && t >= valid) continue;
+        float out[kS];
+        read_shared<kS>(row_c + t * kStates, out);
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) {
+          own_g[s] = a[t][s] * __fmaf_rn(dinner[t], out[s], own_g[s]);
+          if (!kPlain && ((starts >> t) & 1u) != 0u) own_g[s] = 0.0f;
+        }
+      }
+    };
+    const bool plain_tile = valid == kTile && starts == 0u;
+    if (plain_tile) alone(Yes{}); else alone(No{});
+    float total = 0.0f;
+#pragma unroll
+    for (uint32_t t = 0; t < kTile; ++t) total += size[t];
+#pragma unroll
+    for (uint32_t s = 0; s < kS; ++s) {
+      whole[s] = __builtin_amdgcn_exp2f(total * rate[s]);
+      lds.parts[turn][wave][0][lane * kS + s] = whole[s];
+      lds.parts[turn][wave][1][lane * kS + s] = own_h[s];
+      lds.parts[turn][wave][2][lane * kS + s] = own_g[s];
+    }
+    __syncthreads();
+    if (block > from) finish(block - 1u, turn ^ 1u);
+    for (uint32_t w = 0; w < wave; ++w) {
+      const bool cut = ((anew >> (w * kTile)) & 0xFFull) != 0u;
+      float p[kS], own[kS];
+      read_shared<kS>(&lds.parts[turn][w][0][lane * kS], p);
+      read_shared<kS>(&lds.parts[turn][w][1][lane * kS], own);
+#pragma unroll
+      for (uint32_t s = 0; s < kS; ++s) h[s] = cut ? own[s] : __fmaf_rn(p[s], h[s], own[s]);
+    }
+    for (uint32_t w = kWaves - 1u; w > wave; --w) {
+      const bool cut = ((anew >> (w * kTile)) & 0xFFull) != 0u;
+      float p[kS], own[kS];
+      read_shared<kS>(&lds.parts[turn][w][0][lane * kS], p);
+      read_shared<kS>(&lds.parts[turn][w][2][lane * kS], own);
+#pragma unroll
+      for (uint32_t s = 0; s < kS; ++s) g[s] = cut ? own[s] : __fmaf_rn(p[s], g[s], own[s]);
+    }
+    float inner[kTile] = {}, came[kTile] = {}, slower[kTile] = {}, da[kS] = {};
+    auto walk = [&](auto plain) __attribute__((always_inline)) {
+      constexpr bool kPlain = decltype(plain){};
+      float after[kTile][kS];
+#pragma unroll
+      for (uint32_t t = 0; t < kTile; ++t) {
+        if (!kPlain && t >= valid) continue;
+        float in[kS];
+        read_shared<kS>(row_b + t * kStates, in);
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) {
+          const float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
+          after[t][s] = __fmaf_rn(a[t][s], !kPlain && ((starts >> t) & 1u) != 0u ? 0.0f : prior, fed[t] * in[s]);
+        }
+      }
+#pragma unroll
+      for (uint32_t t = kTile; t-- > 0u;) {
+        if (!kPlain && t >= valid) continue;
+        float in[kS], out[kS];
+        read_shared<kS>(row_b + t * kStates, in);
+        read_shared<kS>(row_c + t * kStates, out);
+        const bool anew_here = !kPlain && ((starts >> t) & 1u) != 0u;
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) {
+          float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
+          if (anew_here) prior = 0.0f;
+          inner[t] = __fmaf_rn(after[t][s], out[s], inner[t]);
+          sums[(kTile + t) * kS + s] = __fmaf_rn(dinner[t], after[t][s], sums[(kTile + t) * kS + s]);
+          const float d = __fmaf_rn(dinner[t], out[s], g[s]);
+          came[t] = __fmaf_rn(d, in[s], came[t]);
+          sums[t * kS + s] = __fmaf_rn(fed[t], d, sums[t * kS + s]);
+          g[s] = a[t][s] * d;
+          const float lost = g[s] * prior;                         // the gradient of the decay's exponent
+          slower[t] = __fmaf_rn(lost, rate[s], slower[t]);
+          da[s] = __fmaf_rn(lost, size[t], da[s]);
+          if (anew_here) g[s] = 0.0f;
+        }
+      }
+    };
+    if (plain_tile) walk(Yes{}); else walk(No{});
+    if (G.dh0 && chunk == 0u && wave == 0u) write_states(G.dh0 + b * row, A, at, g);
+    if (!gate && A.d == nullptr) {     // (nothing asks for it)
+#pragma unroll
+      for (uint32_t t = 0; t < kTile; ++t) inner[t] = 0.0f;
+    }
+    sum_for_owners<kQ>(inner, lane);
+    sum_for_owners<kQ>(came, lane);
+    sum_for_owners<kQ>(slower, lane);
+    float dd = 0.0f, dbias = 0.0f;
+    const uint32_t behind = steps_in(t0, kTile, A.steps);
+#pragma unroll
+    for (uint32_t j = 0; j < kOwn; ++j) {
+      const bool there = at.own + j < valid;
+      const float dv = there ? __fmaf_rn(came[j], input[j], slower[j] * kLn2) * grow[j] : 0.0f;
+      const float dx = there ? __fmaf_rn(came[j], size_own[j], dinner_own[j] * through) : 0.0f;
+      const float dgate = there ? __fmaf_rn(through, input[j], inner[j]) * dgate_by[j] : 0.0f;
+      dd += there ? dinner_own[j] * input[j] : 0.0f;
+      dbias += dv;
+      if (at.owner && at.own + j < behind) {
+        const uint32_t t = t0 + at.own + j;
+        *element<T>(G.dx, b, t, at.c) = static_cast<T>(dx);
+        *element<T>(G.ddelta, b, t, at.c) = static_cast<T>(dv);
+        if (gate) *element<T>(G.dgate, b, t, at.c) = static_cast<T>(dgate);
+      }
+    }
+#pragma unroll
+    for (uint32_t s = 0; s < kS; ++s) lds.da[turn][wave][lane * kS + s] = da[s];
+    const bool counts = kQ < 16 || at.q % 2u == 0u;
+    lds.own[turn][wave][0][lane] = counts ? dd : 0.0f;
+    lds.own[turn][wave][1][lane] = counts ? dbias : 0.0f;
+  }
+  __syncthreads();
+  if (from < upto) finish(upto - 1u, (upto - 1u - from) & 1u);
+  uint32_t base = 0u;
+  sum_channels<32, kQ, 2 * kTile * kS>(sums, lane, base);
+  constexpr int kLeft = left_of<32, kQ, 2 * kTile * kS>();
+  const uint32_t both = A.groups * A.states;
+#pragma unroll
+  for (int i = 0; i < kLeft; ++i) {
+    const uint32_t id = base + i, which = id / (kTile * kS), t = id / kS % kTile, state = lane % kQ * kS + id % kS;
+    if (t0 + t < A.steps && state < A.states)
+      K.rows[(((static_cast<uint64_t>(split) * A.batch + b) * A.steps + t0 + t) * 2u + which) * both + group * A.states + state] = sums[i];
+  }
+}
+
+// Gradients of B and C from the splits' parts.
+template <typename T>
+__global__ void __launch_bounds__(256) scan_rows_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
+  const uint64_t both = static_cast<uint64_t>(A.groups) * A.states, all = static_cast<uint64_t>(A.batch) * A.steps * 2u * both, i = (begin + blockIdx.x) * 256u + threadIdx.x;
+  if (i >= all) return;
+  float sum = 0.0f;
+#pragma unroll 8
+  for (uint32_t k = 0; k < K.splits; ++k) sum += K.rows[k * all + i];
+  const uint64_t step = i / (2u * both), in_step = i % (2u * both);
+  const uint32_t j = static_cast<uint32_t>(in_step % both), b = static_cast<uint32_t>(step / A.steps), t = static_cast<uint32_t>(step % A.steps);
+  *element<T>(in_step < both ? G.db : G.dc, b, t, j) = static_cast<T>(sum);
+}
+
+// Sequences without steps hand on what comes in.
+__global__ void __launch_bounds__(256) scan_hand_on_kernel(const float* dh_last, float* dh0, uint64_t count, uint64_t begin) {
+  const uint64_t i = (begin + blockIdx.x) * 256u + threadIdx.x;
+  if (i < count) dh0[i] = dh_last ? dh_last[i] : 0.0f;
+}
+
+RearCut rear_cut(const ScanArgs& a) {
+  constexpr uint64_t kEnough = 1024;                                                  // workgroups of the third launch that fill the device
+  RearCut K{};
+  const uint32_t channels = wave_channels(a.states), each = a.width / a.groups;
+  K.chunks = (a.steps + kChunk - 1u) / kChunk;
+  K.across = (each + kRearWaves * channels - 1u) / (kRearWaves * channels);
+  K.blocks = (each + channels - 1u) / channels;
+  const uint64_t apart = static_cast<uint64_t>(a.batch) * K.chunks * a.groups;
+  const uint64_t want = apart > 0u ? (kEnough + apart - 1u) / apart : 1u;
+  K.splits = static_cast<uint32_t>(want < K.blocks ? want : K.blocks);
+  return K;
+}
+
+struct RearWords {
+  uint64_t ends, sums, cuts, parts, rows;                                             // 32-bit words of each
+  uint64_t all() const { return ends + sums + cuts + parts + rows; }
+};
+RearWords rear_words(const ScanArgs& a, const RearCut& k) {
+  const uint64_t slots = static_cast<uint64_t>(a.batch) * k.chunks, joined = k.chunks > 1u ? slots : 0u;
+  return RearWords{joined * a.width * a.states, joined * a.width, joined, slots * a.width * (a.states + 2u),
+                   static_cast<uint64_t>(k.splits) * a.batch * a.steps * 2u * a.groups * a.states};
+}
+
+}  // namespace
+
+uint64_t scan_backward_scratch_words(const ScanArgs& a) { return (rear_words(a, rear_cut(a)).all() + 1u) / 2u; }
+
+hipError_t launch_scan_backward(const ScanArgs& a, const ScanGradArgs& g, int dtype, unsigned long long* scratch, hipStream_t s) {
+  RearCut K = rear_cut(a);
+  const RearWords W = rear_words(a, K);
+  K.ends = reinterpret_cast<float*>(scratch);
+  K.sums = K.ends + W.ends;
+  K.cuts = reinterpret_cast<uint32_t*>(K.sums + W.sums);
+  K.parts = reinterpret_cast<float*>(K.cuts + W.cuts);
+  K.rows = K.parts + W.parts;
+  const uint64_t slots = static_cast<uint64_t>(a.batch) * K.chunks, weights = static_cast<uint64_t>(a.width) * a.states;
+  if (slots > 0u) {
+    const hipError_t e = by_states(a.states, dtype, [&](auto type, auto states, auto lanes) {
+      using T = decltype(type);
+      constexpr int kS = decltype(states)::value, kQ = decltype(lanes)::value;
+      if (K.chunks > 1u) {
+        in_grids((slots - a.batch) * a.groups * K.across, [&](uint64_t begin, dim3 grid) { scan_rear_kernel<T, kS, kQ><<<grid, dim3(64 * kRearWaves), 0, s>>>(a, g, K, begin); });
+        in_grids((a.batch * weights + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_rear_join_kernel<<<grid, dim3(256), 0, s>>>(a, g, K, begin); });
+      }
+      in_grids(slots * a.groups * K.splits, [&](uint64_t begin, dim3 grid) { scan_backward_kernel<T, kS, kQ><<<grid, dim3(64 * kWaves), 0, s>>>(a, g, K, begin); });
+      const uint64_t all = static_cast<uint64_t>(a.batch) * a.steps * 2u * a.groups * a.states;
+      in_grids((all + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_rows_kernel<T><<<grid, dim3(256), 0, s>>>(a, g, K, begin); });
+      return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+  } else if (g.dh0) {
+    const uint64_t count = a.batch * weights;
+    in_grids((count + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_hand_on_kernel<<<grid, dim3(256), 0, s>>>(g.dh_last, g.dh0, count, begin); });
+  }
+  return launch_sum_parts(PartsArgs{K.parts, slots, weights + 2u * a.width, {g.da, g.dd, g.ddelta_bias}, {weights, weights + a.width, weights + 2u * a.width}}, s);
+}
+
+}  // namespace rgc
