@@ -471,8 +471,10 @@ int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* convolu
  *    h0 if it has none.
  *  - A rate of -inf is read as the lowest finite one.  A state that is infinite or NaN makes the later ones so, until one starts anew.
  * h_last may be h0 itself; steps == 1 is the serving form.
- * Limits: batch, steps >= 0, both < 2^31; 1 <= width <= RGC_WIDTH_MAX, a multiple of `groups`; 1 <= states <= RGC_SCAN_STATES_MAX. */
-#define RGC_SCAN_CHUNK 64
+ * Limits: batch, steps >= 0, both < 2^31; 1 <= width <= RGC_WIDTH_MAX, a multiple of `groups`; 1 <= states <= RGC_SCAN_STATES_MAX; strides of steps at most
+ * RGC_SCAN_STRIDE_MAX elements. */
+#define RGC_SCAN_CHUNK 32
+#define RGC_SCAN_STRIDE_MAX 134217728
 #define RGC_SCAN_STATES_MAX 64
 
 typedef struct {

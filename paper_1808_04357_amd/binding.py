@@ -32,7 +32,7 @@ RGC_BF16 = 1
 RGC_F16 = 2
 RGC_TOP_MAX = 128
 RGC_RECURRENCE_CHUNK = 256
-RGC_SCAN_CHUNK = 64
+RGC_SCAN_CHUNK = 32
 RGC_SCAN_STATES_MAX = 64
 RGC_TAPS_MAX = 8
 

@@ -1459,6 +1459,11 @@ ConvArgs convolution_args(const rgc_convolution* r) {
   return A;
 }
 
+// (Eight steps of a row are addressed by 32 bits.)
+bool scan_sequence_fits(const rgc_sequence& v, const rgc_scan* r, int32_t width, bool written) {
+  return sequence_fits(v, r->batch, r->steps, width, r->dtype, written) && (r->steps <= 1 || v.step_stride <= RGC_SCAN_STRIDE_MAX);
+}
+
 // (steps == 0: only h0 and h_last are there; batch == 0: nothing is)
 bool scan_fits(const rgc_scan* r) {
   if (r->batch < 0 || r->batch > kInt32Most || r->steps < 0 || r->steps > kInt32Most || r->width < 1 || r->width > RGC_WIDTH_MAX) return false;
@@ -1467,7 +1472,7 @@ bool scan_fits(const rgc_scan* r) {
   if (!r->a || !words_aligned({r->a, r->d, r->delta_bias, r->lengths, r->h0, r->h_last, r->kept})) return false;
   if (r->batch == 0 || r->steps == 0) return true;
   const int32_t both = r->groups * r->states;
-  auto fits = [&](const rgc_sequence& v, int32_t width) { return sequence_fits(v, r->batch, r->steps, width, r->dtype, false); };
+  auto fits = [&](const rgc_sequence& v, int32_t width) { return scan_sequence_fits(v, r, width, false); };
   return fits(r->x, r->width) && fits(r->delta, r->width) && fits(r->b, both) && fits(r->c, both) && (!r->gate.data || fits(r->gate, r->width));
 }
 
@@ -1704,7 +1709,7 @@ int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* r, cons
 
 int rgc_selective_scan(rgc_ctx* ctx, const rgc_scan* r, void* hip_stream) {
   if (!ctx || !r || !scan_fits(r)) return RGC_EINVAL;
-  if (r->batch > 0 && r->steps > 0 && !sequence_fits(r->y, r->batch, r->steps, r->width, r->dtype, true)) return RGC_EINVAL;
+  if (r->batch > 0 && r->steps > 0 && !scan_sequence_fits(r->y, r, r->width, true)) return RGC_EINVAL;
   if (r->batch == 0) return RGC_OK;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
@@ -1720,7 +1725,7 @@ int rgc_selective_scan_backward(rgc_ctx* ctx, const rgc_scan* r, const rgc_scan_
   if (!ctx || !r || !g || !scan_fits(r) || !g->da || !words_aligned({g->da, g->dd, g->ddelta_bias, g->dh_last, g->dh0})) return RGC_EINVAL;
   if (r->batch > 0 && r->steps > 0) {
     const int32_t both = r->groups * r->states;
-    auto fits = [&](const rgc_sequence& v, int32_t width, bool written) { return sequence_fits(v, r->batch, r->steps, width, r->dtype, written); };
+    auto fits = [&](const rgc_sequence& v, int32_t width, bool written) { return scan_sequence_fits(v, r, width, written); };
     if (!r->kept || !fits(g->dy, r->width, false) || !fits(g->dx, r->width, true) || !fits(g->ddelta, r->width, true)) return RGC_EINVAL;
     if (!fits(g->db, both, true) || !fits(g->dc, both, true) || (r->gate.data && !fits(g->dgate, r->width, true))) return RGC_EINVAL;
   }

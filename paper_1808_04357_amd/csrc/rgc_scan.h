@@ -1,6 +1,6 @@
 // What the kernels of the selective scan share (rgc_scan.hip, rgc_scan_backward.hip).
 //
-// A wave takes 64 / kQ channels of a sequence: kQ lanes have a channel's states, kS each, and kTile steps at a time. What a step has once for all of a channel's states (its size,
+// A wave takes 64 / kQ channels of a sequence: kQ lanes have a channel's states, kS each, and kT steps at a time. What a step has once for all of a channel's states (its size,
 // its input, ...) is computed by one of the channel's lanes, its owner, and handed to the others through shared memory; sums over a channel's states go the other way, by exchanges
 // between neighbouring lanes that leave every owner its steps' sums.  B and C, which all channels of a group share, lie in shared memory in 32 bits.
 #pragma once
@@ -16,17 +16,16 @@
 namespace rgc {
 namespace {
 
-constexpr uint32_t kChunk = 64;        // steps between kept states (RGC_SCAN_CHUNK)
-constexpr uint32_t kTile = 8;          // steps of a wave at a time
+constexpr uint32_t kChunk = 32;        // steps between kept states (RGC_SCAN_CHUNK)
 constexpr float kLn2 = 0.693147180559945309f;
 
 template <int kCtrl>
 __device__ __forceinline__ float from_lane(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xF, 0xF, true));
 }
-// One level of the exchange: lanes whose number has kBit keep the upper half of their sums, the others the lower, and get what the lane across has for it.
-template <int kCtrl, int kBit, int kCount>
-__device__ __forceinline__ void exchange(float (&v)[kTile], uint32_t lane) {
+// One level of the exchange: lanes whose number has kBit keep the upper half of their kCount sums, the others the lower, and get what the lane across has for it.
+template <int kCtrl, int kBit, int kCount, int kAll>
+__device__ __forceinline__ void exchange(float (&v)[kAll], uint32_t lane) {
   if constexpr (kCount >= 2) {
     const bool upper = (lane & kBit) != 0u;
 #pragma unroll
@@ -38,69 +37,107 @@ __device__ __forceinline__ void exchange(float (&v)[kTile], uint32_t lane) {
     v[0] += from_lane<kCtrl>(v[0]);
   }
 }
-// v[t]: a lane's part of step t's sum over the channel's states; afterwards v[0 .. steps it owns) are its steps' sums.
+// The sum over a channel's lanes, in all of them.
 template <int kQ>
-__device__ __forceinline__ void sum_for_owners(float (&v)[kTile], uint32_t lane) {
+__device__ __forceinline__ float sum_lanes(float v) {
+  if constexpr (kQ >= 16) v += from_lane<0x140>(v);
+  if constexpr (kQ >= 8) v += from_lane<0x141>(v);
+  if constexpr (kQ >= 4) v += from_lane<0x4E>(v);
+  if constexpr (kQ >= 2) v += from_lane<0xB1>(v);
+  return v;
+}
+// v[t]: a lane's part of step t's sum over the channel's states; afterwards v[0 .. steps it owns) are its steps' sums.
+template <int kQ, int kT>
+__device__ __forceinline__ void sum_for_owners(float (&v)[kT], uint32_t lane) {
   static_assert(kQ == 1 || kQ == 2 || kQ == 4 || kQ == 8 || kQ == 16, "lanes of a channel");
-  if constexpr (kQ >= 16) exchange<0x140, 8, kTile>(v, lane);                         // row_mirror
-  if constexpr (kQ >= 8) exchange<0x141, 4, kQ >= 16 ? kTile / 2 : kTile>(v, lane);   // row_half_mirror
-  if constexpr (kQ >= 4) exchange<0x4E, 2, kQ >= 16 ? kTile / 4 : kQ >= 8 ? kTile / 2 : kTile>(v, lane);                            // quad_perm 2 3 0 1
-  if constexpr (kQ >= 2) exchange<0xB1, 1, kQ >= 16 ? kTile / 8 : kQ >= 8 ? kTile / 4 : kQ >= 4 ? kTile / 2 : kTile>(v, lane);      // quad_perm 1 0 3 2
+  constexpr int k8 = kQ >= 16 ? kT / 2 : kT, k4 = kQ >= 8 ? k8 / 2 : k8, k2 = kQ >= 4 ? k4 / 2 : k4;      // sums left before a level (0 as one)
+  if constexpr (kQ >= 16) exchange<0x140, 8, kT>(v, lane);       // row_mirror
+  if constexpr (kQ >= 8) exchange<0x141, 4, k8>(v, lane);        // row_half_mirror
+  if constexpr (kQ >= 4) exchange<0x4E, 2, k4>(v, lane);         // quad_perm 2 3 0 1
+  if constexpr (kQ >= 2) exchange<0xB1, 1, k2>(v, lane);         // quad_perm 1 0 3 2
 }
 
 // Where a lane is: its channel, its states, its steps of a tile.
-template <int kS, int kQ>
+template <int kS, int kQ, int kT>
 struct Spot {
-  static constexpr uint32_t kChannels = 64 / kQ, kStates = kS * kQ, kOwn = kQ >= 8 ? 1 : kTile / kQ;
+  static constexpr uint32_t kChannels = 64 / kQ, kStates = kS * kQ, kOwn = kQ >= kT ? 1 : kT / kQ, kShare = kQ > kT ? kQ / kT : 1;      // kShare lanes own the same step
   uint32_t lane, channel, q, own;      // within the wave; the first of its steps
   uint32_t c;                          // of the sequence (the group's last one in a lane behind it)
-  bool mine, owner;                    // it is a channel of the group; the lane stores its steps' results
+  bool mine, first, owner;             // it is a channel of the group; the first lane that owns its step; the lane stores its steps' results
   // block: how many waves' channels of the group come before
-  __device__ Spot(const ScanArgs& A, uint32_t group, uint32_t block) {
+  __device__ Spot(const ScanArgs& A, uint32_t group, uint32_t block) : Spot(A, group, block, threadIdx.x & 63u) {}
+  __device__ Spot(const ScanArgs& A, uint32_t group, uint32_t block, uint32_t in_wave) {
     const uint32_t each = A.width / A.groups;
-    lane = threadIdx.x & 63u;
+    lane = in_wave;
     channel = lane / kQ;
     q = lane % kQ;
-    own = kQ == 16 ? q / 2u : q * kOwn;
+    own = q * kOwn / kShare;
     const uint32_t at = block * kChannels + channel;
     mine = at < each;
-    owner = mine && (kQ < 16 || q % 2u == 0u);
+    first = q % kShare == 0u;
+    owner = mine && first;
     c = group * each + min(at, each - 1u);
   }
 };
 
-// A channel's rates for the lane's states, in powers of two.  Finite, so that a step that is not there (its size 0) has the decay 1.
+// Where a lane's states lie in a [.., width, states] tensor: bytes from its row for the sequence (and chunk), which is the same for the whole wave.
+template <int kS, int kQ, int kT>
+__device__ __forceinline__ uint32_t states_at(const ScanArgs& A, const Spot<kS, kQ, kT>& at) {
+  return (at.c * A.states + at.q * kS) * static_cast<uint32_t>(sizeof(float));
+}
+// The states that lie there; zeros for those that a channel does not have.  (No branch but one that the whole wave takes.)
 template <int kS, int kQ>
-__device__ __forceinline__ void rates_of(const ScanArgs& A, const Spot<kS, kQ>& at, float (&rate)[kS]) {
+__device__ __forceinline__ void read_states(const float* row, const ScanArgs& A, uint32_t q, uint32_t offset, float (&h)[kS]) {
+  const char* base = reinterpret_cast<const char*>(row);
+  if (A.states == kS * kQ) {
+    if constexpr (kS == 4 || kS == 2) {
+      const Raw<float, kS> r = read_at<float, kS>(reinterpret_cast<const float*>(base + offset));
+#pragma unroll
+      for (uint32_t s = 0; s < kS; ++s) h[s] = r.v[s];
+    } else {
+#pragma unroll
+      for (uint32_t s = 0; s < kS; ++s) h[s] = *reinterpret_cast<const float*>(base + (offset + s * 4u));
+    }
+  } else {
+    const uint32_t first = offset - q * kS * 4u;
+#pragma unroll
+    for (uint32_t s = 0; s < kS; ++s) {
+      const float v = *reinterpret_cast<const float*>(base + (first + min(q * kS + s, A.states - 1u) * 4u));
+      h[s] = q * kS + s < A.states ? v : 0.0f;
+    }
+  }
+}
+template <int kS, int kQ, int kT>
+__device__ __forceinline__ void write_states(float* row, const ScanArgs& A, const Spot<kS, kQ, kT>& at, const float (&h)[kS]) {
+  if (!at.mine) return;
+  float* p = reinterpret_cast<float*>(reinterpret_cast<char*>(row) + states_at(A, at));
+  if ((kS == 4 || kS == 2) && A.states == kS * kQ) {
+    write_at<float, kS == 3 ? 1 : kS>(p, *reinterpret_cast<const float(*)[kS == 3 ? 1 : kS]>(&h));
+  } else {
+#pragma unroll
+    for (uint32_t s = 0; s < kS; ++s)
+      if (at.q * kS + s < A.states) p[s] = h[s];
+  }
+}
+
+// A channel's rates for the lane's states, in powers of two.  Finite, so that a step that is not there (its size 0) has the decay 1.
+template <int kS>
+__device__ __forceinline__ void finite_rates(float (&rate)[kS]) {
 #pragma unroll
   for (uint32_t s = 0; s < kS; ++s) {
-    const uint32_t n = at.q * kS + s;
-    float r = n < A.states ? A.a[static_cast<uint64_t>(at.c) * A.states + n] * kLog2e : 0.0f;
+    float r = rate[s] * kLog2e;
     r = r > 3.0e38f ? 3.0e38f : r;
     rate[s] = r < -3.0e38f ? -3.0e38f : r;
   }
 }
-
-// The lane's states of a [.., width, states] tensor whose row for the sequence (and chunk) begins at `from`.
-template <int kS, int kQ>
-__device__ __forceinline__ void read_states(const float* from, const ScanArgs& A, const Spot<kS, kQ>& at, float (&h)[kS]) {
-  const float* p = from + static_cast<uint64_t>(at.c) * A.states + at.q * kS;
-  if (kS == 4 && A.states == kS * kQ) {
-    const Raw<float, 4> r = read_at<float, 4>(p);
-#pragma unroll
-    for (uint32_t s = 0; s < kS; ++s) h[s] = r.v[s & 3u];
-  } else {
-#pragma unroll
-    for (uint32_t s = 0; s < kS; ++s) h[s] = at.q * kS + s < A.states ? p[s] : 0.0f;
-  }
+template <int kS, int kQ, int kT>
+__device__ __forceinline__ void rates_of(const ScanArgs& A, const Spot<kS, kQ, kT>& at, float (&rate)[kS]) {
+  read_states<kS, kQ>(A.a, A, at.q, states_at(A, at), rate);
+  finite_rates(rate);
 }
-template <int kS, int kQ>
-__device__ __forceinline__ void write_states(float* to, const ScanArgs& A, const Spot<kS, kQ>& at, const float (&h)[kS]) {
-  if (!at.mine) return;
-  float* p = to + static_cast<uint64_t>(at.c) * A.states + at.q * kS;
-#pragma unroll
-  for (uint32_t s = 0; s < kS; ++s)
-    if (at.q * kS + s < A.states) p[s] = h[s];
+template <int kS, int kQ, int kT>
+__device__ __forceinline__ void read_states(const float* row, const ScanArgs& A, const Spot<kS, kQ, kT>& at, float (&h)[kS]) {
+  read_states<kS, kQ>(row, A, at.q, states_at(A, at), h);
 }
 
 // ln(1 + exp(v)), with what it is beside exp(v) where that is small: the power is corrected by what its exponent lost in rounding, the sum 1 + e by what it lost.
@@ -129,6 +166,43 @@ __device__ __forceinline__ T* element(const SequenceView& v, uint32_t b, uint32_
   return static_cast<T*>(v.data) + (b * v.batch_stride + t * v.step_stride + c);
 }
 
+// A lane's elements of one tensor: a row's address, the same for the whole wave, and the lane's own steps and channel as 32 bits of offset from it.  (A tile's steps span less than
+// 2^32 bytes: the host refuses strides beyond.)
+template <typename T>
+struct Column {
+  char* row;
+  int64_t step;
+  uint32_t offset;
+  __device__ Column(const SequenceView& v, uint32_t b, uint32_t first, uint32_t own, uint32_t c)
+      : row(reinterpret_cast<char*>(element<T>(v, b, first, 0u))), step(v.step_stride * static_cast<int64_t>(sizeof(T))),
+        offset((own * static_cast<uint32_t>(v.step_stride) + c) * static_cast<uint32_t>(sizeof(T))) {}
+  // the j-th step behind the lane's first, a uniform number of bytes along the row
+  __device__ T& at(uint32_t j, uint32_t along = 0u) const { return *reinterpret_cast<T*>(row + static_cast<int64_t>(j) * step + (offset + along)); }
+};
+
+// A chunk's rows of B or C on their way to shared memory in 32 bits, kStates a step (zeros behind the group's states), by the workgroup's kThreads threads: asked for well before they are needed.
+template <typename T, uint32_t kStates, uint32_t kThreads>
+struct Staged {
+  static constexpr uint32_t kEach = (kChunk * kStates + kThreads - 1u) / kThreads;
+  T v[kEach];
+  __device__ void ask(const SequenceView& from, const ScanArgs& A, uint32_t b, uint32_t g, uint32_t first, uint32_t count) {
+    const char* row = reinterpret_cast<const char*>(element<T>(from, b, first, g * A.states));
+    const int64_t step = from.step_stride * static_cast<int64_t>(sizeof(T));
+#pragma unroll
+    for (uint32_t r = 0; r < kEach; ++r) {
+      const uint32_t i = threadIdx.x + r * kThreads, t = i / kStates, n = i % kStates;
+      v[r] = t < count && n < A.states ? *reinterpret_cast<const T*>(row + t * step + n * sizeof(T)) : static_cast<T>(0.0f);
+    }
+  }
+  __device__ void put(float* to) const {
+#pragma unroll
+    for (uint32_t r = 0; r < kEach; ++r) {
+      const uint32_t i = threadIdx.x + r * kThreads;
+      if (kChunk * kStates % kThreads == 0u || i < kChunk * kStates) to[i] = static_cast<float>(v[r]);
+    }
+  }
+};
+
 // An owner's steps of one tensor, from step `first` on; those at `end` and beyond are not looked at and read as 0.
 template <typename T, uint32_t kOwn>
 struct Own {
@@ -146,19 +220,22 @@ struct Own {
   }
 };
 
-// Rows of B or C in 32 bits: steps [first, first + count) of group g, kStates apart (zeros behind the group's states), by the workgroup's kThreads threads.
+// A chunk's rows of B or C in 32 bits: `count` of them, and zeros behind, kStates a step, by the workgroup's kThreads threads.
 template <typename T, uint32_t kStates, uint32_t kThreads>
 __device__ __forceinline__ void stage(float* to, const SequenceView& from, const ScanArgs& A, uint32_t b, uint32_t g, uint32_t first, uint32_t count) {
-  for (uint32_t i = threadIdx.x; i < count * kStates; i += kThreads) {
-    const uint32_t t = i / kStates, n = i % kStates;
-    to[i] = n < A.states ? static_cast<float>(*element<T>(from, b, first + t, g * A.states + n)) : 0.0f;
-  }
+  Staged<T, kStates, kThreads> rows;
+  rows.ask(from, A, b, g, first, count);
+  rows.put(to);
 }
 
 // kS neighbouring numbers of shared memory.
 template <int kS>
 __device__ __forceinline__ void read_shared(const float* p, float (&v)[kS]) {
-  if constexpr (kS == 4) {
+  if constexpr (kS == 2) {
+    typedef float two __attribute__((ext_vector_type(2)));
+    const two r = *reinterpret_cast<const two*>(p);
+    v[0] = r.x, v[1] = r.y;
+  } else if constexpr (kS == 4) {
     typedef float four __attribute__((ext_vector_type(4)));
     const four r = *reinterpret_cast<const four*>(p);
     v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w;
@@ -167,13 +244,37 @@ __device__ __forceinline__ void read_shared(const float* p, float (&v)[kS]) {
     for (int s = 0; s < kS; ++s) v[s] = p[s];
   }
 }
-__device__ __forceinline__ void read_tile(const float* p, float (&v)[kTile]) {
-  float low[4], high[4];
-  read_shared<4>(p, low);
-  read_shared<4>(p + 4, high);
+template <int kS>
+__device__ __forceinline__ void write_shared(float* p, const float (&v)[kS]) {
+  if constexpr (kS == 2) {
+    typedef float two __attribute__((ext_vector_type(2)));
+    *reinterpret_cast<two*>(p) = two{v[0], v[1]};
+  } else if constexpr (kS == 4) {
+    typedef float four __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<four*>(p) = four{v[0], v[1], v[2], v[3]};
+  } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = low[i], v[i + 4] = high[i];
+    for (int s = 0; s < kS; ++s) p[s] = v[s];
+  }
 }
+template <int kT>
+__device__ __forceinline__ void read_tile(const float* p, float (&v)[kT]) {
+#pragma unroll
+  for (int t = 0; t < kT; t += 4) {
+    float part[4];
+    read_shared<4>(p + t, part);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[t + i] = part[i];
+  }
+}
+
+// A number that the compiler takes for a new one here: it does not compute what follows from it earlier, to hold it in registers all the way to its use.
+__device__ __forceinline__ uint32_t here(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+// A number that is computed here, and not where it is used, from the several that it is made of.
+__device__ __forceinline__ void held(float& v) { asm volatile("" : "+v"(v)); }
 
 // What lanes of one wave have written to shared memory is there for the others of it.  (The wave's accesses are carried out in their order; the compiler keeps it.)
 __device__ __forceinline__ void wave_sync() {
@@ -181,18 +282,18 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Bit i: the state starts anew at step first + i (of those the row has).
+// Bit i: the state starts anew at step first + i (of the chunk that begins there, and of those the row has).
 __device__ __forceinline__ uint64_t anew_from(const ScanArgs& A, uint32_t b, uint32_t first, uint32_t n) {
   if (!A.resets) return 0u;
-  const uint32_t t = first + (threadIdx.x & 63u);
-  return __ballot(t < n && A.resets[static_cast<uint64_t>(b) * A.steps + t] != 0);
+  const uint32_t i = threadIdx.x & 63u, t = first + i;
+  return __ballot(i < kChunk && t < n && A.resets[static_cast<uint64_t>(b) * A.steps + t] != 0);
 }
 
 // Steps of [first, first + most) that are before `end`.
 __device__ __forceinline__ uint32_t steps_in(uint32_t first, uint32_t most, uint32_t end) { return min(max(end, first) - first, most); }
 
-// Calls f with the type, the states a lane and the lanes a channel as constants.  Fewer lanes a channel mean fewer exchanges, more of them fewer registers.
-template <typename F>
+// Calls f with the type, the states a lane and the lanes a channel as constants.  Fewer lanes a channel mean fewer exchanges and less to be done once a channel, more of them more waves.
+template <bool kBackward, typename F>
 hipError_t by_states(uint32_t states, int dtype, F&& f) {
   auto with = [&](auto s, auto q) {
     if (dtype == 0) return f(float{}, s, q);
@@ -200,17 +301,27 @@ hipError_t by_states(uint32_t states, int dtype, F&& f) {
     return f(_Float16{}, s, q);
   };
   typedef std::integral_constant<int, 1> One;
+  typedef std::integral_constant<int, 2> Two;
+  typedef std::integral_constant<int, 3> Three;
   typedef std::integral_constant<int, 4> Four;
+  typedef std::integral_constant<int, 8> Eight;
   if (states == 1u) return with(One{}, One{});
   if (states <= 4u) return with(Four{}, One{});
-  if (states <= 8u) return with(Four{}, std::integral_constant<int, 2>{});
-  if (states <= 16u) return with(Four{}, Four{});
-  if (states <= 24u) return with(std::integral_constant<int, 3>{}, std::integral_constant<int, 8>{});
-  if (states <= 32u) return with(Four{}, std::integral_constant<int, 8>{});
+  if (states <= 8u) return with(Four{}, Two{});
+  if constexpr (kBackward) {
+    if (states <= 16u) return with(Four{}, Four{});
+  } else {
+    if (states <= 16u) return with(Two{}, Eight{});
+  }
+  if (states <= 24u) return with(Three{}, Eight{});
+  if (states <= 32u) return with(Four{}, Eight{});
   return with(Four{}, std::integral_constant<int, 16>{});
 }
 // The same choice for the host: channels of a wave.
-inline uint32_t wave_channels(uint32_t states) { return states <= 4u ? 64u : states <= 8u ? 32u : states <= 16u ? 16u : states <= 32u ? 8u : 4u; }
+template <bool kBackward>
+uint32_t wave_channels(uint32_t states) {
+  return states <= 4u ? 64u : states <= 8u ? 32u : states <= 16u ? (kBackward ? 16u : 8u) : states <= 32u ? 8u : 4u;
+}
 
 }  // namespace
 }  // namespace rgc

@@ -15,14 +15,17 @@ namespace rgc {
 namespace {
 
 constexpr uint32_t kWaves = 4;         // of a workgroup
+constexpr uint32_t kTile = 8;          // steps of a wave at a time
 
 // kSummary: what a stretch does to a state, instead of its results.
+// What memory gives is asked for early: x, delta and the gate of kTiles tiles while those before are walked, B and C of a chunk during the chunk before.
 template <typename T, int kS, int kQ, bool kSummary>
 __global__ void __launch_bounds__(64 * kWaves) scan_kernel(ScanArgs A, ScanCut K, uint64_t begin) {
-  typedef Spot<kS, kQ> At;
+  typedef Spot<kS, kQ, kTile> At;
   constexpr uint32_t kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
-  __shared__ __attribute__((aligned(16))) float rows_b[kChunk * kStates], rows_c[kSummary ? 1 : kChunk * kStates];
-  __shared__ __attribute__((aligned(16))) float sizes[kWaves][kChannels * kTile], feeds[kWaves][kChannels * kTile];
+  constexpr uint32_t kTiles = kOwn == 1 ? 4 : kOwn == 2 ? 2 : 1, kSteps = kTiles * kTile, kApart = kTiles > 1 ? kSteps + 4 : kSteps;   // (apart: lanes of neighbouring channels in other banks)
+  __shared__ __attribute__((aligned(16))) float rows_b[2][kChunk * kStates], rows_c[2][kSummary ? 4 : kChunk * kStates];
+  __shared__ __attribute__((aligned(16))) float sizes[kWaves][kChannels * kApart], feeds[kWaves][kChannels * kApart];
   uint64_t rest = begin + blockIdx.x;
   const uint32_t wave = uniform(threadIdx.x >> 6);
   const uint32_t block = uniform(static_cast<uint32_t>(rest % K.across)) * kWaves + wave;
@@ -34,104 +37,141 @@ __global__ void __launch_bounds__(64 * kWaves) scan_kernel(ScanArgs A, ScanCut K
   const At at(A, g, block);
   const uint32_t n = steps_of(A.lengths, b, A.steps);
   const uint64_t states_of_row = static_cast<uint64_t>(A.width) * A.states;
+  const uint32_t first_chunk = stretch * K.stretch, last_chunk = min(first_chunk + K.stretch, K.chunks);
+  const bool gate = !kSummary && A.gate.data != nullptr;
   float rate[kS], h[kS] = {};
+  Staged<T, kStates, 64 * kWaves> next_b, next_c;
+  auto ask_rows = [&](uint32_t chunk) {
+    const uint32_t count = steps_in(chunk * kChunk, kChunk, n);
+    next_b.ask(A.b, A, b, g, chunk * kChunk, count);
+    if constexpr (!kSummary) next_c.ask(A.c, A, b, g, chunk * kChunk, count);
+  };
+  auto put_rows = [&](uint32_t chunk) {
+    next_b.put(rows_b[chunk & 1u]);
+    if constexpr (!kSummary) next_c.put(rows_c[chunk & 1u]);
+  };
+  T x[kTiles][kOwn], v[kTiles][kOwn], z[kTiles][kOwn];
+  Column<T> from_x(A.x, b, first_chunk * kChunk, at.own, at.c), from_v(A.delta, b, first_chunk * kChunk, at.own, at.c), from_z(gate ? A.gate : A.x, b, first_chunk * kChunk, at.own, at.c);
+  auto ask = [&](uint32_t t0) {                                                       // the next steps; those behind the row's end are not looked at
+    auto each = [&](auto whole) __attribute__((always_inline)) {
+#pragma unroll
+      for (uint32_t m = 0; m < kTiles; ++m) {
+#pragma unroll
+        for (uint32_t j = 0; j < kOwn; ++j) {
+          x[m][j] = v[m][j] = z[m][j] = static_cast<T>(0.0f);
+          if (decltype(whole){} || t0 + m * kTile + at.own + j < n) {
+            x[m][j] = from_x.at(m * kTile + j);
+            v[m][j] = from_v.at(m * kTile + j);
+            if (gate) z[m][j] = from_z.at(m * kTile + j);
+          }
+        }
+      }
+    };
+    if (t0 + kSteps <= n) each(Yes{}); else each(No{});
+    from_x.row += kSteps * from_x.step, from_v.row += kSteps * from_v.step, from_z.row += kSteps * from_z.step;
+  };
+  const uint32_t first_step = first_chunk * kChunk, end = min(n, last_chunk * kChunk);      // of the stretch's walk
+  if (first_step < end) {
+    ask_rows(first_chunk);
+    ask(first_step);
+  }
   rates_of(A, at, rate);
   const float through = !kSummary && A.d ? A.d[at.c] : 0.0f, bias = A.delta_bias ? A.delta_bias[at.c] : 0.0f;
   if constexpr (!kSummary) {
     if (K.stretches > 1u) read_states(K.starts + (static_cast<uint64_t>(b) * K.stretches + stretch) * states_of_row, A, at, h);
     else if (A.h0) read_states(A.h0 + b * states_of_row, A, at, h);
   }
+  if (first_step < end) {
+    put_rows(first_chunk);
+    __syncthreads();
+  }
   float total = 0.0f;                  // of the owner's steps' sizes
   uint64_t cut = 0u;
-  const uint32_t last_chunk = min((stretch + 1u) * K.stretch, K.chunks);
-  for (uint32_t chunk = stretch * K.stretch; chunk < last_chunk; ++chunk) {
+  Column<T> to_y(kSummary ? A.x : A.y, b, first_step, at.own, at.c);
+  for (uint32_t chunk = first_chunk; chunk < last_chunk; ++chunk) {
     const uint32_t first = chunk * kChunk, count = steps_in(first, kChunk, n);
     if (!kSummary && A.kept) write_states(A.kept + (static_cast<uint64_t>(b) * K.chunks + chunk) * states_of_row, A, at, h);
-    if (count > 0u) {                  // (the same for the whole workgroup)
-      __syncthreads();
-      stage<T, kStates, 64 * kWaves>(rows_b, A.b, A, b, g, first, count);
-      if constexpr (!kSummary) stage<T, kStates, 64 * kWaves>(rows_c, A.c, A, b, g, first, count);
-      __syncthreads();
-    }
+    const bool more = chunk + 1u < last_chunk && first + kChunk < n;
+    if (more) ask_rows(chunk + 1u);
     const uint64_t anew = anew_from(A, b, first, n);
     cut |= anew;
-    Own<T, kOwn> x, v, z;
-    auto ask = [&](uint32_t t) {
-      if (t + kTile <= n) {
-        x.read(A.x, b, t + at.own, at.c), v.read(A.delta, b, t + at.own, at.c);
-        if (!kSummary && A.gate.data) z.read(A.gate, b, t + at.own, at.c);
-      } else {
-        x.read(A.x, b, t + at.own, n, at.c), v.read(A.delta, b, t + at.own, n, at.c);
-        if (!kSummary && A.gate.data) z.read(A.gate, b, t + at.own, n, at.c);
-      }
-    };
-    if (count > 0u) ask(first);
-    for (uint32_t tile = 0; tile < count; tile += kTile) {
-      const uint32_t t0 = first + tile, valid = min(count - tile, kTile);
-      float input[kOwn], shown[kOwn];
+    const float *const in_b = rows_b[chunk & 1u] + at.q * kS, *const in_c = rows_c[chunk & 1u] + (kSummary ? 0u : at.q * kS);
+    for (uint32_t part = 0; part < count; part += kSteps) {
+      const uint32_t t0 = first + part;
+      float input[kTiles][kOwn], shown[kTiles][kOwn];
 #pragma unroll
-      for (uint32_t j = 0; j < kOwn; ++j) {
-        float grow, size = size_of(A, static_cast<float>(v.v[j]), bias, grow);
-        if (t0 + at.own + j >= n) size = 0.0f;                                       // (what is not there was read as 0)
-        input[j] = static_cast<float>(x.v[j]);
-        sizes[wave][at.channel * kTile + at.own + j] = size;
-        feeds[wave][at.channel * kTile + at.own + j] = size * input[j];
-        if constexpr (kSummary) {
-          total += size;
-        } else {
-          shown[j] = 1.0f;
-          if (A.gate.data) {
-            const float zj = static_cast<float>(z.v[j]);
-            float open, shut;
-            gate_of(zj, open, shut);
-            shown[j] = zj * open;
+      for (uint32_t m = 0; m < kTiles; ++m) {
+#pragma unroll
+        for (uint32_t j = 0; j < kOwn; ++j) {
+          float grow, size = size_of(A, static_cast<float>(v[m][j]), bias, grow);
+          if (t0 + m * kTile + at.own + j >= n) size = 0.0f;                         // (what is not there was read as 0)
+          input[m][j] = static_cast<float>(x[m][j]);
+          sizes[wave][at.channel * kApart + m * kTile + at.own + j] = size;
+          feeds[wave][at.channel * kApart + m * kTile + at.own + j] = size * input[m][j];
+          if constexpr (kSummary) {
+            total += size;
+          } else {
+            shown[m][j] = 1.0f;
+            if (gate) {
+              const float zj = static_cast<float>(z[m][j]);
+              float open, shut;
+              gate_of(zj, open, shut);
+              shown[m][j] = zj * open;
+            }
           }
         }
       }
-      if (tile + kTile < count) ask(t0 + kTile);
+      if (t0 + kSteps < end) ask(t0 + kSteps);
       wave_sync();
-      float size[kTile], fed[kTile], y[kTile] = {};
-      read_tile(&sizes[wave][at.channel * kTile], size);
-      read_tile(&feeds[wave][at.channel * kTile], fed);
-      const uint32_t starts = static_cast<uint32_t>(anew >> tile) & 0xFFu;
-      auto walk = [&](auto plain) __attribute__((always_inline)) {
-        constexpr bool kPlain = decltype(plain){};
 #pragma unroll
-        for (uint32_t t = 0; t < kTile; ++t) {
-          if (!kPlain && t >= valid) continue;
-          float in[kS], out[kS];
-          read_shared<kS>(&rows_b[(tile + t) * kStates + at.q * kS], in);
-          if constexpr (!kSummary) read_shared<kS>(&rows_c[(tile + t) * kStates + at.q * kS], out);
+      for (uint32_t m = 0; m < kTiles; ++m) {
+        const uint32_t tile = part + m * kTile, valid = steps_in(tile, kTile, count);
+        if (valid == 0u) continue;
+        float size[kTile], fed[kTile], y[kTile] = {};
+        read_tile(&sizes[wave][at.channel * kApart + m * kTile], size);
+        read_tile(&feeds[wave][at.channel * kApart + m * kTile], fed);
+        const uint32_t starts = static_cast<uint32_t>(anew >> tile) & 0xFFu;
+        // (a step that is not there has the size 0 and brings nothing: it leaves the states as they are)
+        auto walk = [&](auto with_starts) __attribute__((always_inline)) {
 #pragma unroll
-          for (uint32_t s = 0; s < kS; ++s) {
-            if (!kPlain && ((starts >> t) & 1u) != 0u) h[s] = 0.0f;
-            h[s] = __fmaf_rn(__builtin_amdgcn_exp2f(size[t] * rate[s]), h[s], fed[t] * in[s]);
-            if constexpr (!kSummary) y[t] = __fmaf_rn(h[s], out[s], y[t]);
+          for (uint32_t t = 0; t < kTile; ++t) {
+            float in[kS], out[kS];
+            read_shared<kS>(in_b + (tile + t) * kStates, in);
+            if constexpr (!kSummary) read_shared<kS>(in_c + (tile + t) * kStates, out);
+#pragma unroll
+            for (uint32_t s = 0; s < kS; ++s) {
+              if (with_starts && ((starts >> t) & 1u) != 0u) h[s] = 0.0f;
+              h[s] = __fmaf_rn(__builtin_amdgcn_exp2f(size[t] * rate[s]), h[s], fed[t] * in[s]);
+              if constexpr (!kSummary) y[t] = __fmaf_rn(h[s], out[s], y[t]);
+            }
           }
-        }
-      };
-      if (valid == kTile && starts == 0u) walk(Yes{}); else walk(No{});
-      wave_sync();                     // (before the next tile's sizes take their place)
-      if constexpr (!kSummary) {
-        sum_for_owners<kQ>(y, at.lane);
-        T* to = element<T>(A.y, b, t0 + at.own, at.c);
+        };
+        if (starts == 0u) walk(No{}); else walk(Yes{});
+        if constexpr (!kSummary) {
+          sum_for_owners<kQ, kTile>(y, at.lane);
 #pragma unroll
-        for (uint32_t j = 0; j < kOwn; ++j, to += A.y.step_stride)
-          if (at.owner && at.own + j < valid) *to = static_cast<T>(__fmaf_rn(through, input[j], y[j]) * shown[j]);
+          for (uint32_t j = 0; j < kOwn; ++j)
+            if (at.owner && at.own + j < valid) to_y.at(m * kTile + j) = static_cast<T>(__fmaf_rn(through, input[m][j], y[j]) * shown[m][j]);
+        }
       }
+      wave_sync();                     // (before the next tiles' sizes take their place)
+      to_y.row += kSteps * to_y.step;
     }
     if constexpr (!kSummary) {
       const uint32_t behind = steps_in(first, kChunk, A.steps);
       for (uint32_t t = count + at.q; t < behind; t += kQ)
         if (at.mine) *element<T>(A.y, b, first + t, at.c) = static_cast<T>(0.0f);
     }
+    if (more) {
+      put_rows(chunk + 1u);
+      __syncthreads();
+    }
   }
   if constexpr (kSummary) {
     const uint64_t slot = static_cast<uint64_t>(b) * K.stretches + stretch;
     write_states(K.starts + slot * states_of_row, A, at, h);
-    if (kQ == 16 && !at.owner) total = 0.0f;
-#pragma unroll
-    for (uint32_t m = 1; m < kQ; m <<= 1) total += __shfl_xor(total, m);
+    if (!at.first) total = 0.0f;
+    total = sum_lanes<kQ>(total);
     if (at.mine && at.q == 0u) K.sums[slot * A.width + at.c] = total;
     if (g == 0u && block == 0u && at.lane == 0u) K.cuts[slot] = cut != 0u ? 1u : 0u;
   } else {
@@ -177,7 +217,7 @@ ScanCut scan_cut(const ScanArgs& a) {
   constexpr uint64_t kFew = 768, kEnough = 4096;
   ScanCut K{};
   K.chunks = (a.steps + kChunk - 1u) / kChunk;
-  const uint32_t channels = kWaves * wave_channels(a.states), each = a.width / a.groups;
+  const uint32_t channels = kWaves * wave_channels<false>(a.states), each = a.width / a.groups;
   K.across = (each + channels - 1u) / channels;
   const uint64_t waves = static_cast<uint64_t>(a.batch) * a.groups * ((each + channels / kWaves - 1u) / (channels / kWaves));
   K.stretches = 1u;
@@ -204,7 +244,7 @@ hipError_t launch_scan(const ScanArgs& a, int dtype, unsigned long long* scratch
     K.sums = K.starts + slots * a.width * a.states;
     K.cuts = reinterpret_cast<uint32_t*>(K.sums + slots * a.width);
   }
-  return by_states(a.states, dtype, [&](auto type, auto states, auto lanes) {
+  return by_states<false>(a.states, dtype, [&](auto type, auto states, auto lanes) {
     using T = decltype(type);
     constexpr int kS = decltype(states)::value, kQ = decltype(lanes)::value;
     if (K.stretches > 1u) {

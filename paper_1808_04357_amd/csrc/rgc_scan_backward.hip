@@ -4,7 +4,7 @@
 // So the gradients go through the steps as the states do, the other way.
 //  1. Every chunk but the first from a gradient of zero behind it: what it hands on, and the sum of its steps' sizes (scan_rear_kernel).
 //  2. What comes in behind each chunk, from the last one to the first (scan_rear_join_kernel).  With one chunk neither is needed.
-//  3. A workgroup for each chunk and group of channels (scan_backward_kernel).  Its eight waves take eight steps each, of as many channels as a wave has at a time: each makes its powers,
+//  3. A workgroup for each chunk and group of channels (scan_backward_kernel).  Its eight waves take four steps each, of as many channels as a wave has at a time: each makes its powers,
 //     what its steps do to a state and to a gradient (both from zero), hears from the others what state it begins and what gradient it ends with, and walks its steps in both directions out of
 //     registers: B's and C's gradients, sums over channels, stay in registers over all of the workgroup's channels; those of A, D and delta's bias, sums over steps, are added up over the waves.
 //  4. The workgroups' parts of both are added up in an order made of the sizes alone (scan_rows_kernel, launch_sum_parts).
@@ -19,7 +19,7 @@ namespace rgc {
 namespace {
 
 constexpr uint32_t kRearWaves = 4;     // of a workgroup of the first launch
-constexpr uint32_t kWaves = kChunk / kTile;
+constexpr uint32_t kWaves = 8, kTile = kChunk / kWaves, kRearTile = 8;      // of the third launch; steps of a wave of it and of the first at a time
 
 struct RearCut {
   uint32_t chunks, across;             // workgroups of the first launch for a group's channels
@@ -45,7 +45,8 @@ __device__ __forceinline__ float shown_of(bool gate, float z, float& slope) {
 
 template <typename T, int kS, int kQ>
 __global__ void __launch_bounds__(64 * kRearWaves) scan_rear_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
-  typedef Spot<kS, kQ> At;
+  typedef Spot<kS, kQ, kRearTile> At;
+  constexpr uint32_t kTile = kRearTile;
   constexpr uint32_t kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
   __shared__ __attribute__((aligned(16))) float rows_c[kChunk * kStates], sizes[kRearWaves][kChannels * kTile], grads[kRearWaves][kChannels * kTile];
   uint64_t rest = begin + blockIdx.x;
@@ -66,55 +67,54 @@ __global__ void __launch_bounds__(64 * kRearWaves) scan_rear_kernel(ScanArgs A, 
   const uint64_t anew = anew_from(A, b, first, n);
   float total = 0.0f;
   const uint32_t tiles = (count + kTile - 1u) / kTile;
-  Own<T, kOwn> v, z, dy;
-  auto ask = [&](uint32_t t) {
-    if (t + kTile <= n) {
-      v.read(A.delta, b, t + at.own, at.c), dy.read(G.dy, b, t + at.own, at.c);
-      if (gate) z.read(A.gate, b, t + at.own, at.c);
-    } else {
-      v.read(A.delta, b, t + at.own, n, at.c), dy.read(G.dy, b, t + at.own, n, at.c);
-      if (gate) z.read(A.gate, b, t + at.own, n, at.c);
-    }
-  };
-  if (tiles > 0u) ask(first + (tiles - 1u) * kTile);
-  for (uint32_t i = tiles; i-- > 0u;) {
-    const uint32_t tile = i * kTile, t0 = first + tile, valid = min(count - tile, kTile);
+  T v[kOwn], z[kOwn], dy[kOwn];
+  const Column<T> v_at(A.delta, b, first, at.own, at.c), z_at(gate ? A.gate : A.delta, b, first, at.own, at.c), dy_at(G.dy, b, first, at.own, at.c);
+  auto ask = [&](uint32_t tile) {
 #pragma unroll
     for (uint32_t j = 0; j < kOwn; ++j) {
-      float grow, slope, size = size_of(A, static_cast<float>(v.v[j]), bias, grow);
+      v[j] = z[j] = dy[j] = static_cast<T>(0.0f);
+      if (tile + kTile <= count || tile + at.own + j < count) {
+        v[j] = v_at.at(tile + j), dy[j] = dy_at.at(tile + j);
+        if (gate) z[j] = z_at.at(tile + j);
+      }
+    }
+  };
+  if (tiles > 0u) ask((tiles - 1u) * kTile);
+  for (uint32_t i = tiles; i-- > 0u;) {
+    const uint32_t tile = i * kTile, t0 = first + tile;
+#pragma unroll
+    for (uint32_t j = 0; j < kOwn; ++j) {
+      float grow, slope, size = size_of(A, static_cast<float>(v[j]), bias, grow);
       if (t0 + at.own + j >= n) size = 0.0f;
       total += size;
       sizes[wave][at.channel * kTile + at.own + j] = size;
-      grads[wave][at.channel * kTile + at.own + j] = static_cast<float>(dy.v[j]) * shown_of(gate, gate ? static_cast<float>(z.v[j]) : 0.0f, slope);
+      grads[wave][at.channel * kTile + at.own + j] = static_cast<float>(dy[j]) * shown_of(gate, gate ? static_cast<float>(z[j]) : 0.0f, slope);
     }
-    if (i > 0u) ask(t0 - kTile);
+    if (i > 0u) ask(tile - kTile);
     wave_sync();
     float size[kTile], dinner[kTile];
     read_tile(&sizes[wave][at.channel * kTile], size);
     read_tile(&grads[wave][at.channel * kTile], dinner);
-    const uint32_t starts = static_cast<uint32_t>(anew >> tile) & 0xFFu;
-    auto walk = [&](auto plain) __attribute__((always_inline)) {
-      constexpr bool kPlain = decltype(plain){};
+    const uint32_t starts = static_cast<uint32_t>(anew >> tile) & ((1u << kTile) - 1u);
+    auto walk = [&](auto with_starts) __attribute__((always_inline)) {
 #pragma unroll
       for (uint32_t t = kTile; t-- > 0u;) {
-        if (!kPlain && t >= valid) continue;
         float out[kS];
         read_shared<kS>(&rows_c[(tile + t) * kStates + at.q * kS], out);
 #pragma unroll
         for (uint32_t s = 0; s < kS; ++s) {
           g[s] = __builtin_amdgcn_exp2f(size[t] * rate[s]) * __fmaf_rn(dinner[t], out[s], g[s]);
-          if (!kPlain && ((starts >> t) & 1u) != 0u) g[s] = 0.0f;
+          if (with_starts && ((starts >> t) & 1u) != 0u) g[s] = 0.0f;
         }
       }
     };
-    if (valid == kTile && starts == 0u) walk(Yes{}); else walk(No{});
+    if (starts == 0u) walk(No{}); else walk(Yes{});
     wave_sync();
   }
   const uint64_t slot = static_cast<uint64_t>(b) * K.chunks + chunk;
   write_states(K.ends + slot * (static_cast<uint64_t>(A.width) * A.states), A, at, g);
-  if (kQ == 16 && !at.owner) total = 0.0f;
-#pragma unroll
-  for (uint32_t m = 1; m < kQ; m <<= 1) total += __shfl_xor(total, m);
+  if (!at.first) total = 0.0f;
+  total = sum_lanes<kQ>(total);
   if (at.mine && at.q == 0u) K.sums[slot * A.width + at.c] = total;
   if (group == 0u && block == 0u && at.lane == 0u) K.cuts[slot] = anew != 0u ? 1u : 0u;
 }
@@ -181,12 +181,12 @@ struct SharedBackward {
   float rows_b[kChunk * kStates], rows_c[kChunk * kStates];
   float of_step[kWaves][3][kChannels * kTile];     // sizes, size * input, gradient before the gate
   float parts[2][kWaves][3][64 * kS];              // what a wave's steps do: decay, state, gradient
-  float da[2][kWaves][64 * kS], own[2][kWaves][2][64];
+  float da[2][kWaves][64 * kS], own[2][kWaves][2][kChannels];
 };
 
 template <typename T, int kS, int kQ>
 __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
-  typedef Spot<kS, kQ> At;
+  typedef Spot<kS, kQ, kTile> At;
   constexpr uint32_t kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
   __shared__ __attribute__((aligned(16))) SharedBackward<kS, kQ> lds;
   uint64_t rest = begin + blockIdx.x;
@@ -197,83 +197,94 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
   const uint32_t chunk = uniform(static_cast<uint32_t>(rest % K.chunks)), b = uniform(static_cast<uint32_t>(rest / K.chunks));
   const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, each = A.width / A.groups;
   const uint32_t n = steps_of(A.lengths, b, A.steps), first = chunk * kChunk, count = steps_in(first, kChunk, n);
-  const uint32_t t0 = first + wave * kTile, valid = steps_in(t0, kTile, n);
+  const uint32_t t0 = first + wave * kTile, valid = steps_in(t0, kTile, n), behind = steps_in(t0, kTile, A.steps);
   const bool gate = A.gate.data != nullptr;
   const uint64_t row = static_cast<uint64_t>(A.width) * A.states, slot = static_cast<uint64_t>(b) * K.chunks + chunk;
   stage<T, kStates, 64 * kWaves>(lds.rows_b, A.b, A, b, group, first, count);
   stage<T, kStates, 64 * kWaves>(lds.rows_c, A.c, A, b, group, first, count);
-  __syncthreads();
   const uint64_t anew = anew_from(A, b, first, n);
-  const uint32_t starts = static_cast<uint32_t>(anew >> (wave * kTile)) & 0xFFu;
+  constexpr uint32_t kBits = (1u << kTile) - 1u;
+  const uint32_t starts = static_cast<uint32_t>(anew >> (wave * kTile)) & kBits;
   float sums[2 * kTile * kS] = {};     // of the gradients of B and C
   // the sums over the waves of what an earlier turn left
-  auto finish = [&](uint32_t block, uint32_t turn) {
+  auto finish = [&](uint32_t block, uint32_t turn) __attribute__((always_inline)) {
     float* to = K.parts + slot * (row + 2u * A.width);
-    const uint32_t id = threadIdx.x;
+    const uint32_t id = here(threadIdx.x);
+    float sum = 0.0f;
     if (id < 64u * kS) {
-      const uint32_t l = id / kS, state = l % kQ * kS + id % kS, c = block * kChannels + l / kQ;
-      float sum = 0.0f;
 #pragma unroll
       for (uint32_t w = 0; w < kWaves; ++w) sum += lds.da[turn][w][id];
-      if (c < each && state < A.states) to[static_cast<uint64_t>(group * each + c) * A.states + state] = sum;
+      const uint32_t l = id / kS, state = l % kQ * kS + id % kS, c = block * kChannels + l / kQ;
+      if (c < each && state < A.states) to[(group * each + c) * A.states + state] = sum;
     } else if (id < 64u * kS + 2u * kChannels) {
       const uint32_t which = (id - 64u * kS) / kChannels, channel = (id - 64u * kS) % kChannels, c = block * kChannels + channel;
-      float sum = 0.0f;
-      for (uint32_t w = 0; w < kWaves; ++w) {
-        for (uint32_t q = 0; q < kQ; ++q) sum += lds.own[turn][w][which][channel * kQ + q];
-      }
-      if (c < each) to[row + which * A.width + group * each + c] = sum;
+#pragma unroll
+      for (uint32_t w = 0; w < kWaves; ++w) sum += lds.own[turn][w][which][channel];
+      if (c < each) to[static_cast<uint32_t>(row) + which * A.width + group * each + c] = sum;
     }
   };
   const uint32_t per = (K.blocks + K.splits - 1u) / K.splits, from = split * per, upto = min(from + per, K.blocks);
-  Own<T, kOwn> x, v, z, dy;
-  float h_in[kS], g_in[kS];
-  auto ask = [&](uint32_t block) {
-    const At at(A, group, block);
+  const uint32_t own_step = At(A, group, 0u).own;
+  const Column<T> x_at(A.x, b, t0, own_step, group * each), v_at(A.delta, b, t0, own_step, group * each), z_at(gate ? A.gate : A.x, b, t0, own_step, group * each),
+      dy_at(G.dy, b, t0, own_step, group * each), dx_at(G.dx, b, t0, own_step, group * each), dv_at(G.ddelta, b, t0, own_step, group * each),
+      dz_at(gate ? G.dgate : G.dx, b, t0, own_step, group * each);
+  T x[kOwn], v[kOwn], z[kOwn], dy[kOwn];
+  float rate_in[kS], h_in[kS], g_in[kS] = {}, through_in, bias_in;
+  // what a stretch of channels needs from memory, asked for while the one before is worked on; steps that are not there are not looked at
+  auto ask = [&](uint32_t block) __attribute__((always_inline)) {
+    const At at(A, group, block, here(lane));
+    const uint32_t along = (at.c - group * each) * static_cast<uint32_t>(sizeof(T));
     if (valid == kTile) {
-      x.read(A.x, b, t0 + at.own, at.c), v.read(A.delta, b, t0 + at.own, at.c), dy.read(G.dy, b, t0 + at.own, at.c);
-      if (gate) z.read(A.gate, b, t0 + at.own, at.c);
-    } else if (valid > 0u) {
-      x.read(A.x, b, t0 + at.own, n, at.c), v.read(A.delta, b, t0 + at.own, n, at.c), dy.read(G.dy, b, t0 + at.own, n, at.c);
-      if (gate) z.read(A.gate, b, t0 + at.own, n, at.c);
-    }
-    read_states(A.kept + slot * row, A, at, h_in);
-    if (K.chunks > 1u) {
-      read_states(K.ends + slot * row, A, at, g_in);
-    } else if (G.dh_last) {
-      read_states(G.dh_last + b * row, A, at, g_in);
+#pragma unroll
+      for (uint32_t j = 0; j < kOwn; ++j) {
+        x[j] = x_at.at(j, along), v[j] = v_at.at(j, along), dy[j] = dy_at.at(j, along);
+        z[j] = gate ? z_at.at(j, along) : static_cast<T>(0.0f);
+      }
     } else {
 #pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) g_in[s] = 0.0f;
+      for (uint32_t j = 0; j < kOwn; ++j) {
+        x[j] = v[j] = z[j] = dy[j] = static_cast<T>(0.0f);
+        if (at.own + j < valid) {
+          x[j] = x_at.at(j, along), v[j] = v_at.at(j, along), dy[j] = dy_at.at(j, along);
+          if (gate) z[j] = z_at.at(j, along);
+        }
+      }
     }
+    read_states(A.a, A, at, rate_in);
+    read_states(A.kept + slot * row, A, at, h_in);
+    if (K.chunks > 1u) read_states(K.ends + slot * row, A, at, g_in);
+    else if (G.dh_last) read_states(G.dh_last + b * row, A, at, g_in);
+    through_in = A.d ? A.d[at.c] : 0.0f;
+    bias_in = A.delta_bias ? A.delta_bias[at.c] : 0.0f;
   };
   if (from < upto) ask(from);
+  __syncthreads();
   for (uint32_t block = from; block < upto; ++block) {
     const uint32_t turn = (block - from) & 1u;
-    const At at(A, group, block);
-    float rate[kS];
-    rates_of(A, at, rate);
-    const float through = A.d ? A.d[at.c] : 0.0f, bias = A.delta_bias ? A.delta_bias[at.c] : 0.0f;
+    const At at(A, group, block, here(lane));
+    const uint32_t along = (at.c - group * each) * static_cast<uint32_t>(sizeof(T));
     float input[kOwn], grow[kOwn], size_own[kOwn], dinner_own[kOwn], dgate_by[kOwn];      // dgate_by: the gate's gradient, without its factor `inner`
-    float h[kS], g[kS];
+    float h[kS], g[kS], rate[kS];
+    const float through = through_in;
     float *const of_size = lds.of_step[wave][0] + at.channel * kTile, *const of_fed = lds.of_step[wave][1] + at.channel * kTile, *const of_grad = lds.of_step[wave][2] + at.channel * kTile;
 #pragma unroll
     for (uint32_t j = 0; j < kOwn; ++j) {
-      float slope = 0.0f;
-      input[j] = grow[j] = size_own[j] = dinner_own[j] = dgate_by[j] = 0.0f;
-      if (at.mine && valid > 0u && t0 + at.own + j < n) {        // (lanes behind the group have no part in its sums)
-        input[j] = static_cast<float>(x.v[j]);
-        size_own[j] = size_of(A, static_cast<float>(v.v[j]), bias, grow[j]);
-        const float given = static_cast<float>(dy.v[j]);
-        dinner_own[j] = given * shown_of(gate, gate ? static_cast<float>(z.v[j]) : 0.0f, slope);
-        dgate_by[j] = given * slope;
-      }
+      float slope;
+      const bool there = at.mine && at.own + j < valid;           // (lanes behind the group have no part in its sums)
+      input[j] = there ? static_cast<float>(x[j]) : 0.0f;
+      const float size = size_of(A, static_cast<float>(v[j]), bias_in, grow[j]), given = there ? static_cast<float>(dy[j]) : 0.0f;
+      size_own[j] = there ? size : 0.0f;
+      dinner_own[j] = given * shown_of(gate, static_cast<float>(z[j]), slope);
+      dgate_by[j] = given * slope;
+      if (!there) dinner_own[j] = dgate_by[j] = 0.0f;
+      held(input[j]), held(size_own[j]), held(grow[j]), held(dinner_own[j]), held(dgate_by[j]);
       of_size[at.own + j] = size_own[j];
       of_fed[at.own + j] = size_own[j] * input[j];
       of_grad[at.own + j] = dinner_own[j];
     }
 #pragma unroll
-    for (uint32_t s = 0; s < kS; ++s) h[s] = at.mine ? h_in[s] : 0.0f, g[s] = at.mine ? g_in[s] : 0.0f;
+    for (uint32_t s = 0; s < kS; ++s) rate[s] = rate_in[s], h[s] = at.mine ? h_in[s] : 0.0f, g[s] = at.mine ? g_in[s] : 0.0f;
+    finite_rates(rate);
     if (block + 1u < upto) ask(block + 1u);
     wave_sync();
     float size[kTile], fed[kTile], dinner[kTile];
@@ -281,86 +292,82 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
     read_tile(of_fed, fed);
     read_tile(of_grad, dinner);
     wave_sync();
-    const float *const row_b = lds.rows_b + wave * kTile * kStates + at.q * kS, *const row_c = lds.rows_c + wave * kTile * kStates + at.q * kS;
+    const float *const row_b = lds.rows_b + (wave * kTile * kStates + at.q * kS), *const row_c = lds.rows_c + (wave * kTile * kStates + at.q * kS);
+    // (a step that is not there has the size 0 and brings nothing: it leaves states and gradients as they are)
     float a[kTile][kS], own_h[kS] = {}, own_g[kS] = {}, whole[kS];
-    auto alone = [&](auto plain) __attribute__((always_inline)) {
-      constexpr bool kPlain = decltype(plain){};
+    auto alone = [&](auto with_starts) __attribute__((always_inline)) {
 #pragma unroll
       for (uint32_t t = 0; t < kTile; ++t) {
-        if (!kPlain && t >= valid) continue;
         float in[kS];
         read_shared<kS>(row_b + t * kStates, in);
 #pragma unroll
         for (uint32_t s = 0; s < kS; ++s) {
           a[t][s] = __builtin_amdgcn_exp2f(size[t] * rate[s]);
-          if (!kPlain && ((starts >> t) & 1u) != 0u) own_h[s] = 0.0f;
+          if (with_starts && ((starts >> t) & 1u) != 0u) own_h[s] = 0.0f;
           own_h[s] = __fmaf_rn(a[t][s], own_h[s], fed[t] * in[s]);
         }
       }
 #pragma unroll
       for (uint32_t t = kTile; t-- > 0u;) {
-        if (!kPlain && t >= valid) continue;
         float out[kS];
         read_shared<kS>(row_c + t * kStates, out);
 #pragma unroll
         for (uint32_t s = 0; s < kS; ++s) {
           own_g[s] = a[t][s] * __fmaf_rn(dinner[t], out[s], own_g[s]);
-          if (!kPlain && ((starts >> t) & 1u) != 0u) own_g[s] = 0.0f;
+          if (with_starts && ((starts >> t) & 1u) != 0u) own_g[s] = 0.0f;
         }
       }
     };
-    const bool plain_tile = valid == kTile && starts == 0u;
-    if (plain_tile) alone(Yes{}); else alone(No{});
+    if (starts == 0u) alone(No{}); else alone(Yes{});
     float total = 0.0f;
 #pragma unroll
     for (uint32_t t = 0; t < kTile; ++t) total += size[t];
 #pragma unroll
-    for (uint32_t s = 0; s < kS; ++s) {
-      whole[s] = __builtin_amdgcn_exp2f(total * rate[s]);
-      lds.parts[turn][wave][0][lane * kS + s] = whole[s];
-      lds.parts[turn][wave][1][lane * kS + s] = own_h[s];
-      lds.parts[turn][wave][2][lane * kS + s] = own_g[s];
-    }
+    for (uint32_t s = 0; s < kS; ++s) whole[s] = __builtin_amdgcn_exp2f(total * rate[s]);
+    write_shared<kS>(&lds.parts[turn][wave][0][at.lane * kS], whole);
+    write_shared<kS>(&lds.parts[turn][wave][1][at.lane * kS], own_h);
+    write_shared<kS>(&lds.parts[turn][wave][2][at.lane * kS], own_g);
     __syncthreads();
+    // the state before the wave's steps and the gradient behind them, from the other waves' stretches
+    auto hear = [&](auto with_starts) __attribute__((always_inline)) {
+      for (uint32_t w = 0; w < wave; ++w) {
+        float p[kS], own[kS];
+        read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
+        read_shared<kS>(&lds.parts[turn][w][1][at.lane * kS], own);
+        const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) h[s] = cut ? own[s] : __fmaf_rn(p[s], h[s], own[s]);
+      }
+      for (uint32_t w = kWaves - 1u; w > wave; --w) {
+        float p[kS], own[kS];
+        read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
+        read_shared<kS>(&lds.parts[turn][w][2][at.lane * kS], own);
+        const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) g[s] = cut ? own[s] : __fmaf_rn(p[s], g[s], own[s]);
+      }
+    };
+    if (anew == 0u) hear(No{}); else hear(Yes{});
     if (block > from) finish(block - 1u, turn ^ 1u);
-    for (uint32_t w = 0; w < wave; ++w) {
-      const bool cut = ((anew >> (w * kTile)) & 0xFFull) != 0u;
-      float p[kS], own[kS];
-      read_shared<kS>(&lds.parts[turn][w][0][lane * kS], p);
-      read_shared<kS>(&lds.parts[turn][w][1][lane * kS], own);
-#pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) h[s] = cut ? own[s] : __fmaf_rn(p[s], h[s], own[s]);
-    }
-    for (uint32_t w = kWaves - 1u; w > wave; --w) {
-      const bool cut = ((anew >> (w * kTile)) & 0xFFull) != 0u;
-      float p[kS], own[kS];
-      read_shared<kS>(&lds.parts[turn][w][0][lane * kS], p);
-      read_shared<kS>(&lds.parts[turn][w][2][lane * kS], own);
-#pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) g[s] = cut ? own[s] : __fmaf_rn(p[s], g[s], own[s]);
-    }
     float inner[kTile] = {}, came[kTile] = {}, slower[kTile] = {}, da[kS] = {};
-    auto walk = [&](auto plain) __attribute__((always_inline)) {
-      constexpr bool kPlain = decltype(plain){};
+    auto walk = [&](auto with_starts) __attribute__((always_inline)) {
       float after[kTile][kS];
 #pragma unroll
       for (uint32_t t = 0; t < kTile; ++t) {
-        if (!kPlain && t >= valid) continue;
         float in[kS];
         read_shared<kS>(row_b + t * kStates, in);
 #pragma unroll
         for (uint32_t s = 0; s < kS; ++s) {
           const float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
-          after[t][s] = __fmaf_rn(a[t][s], !kPlain && ((starts >> t) & 1u) != 0u ? 0.0f : prior, fed[t] * in[s]);
+          after[t][s] = __fmaf_rn(a[t][s], with_starts && ((starts >> t) & 1u) != 0u ? 0.0f : prior, fed[t] * in[s]);
         }
       }
 #pragma unroll
       for (uint32_t t = kTile; t-- > 0u;) {
-        if (!kPlain && t >= valid) continue;
         float in[kS], out[kS];
         read_shared<kS>(row_b + t * kStates, in);
         read_shared<kS>(row_c + t * kStates, out);
-        const bool anew_here = !kPlain && ((starts >> t) & 1u) != 0u;
+        const bool anew_here = with_starts && ((starts >> t) & 1u) != 0u;
 #pragma unroll
         for (uint32_t s = 0; s < kS; ++s) {
           float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
@@ -378,17 +385,12 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
         }
       }
     };
-    if (plain_tile) walk(Yes{}); else walk(No{});
+    if (starts == 0u) walk(No{}); else walk(Yes{});
     if (G.dh0 && chunk == 0u && wave == 0u) write_states(G.dh0 + b * row, A, at, g);
-    if (!gate && A.d == nullptr) {     // (nothing asks for it)
-#pragma unroll
-      for (uint32_t t = 0; t < kTile; ++t) inner[t] = 0.0f;
-    }
-    sum_for_owners<kQ>(inner, lane);
-    sum_for_owners<kQ>(came, lane);
-    sum_for_owners<kQ>(slower, lane);
+    sum_for_owners<kQ, kTile>(inner, lane);
+    sum_for_owners<kQ, kTile>(came, lane);
+    sum_for_owners<kQ, kTile>(slower, lane);
     float dd = 0.0f, dbias = 0.0f;
-    const uint32_t behind = steps_in(t0, kTile, A.steps);
 #pragma unroll
     for (uint32_t j = 0; j < kOwn; ++j) {
       const bool there = at.own + j < valid;
@@ -398,17 +400,16 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
       dd += there ? dinner_own[j] * input[j] : 0.0f;
       dbias += dv;
       if (at.owner && at.own + j < behind) {
-        const uint32_t t = t0 + at.own + j;
-        *element<T>(G.dx, b, t, at.c) = static_cast<T>(dx);
-        *element<T>(G.ddelta, b, t, at.c) = static_cast<T>(dv);
-        if (gate) *element<T>(G.dgate, b, t, at.c) = static_cast<T>(dgate);
+        dx_at.at(j, along) = static_cast<T>(dx);
+        dv_at.at(j, along) = static_cast<T>(dv);
+        if (gate) dz_at.at(j, along) = static_cast<T>(dgate);
       }
     }
-#pragma unroll
-    for (uint32_t s = 0; s < kS; ++s) lds.da[turn][wave][lane * kS + s] = da[s];
-    const bool counts = kQ < 16 || at.q % 2u == 0u;
-    lds.own[turn][wave][0][lane] = counts ? dd : 0.0f;
-    lds.own[turn][wave][1][lane] = counts ? dbias : 0.0f;
+    
+    dd = sum_lanes<kQ>(at.first ? dd : 0.0f);
+    dbias = sum_lanes<kQ>(at.first ? dbias : 0.0f);
+    write_shared<kS>(&lds.da[turn][wave][at.lane * kS], da);
+    if (at.q == 0u) lds.own[turn][wave][0][at.channel] = dd, lds.own[turn][wave][1][at.channel] = dbias;
   }
   __syncthreads();
   if (from < upto) finish(upto - 1u, (upto - 1u - from) & 1u);
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
   for (int i = 0; i < kLeft; ++i) {
     const uint32_t id = base + i, which = id / (kTile * kS), t = id / kS % kTile, state = lane % kQ * kS + id % kS;
     if (t0 + t < A.steps && state < A.states)
-      K.rows[(((static_cast<uint64_t>(split) * A.batch + b) * A.steps + t0 + t) * 2u + which) * both + group * A.states + state] = sums[i];
+      K.rows[(((static_cast<uint64_t>(split) * A.batch + b) * A.steps + t0 + t) * 2u + which) * both + group * A.states + state] = first + wave * kTile + t < n ? sums[i] : 0.0f;
   }
 }
 
@@ -446,7 +447,7 @@ __global__ void __launch_bounds__(256) scan_hand_on_kernel(const float* dh_last,
 RearCut rear_cut(const ScanArgs& a) {
   constexpr uint64_t kEnough = 1024;                                                  // workgroups of the third launch that fill the device
   RearCut K{};
-  const uint32_t channels = wave_channels(a.states), each = a.width / a.groups;
+  const uint32_t channels = wave_channels<true>(a.states), each = a.width / a.groups;
   K.chunks = (a.steps + kChunk - 1u) / kChunk;
   K.across = (each + kRearWaves * channels - 1u) / (kRearWaves * channels);
   K.blocks = (each + channels - 1u) / channels;
@@ -480,7 +481,7 @@ hipError_t launch_scan_backward(const ScanArgs& a, const ScanGradArgs& g, int dt
   K.rows = K.parts + W.parts;
   const uint64_t slots = static_cast<uint64_t>(a.batch) * K.chunks, weights = static_cast<uint64_t>(a.width) * a.states;
   if (slots > 0u) {
-    const hipError_t e = by_states(a.states, dtype, [&](auto type, auto states, auto lanes) {
+    const hipError_t e = by_states<true>(a.states, dtype, [&](auto type, auto states, auto lanes) {
       using T = decltype(type);
       constexpr int kS = decltype(states)::value, kQ = decltype(lanes)::value;
       if (K.chunks > 1u) {

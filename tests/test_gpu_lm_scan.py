@@ -275,7 +275,7 @@ def test_sizes_far_out(rgc, ctx):
     x, a = torch.ones(1, steps, width, device="cuda"), torch.full((width, 4), -1e-3, device="cuda")
     b = torch.ones(1, steps, 4, device="cuda")
     y, h = torch.empty_like(x), torch.empty(1, width, 4, device="cuda")
-    kept = torch.empty(1, 2, width, 4, device="cuda")
+    kept = torch.empty(1, -(-steps // rgc.RGC_SCAN_CHUNK), width, 4, device="cuda")
     call = rgc.Scan(x, delta, a, b, b, y, softplus=True, h_last=h, states=kept)
     rgc.rgc_selective_scan(ctx, call)
     out = [torch.empty_like(x), torch.empty_like(x), torch.empty_like(a), torch.empty_like(b), torch.empty_like(b)]
@@ -359,7 +359,7 @@ def test_gradients_are_those_of_differences(rgc, ctx):
     inputs = {"x": rand(batch, steps, width), "delta": rand(batch, steps, width) - 2.0, "a": -torch.rand(width, states, generator=g, device="cuda") - 0.1, "b": rand(batch, steps, states),
               "c": rand(batch, steps, states), "d": rand(width), "gate": rand(batch, steps, width), "delta_bias": rand(width), "h0": rand(batch, width, states)}
     dy, dh, y, h = rand(batch, steps, width), rand(batch, width, states), torch.empty(batch, steps, width, device="cuda"), torch.empty(batch, width, states, device="cuda")
-    kept = torch.empty(batch, 2, width, states, device="cuda")
+    kept = torch.empty(batch, -(-steps // rgc.RGC_SCAN_CHUNK), width, states, device="cuda")
 
     def call(t):
         return rgc.Scan(t["x"], t["delta"], t["a"], t["b"], t["c"], y, d=t["d"], gate=t["gate"], delta_bias=t["delta_bias"], softplus=True, h0=t["h0"], h_last=h, states=kept)
