@@ -90,13 +90,12 @@ template <int kS, int kQ>
 __device__ __forceinline__ void read_states(const float* row, const ScanArgs& A, uint32_t q, uint32_t offset, float (&h)[kS]) {
   const char* base = reinterpret_cast<const char*>(row);
   if (A.states == kS * kQ) {
-    if constexpr (kS == 4 || kS == 2) {
-      const Raw<float, kS> r = read_at<float, kS>(reinterpret_cast<const float*>(base + offset));
+    constexpr int kVec = kS % 4 == 0 ? 4 : kS % 2 == 0 ? 2 : 1;
 #pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) h[s] = r.v[s];
-    } else {
+    for (int s = 0; s < kS; s += kVec) {
+      const Raw<float, kVec> r = read_at<float, kVec>(reinterpret_cast<const float*>(base + (offset + s * 4u)));
 #pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) h[s] = *reinterpret_cast<const float*>(base + (offset + s * 4u));
+      for (int i = 0; i < kVec; ++i) h[s + i] = r.v[i];
     }
   } else {
     const uint32_t first = offset - q * kS * 4u;
@@ -111,8 +110,10 @@ template <int kS, int kQ, int kT>
 __device__ __forceinline__ void write_states(float* row, const ScanArgs& A, const Spot<kS, kQ, kT>& at, const float (&h)[kS]) {
   if (!at.mine) return;
   float* p = reinterpret_cast<float*>(reinterpret_cast<char*>(row) + states_at(A, at));
-  if ((kS == 4 || kS == 2) && A.states == kS * kQ) {
-    write_at<float, kS == 3 ? 1 : kS>(p, *reinterpret_cast<const float(*)[kS == 3 ? 1 : kS]>(&h));
+  constexpr int kVec = kS % 4 == 0 ? 4 : kS % 2 == 0 ? 2 : 1;
+  if (kVec > 1 && A.states == kS * kQ) {
+#pragma unroll
+    for (int s = 0; s < kS; s += kVec) write_at<float, kVec>(p + s, *reinterpret_cast<const float(*)[kVec]>(&h[s]));
   } else {
 #pragma unroll
     for (uint32_t s = 0; s < kS; ++s)
@@ -220,41 +221,43 @@ struct Own {
   }
 };
 
-// A chunk's rows of B or C in 32 bits: `count` of them, and zeros behind, kStates a step, by the workgroup's kThreads threads.
-template <typename T, uint32_t kStates, uint32_t kThreads>
-__device__ __forceinline__ void stage(float* to, const SequenceView& from, const ScanArgs& A, uint32_t b, uint32_t g, uint32_t first, uint32_t count) {
-  Staged<T, kStates, kThreads> rows;
-  rows.ask(from, A, b, g, first, count);
-  rows.put(to);
+// kRows rows of B or C in 32 bits, `count` of them from memory and zeros behind, kStates a step, by so many threads.
+template <typename T, uint32_t kRows, uint32_t kStates>
+__device__ __forceinline__ void stage(float* to, const SequenceView& from, const ScanArgs& A, uint32_t b, uint32_t g, uint32_t first, uint32_t count, uint32_t threads) {
+  const char* row = reinterpret_cast<const char*>(element<T>(from, b, first, g * A.states));
+  const int64_t step = from.step_stride * static_cast<int64_t>(sizeof(T));
+#pragma unroll 2
+  for (uint32_t i = threadIdx.x; i < kRows * kStates; i += threads) {
+    const uint32_t t = i / kStates, n = i % kStates;
+    to[i] = t < count && n < A.states ? static_cast<float>(*reinterpret_cast<const T*>(row + t * step + n * sizeof(T))) : 0.0f;
+  }
 }
 
-// kS neighbouring numbers of shared memory.
+// kS neighbouring numbers of shared memory, four or two at a time.
+typedef float Two __attribute__((ext_vector_type(2)));
+typedef float Four __attribute__((ext_vector_type(4)));
 template <int kS>
 __device__ __forceinline__ void read_shared(const float* p, float (&v)[kS]) {
-  if constexpr (kS == 2) {
-    typedef float two __attribute__((ext_vector_type(2)));
-    const two r = *reinterpret_cast<const two*>(p);
-    v[0] = r.x, v[1] = r.y;
-  } else if constexpr (kS == 4) {
-    typedef float four __attribute__((ext_vector_type(4)));
-    const four r = *reinterpret_cast<const four*>(p);
-    v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w;
-  } else {
 #pragma unroll
-    for (int s = 0; s < kS; ++s) v[s] = p[s];
+  for (int s = 0; s < kS; s += kS % 4 == 0 ? 4 : kS % 2 == 0 ? 2 : 1) {
+    if constexpr (kS % 4 == 0) {
+      const Four r = *reinterpret_cast<const Four*>(p + s);
+      v[s] = r.x, v[s + 1] = r.y, v[s + 2] = r.z, v[s + 3] = r.w;
+    } else if constexpr (kS % 2 == 0) {
+      const Two r = *reinterpret_cast<const Two*>(p + s);
+      v[s] = r.x, v[s + 1] = r.y;
+    } else {
+      v[s] = p[s];
+    }
   }
 }
 template <int kS>
 __device__ __forceinline__ void write_shared(float* p, const float (&v)[kS]) {
-  if constexpr (kS == 2) {
-    typedef float two __attribute__((ext_vector_type(2)));
-    *reinterpret_cast<two*>(p) = two{v[0], v[1]};
-  } else if constexpr (kS == 4) {
-    typedef float four __attribute__((ext_vector_type(4)));
-    *reinterpret_cast<four*>(p) = four{v[0], v[1], v[2], v[3]};
-  } else {
 #pragma unroll
-    for (int s = 0; s < kS; ++s) p[s] = v[s];
+  for (int s = 0; s < kS; s += kS % 4 == 0 ? 4 : kS % 2 == 0 ? 2 : 1) {
+    if constexpr (kS % 4 == 0) *reinterpret_cast<Four*>(p + s) = Four{v[s], v[s + 1], v[s + 2], v[s + 3]};
+    else if constexpr (kS % 2 == 0) *reinterpret_cast<Two*>(p + s) = Two{v[s], v[s + 1]};
+    else p[s] = v[s];
   }
 }
 template <int kT>
@@ -282,45 +285,56 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Bit i: the state starts anew at step first + i (of the chunk that begins there, and of those the row has).
-__device__ __forceinline__ uint64_t anew_from(const ScanArgs& A, uint32_t b, uint32_t first, uint32_t n) {
+// Bit i: the state starts anew at step first + i (of the next `most`, and of those the row has).
+__device__ __forceinline__ uint64_t anew_from(const ScanArgs& A, uint32_t b, uint32_t first, uint32_t most, uint32_t n) {
   if (!A.resets) return 0u;
   const uint32_t i = threadIdx.x & 63u, t = first + i;
-  return __ballot(i < kChunk && t < n && A.resets[static_cast<uint64_t>(b) * A.steps + t] != 0);
+  return __ballot(i < most && t < n && A.resets[static_cast<uint64_t>(b) * A.steps + t] != 0);
 }
 
 // Steps of [first, first + most) that are before `end`.
 __device__ __forceinline__ uint32_t steps_in(uint32_t first, uint32_t most, uint32_t end) { return min(max(end, first) - first, most); }
 
-// Calls f with the type, the states a lane and the lanes a channel as constants.  Fewer lanes a channel mean fewer exchanges and less to be done once a channel, more of them more waves.
+// How many states a lane has and how many lanes a channel: fewer lanes mean fewer exchanges and less to be done once a channel, more of them more waves and fewer registers.
+template <int kStatesOfLane, int kLanes, int kStepsAtOnce>
+struct Layout {
+  static constexpr int kS = kStatesOfLane, kQ = kLanes, kT = kStepsAtOnce;
+};
+// Calls f with the type and the layout.  Backward, us, 8 x 4096 x 2048 bf16 with 16 states (20 x 35 x 1500 fp32): two states a lane, eight steps, four waves a workgroup 1547 (53), four states, four
+// steps, eight waves 1711 (63; all of a compute unit's waves wait at one barrier), four states and eight steps do not fit into registers.
 template <bool kBackward, typename F>
 hipError_t by_states(uint32_t states, int dtype, F&& f) {
-  auto with = [&](auto s, auto q) {
-    if (dtype == 0) return f(float{}, s, q);
-    if (dtype == 1) return f(__bf16{}, s, q);
-    return f(_Float16{}, s, q);
+  auto with = [&](auto layout) {
+    if (dtype == 0) return f(float{}, layout);
+    if (dtype == 1) return f(__bf16{}, layout);
+    return f(_Float16{}, layout);
   };
-  typedef std::integral_constant<int, 1> One;
-  typedef std::integral_constant<int, 2> Two;
-  typedef std::integral_constant<int, 3> Three;
-  typedef std::integral_constant<int, 4> Four;
-  typedef std::integral_constant<int, 8> Eight;
-  if (states == 1u) return with(One{}, One{});
-  if (states <= 4u) return with(Four{}, One{});
-  if (states <= 8u) return with(Four{}, Two{});
+  if (states == 1u) return with(Layout<1, 1, 8>{});
   if constexpr (kBackward) {
-    if (states <= 16u) return with(Four{}, Four{});
+    if (states <= 4u) return with(Layout<2, 2, 8>{});
+    if (states <= 8u) return with(Layout<2, 4, 8>{});
+    if (states <= 16u) return with(Layout<2, 8, 8>{});
+    if (states <= 24u) return with(Layout<3, 8, 8>{});
+    if (states <= 32u) return with(Layout<2, 16, 8>{});
+    return with(Layout<4, 16, 4>{});
   } else {
-    if (states <= 16u) return with(Two{}, Eight{});
+    if (states <= 4u) return with(Layout<4, 1, 8>{});
+    if (states <= 8u) return with(Layout<4, 2, 8>{});
+    if (states <= 16u) return with(Layout<2, 8, 8>{});
+    if (states <= 24u) return with(Layout<3, 8, 8>{});
+    if (states <= 32u) return with(Layout<4, 8, 8>{});
+    return with(Layout<4, 16, 8>{});
   }
-  if (states <= 24u) return with(Three{}, Eight{});
-  if (states <= 32u) return with(Four{}, Eight{});
-  return with(Four{}, std::integral_constant<int, 16>{});
 }
 // The same choice for the host: channels of a wave.
 template <bool kBackward>
 uint32_t wave_channels(uint32_t states) {
-  return states <= 4u ? 64u : states <= 8u ? 32u : states <= 16u ? (kBackward ? 16u : 8u) : states <= 32u ? 8u : 4u;
+  uint32_t channels = 0u;
+  (void)by_states<kBackward>(states, 0, [&](auto, auto layout) {
+    channels = 64u / decltype(layout)::kQ;
+    return hipSuccess;
+  });
+  return channels;
 }
 
 }  // namespace

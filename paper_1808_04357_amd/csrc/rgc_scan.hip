@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(64 * kWaves) scan_kernel(ScanArgs A, ScanCut K
     if (!kSummary && A.kept) write_states(A.kept + (static_cast<uint64_t>(b) * K.chunks + chunk) * states_of_row, A, at, h);
     const bool more = chunk + 1u < last_chunk && first + kChunk < n;
     if (more) ask_rows(chunk + 1u);
-    const uint64_t anew = anew_from(A, b, first, n);
+    const uint64_t anew = anew_from(A, b, first, kChunk, n);
     cut |= anew;
     const float *const in_b = rows_b[chunk & 1u] + at.q * kS, *const in_c = rows_c[chunk & 1u] + (kSummary ? 0u : at.q * kS);
     for (uint32_t part = 0; part < count; part += kSteps) {
@@ -244,9 +244,9 @@ hipError_t launch_scan(const ScanArgs& a, int dtype, unsigned long long* scratch
     K.sums = K.starts + slots * a.width * a.states;
     K.cuts = reinterpret_cast<uint32_t*>(K.sums + slots * a.width);
   }
-  return by_states<false>(a.states, dtype, [&](auto type, auto states, auto lanes) {
+  return by_states<false>(a.states, dtype, [&](auto type, auto layout) {
     using T = decltype(type);
-    constexpr int kS = decltype(states)::value, kQ = decltype(lanes)::value;
+    constexpr int kS = decltype(layout)::kS, kQ = decltype(layout)::kQ;
     if (K.stretches > 1u) {
       in_grids(workgroups(a, K, K.stretches - 1u), [&](uint64_t begin, dim3 grid) { scan_kernel<T, kS, kQ, true><<<grid, dim3(64 * kWaves), 0, s>>>(a, K, begin); });
       const uint64_t all = static_cast<uint64_t>(a.batch) * a.width * a.states;

@@ -4,7 +4,7 @@
 // So the gradients go through the steps as the states do, the other way.
 //  1. Every chunk but the first from a gradient of zero behind it: what it hands on, and the sum of its steps' sizes (scan_rear_kernel).
 //  2. What comes in behind each chunk, from the last one to the first (scan_rear_join_kernel).  With one chunk neither is needed.
-//  3. A workgroup for each chunk and group of channels (scan_backward_kernel).  Its eight waves take four steps each, of as many channels as a wave has at a time: each makes its powers,
+//  3. A workgroup for each chunk and group of channels (scan_backward_kernel).  Its waves take eight steps each, of as many channels as a wave has at a time: each makes its powers,
 //     what its steps do to a state and to a gradient (both from zero), hears from the others what state it begins and what gradient it ends with, and walks its steps in both directions out of
 //     registers: B's and C's gradients, sums over channels, stay in registers over all of the workgroup's channels; those of A, D and delta's bias, sums over steps, are added up over the waves.
 //  4. The workgroups' parts of both are added up in an order made of the sizes alone (scan_rows_kernel, launch_sum_parts).
@@ -19,10 +19,10 @@ namespace rgc {
 namespace {
 
 constexpr uint32_t kRearWaves = 4;     // of a workgroup of the first launch
-constexpr uint32_t kWaves = 8, kTile = kChunk / kWaves, kRearTile = 8;      // of the third launch; steps of a wave of it and of the first at a time
+constexpr uint32_t kRearTile = 8;      // steps of a wave at a time in the first launch
 
 struct RearCut {
-  uint32_t chunks, across;             // workgroups of the first launch for a group's channels
+  uint32_t chunks, across;             // chunks of a sequence, workgroups of the first launch for a group's channels
   uint32_t splits, blocks;             // workgroups of the third for them, stretches of a wave's channels
   float* ends;                         // [batch][chunks][width][states]: what a chunk hands on from 0, then what comes in behind it
   float* sums;                         // [batch][chunks][width]
@@ -62,9 +62,9 @@ __global__ void __launch_bounds__(64 * kRearWaves) scan_rear_kernel(ScanArgs A, 
   float rate[kS], g[kS] = {};
   rates_of(A, at, rate);
   const float bias = A.delta_bias ? A.delta_bias[at.c] : 0.0f;
-  stage<T, kStates, 64 * kRearWaves>(rows_c, A.c, A, b, group, first, count);
+  stage<T, kChunk, kStates>(rows_c, A.c, A, b, group, first, count, 64u * kRearWaves);
   __syncthreads();
-  const uint64_t anew = anew_from(A, b, first, n);
+  const uint64_t anew = anew_from(A, b, first, kChunk, n);
   float total = 0.0f;
   const uint32_t tiles = (count + kTile - 1u) / kTile;
   T v[kOwn], z[kOwn], dy[kOwn];
@@ -175,20 +175,20 @@ __device__ __forceinline__ void sum_channels(float (&v)[kAll], uint32_t lane, ui
   }
 }
 
-template <int kS, int kQ>
+template <int kS, int kQ, int kT>
 struct SharedBackward {
-  static constexpr uint32_t kStates = kS * kQ, kChannels = 64 / kQ;
+  static constexpr uint32_t kStates = kS * kQ, kChannels = 64 / kQ, kTile = kT, kWaves = kChunk / kTile;
   float rows_b[kChunk * kStates], rows_c[kChunk * kStates];
   float of_step[kWaves][3][kChannels * kTile];     // sizes, size * input, gradient before the gate
   float parts[2][kWaves][3][64 * kS];              // what a wave's steps do: decay, state, gradient
   float da[2][kWaves][64 * kS], own[2][kWaves][2][kChannels];
 };
 
-template <typename T, int kS, int kQ>
-__global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
-  typedef Spot<kS, kQ, kTile> At;
-  constexpr uint32_t kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
-  __shared__ __attribute__((aligned(16))) SharedBackward<kS, kQ> lds;
+template <typename T, int kS, int kQ, int kT>
+__global__ void __launch_bounds__(64 * (kChunk / kT)) scan_backward_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
+  typedef Spot<kS, kQ, kT> At;
+  constexpr uint32_t kTile = kT, kWaves = kChunk / kTile, kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
+  __shared__ __attribute__((aligned(16))) SharedBackward<kS, kQ, kT> lds;
   uint64_t rest = begin + blockIdx.x;
   const uint32_t split = uniform(static_cast<uint32_t>(rest % K.splits));
   rest /= K.splits;
@@ -200,30 +200,55 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
   const uint32_t t0 = first + wave * kTile, valid = steps_in(t0, kTile, n), behind = steps_in(t0, kTile, A.steps);
   const bool gate = A.gate.data != nullptr;
   const uint64_t row = static_cast<uint64_t>(A.width) * A.states, slot = static_cast<uint64_t>(b) * K.chunks + chunk;
-  stage<T, kStates, 64 * kWaves>(lds.rows_b, A.b, A, b, group, first, count);
-  stage<T, kStates, 64 * kWaves>(lds.rows_c, A.c, A, b, group, first, count);
-  const uint64_t anew = anew_from(A, b, first, n);
+  const uint32_t per = (K.blocks + K.splits - 1u) / K.splits, from = split * per, upto = min(from + per, K.blocks);
+  if (count == 0u) {                   // (the same for the whole workgroup) nothing of the row is here: zeros, and what comes in behind the chunk goes on before it
+    const uint32_t first_channel = min(from * kChannels, each), channels = min(upto * kChannels, each) - min(first_channel, min(upto * kChannels, each));
+    const uint32_t length = steps_in(first, kChunk, A.steps), both = A.groups * A.states;
+    for (uint32_t i = threadIdx.x; i < channels; i += 64u * kWaves) {
+      const uint32_t c = group * each + first_channel + i;
+      for (uint32_t t = 0; t < length; ++t) {
+        *element<T>(G.dx, b, first + t, c) = static_cast<T>(0.0f);
+        *element<T>(G.ddelta, b, first + t, c) = static_cast<T>(0.0f);
+        if (gate) *element<T>(G.dgate, b, first + t, c) = static_cast<T>(0.0f);
+      }
+      float* to = K.parts + slot * (row + 2u * A.width);
+      to[row + c] = to[row + A.width + c] = 0.0f;
+    }
+    for (uint32_t i = threadIdx.x; i < channels * A.states; i += 64u * kWaves) {
+      const uint64_t at = static_cast<uint64_t>(group * each + first_channel) * A.states + i;
+      K.parts[slot * (row + 2u * A.width) + at] = 0.0f;
+      if (G.dh0 && chunk == 0u) G.dh0[b * row + at] = K.chunks > 1u ? K.ends[slot * row + at] : G.dh_last ? G.dh_last[b * row + at] : 0.0f;
+    }
+    for (uint32_t i = threadIdx.x; i < length * 2u * A.states; i += 64u * kWaves) {
+      const uint32_t t = i / (2u * A.states), which = i / A.states % 2u, state = i % A.states;
+      K.rows[(((static_cast<uint64_t>(split) * A.batch + b) * A.steps + first + t) * 2u + which) * both + group * A.states + state] = 0.0f;
+    }
+    return;
+  }
+  stage<T, kChunk, kStates>(lds.rows_b, A.b, A, b, group, first, count, 64u * kWaves);
+  stage<T, kChunk, kStates>(lds.rows_c, A.c, A, b, group, first, count, 64u * kWaves);
+  const uint64_t anew = anew_from(A, b, first, kChunk, n);
   constexpr uint32_t kBits = (1u << kTile) - 1u;
   const uint32_t starts = static_cast<uint32_t>(anew >> (wave * kTile)) & kBits;
   float sums[2 * kTile * kS] = {};     // of the gradients of B and C
   // the sums over the waves of what an earlier turn left
   auto finish = [&](uint32_t block, uint32_t turn) __attribute__((always_inline)) {
     float* to = K.parts + slot * (row + 2u * A.width);
-    const uint32_t id = here(threadIdx.x);
-    float sum = 0.0f;
-    if (id < 64u * kS) {
+    for (uint32_t id = here(threadIdx.x); id < 64u * kS + 2u * kChannels; id += 64u * kWaves) {
+      float sum = 0.0f;
+      if (id < 64u * kS) {
 #pragma unroll
-      for (uint32_t w = 0; w < kWaves; ++w) sum += lds.da[turn][w][id];
-      const uint32_t l = id / kS, state = l % kQ * kS + id % kS, c = block * kChannels + l / kQ;
-      if (c < each && state < A.states) to[(group * each + c) * A.states + state] = sum;
-    } else if (id < 64u * kS + 2u * kChannels) {
-      const uint32_t which = (id - 64u * kS) / kChannels, channel = (id - 64u * kS) % kChannels, c = block * kChannels + channel;
+        for (uint32_t w = 0; w < kWaves; ++w) sum += lds.da[turn][w][id];
+        const uint32_t l = id / kS, state = l % kQ * kS + id % kS, c = block * kChannels + l / kQ;
+        if (c < each && state < A.states) to[(group * each + c) * A.states + state] = sum;
+      } else {
+        const uint32_t which = (id - 64u * kS) / kChannels, channel = (id - 64u * kS) % kChannels, c = block * kChannels + channel;
 #pragma unroll
-      for (uint32_t w = 0; w < kWaves; ++w) sum += lds.own[turn][w][which][channel];
-      if (c < each) to[static_cast<uint32_t>(row) + which * A.width + group * each + c] = sum;
+        for (uint32_t w = 0; w < kWaves; ++w) sum += lds.own[turn][w][which][channel];
+        if (c < each) to[static_cast<uint32_t>(row) + which * A.width + group * each + c] = sum;
+      }
     }
   };
-  const uint32_t per = (K.blocks + K.splits - 1u) / K.splits, from = split * per, upto = min(from + per, K.blocks);
   const uint32_t own_step = At(A, group, 0u).own;
   const Column<T> x_at(A.x, b, t0, own_step, group * each), v_at(A.delta, b, t0, own_step, group * each), z_at(gate ? A.gate : A.x, b, t0, own_step, group * each),
       dy_at(G.dy, b, t0, own_step, group * each), dx_at(G.dx, b, t0, own_step, group * each), dv_at(G.ddelta, b, t0, own_step, group * each),
@@ -259,6 +284,7 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
   };
   if (from < upto) ask(from);
   __syncthreads();
+  auto turns = [&](auto with_starts) __attribute__((always_inline)) {
   for (uint32_t block = from; block < upto; ++block) {
     const uint32_t turn = (block - from) & 1u;
     const At at(A, group, block, here(lane));
@@ -295,30 +321,27 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
     const float *const row_b = lds.rows_b + (wave * kTile * kStates + at.q * kS), *const row_c = lds.rows_c + (wave * kTile * kStates + at.q * kS);
     // (a step that is not there has the size 0 and brings nothing: it leaves states and gradients as they are)
     float a[kTile][kS], own_h[kS] = {}, own_g[kS] = {}, whole[kS];
-    auto alone = [&](auto with_starts) __attribute__((always_inline)) {
 #pragma unroll
-      for (uint32_t t = 0; t < kTile; ++t) {
-        float in[kS];
-        read_shared<kS>(row_b + t * kStates, in);
+    for (uint32_t t = 0; t < kTile; ++t) {
+      float in[kS];
+      read_shared<kS>(row_b + t * kStates, in);
 #pragma unroll
-        for (uint32_t s = 0; s < kS; ++s) {
-          a[t][s] = __builtin_amdgcn_exp2f(size[t] * rate[s]);
-          if (with_starts && ((starts >> t) & 1u) != 0u) own_h[s] = 0.0f;
-          own_h[s] = __fmaf_rn(a[t][s], own_h[s], fed[t] * in[s]);
-        }
+      for (uint32_t s = 0; s < kS; ++s) {
+        a[t][s] = __builtin_amdgcn_exp2f(size[t] * rate[s]);
+        if (with_starts && ((starts >> t) & 1u) != 0u) own_h[s] = 0.0f;
+        own_h[s] = t == 0u ? fed[t] * in[s] : __fmaf_rn(a[t][s], own_h[s], fed[t] * in[s]);
       }
+    }
 #pragma unroll
-      for (uint32_t t = kTile; t-- > 0u;) {
-        float out[kS];
-        read_shared<kS>(row_c + t * kStates, out);
+    for (uint32_t t = kTile; t-- > 0u;) {
+      float out[kS];
+      read_shared<kS>(row_c + t * kStates, out);
 #pragma unroll
-        for (uint32_t s = 0; s < kS; ++s) {
-          own_g[s] = a[t][s] * __fmaf_rn(dinner[t], out[s], own_g[s]);
-          if (with_starts && ((starts >> t) & 1u) != 0u) own_g[s] = 0.0f;
-        }
+      for (uint32_t s = 0; s < kS; ++s) {
+        own_g[s] = a[t][s] * (t + 1u == kTile ? dinner[t] * out[s] : __fmaf_rn(dinner[t], out[s], own_g[s]));
+        if (with_starts && ((starts >> t) & 1u) != 0u) own_g[s] = 0.0f;
       }
-    };
-    if (starts == 0u) alone(No{}); else alone(Yes{});
+    }
     float total = 0.0f;
 #pragma unroll
     for (uint32_t t = 0; t < kTile; ++t) total += size[t];
@@ -329,63 +352,61 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
     write_shared<kS>(&lds.parts[turn][wave][2][at.lane * kS], own_g);
     __syncthreads();
     // the state before the wave's steps and the gradient behind them, from the other waves' stretches
-    auto hear = [&](auto with_starts) __attribute__((always_inline)) {
-      for (uint32_t w = 0; w < wave; ++w) {
-        float p[kS], own[kS];
-        read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
-        read_shared<kS>(&lds.parts[turn][w][1][at.lane * kS], own);
-        const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
 #pragma unroll
-        for (uint32_t s = 0; s < kS; ++s) h[s] = cut ? own[s] : __fmaf_rn(p[s], h[s], own[s]);
-      }
-      for (uint32_t w = kWaves - 1u; w > wave; --w) {
-        float p[kS], own[kS];
-        read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
-        read_shared<kS>(&lds.parts[turn][w][2][at.lane * kS], own);
-        const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
+    for (uint32_t w = 0; w + 1u < kWaves; ++w) {
+      if (w >= wave) break;
+      float p[kS], own[kS];
+      read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
+      read_shared<kS>(&lds.parts[turn][w][1][at.lane * kS], own);
+      const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
 #pragma unroll
-        for (uint32_t s = 0; s < kS; ++s) g[s] = cut ? own[s] : __fmaf_rn(p[s], g[s], own[s]);
-      }
-    };
-    if (anew == 0u) hear(No{}); else hear(Yes{});
+      for (uint32_t s = 0; s < kS; ++s) h[s] = cut ? own[s] : __fmaf_rn(p[s], h[s], own[s]);
+    }
+#pragma unroll
+    for (uint32_t w = kWaves - 1u; w > 0u; --w) {
+      if (w <= wave) break;
+      float p[kS], own[kS];
+      read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
+      read_shared<kS>(&lds.parts[turn][w][2][at.lane * kS], own);
+      const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
+#pragma unroll
+      for (uint32_t s = 0; s < kS; ++s) g[s] = cut ? own[s] : __fmaf_rn(p[s], g[s], own[s]);
+    }
     if (block > from) finish(block - 1u, turn ^ 1u);
     float inner[kTile] = {}, came[kTile] = {}, slower[kTile] = {}, da[kS] = {};
-    auto walk = [&](auto with_starts) __attribute__((always_inline)) {
-      float after[kTile][kS];
+    float after[kTile][kS];
 #pragma unroll
-      for (uint32_t t = 0; t < kTile; ++t) {
-        float in[kS];
-        read_shared<kS>(row_b + t * kStates, in);
+    for (uint32_t t = 0; t < kTile; ++t) {
+      float in[kS];
+      read_shared<kS>(row_b + t * kStates, in);
 #pragma unroll
-        for (uint32_t s = 0; s < kS; ++s) {
-          const float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
-          after[t][s] = __fmaf_rn(a[t][s], with_starts && ((starts >> t) & 1u) != 0u ? 0.0f : prior, fed[t] * in[s]);
-        }
+      for (uint32_t s = 0; s < kS; ++s) {
+        const float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
+        after[t][s] = __fmaf_rn(a[t][s], with_starts && ((starts >> t) & 1u) != 0u ? 0.0f : prior, fed[t] * in[s]);
       }
+    }
 #pragma unroll
-      for (uint32_t t = kTile; t-- > 0u;) {
-        float in[kS], out[kS];
-        read_shared<kS>(row_b + t * kStates, in);
-        read_shared<kS>(row_c + t * kStates, out);
-        const bool anew_here = with_starts && ((starts >> t) & 1u) != 0u;
+    for (uint32_t t = kTile; t-- > 0u;) {
+      float in[kS], out[kS];
+      read_shared<kS>(row_b + t * kStates, in);
+      read_shared<kS>(row_c + t * kStates, out);
+      const bool anew_here = with_starts && ((starts >> t) & 1u) != 0u;
 #pragma unroll
-        for (uint32_t s = 0; s < kS; ++s) {
-          float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
-          if (anew_here) prior = 0.0f;
-          inner[t] = __fmaf_rn(after[t][s], out[s], inner[t]);
-          sums[(kTile + t) * kS + s] = __fmaf_rn(dinner[t], after[t][s], sums[(kTile + t) * kS + s]);
-          const float d = __fmaf_rn(dinner[t], out[s], g[s]);
-          came[t] = __fmaf_rn(d, in[s], came[t]);
-          sums[t * kS + s] = __fmaf_rn(fed[t], d, sums[t * kS + s]);
-          g[s] = a[t][s] * d;
-          const float lost = g[s] * prior;                         // the gradient of the decay's exponent
-          slower[t] = __fmaf_rn(lost, rate[s], slower[t]);
-          da[s] = __fmaf_rn(lost, size[t], da[s]);
-          if (anew_here) g[s] = 0.0f;
-        }
+      for (uint32_t s = 0; s < kS; ++s) {
+        float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
+        if (anew_here) prior = 0.0f;
+        inner[t] = __fmaf_rn(after[t][s], out[s], inner[t]);
+        sums[(kTile + t) * kS + s] = __fmaf_rn(dinner[t], after[t][s], sums[(kTile + t) * kS + s]);
+        const float d = __fmaf_rn(dinner[t], out[s], g[s]);
+        came[t] = __fmaf_rn(d, in[s], came[t]);
+        sums[t * kS + s] = __fmaf_rn(fed[t], d, sums[t * kS + s]);
+        g[s] = a[t][s] * d;
+        const float lost = g[s] * prior;                           // the gradient of the decay's exponent
+        slower[t] = __fmaf_rn(lost, rate[s], slower[t]);
+        da[s] = __fmaf_rn(lost, size[t], da[s]);
+        if (anew_here) g[s] = 0.0f;
       }
-    };
-    if (starts == 0u) walk(No{}); else walk(Yes{});
+    }
     if (G.dh0 && chunk == 0u && wave == 0u) write_states(G.dh0 + b * row, A, at, g);
     sum_for_owners<kQ, kTile>(inner, lane);
     sum_for_owners<kQ, kTile>(came, lane);
@@ -411,6 +432,9 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
     write_shared<kS>(&lds.da[turn][wave][at.lane * kS], da);
     if (at.q == 0u) lds.own[turn][wave][0][at.channel] = dd, lds.own[turn][wave][1][at.channel] = dbias;
   }
+  };
+  // (in a chunk where nothing starts anew nothing has to be looked at for it; the same for the whole workgroup)
+  if (anew == 0u) turns(No{}); else turns(Yes{});
   __syncthreads();
   if (from < upto) finish(upto - 1u, (upto - 1u - from) & 1u);
   uint32_t base = 0u;
@@ -481,14 +505,16 @@ hipError_t launch_scan_backward(const ScanArgs& a, const ScanGradArgs& g, int dt
   K.rows = K.parts + W.parts;
   const uint64_t slots = static_cast<uint64_t>(a.batch) * K.chunks, weights = static_cast<uint64_t>(a.width) * a.states;
   if (slots > 0u) {
-    const hipError_t e = by_states<true>(a.states, dtype, [&](auto type, auto states, auto lanes) {
+    const hipError_t e = by_states<true>(a.states, dtype, [&](auto type, auto layout) {
       using T = decltype(type);
-      constexpr int kS = decltype(states)::value, kQ = decltype(lanes)::value;
+      constexpr int kS = decltype(layout)::kS, kQ = decltype(layout)::kQ, kT = decltype(layout)::kT;
       if (K.chunks > 1u) {
         in_grids((slots - a.batch) * a.groups * K.across, [&](uint64_t begin, dim3 grid) { scan_rear_kernel<T, kS, kQ><<<grid, dim3(64 * kRearWaves), 0, s>>>(a, g, K, begin); });
         in_grids((a.batch * weights + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_rear_join_kernel<<<grid, dim3(256), 0, s>>>(a, g, K, begin); });
       }
-      in_grids(slots * a.groups * K.splits, [&](uint64_t begin, dim3 grid) { scan_backward_kernel<T, kS, kQ><<<grid, dim3(64 * kWaves), 0, s>>>(a, g, K, begin); });
+      in_grids(slots * a.groups * K.splits, [&](uint64_t begin, dim3 grid) {
+        scan_backward_kernel<T, kS, kQ, kT><<<grid, dim3(64 * (kChunk / kT)), 0, s>>>(a, g, K, begin);
+      });
       const uint64_t all = static_cast<uint64_t>(a.batch) * a.steps * 2u * a.groups * a.states;
       in_grids((all + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_rows_kernel<T><<<grid, dim3(256), 0, s>>>(a, g, K, begin); });
       return hipGetLastError();
