@@ -138,7 +138,7 @@ struct ScanGradArgs {
 // How a scan is cut along its steps, and what the pieces tell each other.
 struct ScanCut {
   uint32_t chunks, stretch, stretches;   // chunks of a sequence, chunks of a stretch, stretches of a sequence
-  uint32_t across;                       // workgroups for a group's channels
+  uint32_t across, across_summary;       // workgroups for a group's channels, of the walk and of the summary
   float* starts;                         // [batch][stretches][width][states]
   float* sums;                           // [batch][stretches][width]
   uint32_t* cuts;                        // [batch][stretches]: a text begins in it

@@ -300,9 +300,11 @@ template <int kStatesOfLane, int kLanes, int kStepsAtOnce>
 struct Layout {
   static constexpr int kS = kStatesOfLane, kQ = kLanes, kT = kStepsAtOnce;
 };
-// Calls f with the type and the layout.  Backward, us, 8 x 4096 x 2048 bf16 with 16 states (20 x 35 x 1500 fp32): two states a lane, eight steps, four waves a workgroup 1547 (53), four states, four
-// steps, eight waves 1711 (63; all of a compute unit's waves wait at one barrier), four states and eight steps do not fit into registers.
-template <bool kBackward, typename F>
+enum class Kind { kWalk, kSummary, kBackward };      // a walk along the steps for results, for what a stretch does to a state (or a gradient) alone, the backward walk
+// Calls f with the type and the layout.  us, 8 x 4096 x 2048 bf16 with 16 states (20 x 35 x 1500 fp32): backward two states a lane, eight steps, four waves a workgroup 1547 (53), four states, four
+// steps, eight waves 1711 (63; all of a compute unit's waves wait at one barrier), four states and eight steps do not fit into registers; the walk by two states a lane 550, by four 1013 (half
+// the waves: one a SIMD); a summary, which has little to do once a channel and waves enough, by four 262, by two 311.
+template <Kind kKind, typename F>
 hipError_t by_states(uint32_t states, int dtype, F&& f) {
   auto with = [&](auto layout) {
     if (dtype == 0) return f(float{}, layout);
@@ -310,7 +312,7 @@ hipError_t by_states(uint32_t states, int dtype, F&& f) {
     return f(_Float16{}, layout);
   };
   if (states == 1u) return with(Layout<1, 1, 8>{});
-  if constexpr (kBackward) {
+  if constexpr (kKind == Kind::kBackward) {
     if (states <= 4u) return with(Layout<2, 2, 8>{});
     if (states <= 8u) return with(Layout<2, 4, 8>{});
     if (states <= 16u) return with(Layout<2, 8, 8>{});
@@ -320,17 +322,21 @@ hipError_t by_states(uint32_t states, int dtype, F&& f) {
   } else {
     if (states <= 4u) return with(Layout<4, 1, 8>{});
     if (states <= 8u) return with(Layout<4, 2, 8>{});
-    if (states <= 16u) return with(Layout<2, 8, 8>{});
+    if constexpr (kKind == Kind::kSummary) {
+      if (states <= 16u) return with(Layout<4, 4, 8>{});
+    } else {
+      if (states <= 16u) return with(Layout<2, 8, 8>{});
+    }
     if (states <= 24u) return with(Layout<3, 8, 8>{});
     if (states <= 32u) return with(Layout<4, 8, 8>{});
     return with(Layout<4, 16, 8>{});
   }
 }
 // The same choice for the host: channels of a wave.
-template <bool kBackward>
+template <Kind kKind>
 uint32_t wave_channels(uint32_t states) {
   uint32_t channels = 0u;
-  (void)by_states<kBackward>(states, 0, [&](auto, auto layout) {
+  (void)by_states<kKind>(states, 0, [&](auto, auto layout) {
     channels = 64u / decltype(layout)::kQ;
     return hipSuccess;
   });

@@ -28,8 +28,9 @@ __global__ void __launch_bounds__(64 * kWaves) scan_kernel(ScanArgs A, ScanCut K
   __shared__ __attribute__((aligned(16))) float sizes[kWaves][kChannels * kApart], feeds[kWaves][kChannels * kApart];
   uint64_t rest = begin + blockIdx.x;
   const uint32_t wave = uniform(threadIdx.x >> 6);
-  const uint32_t block = uniform(static_cast<uint32_t>(rest % K.across)) * kWaves + wave;
-  rest /= K.across;
+  const uint32_t across = kSummary ? K.across_summary : K.across;
+  const uint32_t block = uniform(static_cast<uint32_t>(rest % across)) * kWaves + wave;
+  rest /= across;
   const uint32_t g = uniform(static_cast<uint32_t>(rest % A.groups));
   rest /= A.groups;
   const uint32_t walked = kSummary ? K.stretches - 1u : K.stretches;                  // (what the last stretch ends with, the walk itself knows)
@@ -208,17 +209,88 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs A, ScanCut K, u
   }
 }
 
-uint64_t workgroups(const ScanArgs& a, const ScanCut& k, uint32_t stretches) { return static_cast<uint64_t>(a.batch) * stretches * a.groups * k.across; }
+// One step: a lane for kS states of a channel, whose kQ lanes are neighbours.  Bound by the states, read and written once.
+template <typename T, int kS, int kQ>
+__global__ void __launch_bounds__(64 * kWaves) scan_step_kernel(ScanArgs A, uint32_t blocks, uint64_t begin, uint64_t waves) {
+  constexpr uint32_t kChannels = 64 / kQ;
+  const uint64_t wave = (begin + blockIdx.x) * kWaves + uniform(threadIdx.x >> 6);
+  if (wave >= waves) return;
+  const uint32_t b = uniform(static_cast<uint32_t>(wave / blocks)), block = uniform(static_cast<uint32_t>(wave % blocks));
+  const uint32_t lane = threadIdx.x & 63u, q = lane % kQ, want = block * kChannels + lane / kQ, c = min(want, A.width - 1u), g = c / (A.width / A.groups);
+  const bool mine = want < A.width, there = steps_of(A.lengths, b, 1u) > 0u;
+  const uint64_t row = b * (static_cast<uint64_t>(A.width) * A.states);
+  const uint32_t at = (c * A.states + q * kS) * 4u;
+  float h[kS] = {}, rate[kS];
+  if (A.h0) read_states<kS, kQ>(A.h0 + row, A, q, at, h);
+  auto put = [&](float* to) {
+    float* p = reinterpret_cast<float*>(reinterpret_cast<char*>(to + row) + at);
+    if (!mine) return;
+    if (kS == 4 && A.states == kS * kQ) {
+      write_at<float, kS>(p, h);
+    } else {
+#pragma unroll
+      for (uint32_t s = 0; s < kS; ++s)
+        if (q * kS + s < A.states) p[s] = h[s];
+    }
+  };
+  if (A.kept) put(A.kept);
+  float y = 0.0f;
+  if (there) {
+    float grow, shown = 1.0f;
+    const float x = static_cast<float>(*element<T>(A.x, b, 0u, c)), size = size_of(A, static_cast<float>(*element<T>(A.delta, b, 0u, c)), A.delta_bias ? A.delta_bias[c] : 0.0f, grow);
+    if (A.gate.data) {
+      const float z = static_cast<float>(*element<T>(A.gate, b, 0u, c));
+      float open, shut;
+      gate_of(z, open, shut);
+      shown = z * open;
+    }
+    const T *in = element<T>(A.b, b, 0u, g * A.states), *out = element<T>(A.c, b, 0u, g * A.states);
+    read_states<kS, kQ>(A.a, A, q, at, rate);
+    finite_rates(rate);
+    const bool anew = A.resets && A.resets[b] != 0;
+#pragma unroll
+    for (uint32_t s = 0; s < kS; ++s) {
+      const uint32_t n = min(q * kS + s, A.states - 1u);
+      if (anew) h[s] = 0.0f;
+      h[s] = __fmaf_rn(__builtin_amdgcn_exp2f(size * rate[s]), h[s], size * x * static_cast<float>(in[n]));
+      if (q * kS + s < A.states) y = __fmaf_rn(h[s], static_cast<float>(out[n]), y);
+    }
+    y = sum_lanes<kQ>(y);
+    y = __fmaf_rn(A.d ? A.d[c] : 0.0f, x, y) * shown;
+  }
+  if (mine && q == 0u) *element<T>(A.y, b, 0u, c) = static_cast<T>(y);
+  if (A.h_last) put(A.h_last);
+}
+
+template <typename T, int kS, int kQ>
+hipError_t launch_step(const ScanArgs& a, hipStream_t s) {
+  const uint32_t blocks = (a.width + 64u / kQ - 1u) / (64u / kQ);
+  const uint64_t waves = static_cast<uint64_t>(a.batch) * blocks;
+  in_grids((waves + kWaves - 1u) / kWaves, [&](uint64_t begin, dim3 grid) { scan_step_kernel<T, kS, kQ><<<grid, dim3(64 * kWaves), 0, s>>>(a, blocks, begin, waves); });
+  return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_step(const ScanArgs& a, hipStream_t s) {
+  if (a.states == 1u) return launch_step<T, 1, 1>(a, s);
+  if (a.states <= 4u) return launch_step<T, 4, 1>(a, s);
+  if (a.states <= 8u) return launch_step<T, 4, 2>(a, s);
+  if (a.states <= 16u) return launch_step<T, 4, 4>(a, s);
+  if (a.states <= 32u) return launch_step<T, 4, 8>(a, s);
+  return launch_step<T, 4, 16>(a, s);
+}
+
+uint64_t workgroups(const ScanArgs& a, uint32_t stretches, uint32_t across) { return static_cast<uint64_t>(a.batch) * stretches * a.groups * across; }
 
 }  // namespace
 
 // Stretches where sequences and channels are fewer waves than kFew: so many that there are kEnough.
 ScanCut scan_cut(const ScanArgs& a) {
-  constexpr uint64_t kFew = 768, kEnough = 4096;
+  constexpr uint64_t kFew = 768, kEnough = 16384;
   ScanCut K{};
   K.chunks = (a.steps + kChunk - 1u) / kChunk;
-  const uint32_t channels = kWaves * wave_channels<false>(a.states), each = a.width / a.groups;
+  const uint32_t channels = kWaves * wave_channels<Kind::kWalk>(a.states), summary = kWaves * wave_channels<Kind::kSummary>(a.states), each = a.width / a.groups;
   K.across = (each + channels - 1u) / channels;
+  K.across_summary = (each + summary - 1u) / summary;
   const uint64_t waves = static_cast<uint64_t>(a.batch) * a.groups * ((each + channels / kWaves - 1u) / (channels / kWaves));
   K.stretches = 1u;
   K.stretch = K.chunks > 0u ? K.chunks : 1u;
@@ -237,6 +309,7 @@ uint64_t scan_scratch_words(const ScanArgs& a) {
 }
 
 hipError_t launch_scan(const ScanArgs& a, int dtype, unsigned long long* scratch, hipStream_t s) {
+  if (a.steps == 1u) return dtype == 0 ? launch_step<float>(a, s) : dtype == 1 ? launch_step<__bf16>(a, s) : launch_step<_Float16>(a, s);
   ScanCut K = scan_cut(a);
   if (K.stretches > 1u) {
     const uint64_t slots = static_cast<uint64_t>(a.batch) * K.stretches;
@@ -244,15 +317,21 @@ hipError_t launch_scan(const ScanArgs& a, int dtype, unsigned long long* scratch
     K.sums = K.starts + slots * a.width * a.states;
     K.cuts = reinterpret_cast<uint32_t*>(K.sums + slots * a.width);
   }
-  return by_states<false>(a.states, dtype, [&](auto type, auto layout) {
-    using T = decltype(type);
-    constexpr int kS = decltype(layout)::kS, kQ = decltype(layout)::kQ;
-    if (K.stretches > 1u) {
-      in_grids(workgroups(a, K, K.stretches - 1u), [&](uint64_t begin, dim3 grid) { scan_kernel<T, kS, kQ, true><<<grid, dim3(64 * kWaves), 0, s>>>(a, K, begin); });
-      const uint64_t all = static_cast<uint64_t>(a.batch) * a.width * a.states;
-      in_grids((all + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_join_kernel<<<grid, dim3(256), 0, s>>>(a, K, begin); });
-    }
-    in_grids(workgroups(a, K, K.stretches), [&](uint64_t begin, dim3 grid) { scan_kernel<T, kS, kQ, false><<<grid, dim3(64 * kWaves), 0, s>>>(a, K, begin); });
+  if (K.stretches > 1u) {
+    const hipError_t e = by_states<Kind::kSummary>(a.states, dtype, [&](auto type, auto layout) {
+      in_grids(workgroups(a, K.stretches - 1u, K.across_summary), [&](uint64_t begin, dim3 grid) {
+        scan_kernel<decltype(type), decltype(layout)::kS, decltype(layout)::kQ, true><<<grid, dim3(64 * kWaves), 0, s>>>(a, K, begin);
+      });
+      return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    const uint64_t all = static_cast<uint64_t>(a.batch) * a.width * a.states;
+    in_grids((all + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_join_kernel<<<grid, dim3(256), 0, s>>>(a, K, begin); });
+  }
+  return by_states<Kind::kWalk>(a.states, dtype, [&](auto type, auto layout) {
+    in_grids(workgroups(a, K.stretches, K.across), [&](uint64_t begin, dim3 grid) {
+      scan_kernel<decltype(type), decltype(layout)::kS, decltype(layout)::kQ, false><<<grid, dim3(64 * kWaves), 0, s>>>(a, K, begin);
+    });
     return hipGetLastError();
   });
 }

@@ -20,10 +20,14 @@ namespace {
 
 constexpr uint32_t kRearWaves = 4;     // of a workgroup of the first launch
 constexpr uint32_t kRearTile = 8;      // steps of a wave at a time in the first launch
+// A sequence of a few steps more than a chunk has is taken as one, by workgroups of more waves: no launch but the third is needed for it, and no workgroups with next to nothing to do.
+// 20 x 35 x 1500 fp32, the backward pass: 63 us, in two chunks 73.  (With layouts whose waves walk eight steps.)
+constexpr uint32_t kWholeWaves = 6, kWholeTile = 8, kWholeStates = 32;
 
 struct RearCut {
-  uint32_t chunks, across;             // chunks of a sequence, workgroups of the first launch for a group's channels
+  uint32_t chunks, kept, across;       // chunks of a sequence, states kept of it, workgroups of the first launch for a group's channels
   uint32_t splits, blocks;             // workgroups of the third for them, stretches of a wave's channels
+  bool whole;                          // a sequence is one chunk, and longer than others
   float* ends;                         // [batch][chunks][width][states]: what a chunk hands on from 0, then what comes in behind it
   float* sums;                         // [batch][chunks][width]
   uint32_t* cuts;                      // [batch][chunks]
@@ -175,20 +179,20 @@ __device__ __forceinline__ void sum_channels(float (&v)[kAll], uint32_t lane, ui
   }
 }
 
-template <int kS, int kQ, int kT>
+template <int kS, int kQ, int kT, uint32_t kWaves>
 struct SharedBackward {
-  static constexpr uint32_t kStates = kS * kQ, kChannels = 64 / kQ, kTile = kT, kWaves = kChunk / kTile;
-  float rows_b[kChunk * kStates], rows_c[kChunk * kStates];
+  static constexpr uint32_t kStates = kS * kQ, kChannels = 64 / kQ, kTile = kT;
+  float rows_b[kWaves * kTile * kStates], rows_c[kWaves * kTile * kStates];
   float of_step[kWaves][3][kChannels * kTile];     // sizes, size * input, gradient before the gate
   float parts[2][kWaves][3][64 * kS];              // what a wave's steps do: decay, state, gradient
   float da[2][kWaves][64 * kS], own[2][kWaves][2][kChannels];
 };
 
-template <typename T, int kS, int kQ, int kT>
-__global__ void __launch_bounds__(64 * (kChunk / kT)) scan_backward_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
+template <typename T, int kS, int kQ, int kT, uint32_t kWaves>
+__global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
   typedef Spot<kS, kQ, kT> At;
-  constexpr uint32_t kTile = kT, kWaves = kChunk / kTile, kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
-  __shared__ __attribute__((aligned(16))) SharedBackward<kS, kQ, kT> lds;
+  constexpr uint32_t kTile = kT, kWalked = kWaves * kTile, kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
+  __shared__ __attribute__((aligned(16))) SharedBackward<kS, kQ, kT, kWaves> lds;
   uint64_t rest = begin + blockIdx.x;
   const uint32_t split = uniform(static_cast<uint32_t>(rest % K.splits));
   rest /= K.splits;
@@ -196,14 +200,14 @@ __global__ void __launch_bounds__(64 * (kChunk / kT)) scan_backward_kernel(ScanA
   rest /= A.groups;
   const uint32_t chunk = uniform(static_cast<uint32_t>(rest % K.chunks)), b = uniform(static_cast<uint32_t>(rest / K.chunks));
   const uint32_t wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63u, each = A.width / A.groups;
-  const uint32_t n = steps_of(A.lengths, b, A.steps), first = chunk * kChunk, count = steps_in(first, kChunk, n);
+  const uint32_t n = steps_of(A.lengths, b, A.steps), first = chunk * kChunk, count = steps_in(first, kWalked, n);
   const uint32_t t0 = first + wave * kTile, valid = steps_in(t0, kTile, n), behind = steps_in(t0, kTile, A.steps);
   const bool gate = A.gate.data != nullptr;
   const uint64_t row = static_cast<uint64_t>(A.width) * A.states, slot = static_cast<uint64_t>(b) * K.chunks + chunk;
   const uint32_t per = (K.blocks + K.splits - 1u) / K.splits, from = split * per, upto = min(from + per, K.blocks);
   if (count == 0u) {                   // (the same for the whole workgroup) nothing of the row is here: zeros, and what comes in behind the chunk goes on before it
     const uint32_t first_channel = min(from * kChannels, each), channels = min(upto * kChannels, each) - min(first_channel, min(upto * kChannels, each));
-    const uint32_t length = steps_in(first, kChunk, A.steps), both = A.groups * A.states;
+    const uint32_t length = steps_in(first, kWalked, A.steps), both = A.groups * A.states;
     for (uint32_t i = threadIdx.x; i < channels; i += 64u * kWaves) {
       const uint32_t c = group * each + first_channel + i;
       for (uint32_t t = 0; t < length; ++t) {
@@ -225,9 +229,9 @@ __global__ void __launch_bounds__(64 * (kChunk / kT)) scan_backward_kernel(ScanA
     }
     return;
   }
-  stage<T, kChunk, kStates>(lds.rows_b, A.b, A, b, group, first, count, 64u * kWaves);
-  stage<T, kChunk, kStates>(lds.rows_c, A.c, A, b, group, first, count, 64u * kWaves);
-  const uint64_t anew = anew_from(A, b, first, kChunk, n);
+  stage<T, kWalked, kStates>(lds.rows_b, A.b, A, b, group, first, count, 64u * kWaves);
+  stage<T, kWalked, kStates>(lds.rows_c, A.c, A, b, group, first, count, 64u * kWaves);
+  const uint64_t anew = anew_from(A, b, first, kWalked, n);
   constexpr uint32_t kBits = (1u << kTile) - 1u;
   const uint32_t starts = static_cast<uint32_t>(anew >> (wave * kTile)) & kBits;
   float sums[2 * kTile * kS] = {};     // of the gradients of B and C
@@ -276,7 +280,7 @@ __global__ void __launch_bounds__(64 * (kChunk / kT)) scan_backward_kernel(ScanA
       }
     }
     read_states(A.a, A, at, rate_in);
-    read_states(A.kept + slot * row, A, at, h_in);
+    read_states(A.kept + (static_cast<uint64_t>(b) * K.kept + chunk) * row, A, at, h_in);
     if (K.chunks > 1u) read_states(K.ends + slot * row, A, at, g_in);
     else if (G.dh_last) read_states(G.dh_last + b * row, A, at, g_in);
     through_in = A.d ? A.d[at.c] : 0.0f;
@@ -469,14 +473,18 @@ __global__ void __launch_bounds__(256) scan_hand_on_kernel(const float* dh_last,
 }
 
 RearCut rear_cut(const ScanArgs& a) {
-  constexpr uint64_t kEnough = 1024;                                                  // workgroups of the third launch that fill the device
+  // Workgroups of the third launch: each has a start of its own (rows to stage), so no more of them than fill the device, a few times over where rows end early and leave workgroups with nothing to
+  // do.  us, 20 x 35 x 1500 fp32 with 512 / 1024 / 2048 53 / 62 / 77; 6 x 1001 x 1502 f16 with 24 states and lengths of 0 to 1001 502 / 271 / 242, 4096 268.
+  const uint64_t kEnough = a.lengths ? 2048 : 512;
   RearCut K{};
-  const uint32_t channels = wave_channels<true>(a.states), each = a.width / a.groups;
-  K.chunks = (a.steps + kChunk - 1u) / kChunk;
-  K.across = (each + kRearWaves * channels - 1u) / (kRearWaves * channels);
+  const uint32_t channels = wave_channels<Kind::kBackward>(a.states), rear = kRearWaves * wave_channels<Kind::kSummary>(a.states), each = a.width / a.groups;
+  K.kept = (a.steps + kChunk - 1u) / kChunk;
+  K.whole = a.steps > kChunk && a.steps <= kWholeWaves * kWholeTile && a.states <= kWholeStates;
+  K.chunks = K.whole ? 1u : K.kept;
+  K.across = (each + rear - 1u) / rear;
   K.blocks = (each + channels - 1u) / channels;
   const uint64_t apart = static_cast<uint64_t>(a.batch) * K.chunks * a.groups;
-  const uint64_t want = apart > 0u ? (kEnough + apart - 1u) / apart : 1u;
+  const uint64_t want = apart > 0u && apart < kEnough ? kEnough / apart : 1u;
   K.splits = static_cast<uint32_t>(want < K.blocks ? want : K.blocks);
   return K;
 }
@@ -505,15 +513,25 @@ hipError_t launch_scan_backward(const ScanArgs& a, const ScanGradArgs& g, int dt
   K.rows = K.parts + W.parts;
   const uint64_t slots = static_cast<uint64_t>(a.batch) * K.chunks, weights = static_cast<uint64_t>(a.width) * a.states;
   if (slots > 0u) {
-    const hipError_t e = by_states<true>(a.states, dtype, [&](auto type, auto layout) {
+    if (K.chunks > 1u) {
+      const hipError_t e = by_states<Kind::kSummary>(a.states, dtype, [&](auto type, auto layout) {
+        in_grids((slots - a.batch) * a.groups * K.across, [&](uint64_t begin, dim3 grid) {
+          scan_rear_kernel<decltype(type), decltype(layout)::kS, decltype(layout)::kQ><<<grid, dim3(64 * kRearWaves), 0, s>>>(a, g, K, begin);
+        });
+        return hipGetLastError();
+      });
+      if (e != hipSuccess) return e;
+      in_grids((a.batch * weights + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_rear_join_kernel<<<grid, dim3(256), 0, s>>>(a, g, K, begin); });
+    }
+    const hipError_t e = by_states<Kind::kBackward>(a.states, dtype, [&](auto type, auto layout) {
       using T = decltype(type);
       constexpr int kS = decltype(layout)::kS, kQ = decltype(layout)::kQ, kT = decltype(layout)::kT;
-      if (K.chunks > 1u) {
-        in_grids((slots - a.batch) * a.groups * K.across, [&](uint64_t begin, dim3 grid) { scan_rear_kernel<T, kS, kQ><<<grid, dim3(64 * kRearWaves), 0, s>>>(a, g, K, begin); });
-        in_grids((a.batch * weights + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_rear_join_kernel<<<grid, dim3(256), 0, s>>>(a, g, K, begin); });
-      }
       in_grids(slots * a.groups * K.splits, [&](uint64_t begin, dim3 grid) {
-        scan_backward_kernel<T, kS, kQ, kT><<<grid, dim3(64 * (kChunk / kT)), 0, s>>>(a, g, K, begin);
+        if (K.whole) {
+          if constexpr (kT == kWholeTile) scan_backward_kernel<T, kS, kQ, kT, kWholeWaves><<<grid, dim3(64 * kWholeWaves), 0, s>>>(a, g, K, begin);
+        } else {
+          scan_backward_kernel<T, kS, kQ, kT, kChunk / kT><<<grid, dim3(64 * (kChunk / kT)), 0, s>>>(a, g, K, begin);
+        }
       });
       const uint64_t all = static_cast<uint64_t>(a.batch) * a.steps * 2u * a.groups * a.states;
       in_grids((all + 255u) / 256u, [&](uint64_t begin, dim3 grid) { scan_rows_kernel<T><<<grid, dim3(256), 0, s>>>(a, g, K, begin); });
