@@ -23,10 +23,11 @@ namespace {
 typedef unsigned long long Pair;       // token << 32 | row; tokens outside the vocabulary have `vocab`, behind all others
 
 constexpr uint32_t kCounted = 4096;    // rows up to which pairs are ranked by counting
-constexpr uint32_t kBlock = 4096;      // rows of a workgroup of the radix sort
+constexpr uint32_t kBlock = 1024;      // rows of a workgroup of the radix sort
+constexpr uint32_t kFewBlocks = 64;    // of those, up to which each adds up the others' counts by itself
 constexpr uint32_t kDigit = 8, kBins = 1u << kDigit;
 constexpr uint32_t kSegment = 32;      // pairs of a segment
-constexpr uint32_t kJoinWaves = 8;
+constexpr uint32_t kJoinWaves = 4;
 constexpr uint32_t kFillRows = 8;      // rows of the table that a wave looks after
 
 __device__ __forceinline__ uint32_t known(int32_t token, uint32_t vocab) {
@@ -121,14 +122,30 @@ __global__ void __launch_bounds__(1024) prefix_kernel(uint32_t* counts, uint32_t
   if (threadIdx.x == 0u) totals[blockIdx.x] = carry;
 }
 
-// Puts a block's pairs where their digit's come, in their order: ranks within a wave by ballots, between waves by their counts.
+// Puts a block's pairs where their digit's come, in their order (totals == null: `before` holds the counts themselves): ranks within a wave by ballots, between waves by their counts.
 __global__ void __launch_bounds__(1024) place_kernel(const Pair* from, const int32_t* tokens, uint32_t rows, uint32_t vocab, uint32_t shift, const uint32_t* before,
                                                      const uint32_t* totals, Pair* to) {
   constexpr uint32_t kRounds = kBlock / 1024u;
   __shared__ uint32_t bins[16][kBins], start[kBins];
   const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
   for (uint32_t i = threadIdx.x; i < 16u * kBins; i += 1024u) (&bins[0][0])[i] = 0u;
-  if (threadIdx.x < kBins) start[threadIdx.x] = totals[threadIdx.x];
+  uint32_t here = 0u;                                 // of the digit, in the blocks before
+  if (threadIdx.x < kBins) {
+    const uint32_t* mine = before + static_cast<uint64_t>(threadIdx.x) * gridDim.x;
+    if (totals) {
+      here = mine[blockIdx.x];
+      start[threadIdx.x] = totals[threadIdx.x];
+    } else {
+      uint32_t all = 0u;
+#pragma unroll 8
+      for (uint32_t i = 0; i < gridDim.x; ++i) {
+        const uint32_t n = mine[i];
+        all += n;
+        here += i < blockIdx.x ? n : 0u;
+      }
+      start[threadIdx.x] = all;
+    }
+  }
   __syncthreads();
   if (wave == 0u) {                                   // where each digit begins
     uint32_t n[kBins / 64u], sum = 0u;
@@ -166,7 +183,7 @@ __global__ void __launch_bounds__(1024) place_kernel(const Pair* from, const int
   }
   __syncthreads();
   if (threadIdx.x < kBins) {
-    uint32_t at = start[threadIdx.x] + before[static_cast<uint64_t>(threadIdx.x) * gridDim.x + blockIdx.x];
+    uint32_t at = start[threadIdx.x] + here;
     for (uint32_t w = 0; w < 16u; ++w) {
       const uint32_t n = bins[w][threadIdx.x];
       bins[w][threadIdx.x] = at;
@@ -312,9 +329,10 @@ __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(EmbedArgs A, Embe
   const uint32_t segment = static_cast<uint32_t>(at / S.across), block = static_cast<uint32_t>(at % S.across), wave = uniform(threadIdx.x >> 6), l = threadIdx.x & 63u;
   const uint32_t first = segment * kSegment, next = first + kSegment;
   if (next >= A.rows) return;
-  const uint32_t token = uniform(token_of(S.sorted[next]));
-  if (token >= A.vocab || uniform(token_of(S.sorted[next - 1u])) != token) return;
-  if (first > 0u && uniform(token_of(S.sorted[first - 1u])) == token) return;     // it began before
+  // (asked for at once: most runs do not span segments, and their workgroups are gone with that)
+  const Pair behind = S.sorted[next], last = S.sorted[next - 1u], before = S.sorted[first > 0u ? first - 1u : 0u];
+  const uint32_t token = uniform(token_of(behind));
+  if (token >= A.vocab || uniform(token_of(last)) != token || (first > 0u && uniform(token_of(before)) == token)) return;     // (the last: it began before)
   const uint32_t end = lower_bound(S.sorted, A.rows, token + 1u);
   const uint32_t parts = (end - 1u) / kSegment - segment + 1u, each = (parts + kJoinWaves - 1u) / kJoinWaves;
   const Channels<kVec> lane(block, A.width);
@@ -411,8 +429,8 @@ hipError_t launch_embed_backward(const EmbedArgs& a, const EmbedGradArgs& g, int
     for (uint32_t p = 0; p < passes; ++p) {
       Pair* to = (passes - 1u - p) % 2u == 0u ? sorted : other;      // the last pass into `sorted`
       count_kernel<<<dim3(blocks), dim3(1024), 0, s>>>(from, a.tokens, a.rows, a.vocab, p * kDigit, counts);
-      prefix_kernel<<<dim3(kBins), dim3(1024), 0, s>>>(counts, blocks, totals);
-      place_kernel<<<dim3(blocks), dim3(1024), 0, s>>>(from, a.tokens, a.rows, a.vocab, p * kDigit, counts, totals, to);
+      if (blocks > kFewBlocks) prefix_kernel<<<dim3(kBins), dim3(1024), 0, s>>>(counts, blocks, totals);
+      place_kernel<<<dim3(blocks), dim3(1024), 0, s>>>(from, a.tokens, a.rows, a.vocab, p * kDigit, counts, blocks > kFewBlocks ? totals : nullptr, to);
       from = to;
     }
   } else if (a.rows > 0u) {
