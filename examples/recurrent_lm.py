@@ -1,7 +1,7 @@
 """A small recurrent language model, trained by distillation on several (virtual) data-parallel workers that exchange compressed gradients.
 
-The operators together, as a program uses them: a teacher scores its tokens (rgc_gated_recurrence, rgc_token_logprobs: its top alternatives), every
-worker's student learns from them (rgc_gated_recurrence, rgc_distill_loss, rgc_gated_recurrence_backward), the gradients are compressed
+The operators together, as a program uses them: a teacher scores its tokens (rgc_embed_tokens, rgc_gated_recurrence, rgc_token_logprobs: its top alternatives), every
+worker's student learns from them (the same, rgc_distill_loss, rgc_gated_recurrence_backward, rgc_embed_tokens_backward), the gradients are compressed
 (rgc_compress_layers), the messages of all workers added up (rgc_decompress_accumulate) and applied; at last the student continues a text one token at
 a time, its state updated in place, with the log probability of what it says and what else it might have said.
 
@@ -56,22 +56,29 @@ class Run:
         self.one = rgc.Recurrence(x[:, :1], gate[:, :1], self.y[:, :1], out_gate=out_gate[:, :1], h0=self.h, h_last=self.h)
         self.logits = empty(batch * steps, model.vocab)
         self.dlogits = torch.empty_like(self.logits)
+        self.tokens = torch.zeros(batch * steps, dtype=torch.int32, device="cuda")
+        self.embedded = empty(batch * steps, width)
+        self.lookup = rgc.Embedding(model.parameters["embedding"], self.tokens, self.embedded)
+
+    def embed(self, ctx, tokens, stream):
+        self.tokens.copy_(tokens.reshape(-1))
+        rgc.rgc_embed_tokens(ctx, self.lookup, stream)
+        return self.embedded
 
     def forward(self, ctx, tokens, stream):
         p = self.model.parameters
-        torch.matmul(p["embedding"][tokens], p["inner"], out=self.inner)
+        torch.matmul(self.embed(ctx, tokens, stream), p["inner"], out=self.inner.view(-1, 3 * self.model.width))
         rgc.rgc_gated_recurrence(ctx, self.recurrence, stream)
         torch.matmul(self.y.view(-1, self.model.width), p["output"], out=self.logits)
 
-    def backward(self, ctx, tokens, stream):
-        """Gradients of the parameters, from self.dlogits."""
+    def backward(self, ctx, stream):
+        """Gradients of the parameters for the tokens of the last forward pass, from self.dlogits."""
         p, width = self.model.parameters, self.model.width
         torch.matmul(self.dlogits, p["output"].t(), out=self.dy.view(-1, width))
         rgc.rgc_gated_recurrence_backward(ctx, self.recurrence, self.grads, stream)
-        dinner, x = self.dinner.view(-1, 3 * width), p["embedding"][tokens].view(-1, width)
-        embedding = torch.zeros_like(p["embedding"])
-        embedding.index_add_(0, tokens.reshape(-1), dinner @ p["inner"].t())
-        return {"embedding": embedding, "inner": x.t() @ dinner, "output": self.y.view(-1, width).t() @ self.dlogits}
+        dinner, embedding = self.dinner.view(-1, 3 * width), torch.empty_like(p["embedding"])
+        rgc.rgc_embed_tokens_backward(ctx, self.lookup, dinner @ p["inner"].t(), embedding, rgc.RGC_OVERWRITE, stream)
+        return {"embedding": embedding, "inner": self.embedded.t() @ dinner, "output": self.y.view(-1, width).t() @ self.dlogits}
 
 
 class Teacher:
@@ -118,7 +125,7 @@ class Worker:
         self.run.forward(self.ctx, tokens, stream)
         self.targets.copy_(following.reshape(-1))
         rgc.rgc_distill_loss(self.ctx, self.distillation, stream)
-        return self.run.backward(self.ctx, tokens, stream)
+        return self.run.backward(self.ctx, stream)
 
     def compress(self, gradients, momentum, stream):
         for flat, g in zip(self.gradients, gradients.values()):
@@ -158,7 +165,7 @@ def continue_text(student, tokens=12, top=3):
     said = rgc.TokenScores(run.logits, target, logprob=logprob)
     token, out = 0, []
     for _ in range(tokens):
-        torch.matmul(p["embedding"][token:token + 1], p["inner"], out=run.inner.view(1, -1))
+        torch.matmul(run.embed(ctx, torch.tensor([token], device="cuda"), stream), p["inner"], out=run.inner.view(1, -1))
         rgc.rgc_gated_recurrence(ctx, run.one, stream)
         torch.matmul(run.y.view(-1, width), p["output"], out=run.logits)
         rgc.rgc_token_logprobs(ctx, scores, stream)
