@@ -124,36 +124,41 @@ __global__ void __launch_bounds__(64 * kWaves) scan_kernel(ScanArgs A, ScanCut K
       }
       if (t0 + kSteps < end) ask(t0 + kSteps);
       wave_sync();
-#pragma unroll
-      for (uint32_t m = 0; m < kTiles; ++m) {
-        const uint32_t tile = part + m * kTile, valid = steps_in(tile, kTile, count);
-        if (valid == 0u) continue;
+      const uint32_t all_starts = static_cast<uint32_t>(anew >> part), left = count - part;
+      // (a step that is not there has the size 0 and brings nothing: it leaves the states as they are)
+      auto walk = [&](uint32_t m, auto with_starts) __attribute__((always_inline)) {
+        const uint32_t tile = part + m * kTile;
         float size[kTile], fed[kTile], y[kTile] = {};
         read_tile(&sizes[wave][at.channel * kApart + m * kTile], size);
         read_tile(&feeds[wave][at.channel * kApart + m * kTile], fed);
-        const uint32_t starts = static_cast<uint32_t>(anew >> tile) & 0xFFu;
-        // (a step that is not there has the size 0 and brings nothing: it leaves the states as they are)
-        auto walk = [&](auto with_starts) __attribute__((always_inline)) {
+        const uint32_t starts = all_starts >> (m * kTile);
 #pragma unroll
-          for (uint32_t t = 0; t < kTile; ++t) {
-            float in[kS], out[kS];
-            read_shared<kS>(in_b + (tile + t) * kStates, in);
-            if constexpr (!kSummary) read_shared<kS>(in_c + (tile + t) * kStates, out);
+        for (uint32_t t = 0; t < kTile; ++t) {
+          float in[kS], out[kS];
+          read_shared<kS>(in_b + (tile + t) * kStates, in);
+          if constexpr (!kSummary) read_shared<kS>(in_c + (tile + t) * kStates, out);
 #pragma unroll
-            for (uint32_t s = 0; s < kS; ++s) {
-              if (with_starts && ((starts >> t) & 1u) != 0u) h[s] = 0.0f;
-              h[s] = __fmaf_rn(__builtin_amdgcn_exp2f(size[t] * rate[s]), h[s], fed[t] * in[s]);
-              if constexpr (!kSummary) y[t] = __fmaf_rn(h[s], out[s], y[t]);
-            }
+          for (uint32_t s = 0; s < kS; ++s) {
+            if (with_starts && ((starts >> t) & 1u) != 0u) h[s] = 0.0f;
+            h[s] = __fmaf_rn(__builtin_amdgcn_exp2f(size[t] * rate[s]), h[s], fed[t] * in[s]);
+            if constexpr (!kSummary) y[t] = __fmaf_rn(h[s], out[s], y[t]);
           }
-        };
-        if (starts == 0u) walk(No{}); else walk(Yes{});
+        }
         if constexpr (!kSummary) {
           sum_for_owners<kQ, kTile>(y, at.lane);
 #pragma unroll
           for (uint32_t j = 0; j < kOwn; ++j)
-            if (at.owner && at.own + j < valid) to_y.at(m * kTile + j) = static_cast<T>(__fmaf_rn(through, input[m][j], y[j]) * shown[m][j]);
+            if (at.owner && (!with_starts || m * kTile + at.own + j < left)) to_y.at(m * kTile + j) = static_cast<T>(__fmaf_rn(through, input[m][j], y[j]) * shown[m][j]);
         }
+      };
+      // where all steps are there and none starts anew, without a branch between the tiles: one tile's sums go on beside the next one's steps
+      if (left >= kSteps && (all_starts & static_cast<uint32_t>((1ull << kSteps) - 1ull)) == 0u) {
+#pragma unroll
+        for (uint32_t m = 0; m < kTiles; ++m) walk(m, No{});
+      } else {
+#pragma unroll
+        for (uint32_t m = 0; m < kTiles; ++m)
+          if (m * kTile < left) walk(m, Yes{});
       }
       wave_sync();                     // (before the next tiles' sizes take their place)
       to_y.row += kSteps * to_y.step;
