@@ -301,9 +301,9 @@ struct Layout {
   static constexpr int kS = kStatesOfLane, kQ = kLanes, kT = kStepsAtOnce;
 };
 enum class Kind { kWalk, kSummary, kBackward };      // a walk along the steps for results, for what a stretch does to a state (or a gradient) alone, the backward walk
-// Calls f with the type and the layout.  us, 8 x 4096 x 2048 bf16 with 16 states (20 x 35 x 1500 fp32): backward two states a lane, eight steps, four waves a workgroup 1547 (53), four states, four
+// Calls f with the type and the layout.  us, 8 x 4096 x 2048 bf16 with 16 states (20 x 35 x 1500 fp32): backward two states a lane, eight steps, four waves a workgroup 1520 (53), four states, four
 // steps, eight waves 1711 (63; all of a compute unit's waves wait at one barrier), four states and eight steps do not fit into registers; the walk by two states a lane 550, by four 1013 (half
-// the waves: one a SIMD); a summary, which has little to do once a channel and waves enough, by four 262, by two 311.
+// the waves: one a SIMD), by one 998; a summary, which has little to do once a channel and waves enough, by four 262, by two 311.
 template <Kind kKind, typename F>
 hipError_t by_states(uint32_t states, int dtype, F&& f) {
   auto with = [&](auto layout) {

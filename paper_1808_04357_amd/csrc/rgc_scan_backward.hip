@@ -179,6 +179,28 @@ __device__ __forceinline__ void sum_channels(float (&v)[kAll], uint32_t lane, ui
   }
 }
 
+// Which of a tile's steps a lane owns, where their sums are made for four steps at a time: the exchange leaves lane q the sum of step q / (kQ / 4) of the four, or of several.
+template <int kQ, int kT>
+struct Owned {
+  static constexpr uint32_t kFours = kT / 4, kPer = kQ >= 4 ? 1 : 4 / kQ, kOwn = kQ > 4 ? (kFours * 4 + kQ - 1) / kQ : kFours * kPer, kLanes = kQ >= 4 ? kQ / 4 : 1;   // kLanes get the same sum
+  static_assert(kFours == 1 || kFours == 2, "one or two times four steps");
+  uint32_t q;
+  // the lane's first step, and the others' distance from it
+  __device__ uint32_t first() const { return kQ > 4 ? (kFours == 2 ? (q & 1u) * 4u : 0u) + q / kLanes : q * kPer; }
+  static constexpr uint32_t apart(uint32_t j) { return kQ > 4 ? 0u : j / kPer * 4u + j % kPer; }
+  // of the lanes that own the same step, the one that stores its results
+  __device__ bool stores() const { return kQ <= 4 || (kFours == 2 ? q / 2u % (kLanes / 2u > 0u ? kLanes / 2u : 1u) == 0u : q % kLanes == 0u); }
+  // takes its sums of the four-th four steps
+  __device__ void take(uint32_t four, const float (&v)[4], float (&own)[kOwn]) const {
+    if constexpr (kQ > 4) {
+      own[0] = kFours == 1 || (q & 1u) == four ? v[0] : own[0];
+    } else {
+#pragma unroll
+      for (uint32_t j = 0; j < kPer; ++j) own[four * kPer + j] = v[j];
+    }
+  }
+};
+
 template <int kS, int kQ, int kT, uint32_t kWaves>
 struct SharedBackward {
   static constexpr uint32_t kStates = kS * kQ, kChannels = 64 / kQ, kTile = kT;
@@ -188,10 +210,14 @@ struct SharedBackward {
   float da[2][kWaves][64 * kS], own[2][kWaves][2][kChannels];
 };
 
+// Two waves a SIMD, of workgroups that wait for different barriers. With 16 states it has 190 registers (the sums of B's and C's gradients are 32 of them); where they are made to be 168, for three
+// waves, they spill, and 8 x 4096 x 2048 bf16 takes 3700 to 4300 us instead of 1520; with the states behind the steps in shared memory instead, which leaves eleven to spill, 2680, and 1720 with two
+// waves. Sums over a channel's states are made for four steps at a time: for eight 206 registers, 1600 (24 states, 6 x 1001 x 1502 f16: 152 instead of 281, as two waves find room).
 template <typename T, int kS, int kQ, int kT, uint32_t kWaves>
 __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, ScanGradArgs G, RearCut K, uint64_t begin) {
   typedef Spot<kS, kQ, kT> At;
-  constexpr uint32_t kTile = kT, kWalked = kWaves * kTile, kOwn = At::kOwn, kStates = At::kStates, kChannels = At::kChannels;
+  typedef Owned<kQ, kT> Mine;
+  constexpr uint32_t kTile = kT, kWalked = kWaves * kTile, kOwn = Mine::kOwn, kStates = At::kStates, kChannels = At::kChannels;
   __shared__ __attribute__((aligned(16))) SharedBackward<kS, kQ, kT, kWaves> lds;
   uint64_t rest = begin + blockIdx.x;
   const uint32_t split = uniform(static_cast<uint32_t>(rest % K.splits));
@@ -253,7 +279,7 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
       }
     }
   };
-  const uint32_t own_step = At(A, group, 0u).own;
+  const uint32_t own_step = Mine{lane % kQ}.first();
   const Column<T> x_at(A.x, b, t0, own_step, group * each), v_at(A.delta, b, t0, own_step, group * each), z_at(gate ? A.gate : A.x, b, t0, own_step, group * each),
       dy_at(G.dy, b, t0, own_step, group * each), dx_at(G.dx, b, t0, own_step, group * each), dv_at(G.ddelta, b, t0, own_step, group * each),
       dz_at(gate ? G.dgate : G.dx, b, t0, own_step, group * each);
@@ -266,16 +292,16 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
     if (valid == kTile) {
 #pragma unroll
       for (uint32_t j = 0; j < kOwn; ++j) {
-        x[j] = x_at.at(j, along), v[j] = v_at.at(j, along), dy[j] = dy_at.at(j, along);
-        z[j] = gate ? z_at.at(j, along) : static_cast<T>(0.0f);
+        x[j] = x_at.at(Mine::apart(j), along), v[j] = v_at.at(Mine::apart(j), along), dy[j] = dy_at.at(Mine::apart(j), along);
+        z[j] = gate ? z_at.at(Mine::apart(j), along) : static_cast<T>(0.0f);
       }
     } else {
 #pragma unroll
       for (uint32_t j = 0; j < kOwn; ++j) {
         x[j] = v[j] = z[j] = dy[j] = static_cast<T>(0.0f);
-        if (at.own + j < valid) {
-          x[j] = x_at.at(j, along), v[j] = v_at.at(j, along), dy[j] = dy_at.at(j, along);
-          if (gate) z[j] = z_at.at(j, along);
+        if (own_step + Mine::apart(j) < valid) {
+          x[j] = x_at.at(Mine::apart(j), along), v[j] = v_at.at(Mine::apart(j), along), dy[j] = dy_at.at(Mine::apart(j), along);
+          if (gate) z[j] = z_at.at(Mine::apart(j), along);
         }
       }
     }
@@ -293,6 +319,8 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
     const uint32_t turn = (block - from) & 1u;
     const At at(A, group, block, here(lane));
     const uint32_t along = (at.c - group * each) * static_cast<uint32_t>(sizeof(T));
+    const Mine mine{at.q};
+    const uint32_t own = mine.first();
     float input[kOwn], grow[kOwn], size_own[kOwn], dinner_own[kOwn], dgate_by[kOwn];      // dgate_by: the gate's gradient, without its factor `inner`
     float h[kS], g[kS], rate[kS];
     const float through = through_in;
@@ -300,7 +328,7 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
 #pragma unroll
     for (uint32_t j = 0; j < kOwn; ++j) {
       float slope;
-      const bool there = at.mine && at.own + j < valid;           // (lanes behind the group have no part in its sums)
+      const bool there = at.mine && own + Mine::apart(j) < valid;           // (lanes behind the group have no part in its sums)
       input[j] = there ? static_cast<float>(x[j]) : 0.0f;
       const float size = size_of(A, static_cast<float>(v[j]), bias_in, grow[j]), given = there ? static_cast<float>(dy[j]) : 0.0f;
       size_own[j] = there ? size : 0.0f;
@@ -308,9 +336,9 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
       dgate_by[j] = given * slope;
       if (!there) dinner_own[j] = dgate_by[j] = 0.0f;
       held(input[j]), held(size_own[j]), held(grow[j]), held(dinner_own[j]), held(dgate_by[j]);
-      of_size[at.own + j] = size_own[j];
-      of_fed[at.own + j] = size_own[j] * input[j];
-      of_grad[at.own + j] = dinner_own[j];
+      of_size[own + Mine::apart(j)] = size_own[j];
+      of_fed[own + Mine::apart(j)] = size_own[j] * input[j];
+      of_grad[own + Mine::apart(j)] = dinner_own[j];
     }
 #pragma unroll
     for (uint32_t s = 0; s < kS; ++s) rate[s] = rate_in[s], h[s] = at.mine ? h_in[s] : 0.0f, g[s] = at.mine ? g_in[s] : 0.0f;
@@ -377,7 +405,7 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
       for (uint32_t s = 0; s < kS; ++s) g[s] = cut ? own[s] : __fmaf_rn(p[s], g[s], own[s]);
     }
     if (block > from) finish(block - 1u, turn ^ 1u);
-    float inner[kTile] = {}, came[kTile] = {}, slower[kTile] = {}, da[kS] = {};
+    float inner[kOwn] = {}, came[kOwn] = {}, slower[kOwn] = {}, da[kS] = {};      // of the lane's own steps, sums over the channel's states; da of its states, over the steps
     float after[kTile][kS];
 #pragma unroll
     for (uint32_t t = 0; t < kTile; ++t) {
@@ -390,49 +418,55 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
       }
     }
 #pragma unroll
-    for (uint32_t t = kTile; t-- > 0u;) {
-      float in[kS], out[kS];
-      read_shared<kS>(row_b + t * kStates, in);
-      read_shared<kS>(row_c + t * kStates, out);
-      const bool anew_here = with_starts && ((starts >> t) & 1u) != 0u;
+    for (uint32_t four = Mine::kFours; four-- > 0u;) {
+      float inner4[4] = {}, came4[4] = {}, slower4[4] = {};
 #pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) {
-        float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
-        if (anew_here) prior = 0.0f;
-        inner[t] = __fmaf_rn(after[t][s], out[s], inner[t]);
-        sums[(kTile + t) * kS + s] = __fmaf_rn(dinner[t], after[t][s], sums[(kTile + t) * kS + s]);
-        const float d = __fmaf_rn(dinner[t], out[s], g[s]);
-        came[t] = __fmaf_rn(d, in[s], came[t]);
-        sums[t * kS + s] = __fmaf_rn(fed[t], d, sums[t * kS + s]);
-        g[s] = a[t][s] * d;
-        const float lost = g[s] * prior;                           // the gradient of the decay's exponent
-        slower[t] = __fmaf_rn(lost, rate[s], slower[t]);
-        da[s] = __fmaf_rn(lost, size[t], da[s]);
-        if (anew_here) g[s] = 0.0f;
+      for (uint32_t i = 4; i-- > 0u;) {
+        const uint32_t t = four * 4u + i;
+        float in[kS], out[kS];
+        read_shared<kS>(row_b + t * kStates, in);
+        read_shared<kS>(row_c + t * kStates, out);
+        const bool anew_here = with_starts && ((starts >> t) & 1u) != 0u;
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) {
+          float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
+          if (anew_here) prior = 0.0f;
+          inner4[i] = __fmaf_rn(after[t][s], out[s], inner4[i]);
+          sums[(kTile + t) * kS + s] = __fmaf_rn(dinner[t], after[t][s], sums[(kTile + t) * kS + s]);
+          const float d = __fmaf_rn(dinner[t], out[s], g[s]);
+          came4[i] = __fmaf_rn(d, in[s], came4[i]);
+          sums[t * kS + s] = __fmaf_rn(fed[t], d, sums[t * kS + s]);
+          g[s] = a[t][s] * d;
+          const float lost = g[s] * prior;                         // the gradient of the decay's exponent
+          slower4[i] = __fmaf_rn(lost, rate[s], slower4[i]);
+          da[s] = __fmaf_rn(lost, size[t], da[s]);
+          if (anew_here) g[s] = 0.0f;
+        }
       }
+      sum_for_owners<kQ, 4>(inner4, lane);
+      sum_for_owners<kQ, 4>(came4, lane);
+      sum_for_owners<kQ, 4>(slower4, lane);
+      mine.take(four, inner4, inner), mine.take(four, came4, came), mine.take(four, slower4, slower);
     }
     if (G.dh0 && chunk == 0u && wave == 0u) write_states(G.dh0 + b * row, A, at, g);
-    sum_for_owners<kQ, kTile>(inner, lane);
-    sum_for_owners<kQ, kTile>(came, lane);
-    sum_for_owners<kQ, kTile>(slower, lane);
     float dd = 0.0f, dbias = 0.0f;
 #pragma unroll
     for (uint32_t j = 0; j < kOwn; ++j) {
-      const bool there = at.own + j < valid;
+      const bool there = own + Mine::apart(j) < valid;
       const float dv = there ? __fmaf_rn(came[j], input[j], slower[j] * kLn2) * grow[j] : 0.0f;
       const float dx = there ? __fmaf_rn(came[j], size_own[j], dinner_own[j] * through) : 0.0f;
       const float dgate = there ? __fmaf_rn(through, input[j], inner[j]) * dgate_by[j] : 0.0f;
       dd += there ? dinner_own[j] * input[j] : 0.0f;
       dbias += dv;
-      if (at.owner && at.own + j < behind) {
-        dx_at.at(j, along) = static_cast<T>(dx);
-        dv_at.at(j, along) = static_cast<T>(dv);
-        if (gate) dz_at.at(j, along) = static_cast<T>(dgate);
+      if (at.mine && mine.stores() && own + Mine::apart(j) < behind) {
+        dx_at.at(Mine::apart(j), along) = static_cast<T>(dx);
+        dv_at.at(Mine::apart(j), along) = static_cast<T>(dv);
+        if (gate) dz_at.at(Mine::apart(j), along) = static_cast<T>(dgate);
       }
     }
     
-    dd = sum_lanes<kQ>(at.first ? dd : 0.0f);
-    dbias = sum_lanes<kQ>(at.first ? dbias : 0.0f);
+    dd = sum_lanes<kQ>(mine.stores() ? dd : 0.0f);
+    dbias = sum_lanes<kQ>(mine.stores() ? dbias : 0.0f);
     write_shared<kS>(&lds.da[turn][wave][at.lane * kS], da);
     if (at.q == 0u) lds.own[turn][wave][0][at.channel] = dd, lds.own[turn][wave][1][at.channel] = dbias;
   }
