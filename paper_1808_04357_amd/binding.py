@@ -44,6 +44,8 @@ EXPORTS = ["rgc_create", "rgc_destroy", "rgc_k_for_density", "rgc_compress_layer
            "rgc_compress_layers_threshold",
            "rgc_token_logprobs", "rgc_token_logprobs_backward", "rgc_distill_loss", "rgc_gated_recurrence",
            "rgc_gated_recurrence_backward",
+           "rgc_embed_tokens", "rgc_embed_tokens_backward", "rgc_causal_convolution", "rgc_causal_convolution_backward",
+           "rgc_selective_scan", "rgc_selective_scan_backward",
            "rgc_decompress_accumulate", "rgc_reset_hints", "rgc_poison_hints", "rgc_limit_optional_scratch", "rgc_limit_looks", "rgc_selftest",
            "rgc_last_paths", "rgc_last_stats", "rgc_last_error", "rgc_decompress_status", "rgc_profile_enable", "rgc_profile_read", "rgc_stream_yardstick", "rgc_strerror"]
 
