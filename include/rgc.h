@@ -449,14 +449,14 @@ typedef struct {
 int rgc_causal_convolution(rgc_ctx* ctx, const rgc_convolution* convolution, void* hip_stream);
 
 /* Its backward pass: gradients of x, of the weights and the bias (summed over batch and steps) and of the kept inputs, from those of y and of `last`.
- * convolution: the descriptor of the forward call; y and last are not read.  Steps beyond a row's length get zeros. */
+ * convolution: the descriptor of the forward call; y and last are not read.  Steps beyond a row's length get zeros.  dx is neither x nor dy. */
 typedef struct {
   rgc_sequence   dy;       /* read only                                                             */
   rgc_sequence   dx;
   float*         dweight;  /* [width][taps]                                                         */
   float*         dbias;    /* [width] or NULL                                                       */
   const void*    dlast;    /* [batch][taps - 1][width] or NULL: zeros                               */
-  void*          dbefore;  /* [batch][taps - 1][width] or NULL                                      */
+  void*          dbefore;  /* [batch][taps - 1][width] or NULL; not dlast itself                    */
 } rgc_convolution_grads;
 
 int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* convolution, const rgc_convolution_grads* grads,
@@ -470,7 +470,7 @@ int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* convolu
  *  - Steps at lengths[b] and beyond (lengths are read as at least 0 and at most `steps`) are not looked at; y is 0 there.  h_last is the state after the row's last step,
  *    h0 if it has none.
  *  - A rate of -inf is read as the lowest finite one.  A state that is infinite or NaN makes the later ones so, until one starts anew.
- * h_last may be h0 itself; steps == 1 is the serving form.
+ * h_last may be h0 itself; y is none of the sequences that are read.  steps == 1 is the serving form.
  * Limits: batch, steps >= 0, both < 2^31; 1 <= width <= RGC_WIDTH_MAX, a multiple of `groups`; 1 <= states <= RGC_SCAN_STATES_MAX; strides of steps at most
  * RGC_SCAN_STRIDE_MAX elements. */
 #define RGC_SCAN_CHUNK 32
@@ -500,7 +500,8 @@ typedef struct {
 int rgc_selective_scan(rgc_ctx* ctx, const rgc_scan* scan, void* hip_stream);
 
 /* Its backward pass.  scan: the descriptor of the forward call, with `kept` as that call left it; y, h0 and h_last are not read.  Gradients of a, d and delta_bias are
- * summed over batch and steps, those of B and C over their group's channels, in orders made of the sizes alone.  Steps beyond a row's length get zeros. */
+ * summed over batch and steps, those of B and C over their group's channels, in orders made of the sizes alone.  Steps beyond a row's length get zeros.
+ * The sequences that are written are none of those that are read, nor one another; dh0 may be dh_last itself. */
 typedef struct {
   rgc_sequence   dy;          /* read only                                                            */
   rgc_sequence   dx, ddelta;

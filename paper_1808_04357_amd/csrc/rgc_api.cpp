@@ -8,6 +8,7 @@
 #include <cmath>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <memory>
 #include <new>
 #include <numeric>
@@ -1464,6 +1465,15 @@ bool scan_sequence_fits(const rgc_sequence& v, const rgc_scan* r, int32_t width,
   return sequence_fits(v, r->batch, r->steps, width, r->dtype, written) && (r->steps <= 1 || v.step_stride <= RGC_SCAN_STRIDE_MAX);
 }
 
+// None of the first ones is one of the others, nor of those behind it.
+bool apart(std::initializer_list<const void*> written, std::initializer_list<const void*> read) {
+  for (auto w = written.begin(); w != written.end(); ++w) {
+    if (!*w) continue;
+    if (std::find(read.begin(), read.end(), *w) != read.end() || std::find(w + 1, written.end(), *w) != written.end()) return false;
+  }
+  return true;
+}
+
 // (steps == 0: only h0 and h_last are there; batch == 0: nothing is)
 bool scan_fits(const rgc_scan* r) {
   if (r->batch < 0 || r->batch > kInt32Most || r->steps < 0 || r->steps > kInt32Most || r->width < 1 || r->width > RGC_WIDTH_MAX) return false;
@@ -1692,6 +1702,7 @@ int rgc_causal_convolution(rgc_ctx* ctx, const rgc_convolution* r, void* hip_str
 int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* r, const rgc_convolution_grads* g, void* hip_stream) {
   if (!ctx || !r || !g || !convolution_fits(r) || !g->dweight || !words_aligned({g->dweight, g->dbias})) return RGC_EINVAL;
   if (!aligned_to(g->dlast, element_size(r->dtype)) || !aligned_to(g->dbefore, element_size(r->dtype))) return RGC_EINVAL;
+  if (r->batch > 0 && r->taps > 1 && g->dlast && g->dlast == g->dbefore) return RGC_EINVAL;
   if (r->batch > 0 && r->steps > 0) {
     if (!sequence_fits(g->dy, r, false) || !sequence_fits(g->dx, r, true) || g->dx.data == g->dy.data || g->dx.data == r->x.data) return RGC_EINVAL;
   }
@@ -1709,7 +1720,9 @@ int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* r, cons
 
 int rgc_selective_scan(rgc_ctx* ctx, const rgc_scan* r, void* hip_stream) {
   if (!ctx || !r || !scan_fits(r)) return RGC_EINVAL;
-  if (r->batch > 0 && r->steps > 0 && !scan_sequence_fits(r->y, r, r->width, true)) return RGC_EINVAL;
+  if (r->batch > 0 && r->steps > 0) {
+    if (!scan_sequence_fits(r->y, r, r->width, true) || !apart({r->y.data}, {r->x.data, r->delta.data, r->gate.data, r->b.data, r->c.data})) return RGC_EINVAL;
+  }
   if (r->batch == 0) return RGC_OK;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
@@ -1728,6 +1741,8 @@ int rgc_selective_scan_backward(rgc_ctx* ctx, const rgc_scan* r, const rgc_scan_
     auto fits = [&](const rgc_sequence& v, int32_t width, bool written) { return scan_sequence_fits(v, r, width, written); };
     if (!r->kept || !fits(g->dy, r->width, false) || !fits(g->dx, r->width, true) || !fits(g->ddelta, r->width, true)) return RGC_EINVAL;
     if (!fits(g->db, both, true) || !fits(g->dc, both, true) || (r->gate.data && !fits(g->dgate, r->width, true))) return RGC_EINVAL;
+    if (!apart({g->dx.data, g->ddelta.data, r->gate.data ? g->dgate.data : nullptr, g->db.data, g->dc.data},
+               {g->dy.data, r->x.data, r->delta.data, r->gate.data, r->b.data, r->c.data})) return RGC_EINVAL;
   }
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");

@@ -285,6 +285,11 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
+// What comes out of a stretch of steps, of what goes in and of what it makes of 0.  Its decay comes in two equal factors: where states grow their product may be beyond all numbers though no state
+// is, and a 0 stays 0.
+__device__ __forceinline__ float half_decay(float rate, float size) { return __builtin_amdgcn_exp2f(0.5f * rate * size); }
+__device__ __forceinline__ float past(float half, float in, float made) { return in == 0.0f ? made : __fmaf_rn(half, half * in, made); }
+
 // Bit i: the state starts anew at step first + i (of the next `most`, and of those the row has).
 __device__ __forceinline__ uint64_t anew_from(const ScanArgs& A, uint32_t b, uint32_t first, uint32_t most, uint32_t n) {
   if (!A.resets) return 0u;

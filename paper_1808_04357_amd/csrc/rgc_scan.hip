@@ -197,19 +197,19 @@ __global__ void __launch_bounds__(256) scan_join_kernel(ScanArgs A, ScanCut K, u
   const float* sums = K.sums + b * K.stretches * A.width + c;
   const uint32_t* cuts = K.cuts + b * K.stretches;
   for (uint32_t k0 = 0; k0 < K.stretches; k0 += kAtOnce) {
-    float ends[kAtOnce], decay[kAtOnce];
+    float ends[kAtOnce], half[kAtOnce];
 #pragma unroll
     for (uint32_t j = 0; j < kAtOnce; ++j) {
       const uint32_t k = min(k0 + j, K.stretches - 1u);                              // (the last one's slot is unset memory, and not used)
       ends[j] = to[k * row];
-      decay[j] = __builtin_amdgcn_exp2f(rate * sums[static_cast<uint64_t>(k) * A.width]);
+      half[j] = half_decay(rate, sums[static_cast<uint64_t>(k) * A.width]);
     }
 #pragma unroll
     for (uint32_t j = 0; j < kAtOnce; ++j) {
       const uint32_t k = k0 + j;
       if (k >= K.stretches) continue;
       to[k * row] = h;
-      if (k + 1u < K.stretches) h = cuts[k] != 0u ? ends[j] : __fmaf_rn(decay[j], h, ends[j]);
+      if (k + 1u < K.stretches) h = cuts[k] != 0u ? ends[j] : past(half[j], h, ends[j]);
     }
   }
 }

@@ -135,19 +135,19 @@ __global__ void __launch_bounds__(256) scan_rear_join_kernel(ScanArgs A, ScanGra
   const uint32_t* cuts = K.cuts + b * K.chunks;
   for (uint32_t done = 0; done < K.chunks; done += kAtOnce) {
     const uint32_t upto = K.chunks - done;                                           // chunks left, the last of them first
-    float ends[kAtOnce], decay[kAtOnce];
+    float ends[kAtOnce], half[kAtOnce];
 #pragma unroll
     for (uint32_t j = 0; j < kAtOnce; ++j) {
       const uint32_t k = max(upto, j + 1u) - j - 1u;                                 // (the first one's slot is unset memory, and not used)
       ends[j] = to[k * row];
-      decay[j] = __builtin_amdgcn_exp2f(rate * sums[static_cast<uint64_t>(k) * A.width]);
+      half[j] = half_decay(rate, sums[static_cast<uint64_t>(k) * A.width]);
     }
 #pragma unroll
     for (uint32_t j = 0; j < kAtOnce; ++j) {
       if (j >= upto) continue;
       const uint32_t k = upto - j - 1u;
       to[k * row] = g;
-      if (k > 0u) g = cuts[k] != 0u ? ends[j] : __fmaf_rn(decay[j], g, ends[j]);
+      if (k > 0u) g = cuts[k] != 0u ? ends[j] : past(half[j], g, ends[j]);
     }
   }
 }
@@ -206,7 +206,7 @@ struct SharedBackward {
   static constexpr uint32_t kStates = kS * kQ, kChannels = 64 / kQ, kTile = kT;
   float rows_b[kWaves * kTile * kStates], rows_c[kWaves * kTile * kStates];
   float of_step[kWaves][3][kChannels * kTile];     // sizes, size * input, gradient before the gate
-  float parts[2][kWaves][3][64 * kS];              // what a wave's steps do: decay, state, gradient
+  float parts[2][kWaves][3][64 * kS];              // what a wave's steps do: half of the decay's exponent, as a factor, state, gradient
   float da[2][kWaves][64 * kS], own[2][kWaves][2][kChannels];
 };
 
@@ -315,161 +315,160 @@ __global__ void __launch_bounds__(64 * kWaves) scan_backward_kernel(ScanArgs A, 
   if (from < upto) ask(from);
   __syncthreads();
   auto turns = [&](auto with_starts) __attribute__((always_inline)) {
-  for (uint32_t block = from; block < upto; ++block) {
-    const uint32_t turn = (block - from) & 1u;
-    const At at(A, group, block, here(lane));
-    const uint32_t along = (at.c - group * each) * static_cast<uint32_t>(sizeof(T));
-    const Mine mine{at.q};
-    const uint32_t own = mine.first();
-    float input[kOwn], grow[kOwn], size_own[kOwn], dinner_own[kOwn], dgate_by[kOwn];      // dgate_by: the gate's gradient, without its factor `inner`
-    float h[kS], g[kS], rate[kS];
-    const float through = through_in;
-    float *const of_size = lds.of_step[wave][0] + at.channel * kTile, *const of_fed = lds.of_step[wave][1] + at.channel * kTile, *const of_grad = lds.of_step[wave][2] + at.channel * kTile;
+    for (uint32_t block = from; block < upto; ++block) {
+      const uint32_t turn = (block - from) & 1u;
+      const At at(A, group, block, here(lane));
+      const uint32_t along = (at.c - group * each) * static_cast<uint32_t>(sizeof(T));
+      const Mine mine{at.q};
+      const uint32_t own = mine.first();
+      float input[kOwn], grow[kOwn], size_own[kOwn], dinner_own[kOwn], dgate_by[kOwn];      // dgate_by: the gate's gradient, without its factor `inner`
+      float h[kS], g[kS], rate[kS];
+      const float through = through_in;
+      float *const of_size = lds.of_step[wave][0] + at.channel * kTile, *const of_fed = lds.of_step[wave][1] + at.channel * kTile, *const of_grad = lds.of_step[wave][2] + at.channel * kTile;
 #pragma unroll
-    for (uint32_t j = 0; j < kOwn; ++j) {
-      float slope;
-      const bool there = at.mine && own + Mine::apart(j) < valid;           // (lanes behind the group have no part in its sums)
-      input[j] = there ? static_cast<float>(x[j]) : 0.0f;
-      const float size = size_of(A, static_cast<float>(v[j]), bias_in, grow[j]), given = there ? static_cast<float>(dy[j]) : 0.0f;
-      size_own[j] = there ? size : 0.0f;
-      dinner_own[j] = given * shown_of(gate, static_cast<float>(z[j]), slope);
-      dgate_by[j] = given * slope;
-      if (!there) dinner_own[j] = dgate_by[j] = 0.0f;
-      held(input[j]), held(size_own[j]), held(grow[j]), held(dinner_own[j]), held(dgate_by[j]);
-      of_size[own + Mine::apart(j)] = size_own[j];
-      of_fed[own + Mine::apart(j)] = size_own[j] * input[j];
-      of_grad[own + Mine::apart(j)] = dinner_own[j];
-    }
-#pragma unroll
-    for (uint32_t s = 0; s < kS; ++s) rate[s] = rate_in[s], h[s] = at.mine ? h_in[s] : 0.0f, g[s] = at.mine ? g_in[s] : 0.0f;
-    finite_rates(rate);
-    if (block + 1u < upto) ask(block + 1u);
-    wave_sync();
-    float size[kTile], fed[kTile], dinner[kTile];
-    read_tile(of_size, size);
-    read_tile(of_fed, fed);
-    read_tile(of_grad, dinner);
-    wave_sync();
-    const float *const row_b = lds.rows_b + (wave * kTile * kStates + at.q * kS), *const row_c = lds.rows_c + (wave * kTile * kStates + at.q * kS);
-    // (a step that is not there has the size 0 and brings nothing: it leaves states and gradients as they are)
-    float a[kTile][kS], own_h[kS] = {}, own_g[kS] = {}, whole[kS];
-#pragma unroll
-    for (uint32_t t = 0; t < kTile; ++t) {
-      float in[kS];
-      read_shared<kS>(row_b + t * kStates, in);
-#pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) {
-        a[t][s] = __builtin_amdgcn_exp2f(size[t] * rate[s]);
-        if (with_starts && ((starts >> t) & 1u) != 0u) own_h[s] = 0.0f;
-        own_h[s] = t == 0u ? fed[t] * in[s] : __fmaf_rn(a[t][s], own_h[s], fed[t] * in[s]);
+      for (uint32_t j = 0; j < kOwn; ++j) {
+        float slope;
+        const bool there = at.mine && own + Mine::apart(j) < valid;           // (lanes behind the group have no part in its sums)
+        input[j] = there ? static_cast<float>(x[j]) : 0.0f;
+        const float size = size_of(A, static_cast<float>(v[j]), bias_in, grow[j]), given = there ? static_cast<float>(dy[j]) : 0.0f;
+        size_own[j] = there ? size : 0.0f;
+        dinner_own[j] = given * shown_of(gate, static_cast<float>(z[j]), slope);
+        dgate_by[j] = given * slope;
+        if (!there) dinner_own[j] = dgate_by[j] = 0.0f;
+        held(input[j]), held(size_own[j]), held(grow[j]), held(dinner_own[j]), held(dgate_by[j]);
+        of_size[own + Mine::apart(j)] = size_own[j];
+        of_fed[own + Mine::apart(j)] = size_own[j] * input[j];
+        of_grad[own + Mine::apart(j)] = dinner_own[j];
       }
-    }
 #pragma unroll
-    for (uint32_t t = kTile; t-- > 0u;) {
-      float out[kS];
-      read_shared<kS>(row_c + t * kStates, out);
+      for (uint32_t s = 0; s < kS; ++s) rate[s] = rate_in[s], h[s] = at.mine ? h_in[s] : 0.0f, g[s] = at.mine ? g_in[s] : 0.0f;
+      finite_rates(rate);
+      if (block + 1u < upto) ask(block + 1u);
+      wave_sync();
+      float size[kTile], fed[kTile], dinner[kTile];
+      read_tile(of_size, size);
+      read_tile(of_fed, fed);
+      read_tile(of_grad, dinner);
+      wave_sync();
+      const float *const row_b = lds.rows_b + (wave * kTile * kStates + at.q * kS), *const row_c = lds.rows_c + (wave * kTile * kStates + at.q * kS);
+      // (a step that is not there has the size 0 and brings nothing: it leaves states and gradients as they are)
+      float a[kTile][kS], own_h[kS] = {}, own_g[kS] = {}, half[kS];
 #pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) {
-        own_g[s] = a[t][s] * (t + 1u == kTile ? dinner[t] * out[s] : __fmaf_rn(dinner[t], out[s], own_g[s]));
-        if (with_starts && ((starts >> t) & 1u) != 0u) own_g[s] = 0.0f;
-      }
-    }
-    float total = 0.0f;
-#pragma unroll
-    for (uint32_t t = 0; t < kTile; ++t) total += size[t];
-#pragma unroll
-    for (uint32_t s = 0; s < kS; ++s) whole[s] = __builtin_amdgcn_exp2f(total * rate[s]);
-    write_shared<kS>(&lds.parts[turn][wave][0][at.lane * kS], whole);
-    write_shared<kS>(&lds.parts[turn][wave][1][at.lane * kS], own_h);
-    write_shared<kS>(&lds.parts[turn][wave][2][at.lane * kS], own_g);
-    __syncthreads();
-    // the state before the wave's steps and the gradient behind them, from the other waves' stretches
-#pragma unroll
-    for (uint32_t w = 0; w + 1u < kWaves; ++w) {
-      if (w >= wave) break;
-      float p[kS], own[kS];
-      read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
-      read_shared<kS>(&lds.parts[turn][w][1][at.lane * kS], own);
-      const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
-#pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) h[s] = cut ? own[s] : __fmaf_rn(p[s], h[s], own[s]);
-    }
-#pragma unroll
-    for (uint32_t w = kWaves - 1u; w > 0u; --w) {
-      if (w <= wave) break;
-      float p[kS], own[kS];
-      read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
-      read_shared<kS>(&lds.parts[turn][w][2][at.lane * kS], own);
-      const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
-#pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) g[s] = cut ? own[s] : __fmaf_rn(p[s], g[s], own[s]);
-    }
-    if (block > from) finish(block - 1u, turn ^ 1u);
-    float inner[kOwn] = {}, came[kOwn] = {}, slower[kOwn] = {}, da[kS] = {};      // of the lane's own steps, sums over the channel's states; da of its states, over the steps
-    float after[kTile][kS];
-#pragma unroll
-    for (uint32_t t = 0; t < kTile; ++t) {
-      float in[kS];
-      read_shared<kS>(row_b + t * kStates, in);
-#pragma unroll
-      for (uint32_t s = 0; s < kS; ++s) {
-        const float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
-        after[t][s] = __fmaf_rn(a[t][s], with_starts && ((starts >> t) & 1u) != 0u ? 0.0f : prior, fed[t] * in[s]);
-      }
-    }
-#pragma unroll
-    for (uint32_t four = Mine::kFours; four-- > 0u;) {
-      float inner4[4] = {}, came4[4] = {}, slower4[4] = {};
-#pragma unroll
-      for (uint32_t i = 4; i-- > 0u;) {
-        const uint32_t t = four * 4u + i;
-        float in[kS], out[kS];
+      for (uint32_t t = 0; t < kTile; ++t) {
+        float in[kS];
         read_shared<kS>(row_b + t * kStates, in);
-        read_shared<kS>(row_c + t * kStates, out);
-        const bool anew_here = with_starts && ((starts >> t) & 1u) != 0u;
 #pragma unroll
         for (uint32_t s = 0; s < kS; ++s) {
-          float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
-          if (anew_here) prior = 0.0f;
-          inner4[i] = __fmaf_rn(after[t][s], out[s], inner4[i]);
-          sums[(kTile + t) * kS + s] = __fmaf_rn(dinner[t], after[t][s], sums[(kTile + t) * kS + s]);
-          const float d = __fmaf_rn(dinner[t], out[s], g[s]);
-          came4[i] = __fmaf_rn(d, in[s], came4[i]);
-          sums[t * kS + s] = __fmaf_rn(fed[t], d, sums[t * kS + s]);
-          g[s] = a[t][s] * d;
-          const float lost = g[s] * prior;                         // the gradient of the decay's exponent
-          slower4[i] = __fmaf_rn(lost, rate[s], slower4[i]);
-          da[s] = __fmaf_rn(lost, size[t], da[s]);
-          if (anew_here) g[s] = 0.0f;
+          a[t][s] = __builtin_amdgcn_exp2f(size[t] * rate[s]);
+          if (with_starts && ((starts >> t) & 1u) != 0u) own_h[s] = 0.0f;
+          own_h[s] = t == 0u ? fed[t] * in[s] : __fmaf_rn(a[t][s], own_h[s], fed[t] * in[s]);
         }
       }
-      sum_for_owners<kQ, 4>(inner4, lane);
-      sum_for_owners<kQ, 4>(came4, lane);
-      sum_for_owners<kQ, 4>(slower4, lane);
-      mine.take(four, inner4, inner), mine.take(four, came4, came), mine.take(four, slower4, slower);
-    }
-    if (G.dh0 && chunk == 0u && wave == 0u) write_states(G.dh0 + b * row, A, at, g);
-    float dd = 0.0f, dbias = 0.0f;
 #pragma unroll
-    for (uint32_t j = 0; j < kOwn; ++j) {
-      const bool there = own + Mine::apart(j) < valid;
-      const float dv = there ? __fmaf_rn(came[j], input[j], slower[j] * kLn2) * grow[j] : 0.0f;
-      const float dx = there ? __fmaf_rn(came[j], size_own[j], dinner_own[j] * through) : 0.0f;
-      const float dgate = there ? __fmaf_rn(through, input[j], inner[j]) * dgate_by[j] : 0.0f;
-      dd += there ? dinner_own[j] * input[j] : 0.0f;
-      dbias += dv;
-      if (at.mine && mine.stores() && own + Mine::apart(j) < behind) {
-        dx_at.at(Mine::apart(j), along) = static_cast<T>(dx);
-        dv_at.at(Mine::apart(j), along) = static_cast<T>(dv);
-        if (gate) dz_at.at(Mine::apart(j), along) = static_cast<T>(dgate);
+      for (uint32_t t = kTile; t-- > 0u;) {
+        float out[kS];
+        read_shared<kS>(row_c + t * kStates, out);
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) {
+          own_g[s] = a[t][s] * (t + 1u == kTile ? dinner[t] * out[s] : __fmaf_rn(dinner[t], out[s], own_g[s]));
+          if (with_starts && ((starts >> t) & 1u) != 0u) own_g[s] = 0.0f;
+        }
       }
+      float total = 0.0f;
+#pragma unroll
+      for (uint32_t t = 0; t < kTile; ++t) total += size[t];
+#pragma unroll
+      for (uint32_t s = 0; s < kS; ++s) half[s] = half_decay(rate[s], total);
+      write_shared<kS>(&lds.parts[turn][wave][0][at.lane * kS], half);
+      write_shared<kS>(&lds.parts[turn][wave][1][at.lane * kS], own_h);
+      write_shared<kS>(&lds.parts[turn][wave][2][at.lane * kS], own_g);
+      __syncthreads();
+      // the state before the wave's steps and the gradient behind them, from the other waves' stretches
+#pragma unroll
+      for (uint32_t w = 0; w + 1u < kWaves; ++w) {
+        if (w >= wave) break;
+        float p[kS], own[kS];
+        read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
+        read_shared<kS>(&lds.parts[turn][w][1][at.lane * kS], own);
+        const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) h[s] = cut ? own[s] : past(p[s], h[s], own[s]);
+      }
+#pragma unroll
+      for (uint32_t w = kWaves - 1u; w > 0u; --w) {
+        if (w <= wave) break;
+        float p[kS], own[kS];
+        read_shared<kS>(&lds.parts[turn][w][0][at.lane * kS], p);
+        read_shared<kS>(&lds.parts[turn][w][2][at.lane * kS], own);
+        const bool cut = with_starts && (static_cast<uint32_t>(anew >> (w * kTile)) & kBits) != 0u;
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) g[s] = cut ? own[s] : past(p[s], g[s], own[s]);
+      }
+      if (block > from) finish(block - 1u, turn ^ 1u);
+      float inner[kOwn] = {}, came[kOwn] = {}, slower[kOwn] = {}, da[kS] = {};      // of the lane's own steps, sums over the channel's states; da of its states, over the steps
+      float after[kTile][kS];
+#pragma unroll
+      for (uint32_t t = 0; t < kTile; ++t) {
+        float in[kS];
+        read_shared<kS>(row_b + t * kStates, in);
+#pragma unroll
+        for (uint32_t s = 0; s < kS; ++s) {
+          const float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
+          after[t][s] = __fmaf_rn(a[t][s], with_starts && ((starts >> t) & 1u) != 0u ? 0.0f : prior, fed[t] * in[s]);
+        }
+      }
+#pragma unroll
+      for (uint32_t four = Mine::kFours; four-- > 0u;) {
+        float inner4[4] = {}, came4[4] = {}, slower4[4] = {};
+#pragma unroll
+        for (uint32_t i = 4; i-- > 0u;) {
+          const uint32_t t = four * 4u + i;
+          float in[kS], out[kS];
+          read_shared<kS>(row_b + t * kStates, in);
+          read_shared<kS>(row_c + t * kStates, out);
+          const bool anew_here = with_starts && ((starts >> t) & 1u) != 0u;
+#pragma unroll
+          for (uint32_t s = 0; s < kS; ++s) {
+            float prior = t == 0u ? h[s] : after[t > 0u ? t - 1u : 0u][s];
+            if (anew_here) prior = 0.0f;
+            inner4[i] = __fmaf_rn(after[t][s], out[s], inner4[i]);
+            sums[(kTile + t) * kS + s] = __fmaf_rn(dinner[t], after[t][s], sums[(kTile + t) * kS + s]);
+            const float d = __fmaf_rn(dinner[t], out[s], g[s]);
+            came4[i] = __fmaf_rn(d, in[s], came4[i]);
+            sums[t * kS + s] = __fmaf_rn(fed[t], d, sums[t * kS + s]);
+            g[s] = a[t][s] * d;
+            const float lost = g[s] * prior;                         // the gradient of the decay's exponent
+            slower4[i] = __fmaf_rn(lost, rate[s], slower4[i]);
+            da[s] = __fmaf_rn(lost, size[t], da[s]);
+            if (anew_here) g[s] = 0.0f;
+          }
+        }
+        sum_for_owners<kQ, 4>(inner4, lane);
+        sum_for_owners<kQ, 4>(came4, lane);
+        sum_for_owners<kQ, 4>(slower4, lane);
+        mine.take(four, inner4, inner), mine.take(four, came4, came), mine.take(four, slower4, slower);
+      }
+      if (G.dh0 && chunk == 0u && wave == 0u) write_states(G.dh0 + b * row, A, at, g);
+      float dd = 0.0f, dbias = 0.0f;
+#pragma unroll
+      for (uint32_t j = 0; j < kOwn; ++j) {
+        const bool there = own + Mine::apart(j) < valid;
+        const float dv = there ? __fmaf_rn(came[j], input[j], slower[j] * kLn2) * grow[j] : 0.0f;
+        const float dx = there ? __fmaf_rn(came[j], size_own[j], dinner_own[j] * through) : 0.0f;
+        const float dgate = there ? __fmaf_rn(through, input[j], inner[j]) * dgate_by[j] : 0.0f;
+        dd += there ? dinner_own[j] * input[j] : 0.0f;
+        dbias += dv;
+        if (at.mine && mine.stores() && own + Mine::apart(j) < behind) {
+          dx_at.at(Mine::apart(j), along) = static_cast<T>(dx);
+          dv_at.at(Mine::apart(j), along) = static_cast<T>(dv);
+          if (gate) dz_at.at(Mine::apart(j), along) = static_cast<T>(dgate);
+        }
+      }
+      dd = sum_lanes<kQ>(mine.stores() ? dd : 0.0f);
+      dbias = sum_lanes<kQ>(mine.stores() ? dbias : 0.0f);
+      write_shared<kS>(&lds.da[turn][wave][at.lane * kS], da);
+      if (at.q == 0u) lds.own[turn][wave][0][at.channel] = dd, lds.own[turn][wave][1][at.channel] = dbias;
     }
-    
-    dd = sum_lanes<kQ>(mine.stores() ? dd : 0.0f);
-    dbias = sum_lanes<kQ>(mine.stores() ? dbias : 0.0f);
-    write_shared<kS>(&lds.da[turn][wave][at.lane * kS], da);
-    if (at.q == 0u) lds.own[turn][wave][0][at.channel] = dd, lds.own[turn][wave][1][at.channel] = dbias;
-  }
   };
   // (in a chunk where nothing starts anew nothing has to be looked at for it; the same for the whole workgroup)
   if (anew == 0u) turns(No{}); else turns(Yes{});

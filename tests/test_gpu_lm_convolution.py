@@ -332,7 +332,8 @@ def test_refusals(rgc, ctx):
         assert refused(**changes)[0] == -1, changes
     for bad in (lambda: rgc.Convolution(x, w.half(), y), lambda: rgc.Convolution(x, w, y.half()), lambda: rgc.Convolution(x, w, y, before=kept[:, :2]), lambda: rgc.Convolution(x, w[:7], y),
                 lambda: rgc.Convolution(x, w, y, lengths=torch.zeros(2, device="cuda")), lambda: rgc.Convolution(x.transpose(1, 2), w, y), lambda: rgc.ConvolutionGrads(call, y, dx, dw[:, :3]),
-                lambda: rgc.ConvolutionGrads(call, y, dx, dw, dlast=kept.half()), lambda: rgc.rgc_causal_convolution_backward(ctx, call, rgc.ConvolutionGrads(call, y, y, dw))):
+                lambda: rgc.ConvolutionGrads(call, y, dx, dw, dlast=kept.half()), lambda: rgc.rgc_causal_convolution_backward(ctx, call, rgc.ConvolutionGrads(call, y, y, dw)),
+                lambda: rgc.rgc_causal_convolution_backward(ctx, call, rgc.ConvolutionGrads(call, y, dx, dw, dlast=kept, dbefore=kept))):
         with pytest.raises(rgc.RgcError):
             bad()
     torch.cuda.synchronize()

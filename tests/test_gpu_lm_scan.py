@@ -292,6 +292,44 @@ def test_sizes_far_out(rgc, ctx):
     assert torch.allclose(out[1].double().cpu(), leaf.grad, rtol=1e4 * U, atol=1e-30)
 
 
+@pytest.mark.parametrize("steps", [33, 47, 48, 49])
+@pytest.mark.parametrize("states", [8, 24, 32, 33])
+def test_a_few_steps_more_than_a_chunk(rgc, ctx, steps, states):
+    resets = np.random.default_rng(steps).random((4, steps)) < 0.1
+    check(rgc, ctx, 4, steps, 21, states, 1, "f32", lengths=np.array([steps, 32, 33, steps - 1], np.int32), garbage=True, resets=resets)
+
+
+def test_states_that_grow(rgc, ctx):
+    """A factor over many steps may be beyond all numbers where no state is."""
+    import torch
+    steps, width, states = 600, 5, 16
+    fives = lambda *s: torch.full(s, 5.0, device="cuda")             # noqa: E731
+    x, dy = torch.zeros(1, steps, width, device="cuda"), torch.zeros(1, steps, width, device="cuda")
+    delta, a, b = torch.ones_like(x), torch.full((width, states), 12.0, device="cuda"), torch.ones(1, steps, states, device="cuda")
+    x[:, -3:], dy[:, :3] = 1.0, 1.0                                  # nothing but zeros is what grows
+    y, h, kept = fives(1, steps, width), fives(1, width, states), fives(1, -(-steps // rgc.RGC_SCAN_CHUNK), width, states)
+    call = rgc.Scan(x, delta, a, b, b, y, h_last=h, states=kept)
+    rgc.rgc_selective_scan(ctx, call)
+    dx, dv, da, db, dc, dh0 = fives(1, steps, width), fives(1, steps, width), fives(width, states), fives(1, steps, states), fives(1, steps, states), fives(1, width, states)
+    rgc.rgc_selective_scan_backward(ctx, call, rgc.ScanGrads(call, dy, dx, dv, da, db, dc, dh0=dh0))
+    e = math.exp(12.0)
+    after = [1.0, 1.0 + e, 1.0 + e + e * e]
+    assert not y[0, :-3].any() and torch.allclose(y[0, -3:, 0].cpu().double(), torch.tensor(after, dtype=torch.float64) * states, rtol=1000 * U)
+    assert torch.allclose(h.cpu().double(), torch.full((1, width, states), after[2], dtype=torch.float64), rtol=1000 * U)
+    assert not dx[0, 3:].any() and torch.allclose(dx[0, :3, 0].cpu().double(), torch.tensor(after[::-1], dtype=torch.float64) * states, rtol=1000 * U)
+    assert torch.allclose(dh0.cpu().double(), torch.full((1, width, states), e * after[2], dtype=torch.float64), rtol=1000 * U)
+    assert not dv.any() and not da.any() and not db.any() and not dc.any()
+    # what is small grows by exp(150) within a chunk; exponents of up to 150 are off by (80 + 4) u of themselves
+    h0, dh_last = torch.full((1, width, states), 1e-37, device="cuda"), torch.full((1, width, states), 2e-37, device="cuda")
+    x.zero_(), dy.zero_(), delta.zero_(), a.fill_(1.0)
+    delta[:, 32:64] = 150.0 / 32.0
+    call = rgc.Scan(x, delta, a, b, b, y, h0=h0, h_last=h, states=kept)
+    rgc.rgc_selective_scan(ctx, call)
+    rgc.rgc_selective_scan_backward(ctx, call, rgc.ScanGrads(call, dy, dx, dv, da, db, dc, dh_last=dh_last, dh0=dh0))
+    for got, of in ((h, h0), (dh0, dh_last)):
+        assert torch.allclose(got.cpu().double(), of.cpu().double() * math.exp(150.0), rtol=150 * 84 * 2 * U)
+
+
 def test_infinite_rates_and_states(rgc, ctx):
     import torch
     x = torch.ones(1, 20, 2, device="cuda")
@@ -439,13 +477,20 @@ def test_refusals(rgc, ctx):
                     dict(softplus=2), dict(a=None), dict(a=a.data_ptr() + 2), dict(x=seq(None, 48, 8)), dict(delta=seq(None, 48, 8)), dict(b=seq(None, 24, 4)), dict(c=seq(None, 24, 4)),
                     dict(b=seq(b.data_ptr(), -24, 4)), dict(x=seq(x.data_ptr() + 2, 48, 8)), dict(gate=seq(x.data_ptr() + 1, 48, 8)), dict(h0=a.data_ptr() + 1), dict(x=seq(x.data_ptr(), 2 ** 50, 8))):
         assert refused(**changes) == (-1, -1), changes
-    for changes in (dict(y=seq(None, 48, 8)), dict(y=seq(y.data_ptr(), 8, 8)), dict(y=seq(y.data_ptr(), 48, 4))):
+    far = 2 ** 27 + 1                                                 # of steps: a tile's are addressed by 32 bits
+    for changes in (dict(x=seq(x.data_ptr(), 8, far)), dict(delta=seq(x.data_ptr(), 8, far)), dict(b=seq(b.data_ptr(), 4, far)), dict(c=seq(c.data_ptr(), 4, far))):
+        assert refused(**changes) == (-1, -1), changes
+    for changes in (dict(y=seq(None, 48, 8)), dict(y=seq(y.data_ptr(), 8, 8)), dict(y=seq(y.data_ptr(), 48, 4)), dict(y=seq(y.data_ptr(), 8, far)), dict(y=call.desc.x), dict(y=call.desc.delta),
+                    dict(gate=call.desc.y)):
         assert refused(**changes)[0] == -1, changes
     for changes in (dict(kept=None), dict(gate=call.desc.x)):          # (no place for the gate's gradient)
         assert refused(**changes)[1] == -1, changes
+    b2, c2 = zeros(2, 6, 4), zeros(2, 6, 4)
+    backward = lambda dy, dx, dv, db, dc: rgc.rgc_selective_scan_backward(ctx, call, rgc.ScanGrads(call, dy, dx, dv, zeros(8, 4), db, dc))      # noqa: E731
     for bad in (lambda: rgc.Scan(x, delta, a, b[..., :3], c, y), lambda: rgc.Scan(x, delta.half(), a, b, c, y), lambda: rgc.Scan(x, delta, a.half(), b, c, y), lambda: rgc.Scan(x, delta, a, b, c, y, groups=3),
                 lambda: rgc.Scan(x, delta, a, b, c, y, groups=2), lambda: rgc.Scan(x, delta, a, b, c, y, h0=zeros(2, 8)), lambda: rgc.Scan(x, delta, a, b, c, y, states=zeros(2, 2, 8, 4)),
-                lambda: rgc.Scan(x, delta, a, b, c, y, resets=zeros(2, 6)), lambda: rgc.ScanGrads(call, x, y, y, a, b, c, dgate=y), lambda: rgc.ScanGrads(call, x, y, y, a[:7], b, c)):
+                lambda: rgc.Scan(x, delta, a, b, c, y, resets=zeros(2, 6)), lambda: rgc.ScanGrads(call, x, y, y, a, b, c, dgate=y), lambda: rgc.ScanGrads(call, x, y, y, a[:7], b, c), lambda: backward(x, y, y, b2, c2), lambda: backward(x, x, y, b2, c2),
+                lambda: backward(x, y, zeros(2, 6, 8), b2, b2), lambda: backward(x, y, zeros(2, 6, 8), b, c2)):
         with pytest.raises(rgc.RgcError):
             bad()
     torch.cuda.synchronize()
