@@ -395,7 +395,7 @@ int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* recurrence
 
 /* Rows of an embedding table, scaled:  out[r] = scale * table[tokens[r]], rounded to its type once.
  * A token outside [0, vocab) is left out: its row is 0, and no row of the table is looked at for it.  A token may come as often as it likes.
- * Limits: 0 <= rows < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 1 <= width <= RGC_WIDTH_MAX; strides not negative, that of out at least width. */
+ * Limits: 0 <= rows < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 1 <= width <= RGC_WIDTH_MAX; strides not negative, that of out at least width.  out is not the table, dtable is not dout. */
 #define RGC_WIDTH_MAX 1048576
 
 typedef struct {

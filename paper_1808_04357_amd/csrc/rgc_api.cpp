@@ -1663,7 +1663,7 @@ int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* r, const r
 int rgc_embed_tokens(rgc_ctx* ctx, const rgc_embedding* a, void* hip_stream) {
   if (!ctx || !a || !embedding_fits(a)) return RGC_EINVAL;
   if (a->rows > 0 && !table_rows_fit(a->table, a->table_stride, a->vocab, a->table_dtype)) return RGC_EINVAL;
-  if (a->rows > 0 && (!table_rows_fit(a->out, a->out_stride, a->rows, a->dtype) || (a->rows > 1 && a->out_stride < a->width))) return RGC_EINVAL;
+  if (a->rows > 0 && (!table_rows_fit(a->out, a->out_stride, a->rows, a->dtype) || (a->rows > 1 && a->out_stride < a->width) || a->out == a->table)) return RGC_EINVAL;
   if (a->rows == 0) return RGC_OK;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");
@@ -1675,7 +1675,7 @@ int rgc_embed_tokens_backward(rgc_ctx* ctx, const rgc_embedding* a, const void* 
                               float* dtable, uint32_t flags, void* hip_stream) {
   if (!ctx || !a || !embedding_fits(a) || !dtable || !words_aligned({dtable})) return RGC_EINVAL;
   if (flags != RGC_OVERWRITE && flags != RGC_ADD_TO_DST) return RGC_EINVAL;
-  if (a->rows > 0 && !table_rows_fit(dout, dout_stride, a->rows, a->dtype)) return RGC_EINVAL;
+  if (a->rows > 0 && (!table_rows_fit(dout, dout_stride, a->rows, a->dtype) || dout == dtable)) return RGC_EINVAL;
   if (a->rows == 0 && flags == RGC_ADD_TO_DST) return RGC_OK;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return fail_hip(hipErrorInvalidDevice, "hipSetDevice");

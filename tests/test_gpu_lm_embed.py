@@ -233,7 +233,7 @@ def test_refusals(rgc, ctx):
     assert refused() == 0
     for changes in (dict(rows=-1), dict(rows=2 ** 31), dict(vocab=0), dict(vocab=4_194_305), dict(width=0), dict(width=2 ** 21), dict(dtype=3), dict(table_dtype=-1),
                     dict(table=None), dict(out=None), dict(tokens=None), dict(out_stride=7), dict(table_stride=-1), dict(scale=math.inf), dict(scale=math.nan),
-                    dict(table=good.table + 2), dict(tokens=good.tokens + 1), dict(out_stride=2 ** 60)):
+                    dict(table=good.table + 2), dict(tokens=good.tokens + 1), dict(out_stride=2 ** 60), dict(out=good.table, out_stride=8)):
         assert refused(**changes) == -1, changes
     dout, dtable = torch.zeros(4, 8, device="cuda"), torch.zeros(10, 8, device="cuda")
     call = rgc.Embedding(table, tokens, out)
@@ -243,7 +243,7 @@ def test_refusals(rgc, ctx):
     for bad in (lambda: rgc.Embedding(table, tokens.long(), out), lambda: rgc.Embedding(table, tokens[:3], out), lambda: rgc.Embedding(table.t(), tokens, out),
                 lambda: rgc.Embedding(table, tokens, out[:, :7]), lambda: rgc.Embedding(table.int(), tokens, out),
                 lambda: rgc.rgc_embed_tokens_backward(ctx, call, dout.half(), dtable), lambda: rgc.rgc_embed_tokens_backward(ctx, call, dout, dtable.half()),
-                lambda: rgc.rgc_embed_tokens_backward(ctx, call, dout, dtable[:9])):
+                lambda: rgc.rgc_embed_tokens_backward(ctx, call, dout, dtable[:9]), lambda: rgc.rgc_embed_tokens_backward(ctx, call, dtable[:4], dtable)):
         with pytest.raises(rgc.RgcError):
             bad()
     torch.cuda.synchronize()
