@@ -449,7 +449,8 @@ typedef struct {
 int rgc_causal_convolution(rgc_ctx* ctx, const rgc_convolution* convolution, void* hip_stream);
 
 /* Its backward pass: gradients of x, of the weights and the bias (summed over batch and steps) and of the kept inputs, from those of y and of `last`.
- * convolution: the descriptor of the forward call; y and last are not read.  Steps beyond a row's length get zeros.  dx is neither x nor dy. */
+ * convolution: the descriptor of the forward call, with `before` as that call read it; y and last are not read.  A call that put `last` in the place of `before` has no gradients (RGC_EINVAL, but
+ * without steps or with one tap, where nothing was replaced): they need a copy of it.  Steps beyond a row's length get zeros.  dx is neither x nor dy. */
 typedef struct {
   rgc_sequence   dy;       /* read only                                                             */
   rgc_sequence   dx;

@@ -1703,6 +1703,8 @@ int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* r, cons
   if (!ctx || !r || !g || !convolution_fits(r) || !g->dweight || !words_aligned({g->dweight, g->dbias})) return RGC_EINVAL;
   if (!aligned_to(g->dlast, element_size(r->dtype)) || !aligned_to(g->dbefore, element_size(r->dtype))) return RGC_EINVAL;
   if (r->batch > 0 && r->taps > 1 && g->dlast && g->dlast == g->dbefore) return RGC_EINVAL;
+  // (what the forward call read of `before` is needed again, and gone if `last` took its place)
+  if (r->batch > 0 && r->steps > 0 && r->taps > 1 && r->last && r->last == r->before) return RGC_EINVAL;
   if (r->batch > 0 && r->steps > 0) {
     if (!sequence_fits(g->dy, r, false) || !sequence_fits(g->dx, r, true) || g->dx.data == g->dy.data || g->dx.data == r->x.data) return RGC_EINVAL;
   }
