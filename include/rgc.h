@@ -501,7 +501,7 @@ typedef struct {
 int rgc_selective_scan(rgc_ctx* ctx, const rgc_scan* scan, void* hip_stream);
 
 /* Its backward pass.  scan: the descriptor of the forward call, with `kept` as that call left it; y, h0 and h_last are not read.  Gradients of a, d and delta_bias are
- * summed over batch and steps, those of B and C over their group's channels, in orders made of the sizes alone.  Steps beyond a row's length get zeros.
+ * summed over batch and steps, those of B and C over their group's channels, in orders made of the sizes (and of whether there are lengths) alone.  Steps beyond a row's length get zeros.
  * The sequences that are written are none of those that are read, nor one another; dh0 may be dh_last itself. */
 typedef struct {
   rgc_sequence   dy;          /* read only                                                            */

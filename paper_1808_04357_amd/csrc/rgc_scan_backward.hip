@@ -10,6 +10,7 @@
 //  4. The workgroups' parts of both are added up in an order made of the sizes alone (scan_rows_kernel, launch_sum_parts).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <type_traits>
 
@@ -506,9 +507,22 @@ __global__ void __launch_bounds__(256) scan_hand_on_kernel(const float* dh_last,
 }
 
 RearCut rear_cut(const ScanArgs& a) {
-  // Workgroups of the third launch: each has a start of its own (rows to stage), so no more of them than fill the device, a few times over where rows end early and leave workgroups with nothing to
-  // do.  us, 20 x 35 x 1500 fp32 with 512 / 1024 / 2048 53 / 62 / 77; 6 x 1001 x 1502 f16 with 24 states and lengths of 0 to 1001 502 / 271 / 242, 4096 268.
-  const uint64_t kEnough = a.lengths ? 2048 : 512;
+  // Workgroups of the third launch: each has a start of its own (rows to stage), so no more of them than fill the device (kFill).  Where rows may end early, a few times as many (kSpare), as all of a
+  // chunk's workgroups behind a row's end have nothing to do; not so for sequences of one chunk, which all rows with steps have, nor down to fewer than kLeast stretches of channels each.
+  // us, the backward call with lengths that are all full / of every size, with kFill, with kSpare and no least, and as it is (without lengths a call takes what all full ones do with kFill):
+  //   20 x 35 x 1500 fp32              56 / 55    84 / 81    56 / 55
+  //   32 x 48 x 4096 bf16             176 / 174  203 / 198  176 / 174
+  //   2 x 500 x 768 fp32               43 / 42    61 / 50    43 / 42
+  //   8 x 100 x 2048 bf16              68 / 66    78 / 60    70 / 51
+  //   8 x 200 x 1024 bf16, 64 states  234 / 222  279 / 175  260 / 170
+  //   8 x 200 x 1024 bf16, 32 states  113 / 108  130 / 90   125 / 86
+  //   128 x 64 x 512 bf16             114 / 111  122 / 118  122 / 118
+  //   1 x 4096 x 1024 bf16            146 / 127  154 / 106  154 / 106
+  //   6 x 1001 x 1502 bf16            298 / 279  257 / 181  257 / 181
+  //   6 x 1001 x 1502 f16, 24 states  386 / 365  336 / 232  337 / 232
+  //   4 x 2048 x 2048 bf16            450 / 395  437 / 256  437 / 257
+  //   16 x 300 x 4096 bf16            567 / 509  549 / 387  549 / 385
+  constexpr uint64_t kFill = 512, kSpare = 2048, kLeast = 8;
   RearCut K{};
   const uint32_t channels = wave_channels<Kind::kBackward>(a.states), rear = kRearWaves * wave_channels<Kind::kSummary>(a.states), each = a.width / a.groups;
   K.kept = (a.steps + kChunk - 1u) / kChunk;
@@ -517,8 +531,9 @@ RearCut rear_cut(const ScanArgs& a) {
   K.across = (each + rear - 1u) / rear;
   K.blocks = (each + channels - 1u) / channels;
   const uint64_t apart = static_cast<uint64_t>(a.batch) * K.chunks * a.groups;
-  const uint64_t want = apart > 0u && apart < kEnough ? kEnough / apart : 1u;
-  K.splits = static_cast<uint32_t>(want < K.blocks ? want : K.blocks);
+  auto splits_of = [&](uint64_t enough) { return std::min<uint64_t>(apart > 0u && apart < enough ? enough / apart : 1u, K.blocks); };
+  K.splits = static_cast<uint32_t>(splits_of(kFill));
+  if (a.lengths && K.chunks > 1u) K.splits = std::max(K.splits, static_cast<uint32_t>(std::min<uint64_t>(splits_of(kSpare), K.blocks / kLeast)));
   return K;
 }
 
