@@ -204,23 +204,6 @@ struct Staged {
   }
 };
 
-// An owner's steps of one tensor, from step `first` on; those at `end` and beyond are not looked at and read as 0.
-template <typename T, uint32_t kOwn>
-struct Own {
-  T v[kOwn];
-  __device__ void read(const SequenceView& s, uint32_t b, uint32_t first, uint32_t end, uint32_t c) {
-    const T* p = element<T>(s, b, first, c);
-#pragma unroll
-    for (uint32_t j = 0; j < kOwn; ++j, p += s.step_stride) v[j] = first + j < end ? *p : static_cast<T>(0.0f);
-  }
-  // all of them are there
-  __device__ void read(const SequenceView& s, uint32_t b, uint32_t first, uint32_t c) {
-    const T* p = element<T>(s, b, first, c);
-#pragma unroll
-    for (uint32_t j = 0; j < kOwn; ++j, p += s.step_stride) v[j] = *p;
-  }
-};
-
 // kRows rows of B or C in 32 bits, `count` of them from memory and zeros behind, kStates a step, by so many threads.
 template <typename T, uint32_t kRows, uint32_t kStates>
 __device__ __forceinline__ void stage(float* to, const SequenceView& from, const ScanArgs& A, uint32_t b, uint32_t g, uint32_t first, uint32_t count, uint32_t threads) {
