@@ -395,7 +395,7 @@ int rgc_gated_recurrence_backward(rgc_ctx* ctx, const rgc_recurrence* recurrence
 
 /* Rows of an embedding table, scaled:  out[r] = scale * table[tokens[r]], rounded to its type once.
  * A token outside [0, vocab) is left out: its row is 0, and no row of the table is looked at for it.  A token may come as often as it likes.
- * Limits: 0 <= rows < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 1 <= width <= RGC_WIDTH_MAX; strides not negative, that of out at least width.  out is not the table, dtable is not dout. */
+ * Limits: 0 <= rows < 2^31, 1 <= vocab <= RGC_VOCAB_MAX, 1 <= width <= RGC_WIDTH_MAX; scale finite; strides not negative, that of out at least width.  out is not the table, dtable is not dout. */
 #define RGC_WIDTH_MAX 1048576
 
 typedef struct {
@@ -470,7 +470,8 @@ int rgc_causal_convolution_backward(rgc_ctx* ctx, const rgc_convolution* convolu
  *  - h before the first step is h0 (0 without one); a reset at step t puts 0 in the place of h_{t-1} there, as between texts packed into one row.
  *  - Steps at lengths[b] and beyond (lengths are read as at least 0 and at most `steps`) are not looked at; y is 0 there.  h_last is the state after the row's last step,
  *    h0 if it has none.
- *  - A rate of -inf is read as the lowest finite one.  A state that is infinite or NaN makes the later ones so, until one starts anew.
+ *  - A rate of -inf is read as the lowest finite one.  A state that is infinite or NaN makes the later ones so, until one starts anew.  exp(delta_t a) is an fp32 number: where delta_t a is above 88.7 it is
+ *    infinite, and so is the state after the step (NaN if it was 0).
  * h_last may be h0 itself; y is none of the sequences that are read.  steps == 1 is the serving form.
  * Limits: batch, steps >= 0, both < 2^31; 1 <= width <= RGC_WIDTH_MAX, a multiple of `groups`; 1 <= states <= RGC_SCAN_STATES_MAX; strides of steps at most
  * RGC_SCAN_STRIDE_MAX elements. */
@@ -502,7 +503,10 @@ int rgc_selective_scan(rgc_ctx* ctx, const rgc_scan* scan, void* hip_stream);
 
 /* Its backward pass.  scan: the descriptor of the forward call, with `kept` as that call left it; y, h0 and h_last are not read.  Gradients of a, d and delta_bias are
  * summed over batch and steps, those of B and C over their group's channels, in orders made of the sizes (and of whether there are lengths) alone.  Steps beyond a row's length get zeros.
- * The sequences that are written are none of those that are read, nor one another; dh0 may be dh_last itself. */
+ * The sequences that are written are none of those that are read, nor one another; dh0 may be dh_last itself.
+ * Scratch of the context, words of 32 bits: batch * chunks * width * (2 * states + 3), chunks = ceil(steps / RGC_SCAN_CHUNK) (width * (states + 2) for sequences that are taken as one chunk, of up to 32 or
+ * 48 steps), and 2 * batch * steps * groups * states for each workgroup of those that share a group's channels (one where batch * chunks * groups is 512 or more; 2048 with lengths): 300 MB for 8 x 4096 steps of
+ * 2048 channels with 16 states. */
 typedef struct {
   rgc_sequence   dy;          /* read only                                                            */
   rgc_sequence   dx, ddelta;

@@ -68,8 +68,8 @@ __device__ __forceinline__ void inputs_before(const ConvArgs& A, uint32_t b, uin
 
 // ---------------------------------------------------------------------------------------------------------------------------------- forward
 
-// us, 1 x 32768 x 1500 and 8 x 4096 x 2048 bf16, four taps, by channels a lane and steps: 4 x 16 43 and 62, 4 x 8 44 and 64, 2 x 16 48 and 68, 2 x 32 54 and 79, 8 x 8 62 and 81 (registers, two
-// waves a SIMD): 4.6 and 4.3 TB/s.
+// us, where the caches are warm (the same call again and again; with others in between 4 x 16 takes 53 and 62: 3.7 and 4.3 TB/s), 1 x 32768 x 1500 and 8 x 4096 x 2048 bf16, four taps, by channels a lane and steps: 4 x 16 43 and 62, 4 x 8 44 and 64, 2 x 16 48 and 68, 2 x 32 54 and 79, 8 x 8 62 and 81 (registers, two
+// waves a SIMD): 4.6 and 4.3 TB/s.  fp32, two channels a lane: 85 and 105, 4.6 and 5.1 TB/s with others in between.
 template <typename T, int kTaps, int kVec, int kSteps>
 __global__ void __launch_bounds__(64 * kWaves) convolution_kernel(ConvArgs A, uint32_t across, uint32_t tiles, uint64_t begin, uint64_t waves) {
   const uint64_t at = (begin + blockIdx.x) * kWaves + uniform(threadIdx.x >> 6);
@@ -140,7 +140,8 @@ struct Walks {
 };
 
 // (Four waves a SIMD: what it waits for is memory.  us, 8 x 4096 x 2048 bf16, four taps: 109; as the compiler likes it, 137 registers and three waves, 126; five waves, which spill 47, 196; the next
-// batch asked for early, 175 registers, 157; walks of 32 steps 121, of 128 138; one channel a lane 164.  More taps have more weights to hold than that leaves room for.)
+// batch asked for early, 175 registers, 157; walks of 32 steps 121, of 128 138; one channel a lane 164.  More taps have more weights to hold than that leaves room for.
+// fp32: 179, 1 x 32768 x 1500 166; bf16 there 104.)
 template <typename T, int kTaps, int kVec>
 __global__ void __launch_bounds__(64 * kWaves, kTaps <= 4 ? 4 : 1) convolution_backward_kernel(ConvArgs A, ConvGradArgs G, Walks K, uint64_t begin) {
   constexpr uint32_t kBatch = 8;                                                      // steps read at once

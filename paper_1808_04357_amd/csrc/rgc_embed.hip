@@ -322,6 +322,8 @@ __global__ void __launch_bounds__(256) sum_kernel(EmbedArgs A, EmbedGradArgs G, 
 }
 
 // A run of several segments that begins in this one: its parts are this segment's second and the first of those after it.
+// One workgroup joins a run however long.  us, the whole call, bf16: 32768 rows x 2048 of 50257 words, tokens all over / one token in half / in all of the rows 139 / 149 / 155; 1048577 x 64, where a
+// run has up to 32769 parts, 160 / 334 / 539.
 template <int kVec>
 __global__ void __launch_bounds__(64 * kJoinWaves) join_kernel(EmbedArgs A, EmbedGradArgs G, Sums S, uint64_t begin) {
   __shared__ float sums[kJoinWaves][64 * kVec];

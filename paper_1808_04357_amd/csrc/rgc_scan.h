@@ -292,6 +292,9 @@ enum class Kind { kWalk, kSummary, kBackward };      // a walk along the steps f
 // Calls f with the type and the layout.  us, 8 x 4096 x 2048 bf16 with 16 states (20 x 35 x 1500 fp32): backward two states a lane, eight steps, four waves a workgroup 1520 (53), four states, four
 // steps, eight waves 1711 (63; all of a compute unit's waves wait at one barrier), four states and eight steps do not fit into registers; the walk by two states a lane 550, by four 1013 (half
 // the waves: one a SIMD), by one 998; a summary, which has little to do once a channel and waves enough, by four 262, by two 311.
+// What that makes of other numbers of states, us, 8 x 1024 x 2048, forward and backward call: 1 state bf16 66 and 129 (fp32 92 and 170), 4 85 and 190 (108 and 233), 8 115 and 268 (125 and 288),
+// 16 126 and 432 (126 and 461), 24 153 and 559 (149 and 582), 32 171 and 850 (168 and 873), 64 335 and 1997 (337 and 2017): above 32 the backward pass has 84 KB of shared memory a workgroup, one a
+// compute unit, and twice the time a state's step.
 template <Kind kKind, typename F>
 hipError_t by_states(uint32_t states, int dtype, F&& f) {
   auto with = [&](auto layout) {

@@ -289,6 +289,16 @@ uint64_t workgroups(const ScanArgs& a, uint32_t stretches, uint32_t across) { re
 }  // namespace
 
 // Stretches where sequences and channels are fewer waves than kFew: so many that there are kEnough.
+// us, 16 states, bf16, sequences of 1024 channels (128 waves), whole / cut, with kEnough 4096, 8192, 16384, 32768:
+//   waves    1024 steps                     8192 steps
+//     128     83 /  27  27  26  26          647 /   97   98  109  142
+//     512     83 /  50  50  56  55          657 /  317  287  274  280
+//     768     83 /  75  66  66  74          683 /  501  451  422  414
+//    1024     83 /  84  80  81  94          686 /  626  572  548  549
+//    1536    102 / 123 114 111 114          859 /  950  829  803  802
+//    2048    103 / 139 133 135 144          880 / 1093 1029 1018 1032
+// and 1 x 32768 x 1500 (188 waves) 2720 / 525 458 439 444.  With 4, 8, 32 and 64 states, and in fp32, cut and whole meet at 1024 waves of 1024 steps too (4 states 252 / 250 244 253 277).  Left as they
+// are: a few chunks would rather be whole whatever the waves (4 x 128 x 1024 13 / 16), long sequences rather cut at 768 and 1024 waves.
 ScanCut scan_cut(const ScanArgs& a) {
   constexpr uint64_t kFew = 768, kEnough = 16384;
   ScanCut K{};

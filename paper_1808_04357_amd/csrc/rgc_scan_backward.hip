@@ -22,7 +22,8 @@ namespace {
 constexpr uint32_t kRearWaves = 4;     // of a workgroup of the first launch
 constexpr uint32_t kRearTile = 8;      // steps of a wave at a time in the first launch
 // A sequence of a few steps more than a chunk has is taken as one, by workgroups of more waves: no launch but the third is needed for it, and no workgroups with next to nothing to do.
-// 20 x 35 x 1500 fp32, the backward pass: 63 us, in two chunks 73.  (With layouts whose waves walk eight steps.)
+// us, the backward call, as one / in two chunks, 33 to 48 steps (the same to 2 us): 20 x 1500 fp32 56 / 63, with 4 states 31 / 37, 24 states 73 / 79, 32 states 95 / 111, 64 x 2048 bf16 171 / 197,
+// 256 x 512 171 / 193, 2 x 4096 36 / 34.  (With layouts whose waves walk eight steps.)
 constexpr uint32_t kWholeWaves = 6, kWholeTile = 8, kWholeStates = 32;
 
 struct RearCut {
