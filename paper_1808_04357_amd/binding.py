@@ -652,7 +652,7 @@ class Convolution:
 
 class ConvolutionGrads:
     """A host ``rgc_convolution_grads`` for a Convolution (keeps the tensors alive).  dy, dx: like x; dweight: float32 [width, taps]; dbias: float32 [width]
-    or None; dlast, dbefore: [batch, taps - 1, width] of x's type or None."""
+    or None; dlast, dbefore: [batch, taps - 1, width] of x's type or None.  A Convolution whose last is its before has no gradients: they need before as the call read it."""
 
     def __init__(self, convolution: Convolution, dy, dx, dweight, dbias=None, dlast=None, dbefore=None):
         x, a = convolution.x, rgc_convolution_grads()
